@@ -281,6 +281,126 @@ GVOTE_API int32_t gvote_recompress(const gvote_params* p, const float* mu, const
                          uint32_t* mask, int32_t* budget, int32_t* b_step,
                          void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------
+ * The pruned cache in use: rows held in 8 bits, single-token attention over them, and eviction by the
+ * attention weight a row has collected (the other common rule for what a cache keeps; Section 4.1 compares
+ * the method with such systems).  A prompt goes gvote_compress* or gvote_accumulate + gvote_evict ->
+ * gvote_store8 (mask); a token goes gvote_append8 -> gvote_attend8; a full cache goes gvote_evict ->
+ * gvote_prune8.
+ *
+ * The 8-bit cache.  K and V [n_kv_heads, total_tokens, d_k] e4m3 codes (1 sign, 4 exponent, 3 fraction bits, no
+ * infinities), in slabs per request as everywhere (cu_seqlens), KV head h of request r holding
+ * kv_len[r][h] rows at the front of its slab.  Rows 64 b .. 64 b + 63 of a (request, head) are a block and
+ * share one scale for K and one for V: scale word gvote_cache8_block_offset(cu_seqlens[r], r) + b of the
+ * head's row of gvote_cache8_row_blocks(total_tokens, batch) floats.  A row's value is code * scale.
+ * A scale is a power of two, the smallest 2^e, e >= -126, with max |x| <= 448 * 2^e over the block's finite
+ * entries: dividing by it is exact, so a code is its value correctly rounded (nearest, ties to the even
+ * code), and a row that moves to a block of another scale keeps its value unless that leaves e4m3's normal
+ * range.  A NaN or an infinity is stored as the NaN code.
+ *
+ * Restrictions of all entry points of this part: d_k a multiple of 16, at most 256; byte strides of the codes
+ * multiples of 16; at most 128 query heads per KV head; total_tokens <= 2^30.  Slabs are addressed by 64-bit
+ * offsets.  A workspace serves one call at a time: calls (or replays of captured graphs) that may overlap on
+ * the GPU need one each; between calls it holds nothing but the status word. */
+#define GVOTE_CACHE8_BLOCK 64
+typedef struct {
+  void* K;                   /* e4m3 codes, device */
+  void* V;
+  float* k_scale;            /* [n_kv_heads][gvote_cache8_row_blocks] */
+  float* v_scale;
+  const int32_t* cu_seqlens; /* [batch+1] slab boundaries */
+  int32_t* kv_len;           /* [batch][n_kv_heads] rows held; values are clamped to 0 .. slab length */
+  int64_t tok_stride;        /* elements (= bytes) between rows, and between heads */
+  int64_t head_stride;
+  int64_t total_tokens;      /* cu_seqlens[batch] */
+  int64_t max_N;             /* longest slab */
+  int32_t batch;
+  int32_t reserved;
+} gvote_cache8;
+static inline int64_t gvote_cache8_row_blocks(int64_t total_tokens, int32_t batch) {
+  return (total_tokens >> 6) + batch;
+}
+static inline int64_t gvote_cache8_block_offset(int64_t cu_seqlens_r, int32_t r) {
+  return (cu_seqlens_r >> 6) + r;
+}
+
+/* Bytes of scratch the entry points of this part accept as `ws`, for slabs of this size and queries of this
+ * size (total_q query tokens in all, max_q of one request at most; 0, 0 for calls without queries).  Where a
+ * call has a source and a destination cache, the larger of both sizes.  Zero-fill it once; status word as
+ * everywhere (gvote_poll_status).  0 on invalid arguments. */
+GVOTE_API size_t gvote_cache_workspace_bytes(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N,
+                                   int64_t total_q, int64_t max_q);
+
+/* The pruning step of Algorithm 1 into the 8-bit cache: the kept rows of K and V (bf16 slabs, as in
+ * gvote_compact; not modified), in ascending order, become rows 0 .. of the head's slab in `cache`, and
+ * cache->kv_len is written.  mask_or_null: keep-mask over slots (null keeps all); kv_len_or_null: rows that
+ * count per (request, head), as in gvote_recompress (bits behind them are ignored).  `cache` has slabs of its own
+ * (same batch); rows that do not fit are dropped and the status word reads GVOTE_ERR_WORKSPACE_TOO_SMALL.
+ * Per-slot side arrays [n_kv_heads, total_tokens] move with the rows: acc -> acc_out, token_pos ->
+ * token_pos_out (with the cache's total_tokens); token_pos_out without token_pos receives the source slot.
+ * What lies behind the last row (codes, scales, side arrays) is left as it was. */
+GVOTE_API int32_t gvote_store8(const gvote_params* p, const void* K, const void* V, int64_t tok_stride, int64_t head_stride,
+                     const uint32_t* mask_or_null, const int32_t* cu_seqlens, const int32_t* kv_len_or_null,
+                     int32_t batch, int64_t total_tokens, int64_t max_N, const gvote_cache8* cache,
+                     const float* acc_or_null, float* acc_out_or_null, const int32_t* token_pos_or_null,
+                     int32_t* token_pos_out_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/* The same from one 8-bit cache into another (the buffers must not overlap): the kept rows of `src`, scaled
+ * anew block by block. */
+GVOTE_API int32_t gvote_prune8(const gvote_params* p, const gvote_cache8* src, const uint32_t* mask_or_null,
+                     const gvote_cache8* dst, const float* acc_or_null, float* acc_out_or_null,
+                     const int32_t* token_pos_or_null, int32_t* token_pos_out_or_null,
+                     void* ws, size_t ws_bytes, void* stream);
+
+/* New tokens' rows join the cache.  K_new, V_new [n_kv_heads, total_new, d_k] bf16 with element strides, requests
+ * packed by cu_new [batch+1] (device; a request may have none), max_new of one request at most.  They become the
+ * rows behind kv_len, and kv_len_out [batch, n_kv_heads] = kv_len + new rows (it may be cache->kv_len itself).
+ * The scale of a block that holds rows already is max(its scale, the new rows' own); when it grows, the block's codes
+ * are rewritten for it.  acc_or_null / token_pos_or_null [n_kv_heads, total_tokens]: the new slots' weight becomes 0,
+ * their position pos_new[row of K_new] (given together with token_pos).  Rows that do not fit the slab are
+ * dropped and reported as in gvote_store8. */
+GVOTE_API int32_t gvote_append8(const gvote_params* p, const void* K_new, const void* V_new, int64_t tok_stride,
+                      int64_t head_stride, const int32_t* cu_new, int64_t total_new, int64_t max_new,
+                      const gvote_cache8* cache, int32_t* kv_len_out, float* acc_or_null, int32_t* token_pos_or_null,
+                      const int32_t* pos_new_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/* Attention of a few tokens per request over the 8-bit cache.  Q, out [total_q, n_q_heads, d_k] bf16 with element
+ * strides (tokens, heads), requests packed by cu_q [batch+1] (device); at most GVOTE_ATTEND8_MAX_Q tokens of a
+ * request.  A request's query tokens are the last rows of its cache (append first): token i of n sees rows
+ * 0 .. kv_len - n + i of a head; a head with fewer rows than that leaves token i nothing, which gives out = 0,
+ * lse = -inf.  Per query head g of KV head h: logits q.k_n / sqrt(d_k), softmax, out = sum of weight * value
+ * (products of the stored values; 32-bit sums), lse_or_null [total_q, n_q_heads] = log of the softmax's
+ * denominator.  acc_out_or_null [n_kv_heads, total_tokens]: for the rows held, acc (null: 0) + the weights summed over
+ * the request's tokens and the head's group; acc_or_null may be acc_out itself.  Deterministic. */
+#define GVOTE_ATTEND8_MAX_Q 32
+GVOTE_API int32_t gvote_attend8(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride,
+                      const int32_t* cu_q, int64_t total_q, int64_t max_q, const gvote_cache8* cache,
+                      void* out, int64_t out_tok_stride, int64_t out_head_stride, float* lse_or_null,
+                      const float* acc_or_null, float* acc_out_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/* Attention weight each cached key collects from a prompt's queries.  Q [total_q, n_q_heads, d_k] bf16 (rotated, element
+ * strides), requests packed by cu_q; K as in gvote_vote (UNPRUNED slabs, or the front of them with kv_len).  A
+ * request's query tokens are the last of its rows, causal as in gvote_attend8: all of the prompt, or a window of
+ * its last tokens.  acc_out [n_kv_heads, total_tokens]: for the rows that count, acc (null: 0) + the softmax weights
+ * summed over the tokens and over the head's group; other entries are left as they were.
+ * lse_or_null [total_q, n_q_heads]: the logarithm of each query's softmax denominator over the keys it sees, when
+ * the prompt's attention has left it (-inf where it sees none); computed here otherwise.  Deterministic. */
+GVOTE_API int32_t gvote_accumulate(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride,
+                         const int32_t* cu_q, int64_t total_q, int64_t max_q, const void* K, int64_t k_tok_stride,
+                         int64_t k_head_stride, const int32_t* cu_seqlens, const int32_t* kv_len_or_null,
+                         int32_t batch, int64_t total_tokens, int64_t max_N, const float* lse_or_null,
+                         const float* acc_or_null, float* acc_out, void* ws, size_t ws_bytes, void* stream);
+
+/* Eviction by collected weight: which rows stay.  Per request and KV head with n rows (kv_len, or the slab), k =
+ * clamp(keep[r][h], 0, n) rows are kept: the last min(n_recent, k), then the first min(p->n_s, what is left of k and n),
+ * then those of largest acc, ties to the lower slot (a NaN counts as the lowest weight).  keep [batch, n_kv_heads] int32 (device), so that heads may keep
+ * different numbers of rows (a budget written by gvote_vote, for instance).  mask and budget (= k) as in gvote_vote:
+ * gvote_compact, gvote_pack, gvote_store8 and gvote_prune8 take the mask. */
+GVOTE_API int32_t gvote_evict(const gvote_params* p, const float* acc, const int32_t* cu_seqlens,
+                    const int32_t* kv_len_or_null, int32_t batch, int64_t total_tokens, int64_t max_N,
+                    const int32_t* keep, int32_t n_recent, uint32_t* mask, int32_t* budget,
+                    void* ws, size_t ws_bytes, void* stream);
+
 /* The same pass for a caller whose tensors live in HOST memory (pinned memory gives full copy
  * speed): all pointers are host pointers, K and V are dense ([n_kv_heads, total_tokens, d_k]),
  * h is dense [total_tokens, d_h].  The call copies the inputs to device buffers it keeps in a

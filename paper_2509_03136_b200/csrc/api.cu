@@ -67,7 +67,7 @@ int32_t validate_params(const gvote_params* p) {
   return GVOTE_OK;
 }
 
-static int32_t validate_batch(int32_t batch, int64_t total_tokens, int64_t max_N) {
+int32_t validate_batch(int32_t batch, int64_t total_tokens, int64_t max_N) {
   if (batch < 1 || total_tokens < 0 || max_N < 0 || max_N > total_tokens) return GVOTE_ERR_INVALID_ARG;
   if (total_tokens > (int64_t)1 << 30) return GVOTE_ERR_UNSUPPORTED_SHAPE;
   return GVOTE_OK;
@@ -125,10 +125,6 @@ WorkspaceMap workspace_map(const gvote_params* p, int32_t batch, int64_t total_t
 }  // namespace gvote
 
 using namespace gvote;
-
-#define REQUIRE_PTR(x) do { if (!(x)) return GVOTE_ERR_INVALID_ARG; if (!aligned16(x)) return GVOTE_ERR_UNALIGNED; } while (0)
-#define OPTIONAL_PTR(x) do { if ((x) && !aligned16(x)) return GVOTE_ERR_UNALIGNED; } while (0)
-#define PROPAGATE(expr) do { int32_t s__ = (expr); if (s__ != GVOTE_OK) return s__; } while (0)
 
 extern "C" {
 

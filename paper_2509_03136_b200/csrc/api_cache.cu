@@ -1,0 +1,173 @@
+// C-ABI entry points of the 8-bit cache and of the eviction (declared in include/gvote.h): argument checks and
+// the workspace size; the kernels are in store8.cu, append8.cu, attend8.cu, accumulate.cu and evict.cu.
+#include "cache8.cuh"
+
+namespace gvote {
+namespace {
+
+int32_t validate_shape(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N) {
+  PROPAGATE(validate_params(p));
+  PROPAGATE(validate_batch(batch, total_tokens, max_N));
+  if (p->d_k % 16 != 0 || p->d_k > kMaxHeadDim8 || p->n_q_heads / p->n_kv_heads > kMaxGroup8) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  // grids: requests on y or z, blocks of every head on x
+  if (batch > 65535 || p->n_kv_heads > 65535) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  if (((total_tokens >> 6) + batch) * (int64_t)p->n_kv_heads > 0x7fffffffLL) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  return GVOTE_OK;
+}
+
+int32_t validate_queries(const gvote_params* p, int64_t total_q, int64_t max_q) {
+  if (total_q < 0 || max_q < 0 || max_q > total_q) return GVOTE_ERR_INVALID_ARG;
+  if (total_q > (int64_t)1 << 30 || max_q * (p->n_q_heads / p->n_kv_heads) > 0x7fffff00LL) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  return GVOTE_OK;
+}
+
+int32_t validate_cache(const gvote_params* p, const gvote_cache8* c) {
+  if (!c) return GVOTE_ERR_INVALID_ARG;
+  PROPAGATE(validate_shape(p, c->batch, c->total_tokens, c->max_N));
+  REQUIRE_PTR(c->K); REQUIRE_PTR(c->V); REQUIRE_PTR(c->k_scale); REQUIRE_PTR(c->v_scale);
+  REQUIRE_PTR(c->cu_seqlens); REQUIRE_PTR(c->kv_len);
+  if (c->tok_stride < p->d_k || c->tok_stride % 16 != 0 || c->head_stride % 16 != 0) return GVOTE_ERR_UNALIGNED;
+  return GVOTE_OK;
+}
+
+bool rows_aligned(int64_t tok, int64_t head, int d_k) { return tok >= d_k && tok % 8 == 0 && head % 8 == 0; }
+
+bool overlap(const void* a, const void* b) { return a == b; }
+
+size_t cache_workspace(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N, int64_t total_q,
+                       int64_t max_q) {
+  size_t n = store8_map(p, batch, total_tokens).total;
+  const size_t a = attend8_map(p, batch, total_tokens, max_N, total_q, max_q).total;
+  const size_t b = accumulate_map(p, batch, total_tokens, max_N, total_q, max_q).total;
+  if (a > n) n = a;
+  return b > n ? b : n;
+}
+
+}  // namespace
+}  // namespace gvote
+
+using namespace gvote;
+
+extern "C" {
+
+size_t gvote_cache_workspace_bytes(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N,
+                                   int64_t total_q, int64_t max_q) {
+  if (validate_shape(p, batch, total_tokens, max_N) != GVOTE_OK || validate_queries(p, total_q, max_q) != GVOTE_OK) return 0;
+  return cache_workspace(p, batch, total_tokens, max_N, total_q, max_q);
+}
+
+int32_t gvote_store8(const gvote_params* p, const void* K, const void* V, int64_t tok_stride, int64_t head_stride,
+                     const uint32_t* mask_or_null, const int32_t* cu_seqlens, const int32_t* kv_len_or_null,
+                     int32_t batch, int64_t total_tokens, int64_t max_N, const gvote_cache8* cache,
+                     const float* acc_or_null, float* acc_out_or_null, const int32_t* token_pos_or_null,
+                     int32_t* token_pos_out_or_null, void* ws, size_t ws_bytes, void* stream) {
+  PROPAGATE(validate_shape(p, batch, total_tokens, max_N));
+  PROPAGATE(validate_cache(p, cache));
+  if (cache->batch != batch) return GVOTE_ERR_INVALID_ARG;
+  REQUIRE_PTR(K); REQUIRE_PTR(V); REQUIRE_PTR(cu_seqlens); REQUIRE_PTR(ws);
+  OPTIONAL_PTR(mask_or_null); OPTIONAL_PTR(kv_len_or_null); OPTIONAL_PTR(acc_or_null); OPTIONAL_PTR(acc_out_or_null);
+  OPTIONAL_PTR(token_pos_or_null); OPTIONAL_PTR(token_pos_out_or_null);
+  if (!acc_or_null != !acc_out_or_null || (token_pos_or_null && !token_pos_out_or_null)) return GVOTE_ERR_INVALID_ARG;
+  if (overlap(acc_or_null, acc_out_or_null) && acc_or_null) return GVOTE_ERR_INVALID_ARG;
+  if (overlap(token_pos_or_null, token_pos_out_or_null) && token_pos_or_null) return GVOTE_ERR_INVALID_ARG;
+  if (kv_len_or_null == cache->kv_len) return GVOTE_ERR_INVALID_ARG;
+  if (!rows_aligned(tok_stride, head_stride, p->d_k)) return GVOTE_ERR_UNALIGNED;
+  if (ws_bytes < store8_map(p, batch, total_tokens).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
+  const SideArrays side{acc_or_null, acc_out_or_null, token_pos_or_null, token_pos_out_or_null};
+  return launch_store8(p, (const __nv_bfloat16*)K, (const __nv_bfloat16*)V, tok_stride, head_stride, nullptr, mask_or_null,
+                       cu_seqlens, kv_len_or_null, batch, total_tokens, cache, side, (char*)ws, (cudaStream_t)stream);
+}
+
+int32_t gvote_prune8(const gvote_params* p, const gvote_cache8* src, const uint32_t* mask_or_null,
+                     const gvote_cache8* dst, const float* acc_or_null, float* acc_out_or_null,
+                     const int32_t* token_pos_or_null, int32_t* token_pos_out_or_null, void* ws, size_t ws_bytes,
+                     void* stream) {
+  PROPAGATE(validate_cache(p, src));
+  PROPAGATE(validate_cache(p, dst));
+  if (src->batch != dst->batch) return GVOTE_ERR_INVALID_ARG;
+  if (overlap(src->K, dst->K) || overlap(src->V, dst->V) || overlap(src->k_scale, dst->k_scale) ||
+      overlap(src->v_scale, dst->v_scale) || overlap(src->kv_len, dst->kv_len)) return GVOTE_ERR_INVALID_ARG;
+  REQUIRE_PTR(ws); OPTIONAL_PTR(mask_or_null); OPTIONAL_PTR(acc_or_null); OPTIONAL_PTR(acc_out_or_null);
+  OPTIONAL_PTR(token_pos_or_null); OPTIONAL_PTR(token_pos_out_or_null);
+  if (!acc_or_null != !acc_out_or_null || (token_pos_or_null && !token_pos_out_or_null)) return GVOTE_ERR_INVALID_ARG;
+  if (overlap(acc_or_null, acc_out_or_null) && acc_or_null) return GVOTE_ERR_INVALID_ARG;
+  if (overlap(token_pos_or_null, token_pos_out_or_null) && token_pos_or_null) return GVOTE_ERR_INVALID_ARG;
+  if (ws_bytes < store8_map(p, src->batch, src->total_tokens).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
+  const SideArrays side{acc_or_null, acc_out_or_null, token_pos_or_null, token_pos_out_or_null};
+  return launch_store8(p, nullptr, nullptr, src->tok_stride, src->head_stride, src, mask_or_null, src->cu_seqlens,
+                       src->kv_len, src->batch, src->total_tokens, dst, side, (char*)ws, (cudaStream_t)stream);
+}
+
+int32_t gvote_append8(const gvote_params* p, const void* K_new, const void* V_new, int64_t tok_stride,
+                      int64_t head_stride, const int32_t* cu_new, int64_t total_new, int64_t max_new,
+                      const gvote_cache8* cache, int32_t* kv_len_out, float* acc_or_null, int32_t* token_pos_or_null,
+                      const int32_t* pos_new_or_null, void* ws, size_t ws_bytes, void* stream) {
+  PROPAGATE(validate_params(p));
+  PROPAGATE(validate_cache(p, cache));
+  if (total_new < 0 || max_new < 0 || max_new > total_new) return GVOTE_ERR_INVALID_ARG;
+  if (total_new > (int64_t)1 << 30) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  if (total_new > 0) {
+    REQUIRE_PTR(K_new); REQUIRE_PTR(V_new);
+    if (!rows_aligned(tok_stride, head_stride, p->d_k)) return GVOTE_ERR_UNALIGNED;
+  }
+  REQUIRE_PTR(cu_new); REQUIRE_PTR(kv_len_out); REQUIRE_PTR(ws);
+  OPTIONAL_PTR(acc_or_null); OPTIONAL_PTR(token_pos_or_null); OPTIONAL_PTR(pos_new_or_null);
+  if (total_new > 0 && !token_pos_or_null != !pos_new_or_null) return GVOTE_ERR_INVALID_ARG;
+  if (ws_bytes < kStatusBytes) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
+  return launch_append8(p, (const __nv_bfloat16*)K_new, (const __nv_bfloat16*)V_new, tok_stride, head_stride, cu_new,
+                        max_new, cache, kv_len_out, acc_or_null, token_pos_or_null, pos_new_or_null, (char*)ws,
+                        (cudaStream_t)stream);
+}
+
+int32_t gvote_attend8(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride,
+                      const int32_t* cu_q, int64_t total_q, int64_t max_q, const gvote_cache8* cache, void* out,
+                      int64_t out_tok_stride, int64_t out_head_stride, float* lse_or_null, const float* acc_or_null,
+                      float* acc_out_or_null, void* ws, size_t ws_bytes, void* stream) {
+  PROPAGATE(validate_params(p));
+  PROPAGATE(validate_cache(p, cache));
+  PROPAGATE(validate_queries(p, total_q, max_q));
+  if (max_q < 1) return GVOTE_ERR_INVALID_ARG;
+  if (max_q > GVOTE_ATTEND8_MAX_Q) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  REQUIRE_PTR(Q); REQUIRE_PTR(cu_q); REQUIRE_PTR(out); REQUIRE_PTR(ws);
+  OPTIONAL_PTR(lse_or_null); OPTIONAL_PTR(acc_or_null); OPTIONAL_PTR(acc_out_or_null);
+  if (acc_or_null && !acc_out_or_null) return GVOTE_ERR_INVALID_ARG;
+  if (q_head_stride < p->d_k || q_head_stride % 8 != 0 || q_tok_stride % 8 != 0) return GVOTE_ERR_UNALIGNED;
+  if (out_head_stride < p->d_k || out_head_stride % 8 != 0 || out_tok_stride % 8 != 0) return GVOTE_ERR_UNALIGNED;
+  if (ws_bytes < attend8_map(p, cache->batch, cache->total_tokens, cache->max_N, total_q, max_q).total)
+    return GVOTE_ERR_WORKSPACE_TOO_SMALL;
+  return launch_attend8(p, (const __nv_bfloat16*)Q, q_tok_stride, q_head_stride, cu_q, total_q, max_q, cache,
+                        (__nv_bfloat16*)out, out_tok_stride, out_head_stride, lse_or_null, acc_or_null, acc_out_or_null,
+                        (char*)ws, (cudaStream_t)stream);
+}
+
+int32_t gvote_accumulate(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride,
+                         const int32_t* cu_q, int64_t total_q, int64_t max_q, const void* K, int64_t k_tok_stride,
+                         int64_t k_head_stride, const int32_t* cu_seqlens, const int32_t* kv_len_or_null, int32_t batch,
+                         int64_t total_tokens, int64_t max_N, const float* lse_or_null, const float* acc_or_null,
+                         float* acc_out, void* ws, size_t ws_bytes, void* stream) {
+  PROPAGATE(validate_shape(p, batch, total_tokens, max_N));
+  PROPAGATE(validate_queries(p, total_q, max_q));
+  if (max_q < 1) return GVOTE_ERR_INVALID_ARG;
+  REQUIRE_PTR(Q); REQUIRE_PTR(cu_q); REQUIRE_PTR(K); REQUIRE_PTR(cu_seqlens); REQUIRE_PTR(acc_out); REQUIRE_PTR(ws);
+  OPTIONAL_PTR(kv_len_or_null); OPTIONAL_PTR(lse_or_null); OPTIONAL_PTR(acc_or_null);
+  if (q_head_stride < p->d_k || q_head_stride % 8 != 0 || q_tok_stride % 8 != 0) return GVOTE_ERR_UNALIGNED;
+  if (!rows_aligned(k_tok_stride, k_head_stride, p->d_k)) return GVOTE_ERR_UNALIGNED;
+  if (ws_bytes < accumulate_map(p, batch, total_tokens, max_N, total_q, max_q).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
+  return launch_accumulate(p, (const __nv_bfloat16*)Q, q_tok_stride, q_head_stride, cu_q, total_q, max_q,
+                           (const __nv_bfloat16*)K, k_tok_stride, k_head_stride, cu_seqlens, kv_len_or_null, batch,
+                           total_tokens, max_N, lse_or_null, acc_or_null, acc_out, (char*)ws, (cudaStream_t)stream);
+}
+
+int32_t gvote_evict(const gvote_params* p, const float* acc, const int32_t* cu_seqlens, const int32_t* kv_len_or_null,
+                    int32_t batch, int64_t total_tokens, int64_t max_N, const int32_t* keep, int32_t n_recent,
+                    uint32_t* mask, int32_t* budget, void* ws, size_t ws_bytes, void* stream) {
+  PROPAGATE(validate_shape(p, batch, total_tokens, max_N));
+  REQUIRE_PTR(acc); REQUIRE_PTR(cu_seqlens); OPTIONAL_PTR(kv_len_or_null); REQUIRE_PTR(keep); REQUIRE_PTR(mask);
+  REQUIRE_PTR(budget); REQUIRE_PTR(ws);
+  if (n_recent < 0) return GVOTE_ERR_INVALID_ARG;
+  if (ws_bytes < kStatusBytes) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
+  return launch_evict(p, acc, cu_seqlens, kv_len_or_null, batch, total_tokens, max_N, keep, n_recent, mask, budget,
+                      (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -60,6 +60,12 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 int32_t validate_params(const gvote_params* p);
+int32_t validate_batch(int32_t batch, int64_t total_tokens, int64_t max_N);
+
+// Argument checks of the entry points: each returns the error code from the calling function.
+#define REQUIRE_PTR(x) do { if (!(x)) return GVOTE_ERR_INVALID_ARG; if (!aligned16(x)) return GVOTE_ERR_UNALIGNED; } while (0)
+#define OPTIONAL_PTR(x) do { if ((x) && !aligned16(x)) return GVOTE_ERR_UNALIGNED; } while (0)
+#define PROPAGATE(expr) do { int32_t s__ = (expr); if (s__ != GVOTE_OK) return s__; } while (0)
 
 // ---------------------------------------------------------------------------------- workspace
 // Status block (first 256 bytes): word 0 = sticky error status, word 1 = where it was raised.

@@ -1,0 +1,297 @@
+// The pruning step of Algorithm 1 into the 8-bit cache (gvote_store8), and from one 8-bit cache into
+// another (gvote_prune8): gather the kept rows in ascending order, find each 64-row block's scale, round.
+//
+//   scale_b = the smallest 2^e with max |x| <= 448 * 2^e over the block, code = e4m3(x / scale_b).
+//
+// Two kernels.  store8_scan_kernel turns each (request, head) bit row into an exclusive popcount prefix per
+// mask word.  store8_kernel gives one CTA one destination block of K and of V: it finds the block's source
+// rows from the prefix (a search with a fan-out of the CTA's 256 threads, two rounds of loads for 2M keys, then
+// every thread lists the set bits of one word), loads all of them into registers (16 values per thread and
+// unit, 16-byte loads), takes the maximum over the CTA, and writes the codes.  Bound by memory: 6 d_k bytes per kept
+// row from bf16, 4 d_k from e4m3; the rows are read once, there is no second pass over them.
+// Out of place: nothing orders the blocks, and a pruned 8-bit cache is small.
+#include "cache8.cuh"
+
+namespace gvote {
+namespace {
+
+constexpr int kStoreThreads = 256;
+constexpr int kScan8Threads = 1024;
+
+// One CTA per (head, request): prefix[h][word] = kept keys among the n rows that count, before this word.
+__global__ void __launch_bounds__(kScan8Threads)
+store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict__ cu, const int32_t* __restrict__ kv_len,
+                   int Hkv, int64_t row_words, int32_t* __restrict__ prefix, int32_t* __restrict__ kept) {
+  __shared__ int warp_tot[kScan8Threads / 32];
+  __shared__ int carry;
+  const int h = blockIdx.x, r = blockIdx.y;
+  const int start = cu[r], n = valid_keys(kv_len, r, Hkv, h, cu[r + 1] - start);
+  const int words = (n + 31) >> 5;
+  const int64_t woff = (int64_t)h * row_words + mask_word_offset(start, r);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) carry = 0;
+  __syncthreads();
+  for (int base = 0; base < words; base += 4 * kScan8Threads) {
+    const int w0 = base + 4 * tid;
+    int c[4], mine = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int w = w0 + j;
+      uint32_t v = w < words ? mask[woff + w] : 0u;
+      if (w == words - 1 && (n & 31)) v &= (1u << (n & 31)) - 1u;
+      c[j] = __popc(v);
+      mine += c[j];
+    }
+    int inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += u;
+    }
+    if (lane == 31) warp_tot[warp] = inc;
+    __syncthreads();
+    if (warp == 0) {
+      int t = warp_tot[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, t, o);
+        if (lane >= o) t += u;
+      }
+      warp_tot[lane] = t;
+    }
+    __syncthreads();
+    int run = carry + (warp ? warp_tot[warp - 1] : 0) + inc - mine;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (w0 + j < words) prefix[woff + w0 + j] = run;
+      run += c[j];
+    }
+    __syncthreads();
+    if (tid == 0) carry += warp_tot[kScan8Threads / 32 - 1];
+    __syncthreads();
+  }
+  if (tid == 0) kept[r * Hkv + h] = carry;
+}
+
+struct StoreArgs {
+  const void* src[2];            // K, V: bf16 or e4m3
+  const float* src_scale[2];     // of an e4m3 source
+  int64_t s_tok, s_head, s_total, s_row_blocks;
+  const uint32_t* mask;          // or null: every row
+  const int32_t* prefix;
+  const int32_t* kept;
+  const int32_t* cu;
+  const int32_t* kv_len;
+  int64_t row_words;
+  uint8_t* dst[2];
+  float* dst_scale[2];
+  int64_t d_tok, d_head, d_total, d_row_blocks;
+  const int32_t* cu8;
+  int32_t* kv_len_out;
+  SideArrays side;
+  int32_t* status;
+  int Hkv, batch, d_k;
+};
+
+// The value of one 16-element unit as floats: of bf16 (two 16-byte words) or of e4m3 codes times their scale.
+template <bool kSrc8>
+struct Unit {
+  uint4 lo, hi;                  // hi: bf16 only
+  float scale;                   // e4m3 only
+  __device__ __forceinline__ void load(const void* base, int64_t elem, float s) {
+    if (kSrc8) {
+      lo = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + elem));
+      scale = s;
+    } else {
+      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + elem);
+      lo = __ldg(q);
+      hi = __ldg(q + 1);
+    }
+  }
+  __device__ __forceinline__ float2 pair(int i) const {        // elements 2 i, 2 i + 1
+    if (kSrc8) {
+      const uint32_t w = (&lo.x)[i >> 1];
+      const float2 f = decode8x2((i & 1) ? (w >> 16) : (w & 0xffffu));
+      return make_float2(f.x * scale, f.y * scale);
+    }
+    const uint32_t w = i < 4 ? (&lo.x)[i] : (&hi.x)[i - 4];
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+};
+
+template <bool kSrc8, int kUnits>     // kUnits: 16-element units of a block's K (or V) per thread
+__global__ void __launch_bounds__(kStoreThreads)
+store8_kernel(const __grid_constant__ StoreArgs a) {
+  __shared__ int s_src[kBlock8];
+  __shared__ float s_max[2][kStoreThreads / 32];
+  const int tid = threadIdx.x;
+  const int h = (int)(blockIdx.x % a.Hkv);
+  const int64_t gb = blockIdx.x / a.Hkv;
+  const int r = a.batch == 1 ? 0 : find_request_by(a.cu8, a.batch, gb, 6);
+  const int dstart = a.cu8[r], cap = a.cu8[r + 1] - dstart;
+  const int b = (int)(gb - block8_offset(dstart, r));
+  const int start = a.cu[r], n = valid_keys(a.kv_len, r, a.Hkv, h, a.cu[r + 1] - start);
+  const int all = a.mask ? a.kept[r * a.Hkv + h] : n;
+  const int m = min(all, cap);
+  if (b == 0 && tid == 0) {
+    a.kv_len_out[r * a.Hkv + h] = m;
+    if (all > cap) { atomicExch(&a.status[0], GVOTE_ERR_WORKSPACE_TOO_SMALL); atomicExch(&a.status[1], 8); }
+  }
+  const int row0 = b * kBlock8;
+  if (row0 >= m) return;
+  const int cnt = min(kBlock8, m - row0);
+  if (!a.mask) {
+    if (tid < cnt) s_src[tid] = row0 + tid;
+    __syncthreads();
+  } else {
+    const int words = (n + 31) >> 5;
+    const int64_t woff = (int64_t)h * a.row_words + mask_word_offset(start, r);
+    // the last word whose prefix does not exceed row0 holds that row (prefix[0] = 0 <= row0)
+    int lo = 0, span = words;
+    while (span > 1) {
+      const int step = (span + kStoreThreads - 1) / kStoreThreads;
+      const int at = tid * step;
+      const bool le = at < span && a.prefix[woff + lo + at] <= row0;
+      const int hit = __syncthreads_count(le) - 1;
+      lo += hit * step;
+      span = min(step, span - hit * step);
+    }
+    for (int base = lo;; base += kStoreThreads) {
+      const int w = base + tid;
+      int end = 0;
+      if (w < words) {
+        uint32_t bits = a.mask[woff + w];
+        if (w == words - 1 && (n & 31)) bits &= (1u << (n & 31)) - 1u;
+        int rank = a.prefix[woff + w] - row0;
+        while (bits && rank < cnt) {
+          if (rank >= 0) s_src[rank] = w * 32 + __ffs((int)bits) - 1;
+          bits &= bits - 1u;
+          ++rank;
+        }
+        end = rank;
+      }
+      if (__syncthreads_or(end >= cnt || w >= words)) break;     // (ranks grow with the words)
+    }
+  }
+  const int dc = a.d_k >> 4;                                     // units per row
+  const int units = cnt * dc;
+  Unit<kSrc8> x[2][kUnits];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    const int u = tid + i * kStoreThreads;
+    if (u < units) {
+      const int j = u / dc, c = u - j * dc, n_src = s_src[j];
+      const int64_t off = (int64_t)h * a.s_head + (int64_t)(start + n_src) * a.s_tok + c * 16;
+      const int64_t sb = (int64_t)h * a.s_row_blocks + block8_offset(start, r) + (n_src >> 6);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) x[t][i].load(a.src[t], off, kSrc8 ? a.src_scale[t][sb] : 0.f);
+    }
+  }
+  float mx[2] = {0.f, 0.f};
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      if (tid + i * kStoreThreads < units) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 f = x[t][i].pair(e);
+          mx[t] = fmaxf(mx[t], fmaxf(finite_abs(f.x), finite_abs(f.y)));
+        }
+      }
+    }
+    mx[t] = warp_max(mx[t]);
+    if ((tid & 31) == 0) s_max[t][tid >> 5] = mx[t];
+  }
+  __syncthreads();
+  const int64_t db = (int64_t)h * a.d_row_blocks + block8_offset(dstart, r) + b;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    float top = s_max[t][0];
+#pragma unroll
+    for (int w = 1; w < kStoreThreads / 32; ++w) top = fmaxf(top, s_max[t][w]);
+    const float scale = scale8_of(top), inv = inverse_pow2(scale);
+    if (tid == t) a.dst_scale[t][db] = scale;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int u = tid + i * kStoreThreads;
+      if (u < units) {
+        const int j = u / dc, c = u - j * dc;
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float2 f0 = x[t][i].pair(2 * q), f1 = x[t][i].pair(2 * q + 1);
+          w[q] = encode8x2(f0.x * inv, f0.y * inv) | (encode8x2(f1.x * inv, f1.y * inv) << 16);
+        }
+        *reinterpret_cast<uint4*>(a.dst[t] + (int64_t)h * a.d_head + (int64_t)(dstart + row0 + j) * a.d_tok + c * 16) =
+            make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+  if (tid < cnt) {
+    const int64_t s = (int64_t)h * a.s_total + start + s_src[tid];
+    const int64_t d = (int64_t)h * a.d_total + dstart + row0 + tid;
+    if (a.side.acc_out) a.side.acc_out[d] = a.side.acc[s];
+    if (a.side.pos_out) a.side.pos_out[d] = a.side.pos ? a.side.pos[s] : s_src[tid];
+  }
+}
+
+template <bool kSrc8>
+int32_t run_store(const StoreArgs& a, unsigned ctas, cudaStream_t st) {
+  const int units = (int)ceil_div(kBlock8 * (a.d_k >> 4), kStoreThreads);   // 1 .. 4
+  auto kernel = units == 1 ? store8_kernel<kSrc8, 1> : units == 2 ? store8_kernel<kSrc8, 2> : store8_kernel<kSrc8, 4>;
+  {
+    LaunchScope scope_("store8_kernel", st);
+    launch_on(kernel, dim3(ctas), dim3(kStoreThreads), 0, st, a);
+  }
+  GVOTE_LAUNCH_CHECK("store8_kernel");
+  return GVOTE_OK;
+}
+
+}  // namespace
+
+StoreMap store8_map(const gvote_params* p, int32_t batch, int64_t total_tokens) {
+  StoreMap m;
+  m.prefix = kStatusBytes;
+  m.kept = align_up(m.prefix + (size_t)p->n_kv_heads * gvote_mask_row_words(total_tokens, batch) * 4, 256);
+  m.total = align_up(m.kept + (size_t)p->n_kv_heads * batch * 4, 256);
+  return m;
+}
+
+int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t tok, int64_t head,
+                      const gvote_cache8* src8, const uint32_t* mask, const int32_t* cu, const int32_t* kv_len,
+                      int32_t batch, int64_t total_tokens, const gvote_cache8* dst, const SideArrays& side, char* ws,
+                      cudaStream_t st) {
+  const int Hkv = p->n_kv_heads;
+  const StoreMap m = store8_map(p, batch, total_tokens);
+  StoreArgs a;
+  a.src[0] = src8 ? src8->K : (const void*)K;
+  a.src[1] = src8 ? src8->V : (const void*)V;
+  a.src_scale[0] = src8 ? src8->k_scale : nullptr;
+  a.src_scale[1] = src8 ? src8->v_scale : nullptr;
+  a.s_tok = tok; a.s_head = head; a.s_total = total_tokens;
+  a.s_row_blocks = gvote_cache8_row_blocks(total_tokens, batch);
+  a.mask = mask;
+  a.prefix = reinterpret_cast<const int32_t*>(ws + m.prefix);
+  a.kept = reinterpret_cast<const int32_t*>(ws + m.kept);
+  a.cu = cu; a.kv_len = kv_len;
+  a.row_words = gvote_mask_row_words(total_tokens, batch);
+  a.dst[0] = (uint8_t*)dst->K; a.dst[1] = (uint8_t*)dst->V;
+  a.dst_scale[0] = dst->k_scale; a.dst_scale[1] = dst->v_scale;
+  a.d_tok = dst->tok_stride; a.d_head = dst->head_stride; a.d_total = dst->total_tokens;
+  a.d_row_blocks = gvote_cache8_row_blocks(dst->total_tokens, batch);
+  a.cu8 = dst->cu_seqlens; a.kv_len_out = dst->kv_len;
+  a.side = side;
+  a.status = reinterpret_cast<int32_t*>(ws);
+  a.Hkv = Hkv; a.batch = batch; a.d_k = p->d_k;
+  if (mask) {
+    LaunchScope scope_("store8_scan_kernel", st);
+    launch_on(store8_scan_kernel, dim3(Hkv, batch), dim3(kScan8Threads), 0, st, mask, cu, kv_len, Hkv, a.row_words,
+              (int32_t*)(ws + m.prefix), (int32_t*)(ws + m.kept));
+    GVOTE_LAUNCH_CHECK("store8_scan_kernel");
+  }
+  const unsigned ctas = (unsigned)(a.d_row_blocks * Hkv);
+  return src8 ? run_store<true>(a, ctas, st) : run_store<false>(a, ctas, st);
+}
+
+}  // namespace gvote

@@ -23,7 +23,8 @@ DTYPE_F32, DTYPE_BF16 = 0, 1
 
 EXPORTS = (
     "gvote_workspace_bytes", "gvote_workspace_queries", "gvote_fit", "gvote_fit_update", "gvote_fit_finish", "gvote_fit_static", "gvote_sample", "gvote_project", "gvote_vote", "gvote_select",
-    "gvote_compact", "gvote_pack", "gvote_overlap", "gvote_compress", "gvote_compress_moments", "gvote_recompress", "gvote_compress_host", "gvote_host_arena_release",
+    "gvote_compact", "gvote_pack", "gvote_overlap", "gvote_compress", "gvote_compress_moments", "gvote_recompress", "gvote_cache_workspace_bytes", "gvote_store8", "gvote_prune8", "gvote_append8", "gvote_attend8",
+    "gvote_accumulate", "gvote_evict", "gvote_compress_host", "gvote_host_arena_release",
     "gvote_poll_status", "gvote_clear_status", "gvote_exact_heads", "gvote_profile_enable", "gvote_profile_report", "gvote_launch_count", "gvote_status_string", "gvote_last_cuda_error",
 )
 
@@ -37,6 +38,42 @@ class GVoteParams(ctypes.Structure):
         ("sel_mode", ctypes.c_int32), ("include_c0", ctypes.c_int32), ("seed", ctypes.c_uint64),
         ("layer_id", ctypes.c_uint32), ("h_dtype", ctypes.c_int32),
     ]
+
+
+class GVoteCache8(ctypes.Structure):
+    """Mirror of `gvote_cache8`."""
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("cu_seqlens", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("tok_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64), ("total_tokens", ctypes.c_int64), ("max_N", ctypes.c_int64),
+        ("batch", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class Cache8:
+    """An 8-bit cache: e4m3 codes K, V (uint8 [n_kv_heads, total_tokens, d_k]), one power-of-two scale per 64 rows
+    of a head (float32 [n_kv_heads, cache8_row_blocks]), slab boundaries cu_seqlens (int32 [batch+1]), rows held
+    kv_len (int32 [batch, n_kv_heads]) and geom = (batch, total_tokens, longest slab).  `alloc_cache8` makes one.
+    The tensors are checked here, once; the entry points take the finished argument block."""
+    __slots__ = ("K", "V", "k_scale", "v_scale", "cu_seqlens", "kv_len", "geom", "shape", "device", "args")
+
+    def __init__(self, K, V, k_scale, v_scale, cu_seqlens, kv_len, geom):
+        batch, total, max_N = geom
+        H, _, d = K.shape
+        blocks = cache8_row_blocks(total, batch)
+        if K.stride() != V.stride():
+            raise ValueError("K and V must share strides")
+        dev = K.device
+        self.args = GVoteCache8(
+            _shaped(K, torch.uint8, (H, total, d), "K", dev, dense=False),
+            _shaped(V, torch.uint8, (H, total, d), "V", dev, dense=False),
+            _shaped(k_scale, torch.float32, (H, blocks), "k_scale", dev),
+            _shaped(v_scale, torch.float32, (H, blocks), "v_scale", dev),
+            _shaped(cu_seqlens, torch.int32, (batch + 1,), "cu_seqlens", dev),
+            _shaped(kv_len, torch.int32, (batch, H), "kv_len", dev), K.stride(1), K.stride(0), total, max_N, batch, 0)
+        self.K, self.V, self.k_scale, self.v_scale = K, V, k_scale, v_scale
+        self.cu_seqlens, self.kv_len, self.geom = cu_seqlens, kv_len, (batch, total, max_N)
+        self.shape, self.device = (H, d), dev
 
 
 class GVoteError(RuntimeError):
@@ -57,6 +94,7 @@ def load():
         raise RuntimeError(f"{_LIB_PATH} is missing: build it with `python -m paper_2509_03136_b200.build` "
                            "(there is no fallback path)")
     lib = ctypes.CDLL(_LIB_PATH)
+    C8 = ctypes.POINTER(GVoteCache8)
     P, vp, i32, i64, sz = ctypes.POINTER(GVoteParams), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     lib.gvote_workspace_bytes.restype = sz
     lib.gvote_workspace_bytes.argtypes = [P, i32, i64, i64]
@@ -93,6 +131,21 @@ def load():
     lib.gvote_compress.restype = i32
     lib.gvote_compress.argtypes = [P, vp, i64, vp, vp, i64, vp, vp, vp, i64, i64, vp, i32, i64, i64, vp, vp, vp,
                                    vp, sz, vp]
+    lib.gvote_cache_workspace_bytes.restype = sz
+    lib.gvote_cache_workspace_bytes.argtypes = [P, i32, i64, i64, i64, i64]
+    lib.gvote_store8.restype = i32
+    lib.gvote_store8.argtypes = [P, vp, vp, i64, i64, vp, vp, vp, i32, i64, i64, C8, vp, vp, vp, vp, vp, sz, vp]
+    lib.gvote_prune8.restype = i32
+    lib.gvote_prune8.argtypes = [P, C8, vp, C8, vp, vp, vp, vp, vp, sz, vp]
+    lib.gvote_append8.restype = i32
+    lib.gvote_append8.argtypes = [P, vp, vp, i64, i64, vp, i64, i64, C8, vp, vp, vp, vp, vp, sz, vp]
+    lib.gvote_attend8.restype = i32
+    lib.gvote_attend8.argtypes = [P, vp, i64, i64, vp, i64, i64, C8, vp, i64, i64, vp, vp, vp, vp, sz, vp]
+    lib.gvote_accumulate.restype = i32
+    lib.gvote_accumulate.argtypes = [P, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, i32, i64, i64, vp, vp, vp, vp,
+                                     sz, vp]
+    lib.gvote_evict.restype = i32
+    lib.gvote_evict.argtypes = [P, vp, vp, vp, i32, i64, i64, vp, i32, vp, vp, vp, sz, vp]
     lib.gvote_compress_host.restype = i32
     lib.gvote_compress_host.argtypes = [P, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     lib.gvote_host_arena_release.restype = None
@@ -198,6 +251,68 @@ def alloc_workspace(p: GVoteParams, batch: int, total_tokens: int, max_N: int, d
     if n == 0:
         raise GVoteError(-1, "gvote_workspace_bytes")
     return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+CACHE8_BLOCK = 64
+ATTEND8_MAX_Q = 32
+
+
+def cache8_row_blocks(total_tokens: int, batch: int) -> int:
+    return (total_tokens >> 6) + batch
+
+
+def cache8_block_offset(cu_r: int, r: int) -> int:
+    return (cu_r >> 6) + r
+
+
+def alloc_cache8(p: GVoteParams, cu_seqlens_host: Sequence[int], device="cuda") -> Cache8:
+    """An empty 8-bit cache with these slabs (zero-filled)."""
+    batch, total, max_N = geom = batch_geometry(cu_seqlens_host)
+    K, V = (torch.zeros(p.n_kv_heads, total, p.d_k, dtype=torch.uint8, device=device) for _ in range(2))
+    ks, vs = (torch.zeros(p.n_kv_heads, cache8_row_blocks(total, batch), device=device) for _ in range(2))
+    cu = torch.tensor([int(x) for x in cu_seqlens_host], dtype=torch.int32, device=device)
+    return Cache8(K, V, ks, vs, cu, torch.zeros(batch, p.n_kv_heads, dtype=torch.int32, device=device), geom)
+
+
+def alloc_cache_workspace(p: GVoteParams, batch: int, total_tokens: int, max_N: int, total_q: int = 0, max_q: int = 0,
+                          device="cuda") -> torch.Tensor:
+    """A zero-filled workspace for the entry points of the 8-bit cache and the eviction: slabs of this geometry,
+    total_q query tokens in all and at most max_q of one request."""
+    n = int(load().gvote_cache_workspace_bytes(ctypes.byref(p), batch, total_tokens, max_N, total_q, max_q))
+    if n == 0:
+        raise GVoteError(-1, "gvote_cache_workspace_bytes")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def _shaped(t: Optional[torch.Tensor], dtype, shape, name: str, dev: torch.device, dense: bool = True) -> Optional[int]:
+    """The pointer of a tensor of this type and shape on `dev`; None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != dev or not t.is_cuda:
+        raise (TypeError if not t.is_cuda else ValueError)(f"{name} is on {t.device}, must be on {dev} (a CUDA device)")
+    if not t.is_contiguous() and (dense or t.stride(-1) != 1):
+        raise TypeError(f"{name} must be contiguous" + ("" if dense else " along its last dimension"))
+    return t.data_ptr() or None
+
+
+def _cache8(p, c: Cache8, name: str):
+    if c.shape != (p.n_kv_heads, p.d_k):
+        raise ValueError(f"{name} holds {c.shape[0]} heads of {c.shape[1]} values, the parameters say "
+                         f"{p.n_kv_heads} of {p.d_k}")
+    return ctypes.byref(c.args)
+
+
+def _launch(entry, dev: torch.device, p, *args, ws: torch.Tensor) -> None:
+    """Calls a library entry point with its workspace on the current stream of the tensors' device."""
+    wp = _shaped(ws, torch.uint8, (ws.numel(),), "ws", dev)
+    here = torch.cuda.current_device()
+    if dev.index != here:
+        raise ValueError(f"the tensors are on {dev}, the current device is cuda:{here}")
+    _check(entry(ctypes.byref(p), *args, wp, ws.numel(), torch.cuda.current_stream(here).cuda_stream), entry.__name__)
 
 
 # ----------------------------------------------------------------------------- entry points
@@ -351,6 +466,95 @@ def gvote_compress(p, h, W_q, b_q, K, V, cu_seqlens, geom, mask, budget, b_step,
                                  _ptr(b_q), _ptr(K), _ptr(V), K.stride(1), K.stride(0), _ptr(cu_seqlens), batch,
                                  total, max_N, _ptr(mask), _ptr(budget), _ptr(b_step), _ptr(ws), ws.numel(),
                                  _stream()), "gvote_compress")
+
+
+def gvote_store8(p, K, V, cu_seqlens, geom, cache: Cache8, ws, mask=None, kv_len=None, acc=None, acc_out=None,
+                 token_pos=None, token_pos_out=None) -> None:
+    """The kept rows of the bf16 slabs K, V into the 8-bit cache; acc and token_pos move with them."""
+    batch, total, max_N = geom
+    H, dst, dev = p.n_kv_heads, (p.n_kv_heads, cache.geom[1]), K.device
+    if K.stride() != V.stride():
+        raise ValueError("K and V must share strides")
+    _launch(load().gvote_store8, dev, p, _shaped(K, torch.bfloat16, (H, total, p.d_k), "K", dev, dense=False),
+            _shaped(V, torch.bfloat16, (H, total, p.d_k), "V", dev, dense=False), K.stride(1), K.stride(0),
+            _shaped(mask, torch.int32, (H, mask_row_words(total, batch)), "mask", dev),
+            _shaped(cu_seqlens, torch.int32, (batch + 1,), "cu_seqlens", dev),
+            _shaped(kv_len, torch.int32, (batch, H), "kv_len", dev), batch, total, max_N, _cache8(p, cache, "cache"),
+            _shaped(acc, torch.float32, (H, total), "acc", dev), _shaped(acc_out, torch.float32, dst, "acc_out", dev),
+            _shaped(token_pos, torch.int32, (H, total), "token_pos", dev),
+            _shaped(token_pos_out, torch.int32, dst, "token_pos_out", dev), ws=ws)
+
+
+def gvote_prune8(p, cache: Cache8, mask, out: Cache8, ws, acc=None, acc_out=None, token_pos=None,
+                 token_pos_out=None) -> None:
+    """The kept rows of one 8-bit cache into another (mask=None keeps all)."""
+    batch, total, _ = cache.geom
+    H, dst, dev = p.n_kv_heads, (p.n_kv_heads, out.geom[1]), cache.device
+    if out.device != dev:
+        raise ValueError(f"out is on {out.device}, must be on {dev}")
+    _launch(load().gvote_prune8, dev, p, _cache8(p, cache, "cache"),
+            _shaped(mask, torch.int32, (H, mask_row_words(total, batch)), "mask", dev), _cache8(p, out, "out"),
+            _shaped(acc, torch.float32, (H, total), "acc", dev), _shaped(acc_out, torch.float32, dst, "acc_out", dev),
+            _shaped(token_pos, torch.int32, (H, total), "token_pos", dev),
+            _shaped(token_pos_out, torch.int32, dst, "token_pos_out", dev), ws=ws)
+
+
+def gvote_append8(p, K_new, V_new, cu_new, max_new: int, cache: Cache8, kv_len_out, ws, acc=None, token_pos=None,
+                  pos_new=None) -> None:
+    """New tokens' rows [n_kv_heads, total_new, d_k] behind the rows the cache holds; kv_len_out may be cache.kv_len."""
+    batch, total, _ = cache.geom
+    H, total_new, dev = p.n_kv_heads, K_new.shape[1], cache.device
+    if total_new and K_new.stride() != V_new.stride():
+        raise ValueError("K_new and V_new must share strides")
+    _launch(load().gvote_append8, dev, p,
+            _shaped(K_new, torch.bfloat16, (H, total_new, p.d_k), "K_new", dev, dense=False),
+            _shaped(V_new, torch.bfloat16, (H, total_new, p.d_k), "V_new", dev, dense=False), K_new.stride(1),
+            K_new.stride(0), _shaped(cu_new, torch.int32, (batch + 1,), "cu_new", dev), total_new, max_new,
+            _cache8(p, cache, "cache"), _shaped(kv_len_out, torch.int32, (batch, H), "kv_len_out", dev),
+            _shaped(acc, torch.float32, (H, total), "acc", dev),
+            _shaped(token_pos, torch.int32, (H, total), "token_pos", dev),
+            _shaped(pos_new, torch.int32, (total_new,), "pos_new", dev), ws=ws)
+
+
+def gvote_attend8(p, Q, cu_q, max_q: int, cache: Cache8, out, ws, lse=None, acc=None, acc_out=None) -> None:
+    """Attention of Q [total_q, n_q_heads, d_k] (a request's tokens are the last rows of its cache) over the 8-bit
+    cache into out; the softmax weights are added to acc_out when it is given."""
+    batch, total, _ = cache.geom
+    H, total_q, dev = p.n_kv_heads, Q.shape[0], cache.device
+    shape = (total_q, p.n_q_heads, p.d_k)
+    _launch(load().gvote_attend8, dev, p, _shaped(Q, torch.bfloat16, shape, "Q", dev, dense=False), Q.stride(0),
+            Q.stride(1), _shaped(cu_q, torch.int32, (batch + 1,), "cu_q", dev), total_q, max_q,
+            _cache8(p, cache, "cache"), _shaped(out, torch.bfloat16, shape, "out", dev, dense=False), out.stride(0),
+            out.stride(1), _shaped(lse, torch.float32, (total_q, p.n_q_heads), "lse", dev),
+            _shaped(acc, torch.float32, (H, total), "acc", dev), _shaped(acc_out, torch.float32, (H, total), "acc_out", dev),
+            ws=ws)
+
+
+def gvote_accumulate(p, Q, cu_q, max_q: int, K, cu_seqlens, geom, acc_out, ws, acc=None, lse=None, kv_len=None) -> None:
+    """acc_out = acc (or 0) + the softmax weights the prompt's queries Q [total_q, n_q_heads, d_k] give to the keys."""
+    batch, total, max_N = geom
+    H, total_q, dev = p.n_kv_heads, Q.shape[0], K.device
+    _launch(load().gvote_accumulate, dev, p,
+            _shaped(Q, torch.bfloat16, (total_q, p.n_q_heads, p.d_k), "Q", dev, dense=False), Q.stride(0), Q.stride(1),
+            _shaped(cu_q, torch.int32, (batch + 1,), "cu_q", dev), total_q, max_q,
+            _shaped(K, torch.bfloat16, (H, total, p.d_k), "K", dev, dense=False), K.stride(1), K.stride(0),
+            _shaped(cu_seqlens, torch.int32, (batch + 1,), "cu_seqlens", dev),
+            _shaped(kv_len, torch.int32, (batch, H), "kv_len", dev), batch, total, max_N,
+            _shaped(lse, torch.float32, (total_q, p.n_q_heads), "lse", dev),
+            _shaped(acc, torch.float32, (H, total), "acc", dev), _shaped(acc_out, torch.float32, (H, total), "acc_out", dev),
+            ws=ws)
+
+
+def gvote_evict(p, acc, cu_seqlens, geom, keep, n_recent: int, mask, budget, ws, kv_len=None) -> None:
+    """Keep-mask of the n_recent last rows, the p.n_s first and the rows of largest acc, keep [batch, n_kv_heads] in all."""
+    batch, total, max_N = geom
+    H, dev = p.n_kv_heads, acc.device
+    _launch(load().gvote_evict, dev, p, _shaped(acc, torch.float32, (H, total), "acc", dev),
+            _shaped(cu_seqlens, torch.int32, (batch + 1,), "cu_seqlens", dev),
+            _shaped(kv_len, torch.int32, (batch, H), "kv_len", dev), batch, total, max_N,
+            _shaped(keep, torch.int32, (batch, H), "keep", dev), n_recent,
+            _shaped(mask, torch.int32, (H, mask_row_words(total, batch)), "mask", dev),
+            _shaped(budget, torch.int32, (batch, H), "budget", dev), ws=ws)
 
 
 def gvote_compress_host(p, h, W_q, b_q, K, V, cu_seqlens, mask, budget, b_step) -> None:
