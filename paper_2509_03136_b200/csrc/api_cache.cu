@@ -11,13 +11,13 @@ int32_t validate_shape(const gvote_params* p, int32_t batch, int64_t total_token
   if (p->d_k % 16 != 0 || p->d_k > kMaxHeadDim8 || p->n_q_heads / p->n_kv_heads > kMaxGroup8) return GVOTE_ERR_UNSUPPORTED_SHAPE;
   // grids: requests on y or z, blocks of every head on x
   if (batch > 65535 || p->n_kv_heads > 65535) return GVOTE_ERR_UNSUPPORTED_SHAPE;
-  if (((total_tokens >> 6) + batch) * (int64_t)p->n_kv_heads > 0x7fffffffLL) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  if (((total_tokens >> 6) + batch) * (int64_t)p->n_kv_heads > 0x3fffffffLL) return GVOTE_ERR_UNSUPPORTED_SHAPE;
   return GVOTE_OK;
 }
 
 int32_t validate_queries(const gvote_params* p, int64_t total_q, int64_t max_q) {
   if (total_q < 0 || max_q < 0 || max_q > total_q) return GVOTE_ERR_INVALID_ARG;
-  if (total_q > (int64_t)1 << 30 || max_q * (p->n_q_heads / p->n_kv_heads) > 0x7fffff00LL) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  if (total_q > (int64_t)1 << 30 || ((total_q * (p->n_q_heads / p->n_kv_heads) >> 6) + 1) * p->n_kv_heads > 0x3fffffffLL) return GVOTE_ERR_UNSUPPORTED_SHAPE;
   return GVOTE_OK;
 }
 
