@@ -299,7 +299,7 @@ GVOTE_API int32_t gvote_recompress(const gvote_params* p, const float* mu, const
  * range.  A NaN or an infinity is stored as the NaN code.
  *
  * Restrictions of all entry points of this part: d_k a multiple of 16, at most 256; byte strides of the codes
- * multiples of 16; at most 128 query heads per KV head; total_tokens <= 2^30.  Slabs are addressed by 64-bit
+ * multiples of 16; at most 1024 KV heads and 128 query heads per KV head; total_tokens <= 2^30.  Slabs are addressed by 64-bit
  * offsets.  A workspace serves one call at a time: calls (or replays of captured graphs) that may overlap on
  * the GPU need one each; between calls it holds nothing but the status word. */
 #define GVOTE_CACHE8_BLOCK 64

@@ -10,7 +10,7 @@ int32_t validate_shape(const gvote_params* p, int32_t batch, int64_t total_token
   PROPAGATE(validate_batch(batch, total_tokens, max_N));
   if (p->d_k % 16 != 0 || p->d_k > kMaxHeadDim8 || p->n_q_heads / p->n_kv_heads > kMaxGroup8) return GVOTE_ERR_UNSUPPORTED_SHAPE;
   // grids: requests on y or z, blocks of every head on x
-  if (batch > 65535 || p->n_kv_heads > 65535) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  if (batch > 65535 || p->n_kv_heads > 1024) return GVOTE_ERR_UNSUPPORTED_SHAPE;
   if (((total_tokens >> 6) + batch) * (int64_t)p->n_kv_heads > 0x3fffffffLL) return GVOTE_ERR_UNSUPPORTED_SHAPE;
   return GVOTE_OK;
 }

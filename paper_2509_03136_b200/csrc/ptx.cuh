@@ -110,6 +110,15 @@ __device__ __forceinline__ void named_barrier_sync(uint32_t id, uint32_t threads
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
+// Four bytes global -> shared, asynchronously; cp_async_arrive makes `bar` count one arrival when this thread's
+// earlier copies have landed (the arrival is one of those the barrier was initialised for).
+__device__ __forceinline__ void cp_async_4(void* smem_dst, const void* gmem_src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(smem_dst)), "l"(gmem_src) : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
 // ---------------------------------------------------------------------------------- tensor memory
 // One full warp allocates `cols` columns (power of two, >= 32); the base address lands in *slot.
 __device__ __forceinline__ void tmem_alloc(uint32_t* slot, uint32_t cols) {
@@ -239,6 +248,9 @@ __device__ __forceinline__ bool elect_one() {
 // innermost first; strides in bytes for dims 1.. (dim 0 is contiguous).  Returns false on failure.
 bool encode_tensor_map_bf16(CUtensorMap* out, const void* base, int rank, const uint64_t* dims,
                             const uint64_t* strides_bytes, const uint32_t* box);
+// The same for a tensor of bytes (box[0] <= 128).
+bool encode_tensor_map_u8(CUtensorMap* out, const void* base, int rank, const uint64_t* dims,
+                          const uint64_t* strides_bytes, const uint32_t* box);
 // Same for a tensor of 2- or 4-byte elements (bf16 / fp32) without swizzle: the box lands in shared
 // memory row after row.  The box's inner extent must be a multiple of 16 bytes.
 bool encode_tensor_map_plain(CUtensorMap* out, const void* base, int elem_bytes, int rank, const uint64_t* dims,

@@ -53,6 +53,12 @@ bool encode_tensor_map_bf16(CUtensorMap* out, const void* base, int rank, const 
                 CU_TENSOR_MAP_L2_PROMOTION_L2_128B, rank, dims, strides_bytes, box);
 }
 
+bool encode_tensor_map_u8(CUtensorMap* out, const void* base, int rank, const uint64_t* dims,
+                          const uint64_t* strides_bytes, const uint32_t* box) {
+  return encode(out, base, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, rank, dims, strides_bytes, box);
+}
+
 bool encode_tensor_map_plain(CUtensorMap* out, const void* base, int elem_bytes, int rank, const uint64_t* dims,
                              const uint64_t* strides_bytes, const uint32_t* box) {
   if (elem_bytes != 2 && elem_bytes != 4) return false;
