@@ -30,6 +30,8 @@
 // kernel turns them into weights once lse is known; a slot belongs to one thread, so the sum has one order.
 //
 // Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
+#include <type_traits>
+
 #include "cache8.cuh"
 #include "ptx.cuh"
 
@@ -96,11 +98,30 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// Two e4m3 codes (low 16 bits) -> two halves.
-__device__ __forceinline__ uint32_t widen(uint32_t c) {
-  uint32_t h;
-  asm("{\n\t.reg .b16 lo;\n\tcvt.u16.u32 lo, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(h) : "r"(c));
-  return h;
+// The same with a zero accumulator.
+__device__ __forceinline__ void mma_16816_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                               uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// Four e4m3 codes -> two pairs of halves (exact).
+__device__ __forceinline__ void widen(uint32_t c, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(c));
+}
+// d = part * f + d * g on pairs of 32-bit floats.
+__device__ __forceinline__ void scale_add2(float& d0, float& d1, float p0, float p1, uint64_t f, uint64_t g) {
+  asm("{\n\t.reg .b64 d, p;\n\tmov.b64 d, {%0, %1};\n\tmov.b64 p, {%2, %3};\n\tmul.rn.f32x2 d, d, %5;\n\t"
+      "fma.rn.f32x2 d, p, %4, d;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "+f"(d0), "+f"(d1)
+      : "f"(p0), "f"(p1), "l"(f), "l"(g));
+}
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
 }
 // Two halves: 1 where the code is the NaN code, else 0.
 __device__ __forceinline__ uint32_t nan_flags(uint32_t c) {
@@ -289,19 +310,16 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     for (; t < seg1; t += a.rings, ++used) {
       const int s = used % a.stages;
       ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait(&my_full[s], (used / a.stages) & 1, 1u << 22));
-      if (ok && row0 < rows) {
+      // One tile.  kEdge: some row does not see all of it, or it reaches behind the last row (kept apart: the tests of
+      // the edge would cost every tile as many instructions again).
+      auto tile = [&](auto edge_tag) {
+        constexpr bool kEdge = decltype(edge_tag)::value;
         const uint8_t* kt = my_ring + (size_t)s * kStageBytes;
         const uint8_t* vt = kt + kBoxes * kBoxBytes;
         const float2 sc = my_scale[s];
         const int key0 = (t - pref[e]) * kTileKeys;
         // ---- S^T: thread holds keys mt * 16 + j8 (+ 8), rows 2 c4, 2 c4 + 1
         float sT[kRt][2][4];
-#pragma unroll
-        for (int rt = 0; rt < kRt; ++rt)
-#pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sT[rt][mt][i] = 0.f;
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
@@ -317,15 +335,19 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               const uint32_t wa = (&ka[k >> 2].x)[k & 3], wb = (&kb[k >> 2].x)[k & 3];
-              const uint32_t a0 = widen(wa), a1 = widen(wb), a2 = widen(wa >> 16), a3 = widen(wb >> 16);
+              uint32_t a0, a1, a2, a3;
+              widen(wa, a0, a2);
+              widen(wb, a1, a3);
 #pragma unroll
-              for (int rt = 0; rt < kRt; ++rt) mma_16816(sT[rt][mt], a0, a1, a2, a3, q[rt][y * 8 + k][0], q[rt][y * 8 + k][1]);
+              for (int rt = 0; rt < kRt; ++rt) {
+                if (y == 0 && k == 0) mma_16816_zero(sT[rt][mt], a0, a1, a2, a3, q[rt][0][0], q[rt][0][1]);
+                else mma_16816(sT[rt][mt], a0, a1, a2, a3, q[rt][y * 8 + k][0], q[rt][y * 8 + k][1]);
+              }
             }
           }
         }
-        const bool edge = key0 + kTileKeys > all_see;                  // some row does not see all of the tile
         uint32_t p[kRt][2][2];
-        float a_old[kRt][2], a_new[kRt][2];
+        uint64_t f_old[kRt], f_new[kRt];                               // factors of the sum so far and of this tile's
 #pragma unroll
         for (int rt = 0; rt < kRt; ++rt) {
           float top[2] = {-INFINITY, -INFINITY};
@@ -334,7 +356,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               float v = sT[rt][mt][i] * (sc.x * factor[rt][i & 1]);
-              if (edge && key0 + mt * 16 + j8 + (i >> 1) * 8 >= limit[rt][i & 1]) v = -INFINITY;
+              if (kEdge && key0 + mt * 16 + j8 + (i >> 1) * 8 >= limit[rt][i & 1]) v = -INFINITY;
               sT[rt][mt][i] = v;
               top[i & 1] = fmaxf(top[i & 1], v);
             }
@@ -352,15 +374,15 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
               }
             }
           }
-          float ref[2];
+          float ref[2], a_old[2], a_new[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
 #pragma unroll
             for (int k = 4; k < 32; k <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], k));
             const float next = fmaxf(m[rt][i], top[i]);
             ref[i] = top[i] == -INFINITY ? 0.f : top[i];
-            a_old[rt][i] = next == -INFINITY ? 0.f : exp2_fast(m[rt][i] - next);
-            a_new[rt][i] = next == -INFINITY ? 0.f : exp2_fast(top[i] - next);
+            a_old[i] = next == -INFINITY ? 0.f : exp2_fast(m[rt][i] - next);
+            a_new[i] = next == -INFINITY ? 0.f : exp2_fast(top[i] - next);
             m[rt][i] = next;
           }
           float add[2] = {0.f, 0.f};
@@ -376,10 +398,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             p[rt][mt][1] = transpose_8x8(pack_half2(w[2], w[3]));
           }
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            l[rt][i] = l[rt][i] * a_old[rt][i] + add[i] * a_new[rt][i];
-            a_new[rt][i] *= sc.y;
-          }
+          for (int i = 0; i < 2; ++i) l[rt][i] = l[rt][i] * a_old[i] + add[i] * a_new[i];
+          f_old[rt] = pack2(a_old[0], a_old[1]);
+          f_new[rt] = pack2(a_new[0] * sc.y, a_new[1] * sc.y);
         }
         // ---- O^T: thread's 16 channels 16 j8 .. of every 128, keys 2 c4, 2 c4 + 1 (+ 8) of each 16
 #pragma unroll
@@ -391,10 +412,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             for (int k = 0; k < 4; ++k) {
               const int key = mt * 16 + 2 * c4 + (k & 1) + (k >> 1) * 8;
               v[mt][k] = *reinterpret_cast<const uint4*>(vt + y * kBoxBytes + key * 128 + ((j8 ^ (key & 7)) << 4));
-              if (edge && key0 + key >= x.n) v[mt][k] = make_uint4(0, 0, 0, 0);     // behind the last row: anything
+              if (kEdge && key0 + key >= x.n) v[mt][k] = make_uint4(0, 0, 0, 0);     // behind the last row: anything
             }
           bool nan_seen = false;
-          if (edge && x.nq > 1) {
+          if (kEdge && x.nq > 1) {
             // A NaN in a row that some of the tokens do not see must not reach them through a weight of zero: it is
             // taken out of the product here and counted for the tokens that see it below.
             bool any = false;
@@ -410,37 +431,35 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           for (int w = 0; w < 4; ++w) {                                // m-tiles 2 w, 2 w + 1
             float part[kRt][2][4];
 #pragma unroll
-            for (int rt = 0; rt < kRt; ++rt)
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) part[rt][i][k] = 0.f;
-#pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
               uint32_t w0 = (&v[mt][0].x)[w], w1 = (&v[mt][1].x)[w], w2 = (&v[mt][2].x)[w], w3 = (&v[mt][3].x)[w];
-              if (nan_seen) {
+              if (kEdge && nan_seen) {
                 auto clean = [](uint32_t u) { return u & ~__vcmpeq4(u & 0x7f7f7f7fu, 0x7f7f7f7fu); };
                 w0 = clean(w0); w1 = clean(w1); w2 = clean(w2); w3 = clean(w3);
               }
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
                 const uint32_t lo = __byte_perm(w0, w1, i ? 0x7362 : 0x5140), hi = __byte_perm(w2, w3, i ? 0x7362 : 0x5140);
-                const uint32_t a0 = widen(lo), a1 = widen(lo >> 16), a2 = widen(hi), a3 = widen(hi >> 16);
+                uint32_t a0, a1, a2, a3;
+                widen(lo, a0, a1);
+                widen(hi, a2, a3);
 #pragma unroll
-                for (int rt = 0; rt < kRt; ++rt) mma_16816(part[rt][i], a0, a1, a2, a3, p[rt][mt][0], p[rt][mt][1]);
+                for (int rt = 0; rt < kRt; ++rt) {
+                  if (mt == 0) mma_16816_zero(part[rt][i], a0, a1, a2, a3, p[rt][0][0], p[rt][0][1]);
+                  else mma_16816(part[rt][i], a0, a1, a2, a3, p[rt][1][0], p[rt][1][1]);
+                }
               }
             }
 #pragma unroll
             for (int rt = 0; rt < kRt; ++rt)
 #pragma unroll
-              for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  float& d = o[rt][y * 8 + 2 * w + i][k];
-                  d = fmaf(part[rt][i][k], a_new[rt][k & 1], d * a_old[rt][k & 1]);
-                }
+              for (int i = 0; i < 2; ++i) {
+                float (&d)[4] = o[rt][y * 8 + 2 * w + i];
+                scale_add2(d[0], d[1], part[rt][i][0], part[rt][i][1], f_new[rt], f_old[rt]);
+                scale_add2(d[2], d[3], part[rt][i][2], part[rt][i][3], f_new[rt], f_old[rt]);
+              }
           }
-          if (nan_seen) {
+          if (kEdge && nan_seen) {
 #pragma unroll
             for (int w = 0; w < 4; ++w)
 #pragma unroll
@@ -466,6 +485,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
                 }
           }
         }
+      };
+      if (ok && row0 < rows) {
+        if ((t - pref[e]) * kTileKeys + kTileKeys > all_see) tile(std::true_type{}); else tile(std::false_type{});
       }
       // ---- the slot is free; row warp 0 asks for the ring's next tile
       __syncwarp();
@@ -541,18 +563,23 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   if (!ok && lane == 0) { atomicExch(&a.status[0], GVOTE_ERR_TIMEOUT); atomicExch(&a.status[1], 13); }
 }
 
-// What an entry's segments say of one row: the maximum, and the sum relative to it.
+// What an entry's segments say of one row: the maximum, and the sum relative to it.  A whole warp asks; the segments are
+// spread over its lanes, so that their loads are in flight together.
 __device__ __forceinline__ float2 merged_ml(const AttendArgs& a, int B, int group, int e, int2 v, int in_group, int entries) {
   const float2* ml = a.part_ml + ((int64_t)group * (entries + B) + e) * a.group_rows + in_group;
   float M = -INFINITY, L = 0.f;
-  for (int b = v.x; b <= v.y; ++b) {
+  for (int b = v.x + (int)(threadIdx.x & 31); v.x >= 0 && b <= v.y; b += 32) {
     const float2 x = ml[(int64_t)b * a.group_rows];
     const float top = fmaxf(M, x.x);
     if (top != -INFINITY) L = L * exp2_fast(M - top) + x.y * exp2_fast(x.x - top);
     else L += x.y;                                      // (a NaN in the sum stays)
     M = top;
   }
-  return make_float2(M, L);
+  const float all = warp_max(M);
+  L = all == -INFINITY ? L : L == 0.f ? 0.f : L * exp2_fast(M - all);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+  return make_float2(all, L);
 }
 
 // Blocks 0 .. entries * max_rows - 1: one row of one entry, merged from its segments when it has several (or none).
@@ -570,7 +597,7 @@ attend8_finish_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows,
     const int group = row / a.group_rows, in_group = row - group * a.group_rows;
     const int2 v = a.info[(int64_t)group * entries + e];
     if (v.x >= 0 && v.x == v.y) return;                 // the first kernel has written it
-    const float2 ml = v.x < 0 ? make_float2(-INFINITY, 0.f) : merged_ml(a, B, group, e, v, in_group, entries);
+    const float2 ml = merged_ml(a, B, group, e, v, in_group, entries);
     const int quads = a.d_k >> 2, part = tid >> 5, lane = tid & 31;
     const int64_t slot0 = ((int64_t)group * (entries + B) + e) * a.group_rows + in_group;
     for (int q = lane; q < quads; q += 32) {
@@ -612,10 +639,9 @@ attend8_finish_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows,
   const int i0 = (int)(gb - ((x.start >> 8) - (a.cu[a.r0] >> 8) + (r - a.r0))) * 256;
   if (i0 >= x.n || i0 < 0) return;
   const int rows = x.nq * a.G;
-  for (int row = tid; row < rows; row += 256) {
+  for (int row = tid >> 5; row < rows; row += 8) {
     const int group = row / a.group_rows;
-    const int2 v = a.info[(int64_t)group * entries + e];
-    const float2 ml = v.x < 0 ? make_float2(-INFINITY, 0.f) : merged_ml(a, B, group, e, v, row - group * a.group_rows, entries);
+    const float2 ml = merged_ml(a, B, group, e, a.info[(int64_t)group * entries + e], row - group * a.group_rows, entries);
     s_neg[row] = ml.x == -INFINITY ? -INFINITY : -(ml.x + log2f(ml.y));
   }
   __syncthreads();
