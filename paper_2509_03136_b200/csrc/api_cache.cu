@@ -34,6 +34,8 @@ bool rows_aligned(int64_t tok, int64_t head, int d_k) { return tok >= d_k && tok
 
 bool overlap(const void* a, const void* b) { return a == b; }
 
+int64_t larger(int64_t a, int64_t b) { return a > b ? a : b; }
+
 size_t cache_workspace(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N, int64_t total_q,
                        int64_t max_q) {
   size_t n = store8_map(p, batch, total_tokens).total;
@@ -72,7 +74,7 @@ int32_t gvote_store8(const gvote_params* p, const void* K, const void* V, int64_
   if (overlap(token_pos_or_null, token_pos_out_or_null) && token_pos_or_null) return GVOTE_ERR_INVALID_ARG;
   if (kv_len_or_null == cache->kv_len) return GVOTE_ERR_INVALID_ARG;
   if (!rows_aligned(tok_stride, head_stride, p->d_k)) return GVOTE_ERR_UNALIGNED;
-  if (ws_bytes < store8_map(p, batch, total_tokens).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
+  if (ws_bytes < store8_map(p, batch, larger(total_tokens, cache->total_tokens)).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
   const SideArrays side{acc_or_null, acc_out_or_null, token_pos_or_null, token_pos_out_or_null};
   return launch_store8(p, (const __nv_bfloat16*)K, (const __nv_bfloat16*)V, tok_stride, head_stride, nullptr, mask_or_null,
                        cu_seqlens, kv_len_or_null, batch, total_tokens, cache, side, (char*)ws, (cudaStream_t)stream);
@@ -92,7 +94,7 @@ int32_t gvote_prune8(const gvote_params* p, const gvote_cache8* src, const uint3
   if (!acc_or_null != !acc_out_or_null || (token_pos_or_null && !token_pos_out_or_null)) return GVOTE_ERR_INVALID_ARG;
   if (overlap(acc_or_null, acc_out_or_null) && acc_or_null) return GVOTE_ERR_INVALID_ARG;
   if (overlap(token_pos_or_null, token_pos_out_or_null) && token_pos_or_null) return GVOTE_ERR_INVALID_ARG;
-  if (ws_bytes < store8_map(p, src->batch, src->total_tokens).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
+  if (ws_bytes < store8_map(p, src->batch, larger(src->total_tokens, dst->total_tokens)).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
   const SideArrays side{acc_or_null, acc_out_or_null, token_pos_or_null, token_pos_out_or_null};
   return launch_store8(p, nullptr, nullptr, src->tok_stride, src->head_stride, src, mask_or_null, src->cu_seqlens,
                        src->kv_len, src->batch, src->total_tokens, dst, side, (char*)ws, (cudaStream_t)stream);

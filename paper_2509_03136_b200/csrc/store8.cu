@@ -4,11 +4,13 @@
 //   scale_b = the smallest 2^e with max |x| <= 448 * 2^e over the block, code = e4m3(x / scale_b).
 //
 // Two kernels.  store8_scan_kernel turns each (request, head) bit row into an exclusive popcount prefix per
-// mask word.  store8_kernel gives one CTA one destination block of K and of V: it finds the block's source
-// rows from the prefix (a search with a fan-out of the CTA's 256 threads, two rounds of loads for 2M keys, then
-// every thread lists the set bits of one word), loads all of them into registers (16 values per thread and
-// unit, 16-byte loads), takes the maximum over the CTA, and writes the codes.  Bound by memory: 6 d_k bytes per kept
-// row from bf16, 4 d_k from e4m3; the rows are read once, there is no second pass over them.
+// mask word, and notes for every destination block the word of its first row and how many rows it gets.
+// store8_kernel gives one CTA one destination block of K and of V: its threads list the set bits of a word each from
+// the noted one on, load all rows into registers (16 values per thread and unit, 16-byte loads), take the maximum
+// over the CTA, and write the codes.  Bound by memory: 6 d_k bytes per kept row from bf16, 4 d_k from e4m3; the rows are
+// read once, there is no second pass over them.  What a CTA waits for before it can ask for its rows is two rounds of
+// small loads (the note; words and prefixes): with a search for the first word in its place, five rounds, they cost
+// more than the rows (store of 17K rows x 8 heads 43 instead of 34 us).
 // Out of place: nothing orders the blocks, and a pruned 8-bit cache is small.
 #include "cache8.cuh"
 
@@ -21,13 +23,16 @@ constexpr int kScan8Threads = 1024;
 // One CTA per (head, request): prefix[h][word] = kept keys among the n rows that count, before this word.
 __global__ void __launch_bounds__(kScan8Threads)
 store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict__ cu, const int32_t* __restrict__ kv_len,
-                   int Hkv, int64_t row_words, int32_t* __restrict__ prefix, int32_t* __restrict__ kept) {
+                   int Hkv, int64_t row_words, int32_t* __restrict__ prefix, const int32_t* __restrict__ cu8,
+                   int64_t row_blocks, int2* __restrict__ note, int32_t* __restrict__ kv_len_out, int32_t* status) {
   __shared__ int warp_tot[kScan8Threads / 32];
   __shared__ int carry;
   const int h = blockIdx.x, r = blockIdx.y;
   const int start = cu[r], n = valid_keys(kv_len, r, Hkv, h, cu[r + 1] - start);
   const int words = (n + 31) >> 5;
   const int64_t woff = (int64_t)h * row_words + mask_word_offset(start, r);
+  const int dstart = cu8[r], cap = cu8[r + 1] - dstart;
+  int2* my_note = note + (int64_t)h * row_blocks + block8_offset(dstart, r);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) carry = 0;
   __syncthreads();
@@ -64,13 +69,21 @@ store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict_
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (w0 + j < words) prefix[woff + w0 + j] = run;
+      // the block whose first row is one of this word's
+      const int b = (run + kBlock8 - 1) >> 6;
+      if (b * kBlock8 < run + c[j] && b * kBlock8 < cap) my_note[b].x = w0 + j;
       run += c[j];
     }
     __syncthreads();
     if (tid == 0) carry += warp_tot[kScan8Threads / 32 - 1];
     __syncthreads();
   }
-  if (tid == 0) kept[r * Hkv + h] = carry;
+  const int m = min(carry, cap);
+  for (int b = tid; b * kBlock8 < cap; b += kScan8Threads) my_note[b].y = min(kBlock8, m - b * kBlock8);   // (<= 0: no rows)
+  if (tid == 0) {
+    kv_len_out[r * Hkv + h] = m;
+    if (carry > cap) { atomicExch(&status[0], GVOTE_ERR_WORKSPACE_TOO_SMALL); atomicExch(&status[1], 8); }
+  }
 }
 
 struct StoreArgs {
@@ -79,7 +92,7 @@ struct StoreArgs {
   int64_t s_tok, s_head, s_total, s_row_blocks;
   const uint32_t* mask;          // or null: every row
   const int32_t* prefix;
-  const int32_t* kept;
+  const int2* note;              // [Hkv][row_blocks of the destination]
   const int32_t* cu;
   const int32_t* kv_len;
   int64_t row_words;
@@ -130,35 +143,20 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
   const int r = a.batch == 1 ? 0 : find_request_by(a.cu8, a.batch, gb, 6);
   const int dstart = a.cu8[r], cap = a.cu8[r + 1] - dstart;
   const int b = (int)(gb - block8_offset(dstart, r));
-  const int start = a.cu[r], n = valid_keys(a.kv_len, r, a.Hkv, h, a.cu[r + 1] - start);
-  const int all = a.mask ? a.kept[r * a.Hkv + h] : n;
-  const int m = min(all, cap);
-  if (b == 0 && tid == 0) {
-    a.kv_len_out[r * a.Hkv + h] = m;
-    if (all > cap) { atomicExch(&a.status[0], GVOTE_ERR_WORKSPACE_TOO_SMALL); atomicExch(&a.status[1], 8); }
-  }
+  const int64_t db = (int64_t)h * a.d_row_blocks + gb;
   const int row0 = b * kBlock8;
-  if (row0 >= m) return;
-  const int cnt = min(kBlock8, m - row0);
-  if (!a.mask) {
-    if (tid < cnt) s_src[tid] = row0 + tid;
-    __syncthreads();
-  } else {
+  if (row0 >= cap && b > 0) return;                              // padding entry of the block list
+  const int start = a.cu[r], n = valid_keys(a.kv_len, r, a.Hkv, h, a.cu[r + 1] - start);
+  int cnt;
+  if (a.mask) {
+    const int2 note = row0 < cap ? a.note[db] : make_int2(0, 0);
+    cnt = note.y;
+    if (cnt <= 0) return;
     const int words = (n + 31) >> 5;
     const int64_t woff = (int64_t)h * a.row_words + mask_word_offset(start, r);
-    // the last word whose prefix does not exceed row0 holds that row (prefix[0] = 0 <= row0)
-    int lo = 0, span = words;
-    while (span > 1) {
-      const int step = (span + kStoreThreads - 1) / kStoreThreads;
-      const int at = tid * step;
-      const bool le = at < span && a.prefix[woff + lo + at] <= row0;
-      const int hit = __syncthreads_count(le) - 1;
-      lo += hit * step;
-      span = min(step, span - hit * step);
-    }
-    for (int base = lo;; base += kStoreThreads) {
+    for (int base = note.x;; base += kStoreThreads) {
       const int w = base + tid;
-      int end = 0;
+      int end = cnt;
       if (w < words) {
         uint32_t bits = a.mask[woff + w];
         if (w == words - 1 && (n & 31)) bits &= (1u << (n & 31)) - 1u;
@@ -170,8 +168,18 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
         }
         end = rank;
       }
-      if (__syncthreads_or(end >= cnt || w >= words)) break;     // (ranks grow with the words)
+      if (__syncthreads_or(end >= cnt)) break;                   // (ranks grow with the words)
     }
+  } else {
+    const int m = min(n, cap);
+    if (b == 0 && tid == 0) {
+      a.kv_len_out[r * a.Hkv + h] = m;
+      if (n > cap) { atomicExch(&a.status[0], GVOTE_ERR_WORKSPACE_TOO_SMALL); atomicExch(&a.status[1], 8); }
+    }
+    cnt = min(kBlock8, m - row0);
+    if (cnt <= 0) return;
+    if (tid < cnt) s_src[tid] = row0 + tid;
+    __syncthreads();
   }
   const int dc = a.d_k >> 4;                                     // units per row
   const int units = cnt * dc;
@@ -204,7 +212,6 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
     if ((tid & 31) == 0) s_max[t][tid >> 5] = mx[t];
   }
   __syncthreads();
-  const int64_t db = (int64_t)h * a.d_row_blocks + block8_offset(dstart, r) + b;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     float top = s_max[t][0];
@@ -253,8 +260,8 @@ int32_t run_store(const StoreArgs& a, unsigned ctas, cudaStream_t st) {
 StoreMap store8_map(const gvote_params* p, int32_t batch, int64_t total_tokens) {
   StoreMap m;
   m.prefix = kStatusBytes;
-  m.kept = align_up(m.prefix + (size_t)p->n_kv_heads * gvote_mask_row_words(total_tokens, batch) * 4, 256);
-  m.total = align_up(m.kept + (size_t)p->n_kv_heads * batch * 4, 256);
+  m.note = align_up(m.prefix + (size_t)p->n_kv_heads * gvote_mask_row_words(total_tokens, batch) * 4, 256);
+  m.total = align_up(m.note + (size_t)p->n_kv_heads * gvote_cache8_row_blocks(total_tokens, batch) * 8, 256);
   return m;
 }
 
@@ -263,7 +270,7 @@ int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_
                       int32_t batch, int64_t total_tokens, const gvote_cache8* dst, const SideArrays& side, char* ws,
                       cudaStream_t st) {
   const int Hkv = p->n_kv_heads;
-  const StoreMap m = store8_map(p, batch, total_tokens);
+  const StoreMap m = store8_map(p, batch, total_tokens > dst->total_tokens ? total_tokens : dst->total_tokens);
   StoreArgs a;
   a.src[0] = src8 ? src8->K : (const void*)K;
   a.src[1] = src8 ? src8->V : (const void*)V;
@@ -273,7 +280,7 @@ int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_
   a.s_row_blocks = gvote_cache8_row_blocks(total_tokens, batch);
   a.mask = mask;
   a.prefix = reinterpret_cast<const int32_t*>(ws + m.prefix);
-  a.kept = reinterpret_cast<const int32_t*>(ws + m.kept);
+  a.note = reinterpret_cast<const int2*>(ws + m.note);
   a.cu = cu; a.kv_len = kv_len;
   a.row_words = gvote_mask_row_words(total_tokens, batch);
   a.dst[0] = (uint8_t*)dst->K; a.dst[1] = (uint8_t*)dst->V;
@@ -287,7 +294,7 @@ int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_
   if (mask) {
     LaunchScope scope_("store8_scan_kernel", st);
     launch_on(store8_scan_kernel, dim3(Hkv, batch), dim3(kScan8Threads), 0, st, mask, cu, kv_len, Hkv, a.row_words,
-              (int32_t*)(ws + m.prefix), (int32_t*)(ws + m.kept));
+              (int32_t*)(ws + m.prefix), a.cu8, a.d_row_blocks, (int2*)(ws + m.note), a.kv_len_out, a.status);
     GVOTE_LAUNCH_CHECK("store8_scan_kernel");
   }
   const unsigned ctas = (unsigned)(a.d_row_blocks * Hkv);
