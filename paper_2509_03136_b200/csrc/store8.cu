@@ -106,29 +106,110 @@ struct StoreArgs {
   int Hkv, batch, d_k;
 };
 
-// The value of one 16-element unit as floats: of bf16 (two 16-byte words) or of e4m3 codes times their scale.
+// A unit: 16 consecutive elements of a row, bf16 (two 16-byte words) or e4m3 codes with their row's scale.
+// The arithmetic works on pairs; 25 instructions per element, in 32-bit floats with a test of every element, had made the
+// kernel bound by their issue (37 us for the 12 us of bytes of 17K rows x 8 heads).
 template <bool kSrc8>
-struct Unit {
-  uint4 lo, hi;                  // hi: bf16 only
-  float scale;                   // e4m3 only
-  __device__ __forceinline__ void load(const void* base, int64_t elem, float s) {
-    if (kSrc8) {
-      lo = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + elem));
-      scale = s;
-    } else {
-      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + elem);
-      lo = __ldg(q);
-      hi = __ldg(q + 1);
-    }
+struct Unit;
+
+__device__ __forceinline__ uint32_t half2_abs_max(uint32_t a, uint32_t b) {      // of |a|, |b|; a NaN loses
+  uint32_t d;
+  asm("{\n\t.reg .b32 x, y;\n\tabs.f16x2 x, %1;\n\tabs.f16x2 y, %2;\n\tmax.f16x2 %0, x, y;\n\t}" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+template <>
+struct Unit<false> {
+  uint4 lo, hi;
+  __device__ __forceinline__ void load(const void* base, int64_t elem, float) {
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + elem);
+    lo = __ldg(q);
+    hi = __ldg(q + 1);
   }
-  __device__ __forceinline__ float2 pair(int i) const {        // elements 2 i, 2 i + 1
-    if (kSrc8) {
-      const uint32_t w = (&lo.x)[i >> 1];
-      const float2 f = decode8x2((i & 1) ? (w >> 16) : (w & 0xffffu));
-      return make_float2(f.x * scale, f.y * scale);
+  __device__ __forceinline__ uint32_t word(int i) const { return i < 4 ? (&lo.x)[i] : (&hi.x)[i - 4]; }
+  // The largest finite magnitude.  Magnitudes of bf16 are ordered like their bits; 0x7f80 and above are not finite.
+  __device__ __forceinline__ float largest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, word(i) & 0x7fff7fffu);
+    if ((m & 0xffffu) >= 0x7f80u || (m >> 16) >= 0x7f80u) {      // rare: leave out what is not finite
+      m = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t a = word(i) & 0x7fffu, b = (word(i) >> 16) & 0x7fffu;
+        m = max(m, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
+      }
     }
-    const uint32_t w = i < 4 ? (&lo.x)[i] : (&hi.x)[i - 4];
-    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    return __uint_as_float(max(m & 0xffffu, m >> 16) << 16);
+  }
+  __device__ __forceinline__ uint4 encode(float scale, float inv) const {
+    uint4 out;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t c[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t w = word(2 * q + k);
+        // (an infinity would be stored as 448, a NaN stays one: the NaN code for both)
+        const float x = __uint_as_float(w << 16) * inv, y = __uint_as_float(w & 0xffff0000u) * inv;
+        c[k] = __nv_cvt_float2_to_fp8x2(make_float2(x, y), __NV_SATFINITE, __NV_E4M3);
+        if ((w & 0x7fffu) >= 0x7f80u) c[k] |= 0x7fu;
+        if ((w & 0x7fff0000u) >= 0x7f800000u) c[k] |= 0x7f00u;
+      }
+      (&out.x)[q] = c[0] | (c[1] << 16);
+    }
+    return out;
+  }
+};
+
+template <>
+struct Unit<true> {
+  uint4 lo;
+  float scale;
+  __device__ __forceinline__ void load(const void* base, int64_t elem, float s) {
+    lo = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + elem));
+    scale = s;
+  }
+  __device__ __forceinline__ float largest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t w = (&lo.x)[q];
+      m = half2_abs_max(m, half2_abs_max(decode8x2_half2(w & 0xffffu), decode8x2_half2(w >> 16)));
+    }
+    const __half2 h = *reinterpret_cast<const __half2*>(&m);
+    const float x = __low2float(h), y = __high2float(h), top = fmaxf(x, y);     // (a NaN on both sides of a max stays)
+    return top == top ? finite_abs(top * scale) : 0.f;
+  }
+  // code * 2^j for the block's own scale: the codes themselves where the scales agree; in halves where 2^j is one (exact as
+  // far as e4m3 can tell: a code has 4 significant bits and the least half, 2^-24, lies far below half its least step)
+  __device__ __forceinline__ uint4 encode(float to, float inv) const {
+    if (scale == to) return lo;
+    uint4 out;
+    const float ratio = scale * inv;
+    if (ratio >= 6.103515625e-05f && ratio <= 32768.f) {
+      const __half2 f = __float2half2_rn(ratio);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t w = (&lo.x)[q];
+        uint32_t c[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t h = decode8x2_half2(k ? w >> 16 : w & 0xffffu);
+          const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&h), f);
+          c[k] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(x), __NV_SATFINITE, __NV_E4M3);
+        }
+        (&out.x)[q] = c[0] | (c[1] << 16);
+      }
+      return out;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t w = (&lo.x)[q];
+      const float2 a = decode8x2(w & 0xffffu), b = decode8x2(w >> 16);
+      (&out.x)[q] = encode8x2(a.x * scale * inv, a.y * scale * inv) | (encode8x2(b.x * scale * inv, b.y * scale * inv) << 16);
+    }
+    return out;
   }
 };
 
@@ -184,32 +265,28 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
   const int dc = a.d_k >> 4;                                     // units per row
   const int units = cnt * dc;
   Unit<kSrc8> x[2][kUnits];
+  int64_t to[kUnits];                                            // where each unit goes, or -1
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
     const int u = tid + i * kStoreThreads;
+    to[i] = -1;
     if (u < units) {
       const int j = u / dc, c = u - j * dc, n_src = s_src[j];
       const int64_t off = (int64_t)h * a.s_head + (int64_t)(start + n_src) * a.s_tok + c * 16;
       const int64_t sb = (int64_t)h * a.s_row_blocks + block8_offset(start, r) + (n_src >> 6);
+      to[i] = (int64_t)h * a.d_head + (int64_t)(dstart + row0 + j) * a.d_tok + c * 16;
 #pragma unroll
       for (int t = 0; t < 2; ++t) x[t][i].load(a.src[t], off, kSrc8 ? a.src_scale[t][sb] : 0.f);
     }
   }
-  float mx[2] = {0.f, 0.f};
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
+    float mx = 0.f;
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-      if (tid + i * kStoreThreads < units) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 f = x[t][i].pair(e);
-          mx[t] = fmaxf(mx[t], fmaxf(finite_abs(f.x), finite_abs(f.y)));
-        }
-      }
-    }
-    mx[t] = warp_max(mx[t]);
-    if ((tid & 31) == 0) s_max[t][tid >> 5] = mx[t];
+    for (int i = 0; i < kUnits; ++i)
+      if (to[i] >= 0) mx = fmaxf(mx, x[t][i].largest());
+    mx = warp_max(mx);
+    if ((tid & 31) == 0) s_max[t][tid >> 5] = mx;
   }
   __syncthreads();
 #pragma unroll
@@ -220,20 +297,8 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
     const float scale = scale8_of(top), inv = inverse_pow2(scale);
     if (tid == t) a.dst_scale[t][db] = scale;
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-      const int u = tid + i * kStoreThreads;
-      if (u < units) {
-        const int j = u / dc, c = u - j * dc;
-        uint32_t w[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float2 f0 = x[t][i].pair(2 * q), f1 = x[t][i].pair(2 * q + 1);
-          w[q] = encode8x2(f0.x * inv, f0.y * inv) | (encode8x2(f1.x * inv, f1.y * inv) << 16);
-        }
-        *reinterpret_cast<uint4*>(a.dst[t] + (int64_t)h * a.d_head + (int64_t)(dstart + row0 + j) * a.d_tok + c * 16) =
-            make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
+    for (int i = 0; i < kUnits; ++i)
+      if (to[i] >= 0) *reinterpret_cast<uint4*>(a.dst[t] + to[i]) = x[t][i].encode(scale, inv);
   }
   if (tid < cnt) {
     const int64_t s = (int64_t)h * a.s_total + start + s_src[tid];
