@@ -105,12 +105,6 @@ __device__ __forceinline__ void mma_16816_zero(float (&d)[4], uint32_t a0, uint3
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// Four e4m3 codes -> two pairs of halves (exact).
-__device__ __forceinline__ void widen(uint32_t c, uint32_t& lo, uint32_t& hi) {
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
-      : "=r"(lo), "=r"(hi)
-      : "r"(c));
-}
 // d = part * f + d * g on pairs of 32-bit floats.
 __device__ __forceinline__ void scale_add2(float& d0, float& d1, float p0, float p1, uint64_t f, uint64_t g) {
   asm("{\n\t.reg .b64 d, p;\n\tmov.b64 d, {%0, %1};\n\tmov.b64 p, {%2, %3};\n\tmul.rn.f32x2 d, d, %5;\n\t"
@@ -336,8 +330,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             for (int k = 0; k < 8; ++k) {
               const uint32_t wa = (&ka[k >> 2].x)[k & 3], wb = (&kb[k >> 2].x)[k & 3];
               uint32_t a0, a1, a2, a3;
-              widen(wa, a0, a2);
-              widen(wb, a1, a3);
+              widen8x4(wa, a0, a2);
+              widen8x4(wb, a1, a3);
 #pragma unroll
               for (int rt = 0; rt < kRt; ++rt) {
                 if (y == 0 && k == 0) mma_16816_zero(sT[rt][mt], a0, a1, a2, a3, q[rt][0][0], q[rt][0][1]);
@@ -441,8 +435,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
               for (int i = 0; i < 2; ++i) {
                 const uint32_t lo = __byte_perm(w0, w1, i ? 0x7362 : 0x5140), hi = __byte_perm(w2, w3, i ? 0x7362 : 0x5140);
                 uint32_t a0, a1, a2, a3;
-                widen(lo, a0, a1);
-                widen(hi, a2, a3);
+                widen8x4(lo, a0, a1);
+                widen8x4(hi, a2, a3);
 #pragma unroll
                 for (int rt = 0; rt < kRt; ++rt) {
                   if (mt == 0) mma_16816_zero(part[rt][i], a0, a1, a2, a3, p[rt][0][0], p[rt][0][1]);

@@ -90,9 +90,27 @@ __device__ __forceinline__ float2 decode8x2(uint32_t c) {       // low 16 bits: 
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c, __NV_E4M3);
   return __half22float2(__half2(h));
 }
-__device__ __forceinline__ uint32_t decode8x2_half2(uint32_t c) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c, __NV_E4M3);
-  return (uint32_t)h.x | ((uint32_t)h.y << 16);
+// Four e4m3 codes -> two pairs of halves (exact; the NaN code -> NaN).
+__device__ __forceinline__ void widen8x4(uint32_t c, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(c));
+}
+// Two pairs of halves -> four e4m3 codes (nearest, ties to even; beyond 448: 448; NaN: the NaN code).
+__device__ __forceinline__ uint32_t narrow8x4(uint32_t lo, uint32_t hi) {
+  uint32_t c;
+  asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f16x2 l, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 h, %2;\n\tmov.b32 %0, {l, h};\n\t}"
+      : "=r"(c)
+      : "r"(lo), "r"(hi));
+  return c;
+}
+// The same of four floats.
+__device__ __forceinline__ uint32_t narrow8x4(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
 }
 
 #endif  // __CUDACC__

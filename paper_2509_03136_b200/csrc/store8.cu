@@ -4,13 +4,13 @@
 //   scale_b = the smallest 2^e with max |x| <= 448 * 2^e over the block, code = e4m3(x / scale_b).
 //
 // Two kernels.  store8_scan_kernel turns each (request, head) bit row into an exclusive popcount prefix per
-// mask word, and notes for every destination block the word of its first row and how many rows it gets.
+// mask word, and notes for every destination block what its CTA would otherwise have to look up (struct Note).
 // store8_kernel gives one CTA one destination block of K and of V: its threads list the set bits of a word each from
 // the noted one on, load all rows into registers (16 values per thread and unit, 16-byte loads), take the maximum
 // over the CTA, and write the codes.  Bound by memory: 6 d_k bytes per kept row from bf16, 4 d_k from e4m3; the rows are
 // read once, there is no second pass over them.  What a CTA waits for before it can ask for its rows is two rounds of
-// small loads (the note; words and prefixes): with a search for the first word in its place, five rounds, they cost
-// more than the rows (store of 17K rows x 8 heads 43 instead of 34 us).
+// small loads (the note; words and prefixes); with five rounds, looking the request up and searching for the first
+// word, a call took a third longer.
 // Out of place: nothing orders the blocks, and a pruned 8-bit cache is small.
 #include "cache8.cuh"
 
@@ -20,11 +20,17 @@ namespace {
 constexpr int kStoreThreads = 256;
 constexpr int kScan8Threads = 1024;
 
+// One per (head, destination block), padding entries of the block list included.
+struct __align__(16) Note {
+  int word, cnt, words, row0;    // first mask word (of the request's), rows, mask words that count, first destination row
+  int r, start, dst, pad;        // request, its first source slot and first destination slot
+};
+
 // One CTA per (head, request): prefix[h][word] = kept keys among the n rows that count, before this word.
 __global__ void __launch_bounds__(kScan8Threads)
 store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict__ cu, const int32_t* __restrict__ kv_len,
                    int Hkv, int64_t row_words, int32_t* __restrict__ prefix, const int32_t* __restrict__ cu8,
-                   int64_t row_blocks, int2* __restrict__ note, int32_t* __restrict__ kv_len_out, int32_t* status) {
+                   int64_t row_blocks, Note* __restrict__ note, int32_t* __restrict__ kv_len_out, int32_t* status) {
   __shared__ int warp_tot[kScan8Threads / 32];
   __shared__ int carry;
   const int h = blockIdx.x, r = blockIdx.y;
@@ -32,7 +38,9 @@ store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict_
   const int words = (n + 31) >> 5;
   const int64_t woff = (int64_t)h * row_words + mask_word_offset(start, r);
   const int dstart = cu8[r], cap = cu8[r + 1] - dstart;
-  int2* my_note = note + (int64_t)h * row_blocks + block8_offset(dstart, r);
+  Note* my_note = note + (int64_t)h * row_blocks + block8_offset(dstart, r);
+  const int64_t list_end = r + 1 < (int)gridDim.y ? block8_offset(cu8[r + 1], r + 1) : row_blocks;
+  const int listed = (int)(list_end - block8_offset(dstart, r));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) carry = 0;
   __syncthreads();
@@ -71,7 +79,7 @@ store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict_
       if (w0 + j < words) prefix[woff + w0 + j] = run;
       // the block whose first row is one of this word's
       const int b = (run + kBlock8 - 1) >> 6;
-      if (b * kBlock8 < run + c[j] && b * kBlock8 < cap) my_note[b].x = w0 + j;
+      if (b * kBlock8 < run + c[j] && b * kBlock8 < cap) my_note[b].word = w0 + j;
       run += c[j];
     }
     __syncthreads();
@@ -79,7 +87,12 @@ store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict_
     __syncthreads();
   }
   const int m = min(carry, cap);
-  for (int b = tid; b * kBlock8 < cap; b += kScan8Threads) my_note[b].y = min(kBlock8, m - b * kBlock8);   // (<= 0: no rows)
+  for (int b = tid; b < listed; b += kScan8Threads) {
+    my_note[b].cnt = min(kBlock8, m - b * kBlock8);                // (<= 0: no rows)
+    my_note[b].words = words;
+    my_note[b].row0 = b * kBlock8;
+    *reinterpret_cast<int4*>(&my_note[b].r) = make_int4(r, start, dstart, 0);
+  }
   if (tid == 0) {
     kv_len_out[r * Hkv + h] = m;
     if (carry > cap) { atomicExch(&status[0], GVOTE_ERR_WORKSPACE_TOO_SMALL); atomicExch(&status[1], 8); }
@@ -92,7 +105,7 @@ struct StoreArgs {
   int64_t s_tok, s_head, s_total, s_row_blocks;
   const uint32_t* mask;          // or null: every row
   const int32_t* prefix;
-  const int2* note;              // [Hkv][row_blocks of the destination]
+  const Note* note;              // [Hkv][row_blocks of the destination]
   const int32_t* cu;
   const int32_t* kv_len;
   int64_t row_words;
@@ -144,19 +157,20 @@ struct Unit<false> {
   }
   __device__ __forceinline__ uint4 encode(float scale, float inv) const {
     uint4 out;
+    uint32_t top = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      uint32_t c[2];
+      const uint32_t a = word(2 * q), b = word(2 * q + 1);
+      top = __vmaxu2(top, __vmaxu2(a & 0x7fff7fffu, b & 0x7fff7fffu));
+      (&out.x)[q] = narrow8x4(__uint_as_float(a << 16) * inv, __uint_as_float(a & 0xffff0000u) * inv,
+                              __uint_as_float(b << 16) * inv, __uint_as_float(b & 0xffff0000u) * inv);
+    }
+    if ((top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u) {  // rare: an infinity is not 448 but the NaN code
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t w = word(2 * q + k);
-        // (an infinity would be stored as 448, a NaN stays one: the NaN code for both)
-        const float x = __uint_as_float(w << 16) * inv, y = __uint_as_float(w & 0xffff0000u) * inv;
-        c[k] = __nv_cvt_float2_to_fp8x2(make_float2(x, y), __NV_SATFINITE, __NV_E4M3);
-        if ((w & 0x7fffu) >= 0x7f80u) c[k] |= 0x7fu;
-        if ((w & 0x7fff0000u) >= 0x7f800000u) c[k] |= 0x7f00u;
-      }
-      (&out.x)[q] = c[0] | (c[1] << 16);
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (((word(2 * q + (k >> 1)) >> (16 * (k & 1))) & 0x7fffu) >= 0x7f80u) (&out.x)[q] |= 0x7fu << (8 * k);
     }
     return out;
   }
@@ -174,8 +188,9 @@ struct Unit<true> {
     uint32_t m = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const uint32_t w = (&lo.x)[q];
-      m = half2_abs_max(m, half2_abs_max(decode8x2_half2(w & 0xffffu), decode8x2_half2(w >> 16)));
+      uint32_t a, b;
+      widen8x4((&lo.x)[q], a, b);
+      m = half2_abs_max(m, half2_abs_max(a, b));
     }
     const __half2 h = *reinterpret_cast<const __half2*>(&m);
     const float x = __low2float(h), y = __high2float(h), top = fmaxf(x, y);     // (a NaN on both sides of a max stays)
@@ -191,15 +206,10 @@ struct Unit<true> {
       const __half2 f = __float2half2_rn(ratio);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const uint32_t w = (&lo.x)[q];
-        uint32_t c[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t h = decode8x2_half2(k ? w >> 16 : w & 0xffffu);
-          const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&h), f);
-          c[k] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(x), __NV_SATFINITE, __NV_E4M3);
-        }
-        (&out.x)[q] = c[0] | (c[1] << 16);
+        uint32_t a, b;
+        widen8x4((&lo.x)[q], a, b);
+        const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&a), f), y = __hmul2(*reinterpret_cast<const __half2*>(&b), f);
+        (&out.x)[q] = narrow8x4(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
       }
       return out;
     }
@@ -214,33 +224,26 @@ struct Unit<true> {
 };
 
 template <bool kSrc8, int kUnits>     // kUnits: 16-element units of a block's K (or V) per thread
-__global__ void __launch_bounds__(kStoreThreads)
+__global__ void __launch_bounds__(kStoreThreads, kUnits <= 2 ? 5 : 2)
 store8_kernel(const __grid_constant__ StoreArgs a) {
   __shared__ int s_src[kBlock8];
   __shared__ float s_max[2][kStoreThreads / 32];
   const int tid = threadIdx.x;
   const int h = (int)(blockIdx.x % a.Hkv);
   const int64_t gb = blockIdx.x / a.Hkv;
-  const int r = a.batch == 1 ? 0 : find_request_by(a.cu8, a.batch, gb, 6);
-  const int dstart = a.cu8[r], cap = a.cu8[r + 1] - dstart;
-  const int b = (int)(gb - block8_offset(dstart, r));
   const int64_t db = (int64_t)h * a.d_row_blocks + gb;
-  const int row0 = b * kBlock8;
-  if (row0 >= cap && b > 0) return;                              // padding entry of the block list
-  const int start = a.cu[r], n = valid_keys(a.kv_len, r, a.Hkv, h, a.cu[r + 1] - start);
-  int cnt;
+  int r, start, dstart, row0, cnt;
   if (a.mask) {
-    const int2 note = row0 < cap ? a.note[db] : make_int2(0, 0);
-    cnt = note.y;
+    const int4 note = *reinterpret_cast<const int4*>(&a.note[db]), where = *reinterpret_cast<const int4*>(&a.note[db].r);
+    cnt = note.y; row0 = note.w; r = where.x; start = where.y; dstart = where.z;
     if (cnt <= 0) return;
-    const int words = (n + 31) >> 5;
     const int64_t woff = (int64_t)h * a.row_words + mask_word_offset(start, r);
     for (int base = note.x;; base += kStoreThreads) {
       const int w = base + tid;
       int end = cnt;
-      if (w < words) {
+      if (w < note.z) {
+        // (bits behind the rows that count come after the last of the cnt ranks)
         uint32_t bits = a.mask[woff + w];
-        if (w == words - 1 && (n & 31)) bits &= (1u << (n & 31)) - 1u;
         int rank = a.prefix[woff + w] - row0;
         while (bits && rank < cnt) {
           if (rank >= 0) s_src[rank] = w * 32 + __ffs((int)bits) - 1;
@@ -252,7 +255,12 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
       if (__syncthreads_or(end >= cnt)) break;                   // (ranks grow with the words)
     }
   } else {
-    const int m = min(n, cap);
+    r = a.batch == 1 ? 0 : find_request_by(a.cu8, a.batch, gb, 6);
+    dstart = a.cu8[r];
+    const int cap = a.cu8[r + 1] - dstart, b = (int)(gb - block8_offset(dstart, r));
+    row0 = b * kBlock8;
+    start = a.cu[r];
+    const int n = valid_keys(a.kv_len, r, a.Hkv, h, a.cu[r + 1] - start), m = min(n, cap);
     if (b == 0 && tid == 0) {
       a.kv_len_out[r * a.Hkv + h] = m;
       if (n > cap) { atomicExch(&a.status[0], GVOTE_ERR_WORKSPACE_TOO_SMALL); atomicExch(&a.status[1], 8); }
@@ -262,29 +270,27 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
     if (tid < cnt) s_src[tid] = row0 + tid;
     __syncthreads();
   }
-  const int dc = a.d_k >> 4;                                     // units per row
-  const int units = cnt * dc;
+  // thread = one unit of every (threads / units per row)-th row
+  const int dc = a.d_k >> 4, step = kStoreThreads / dc, j0 = tid / dc, c0 = (tid - j0 * dc) * 16;
+  const int64_t s0 = (int64_t)h * a.s_head + (int64_t)start * a.s_tok + c0;
+  const int64_t d0 = (int64_t)h * a.d_head + (int64_t)(dstart + row0) * a.d_tok + c0;
+  const int64_t sb = (int64_t)h * a.s_row_blocks + block8_offset(start, r);
+  auto holds = [&](int i) { return j0 < step && j0 + i * step < cnt; };
   Unit<kSrc8> x[2][kUnits];
-  int64_t to[kUnits];                                            // where each unit goes, or -1
 #pragma unroll
-  for (int i = 0; i < kUnits; ++i) {
-    const int u = tid + i * kStoreThreads;
-    to[i] = -1;
-    if (u < units) {
-      const int j = u / dc, c = u - j * dc, n_src = s_src[j];
-      const int64_t off = (int64_t)h * a.s_head + (int64_t)(start + n_src) * a.s_tok + c * 16;
-      const int64_t sb = (int64_t)h * a.s_row_blocks + block8_offset(start, r) + (n_src >> 6);
-      to[i] = (int64_t)h * a.d_head + (int64_t)(dstart + row0 + j) * a.d_tok + c * 16;
+  for (int i = 0; i < kUnits; ++i)
+    if (holds(i)) {
+      const int n_src = s_src[j0 + i * step];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) x[t][i].load(a.src[t], off, kSrc8 ? a.src_scale[t][sb] : 0.f);
+      for (int t = 0; t < 2; ++t)
+        x[t][i].load(a.src[t], s0 + n_src * a.s_tok, kSrc8 ? a.src_scale[t][sb + (n_src >> 6)] : 0.f);
     }
-  }
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     float mx = 0.f;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i)
-      if (to[i] >= 0) mx = fmaxf(mx, x[t][i].largest());
+      if (holds(i)) mx = fmaxf(mx, x[t][i].largest());
     mx = warp_max(mx);
     if ((tid & 31) == 0) s_max[t][tid >> 5] = mx;
   }
@@ -298,7 +304,7 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
     if (tid == t) a.dst_scale[t][db] = scale;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i)
-      if (to[i] >= 0) *reinterpret_cast<uint4*>(a.dst[t] + to[i]) = x[t][i].encode(scale, inv);
+      if (holds(i)) *reinterpret_cast<uint4*>(a.dst[t] + d0 + (j0 + i * step) * a.d_tok) = x[t][i].encode(scale, inv);
   }
   if (tid < cnt) {
     const int64_t s = (int64_t)h * a.s_total + start + s_src[tid];
@@ -310,7 +316,7 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
 
 template <bool kSrc8>
 int32_t run_store(const StoreArgs& a, unsigned ctas, cudaStream_t st) {
-  const int units = (int)ceil_div(kBlock8 * (a.d_k >> 4), kStoreThreads);   // 1 .. 4
+  const int units = (int)ceil_div(kBlock8, kStoreThreads / (a.d_k >> 4));   // 1 .. 4
   auto kernel = units == 1 ? store8_kernel<kSrc8, 1> : units == 2 ? store8_kernel<kSrc8, 2> : store8_kernel<kSrc8, 4>;
   {
     LaunchScope scope_("store8_kernel", st);
@@ -326,7 +332,7 @@ StoreMap store8_map(const gvote_params* p, int32_t batch, int64_t total_tokens) 
   StoreMap m;
   m.prefix = kStatusBytes;
   m.note = align_up(m.prefix + (size_t)p->n_kv_heads * gvote_mask_row_words(total_tokens, batch) * 4, 256);
-  m.total = align_up(m.note + (size_t)p->n_kv_heads * gvote_cache8_row_blocks(total_tokens, batch) * 8, 256);
+  m.total = align_up(m.note + (size_t)p->n_kv_heads * gvote_cache8_row_blocks(total_tokens, batch) * sizeof(Note), 256);
   return m;
 }
 
@@ -345,7 +351,7 @@ int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_
   a.s_row_blocks = gvote_cache8_row_blocks(total_tokens, batch);
   a.mask = mask;
   a.prefix = reinterpret_cast<const int32_t*>(ws + m.prefix);
-  a.note = reinterpret_cast<const int2*>(ws + m.note);
+  a.note = reinterpret_cast<const Note*>(ws + m.note);
   a.cu = cu; a.kv_len = kv_len;
   a.row_words = gvote_mask_row_words(total_tokens, batch);
   a.dst[0] = (uint8_t*)dst->K; a.dst[1] = (uint8_t*)dst->V;
@@ -359,7 +365,7 @@ int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_
   if (mask) {
     LaunchScope scope_("store8_scan_kernel", st);
     launch_on(store8_scan_kernel, dim3(Hkv, batch), dim3(kScan8Threads), 0, st, mask, cu, kv_len, Hkv, a.row_words,
-              (int32_t*)(ws + m.prefix), a.cu8, a.d_row_blocks, (int2*)(ws + m.note), a.kv_len_out, a.status);
+              (int32_t*)(ws + m.prefix), a.cu8, a.d_row_blocks, (Note*)(ws + m.note), a.kv_len_out, a.status);
     GVOTE_LAUNCH_CHECK("store8_scan_kernel");
   }
   const unsigned ctas = (unsigned)(a.d_row_blocks * Hkv);
