@@ -16,17 +16,19 @@
 //   O [128 channels x (4 terms, rows)] += V^T P^T   V as it lies, its channels on the M axis; P as a sum of four terms
 // A term is the e4m3 value nearest to what the terms before it left, times 16 per term, and its columns are added up
 // with the matching power of two in 32 bits.  Three terms hold a row of Q to 2^-12 of each entry and 2^-27 of the
-// row's largest (bf16 itself: 2^-8); four hold a weight to 2^-16 of itself and 2^-27 of the largest.  An mma.sync version
-// that widened the codes in registers issued 690 instructions per 32 rows and was bound by their latency (one token over
-// 128K rows x 4 heads: 30 us for the 20 us of bytes; this kernel ~24).
+// row's largest (bf16 itself: 2^-8); four hold a weight to 2^-16 of itself and 2^-24 of the reference.  An mma.sync version
+// that widened the codes in registers issued 690 instructions per 32 rows and was bound by their latency.
 //
 // The scale of K enters the logit; the scale of V goes into the weight: P = 2^(l + log2(scale_v) - ref), ref the largest such
 // exponent so far, so that a block of large values neither overflows nor drowns what carries the output.  ref only moves
-// when it is passed by 2^4 (the accumulated O is then rescaled in tensor memory: mostly the first tile only).
+// when it is passed by 2^6 (the accumulated O is then rescaled in tensor memory: mostly the first tile only).
 //
-// Warp 0 asks for the tiles (TMA boxes of 32 rows, only those that hold rows), warp 1 issues the MMAs, warps 2 and 3
-// prepare the next segment's Q terms, warps 4-7 are the softmax: thread = cached row of the tile (and channel of the output).
-// S is double buffered, and the MMA of tile i+1's S is issued before that of tile i's O.
+// Warps 0 and 2 ask for the tiles of K and of V (TMA, only the 32-row parts that hold rows) into rings of their own - a tile
+// of K is done with as soon as S is there, a tile of V only after the softmax - warp 1 issues the MMAs, whichever has its
+// operands first, and warp 3 prepares the next segment's Q terms; then come up to four softmax groups of four warps,
+// thread = cached row of the tile (and channel of the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each with
+// references and an O of its own (one group alone needs 3000 clocks of latency for a tile, the memory 1400), with many
+// the groups share a tile's rows out.  S and P are buffered as deep as the MMAs run ahead.
 //
 // Weights for the eviction: the logits are kept (4 bytes per row and query, against 2 d_k per row), and the finishing
 // kernel turns them into weights once lse is known; a slot belongs to one thread, so the sum has one order.
@@ -41,11 +43,12 @@ namespace {
 constexpr int kTileKeys = 128;
 constexpr int kBoxRows = 32;
 constexpr int kMaxEntries = 1024;      // entries per launch: their tiles are added up in shared memory
-constexpr int kMaxStages = 6;
-constexpr int kThreads = 256;
+constexpr int kMaxSlots = 8;           // of a ring
+constexpr int kMaxBuffers = 4;         // of S and of P
 constexpr int kSms = 148;
 constexpr float kNoRef = -1e30f;       // a reference before the first logit
-constexpr float kUp = 4.f;             // weights are formed times 2^4: with a slack of 2^4 they stay below 448
+constexpr float kUp = 2.f;             // weights are formed times 2^2, and
+constexpr float kSlack = 6.f;          // a reference may be passed by 2^6: they stay below 448
 
 struct AttendArgs {
   const __nv_bfloat16* Q;
@@ -61,13 +64,13 @@ struct AttendArgs {
   float* lse;            // or null
   const float* acc;
   float* acc_out;        // or null
-  float* part_o;         // [row groups][entries + CTAs][rows of a group][d_k], each divided by its segment's sum
-  float2* part_ml;       // [row groups][entries + CTAs][rows of a group]  (reference, sum), base 2
+  float* part_o;         // [row groups][entries + CTAs][turns][rows of a group][d_k], each divided by its own sum
+  float2* part_ml;       // [row groups][entries + CTAs][turns][rows of a group]  (reference, sum), base 2
   int2* info;            // [row groups][entries]  first and last CTA of the entry (-1: no rows)
   float* logits;         // [Hkv][max_q * G][total] base 2, when acc_out
   int32_t* status;
   int Hkv, G, r0, batch, d_k, max_q;   // requests r0 .. r0 + batch - 1
-  int stages, group_rows;
+  int k_slots, v_slots, group_rows, turns;
   float scale2;          // log2(e) / sqrt(d_k)
 };
 
@@ -90,20 +93,25 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  for (uint32_t i = 0; i < (1u << 22); ++i) {
+  for (uint32_t i = 0; i < (1u << 20); ++i) {
     if (ptx::mbar_try_wait(bar, parity)) return true;
     if ((i & 255u) == 255u && *abort_flag) return false;
   }
   *abort_flag = 1;
   return false;
 }
-// The or of a predicate over the softmax warps (named barrier 1).
-__device__ __forceinline__ bool softmax_any(bool x) {
+// The or of a predicate over the four warps of a softmax group (named barrier `id`).
+__device__ __forceinline__ bool group_any(int id, bool x) {
   uint32_t r;
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.aligned.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r) : "r"((uint32_t)x) : "memory");
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.aligned.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r) : "r"((uint32_t)x), "r"(id) : "memory");
   return r != 0;
+}
+__device__ __forceinline__ float warp_redux_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 // ---- tcgen05.mma kind::f8f6f4, e4m3 operands in shared memory, 32-bit sums
@@ -130,6 +138,12 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
 // Four floats -> the e4m3 codes nearest to them; the floats become 16 times what the codes leave.
 __device__ __forceinline__ uint32_t take_term(float (&x)[4]) {
   const uint32_t c = narrow8x4(x[0], x[1], x[2], x[3]);
@@ -144,69 +158,101 @@ __device__ __forceinline__ uint32_t take_term(float (&x)[4]) {
 }
 
 struct Tail {
-  uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
-  uint64_t q_full[2], q_empty[2], s_full[2], s_empty[2], p_full[2], p_empty[2], o_full, o_empty;
+  uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
+  uint64_t q_full[2], q_empty[2];
+  uint64_t s_full[kMaxBuffers], s_empty[kMaxBuffers], p_full[kMaxBuffers], p_empty[kMaxBuffers], o_full[4], o_empty[4];
   Entry entry[2];
   uint32_t tmem_slot;
-  int any_nan;
+  int any_nan[2][4];                   // [segment parity][turn]
   volatile int abort_flag;
-  int warp_tot[8];
+  int warp_tot[32];
   int pref[kMaxEntries + 1];
 };
 
-template <int kBoxes, int kRows>
-struct Layout {                        // of tensor memory (columns) and shared memory (bytes)
+template <int kBoxes, int kR, int kRb>  // 128-byte boxes per row; query rows of a softmax group; groups that share a tile's rows
+struct Layout {                         // threads, tensor memory (columns), shared memory (bytes)
+  static constexpr int kTurns = kRb == 1 ? 4 : kRb == 2 ? 2 : 1, kGroups = kTurns * kRb, kThreads = 128 + 128 * kGroups;
+  static constexpr int kRows = kR * kRb, kBuffers = kRb <= 2 ? 4 : 2;
   static constexpr int kN1 = (3 * kRows + 15) / 16 * 16, kN2 = 4 * kRows;
-  static constexpr int kCols = 2 * kN1 + kBoxes * kN2;
+  static constexpr int kO = kBuffers * kN1, kCols = kO + kTurns * kBoxes * kN2;     // O of turn i, box y: kO + (i kBoxes + y) kN2
   static constexpr int kAlloc = kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kStage = 2 * kBoxes * kTileKeys * 128, kQ = kBoxes * kN1 * 128, kP = kN2 * kTileKeys;
-  static constexpr int kNan = kRows * kBoxes * 4 * 4;                   // bits [row][channel]
-  static constexpr int kSmall = 4 * 2 * kRows * 4 + 2 * kRows * 8 + kNan;
-  static constexpr size_t fixed() { return (size_t)2 * kQ + 2 * kP + kSmall + sizeof(Tail); }
+  static constexpr int kSlot = kBoxes * kTileKeys * 128, kQ = kBoxes * kN1 * 128, kP = kN2 * kTileKeys;
+  static constexpr int kNanWords = kR * kBoxes * 4;                    // of a group: bits [row][channel]
+  static constexpr int kSmall = kGroups * 4 * 2 * kR * 4 + 2 * kRows * 8 + 2 * kGroups * kNanWords * 4;
+  static constexpr size_t fixed() { return (size_t)2 * kQ + kBuffers * kP + kSmall + sizeof(Tail); }
 };
 
-template <int kBoxes, int kRows>       // 128-byte boxes per row; query rows of a group, padded
-__global__ void __launch_bounds__(kThreads, 1)
+// The tiles of a CTA in order: entries e with tiles, tiles t of the CTA's share, seg and it counting both.
+struct Walk {
+  int e, t, s0, s1, seg, it;
+  const int* pref;
+  int t0, t1, entries;
+  __device__ __forceinline__ Walk(const int* pref_, int t0_, int t1_, int entries_, int e_first)
+      : e(e_first), seg(0), it(0), pref(pref_), t0(t0_), t1(t1_), entries(entries_) { enter(); }
+  __device__ __forceinline__ bool done() const { return e >= entries || pref[e] >= t1; }
+  __device__ __forceinline__ void enter() {
+    while (!done() && pref[e + 1] == pref[e]) ++e;
+    if (done()) return;
+    s0 = max(t0, pref[e]);
+    s1 = min(t1, pref[e + 1]);
+    t = s0;
+  }
+  __device__ __forceinline__ void next_segment() { it += s1 - t; ++e; ++seg; enter(); }
+  __device__ __forceinline__ void next_tile() {
+    ++it;
+    if (++t == s1) { ++e; ++seg; enter(); }
+  }
+};
+
+template <int kBoxes, int kR, int kRb>
+__global__ void __launch_bounds__((Layout<kBoxes, kR, kRb>::kThreads), 1)
 attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+               const __grid_constant__ CUtensorMap tmKp, const __grid_constant__ CUtensorMap tmVp,
                const __grid_constant__ AttendArgs a) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  using L = Layout<kBoxes, kRows>;
-  uint8_t* ring = smem;                                                // [stage][K boxes, V boxes][128 rows][128]
-  uint8_t* q_sm = ring + (size_t)a.stages * L::kStage;                 // [2][box][N1 rows][128], swizzled
-  uint8_t* p_sm = q_sm + 2 * L::kQ;                                    // [2][N2 / 16][128 keys][16]
-  float* red_sm = reinterpret_cast<float*>(p_sm + 2 * L::kP);          // [4 warps][2 kRows]
-  float* factor_sm = red_sm + 4 * 2 * kRows;                           // [2][kRows] logit per unit of product
-  int* limit_sm = reinterpret_cast<int*>(factor_sm + 2 * kRows);       // [2][kRows] cached rows a query row sees
-  uint32_t* nan_sm = reinterpret_cast<uint32_t*>(limit_sm + 2 * kRows);
-  Tail* tail = reinterpret_cast<Tail*>(nan_sm + L::kNan / 4);
+  using L = Layout<kBoxes, kR, kRb>;
+  uint8_t* k_ring = smem;                                              // [slot][box][128 rows][128], swizzled
+  uint8_t* v_ring = k_ring + (size_t)a.k_slots * L::kSlot;
+  uint8_t* q_sm = v_ring + (size_t)a.v_slots * L::kSlot;               // [2][box][N1 rows][128], swizzled
+  uint8_t* p_sm = q_sm + 2 * L::kQ;                                    // [buffer][N2 / 16][128 keys][16]
+  float* red_all = reinterpret_cast<float*>(p_sm + L::kBuffers * L::kP);   // [group][4 warps][2 kR]
+  float* factor_sm = red_all + L::kGroups * 4 * 2 * kR;                // [2][kRows] logit per unit of product
+  int* limit_sm = reinterpret_cast<int*>(factor_sm + 2 * L::kRows);    // [2][kRows] cached rows a query row sees
+  uint32_t* nan_all = reinterpret_cast<uint32_t*>(limit_sm + 2 * L::kRows);   // [2][group][kR][boxes * 4]
+  Tail* tail = reinterpret_cast<Tail*>(nan_all + 2 * L::kGroups * L::kNanWords);
   int* pref = tail->pref;
   volatile int* abort_flag = &tail->abort_flag;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int entries = a.batch * a.Hkv;
-  const int group0 = blockIdx.y * a.group_rows;                        // first query row of this group
+  const int group0 = blockIdx.y * a.group_rows;                        // first query row of this row group
 
   if (tid == 0) {
-    for (int s = 0; s < kMaxStages; ++s) { ptx::mbar_init(&tail->kv_full[s], 1); ptx::mbar_init(&tail->kv_empty[s], 1); }
-    for (int b = 0; b < 2; ++b) {
-      ptx::mbar_init(&tail->q_full[b], 2); ptx::mbar_init(&tail->q_empty[b], 5);
-      ptx::mbar_init(&tail->s_full[b], 1); ptx::mbar_init(&tail->s_empty[b], 4);
-      ptx::mbar_init(&tail->p_full[b], 4); ptx::mbar_init(&tail->p_empty[b], 1);
+    for (int s = 0; s < kMaxSlots; ++s) {
+      ptx::mbar_init(&tail->k_full[s], 1); ptx::mbar_init(&tail->k_empty[s], 1);
+      ptx::mbar_init(&tail->v_full[s], 1); ptx::mbar_init(&tail->v_empty[s], 1);
     }
-    ptx::mbar_init(&tail->o_full, 1); ptx::mbar_init(&tail->o_empty, 4);
+    for (int b = 0; b < 2; ++b) { ptx::mbar_init(&tail->q_full[b], 1); ptx::mbar_init(&tail->q_empty[b], 1 + 4 * L::kGroups); }
+    for (int b = 0; b < kMaxBuffers; ++b) {
+      ptx::mbar_init(&tail->s_full[b], 1); ptx::mbar_init(&tail->s_empty[b], 4 * kRb);
+      ptx::mbar_init(&tail->p_full[b], 4 * kRb); ptx::mbar_init(&tail->p_empty[b], 1);
+    }
+    for (int b = 0; b < 4; ++b) {
+      ptx::mbar_init(&tail->o_full[b], 1); ptx::mbar_init(&tail->o_empty[b], 4 * kRb);
+      tail->any_nan[0][b] = tail->any_nan[1][b] = 0;
+    }
     tail->abort_flag = (ptx::smem_u32(smem) & 1023u) ? 1 : 0;
-    tail->any_nan = 0;
     ptx::fence_barrier_init();
     ptx::prefetch_tensormap(&tmK);
     ptx::prefetch_tensormap(&tmV);
   }
-  for (int i = tid; i < L::kNan / 4; i += kThreads) nan_sm[i] = 0;
+  for (int i = tid; i < 2 * L::kGroups * L::kNanWords; i += L::kThreads) nan_all[i] = 0;
   if (warp == 1) {
     ptx::tmem_alloc(&tail->tmem_slot, L::kAlloc);
     ptx::tmem_relinquish();
   }
   // ---- tiles before each entry
   {
-    const int per = (entries + kThreads - 1) / kThreads;               // consecutive entries per thread
+    const int per = (entries + L::kThreads - 1) / L::kThreads;         // consecutive entries per thread
     const int e0 = min(tid * per, entries), e1 = min(e0 + per, entries);
     int mine = 0;
     for (int e = e0; e < e1; ++e) {
@@ -237,7 +283,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   // which CTAs hold an entry: the CTA of tile t is the largest c with T c / B <= t
   if (b == 0) {
     int2* info = a.info + (int64_t)blockIdx.y * entries;
-    for (int e = tid; e < entries; e += kThreads) {
+    for (int e = tid; e < entries; e += L::kThreads) {
       const int f = pref[e], l = pref[e + 1] - 1;
       int2 v = make_int2(-1, -1);
       if (l >= f) v = make_int2((int)((((int64_t)f + 1) * B - 1) / T), (int)((((int64_t)l + 1) * B - 1) / T));
@@ -252,249 +298,300 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       if (pref[mid + 1] <= t0) e_first = mid + 1; else hi = mid;
     }
   }
+  Walk at(pref, t0, t1, entries, e_first);
   bool ok = true;
 
-  if (warp == 0) {
-    // ------------------------------------------------------------------ TMA producer
+  if (warp == 0 || warp == 2) {
+    // ------------------------------------------------------------------ TMA producers: K, V
     if (lane == 0) {
-      int it = 0;
-      for (int e = e_first; ok && e < entries && pref[e] < t1; ++e) {
-        if (pref[e + 1] == pref[e]) continue;
-        const Entry x = entry_of(a, e);
-        const int s1 = min(t1, pref[e + 1]);
-        for (int t = max(t0, pref[e]); t < s1; ++t, ++it) {
-          const int s = it % a.stages, key0 = (t - pref[e]) * kTileKeys;
-          ok = wait_or_abort(&tail->kv_empty[s], ((it / a.stages) & 1) ^ 1, abort_flag);
+      const bool is_k = warp == 0;
+      const CUtensorMap* whole_map = is_k ? &tmK : &tmV;
+      const CUtensorMap* part_map = is_k ? &tmKp : &tmVp;
+      uint8_t* ring = is_k ? k_ring : v_ring;
+      uint64_t* full = is_k ? tail->k_full : tail->v_full;
+      uint64_t* empty = is_k ? tail->k_empty : tail->v_empty;
+      const int slots = is_k ? a.k_slots : a.v_slots;
+      int s = 0;
+      uint32_t phase = 0;
+      for (; ok && !at.done(); at.next_segment()) {
+        const Entry x = entry_of(a, at.e);
+        for (int t = at.s0; t < at.s1; ++t) {
+          const int key0 = (t - pref[at.e]) * kTileKeys;
+          ok = wait_or_abort(&empty[s], phase ^ 1u, abort_flag);
           if (!ok) break;
+          uint8_t* dst = ring + (size_t)s * L::kSlot;
           const int parts = min(kTileKeys / kBoxRows, (x.n - key0 + kBoxRows - 1) / kBoxRows);
-          ptx::mbar_arrive_expect_tx(&tail->kv_full[s], (uint32_t)parts * 2 * kBoxes * kBoxRows * 128);
-          uint8_t* dst = ring + (size_t)s * L::kStage;
-          for (int g = 0; g < parts; ++g)
+          ptx::mbar_arrive_expect_tx(&full[s], (uint32_t)parts * kBoxes * kBoxRows * 128);
 #pragma unroll
-            for (int y = 0; y < kBoxes; ++y)
-              ptx::tma_load_3d(dst + (y * kTileKeys + g * kBoxRows) * 128, &tmK, &tail->kv_full[s], y * 128, x.start + key0 + g * kBoxRows, x.h);
-          for (int g = 0; g < parts; ++g)
-#pragma unroll
-            for (int y = 0; y < kBoxes; ++y)
-              ptx::tma_load_3d(dst + ((kBoxes + y) * kTileKeys + g * kBoxRows) * 128, &tmV, &tail->kv_full[s], y * 128, x.start + key0 + g * kBoxRows, x.h);
+          for (int y = 0; y < kBoxes; ++y) {
+            if (parts == kTileKeys / kBoxRows) {
+              ptx::tma_load_3d(dst + y * kTileKeys * 128, whole_map, &full[s], y * 128, x.start + key0, x.h);
+            } else {
+              for (int g = 0; g < parts; ++g)
+                ptx::tma_load_3d(dst + (y * kTileKeys + g * kBoxRows) * 128, part_map, &full[s], y * 128, x.start + key0 + g * kBoxRows, x.h);
+            }
+          }
+          if (++s == slots) { s = 0; phase ^= 1u; }
         }
       }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
+    // S of the next tile, or O of the oldest tile whose weights are there: whichever can be issued.  (Taken in a fixed
+    // order, a tile's V waited for the arrival of the third K after it, and the rings stood half empty.)
     const uint32_t idesc1 = instr_desc_e4m3(kTileKeys, L::kN1, false, false), idesc2 = instr_desc_e4m3(128, L::kN2, true, true);
     const int ksteps = (a.d_k + 31) / 32;
-    int it = 0, seg = 0;
-    struct { int it, seg; bool first, last, valid; } prev = {0, 0, false, false, false};
-    auto second = [&]() {                                              // O of the tile before
-      const int s = prev.it % a.stages, pb = prev.it & 1;
-      ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->p_full[pb], (prev.it >> 1) & 1, abort_flag));
-      if (ok && prev.first) ok = __all_sync(0xffffffffu, wait_or_abort(&tail->o_empty, (prev.seg & 1) ^ 1, abort_flag));
-      if (!ok) return;
-      ptx::tc_fence_after_sync();
-      if (ptx::elect_one()) {
-        const uint64_t pd = smem_desc_mn_plain(ptx::smem_u32(p_sm) + (uint32_t)pb * L::kP, 16 * kTileKeys);
+    Walk behind(pref, t0, t1, entries, e_first);
+    uint32_t o_uses = 0;                                               // bit i: parity of the uses of turn i's O
+    int ks = 0, vs = 0;                                                // ring slots and their phases
+    uint32_t k_phase = 0, v_phase = 0, polls = 0;
+    auto ready = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_test_wait(bar, parity)); };
+    while (ok && !behind.done()) {
+      bool moved = false;
+      if (!at.done()) {
+        const int sb = at.it % L::kBuffers, qb = at.seg & 1;
+        if (ready(&tail->s_empty[sb], ((at.it / L::kBuffers) & 1) ^ 1) && (at.t > at.s0 || ready(&tail->q_full[qb], (at.seg >> 1) & 1)) &&
+            ready(&tail->k_full[ks], k_phase)) {
+          ptx::tc_fence_after_sync();
+          if (ptx::elect_one()) {
 #pragma unroll
-        for (int y = 0; y < kBoxes; ++y) {
-          const uint64_t vd = ptx::smem_desc_k_sw128(ptx::smem_u32(ring) + (uint32_t)(s * L::kStage + (kBoxes + y) * kTileKeys * 128));
+            for (int y = 0; y < kBoxes; ++y) {
+              const uint64_t kd = ptx::smem_desc_k_sw128(ptx::smem_u32(k_ring) + (uint32_t)(ks * L::kSlot + y * kTileKeys * 128));
+              const uint64_t qd = ptx::smem_desc_k_sw128(ptx::smem_u32(q_sm) + (uint32_t)(qb * L::kQ + y * L::kN1 * 128));
 #pragma unroll
-          for (int k = 0; k < kTileKeys / 32; ++k)                     // 32 keys: 4 KB of V, 512 bytes of P
-            umma_e4m3(tmem + (uint32_t)(2 * L::kN1 + y * L::kN2), vd + (uint64_t)(k * (32 * 128 / 16)), pd + (uint64_t)(k * (32 * 16 / 16)),
-                      idesc2, prev.first && k == 0 ? 0u : 1u);
-        }
-        ptx::umma_commit(&tail->p_empty[pb]);
-        ptx::umma_commit(&tail->kv_empty[s]);
-        if (prev.last) ptx::umma_commit(&tail->o_full);
-      }
-      __syncwarp();
-    };
-    for (int e = e_first; ok && e < entries && pref[e] < t1; ++e) {
-      if (pref[e + 1] == pref[e]) continue;
-      const int s0 = max(t0, pref[e]), s1 = min(t1, pref[e + 1]), qb = seg & 1;
-      for (int t = s0; ok && t < s1; ++t, ++it) {
-        const int s = it % a.stages, sb = it & 1;
-        ok = __all_sync(0xffffffffu, wait_or_abort(&tail->kv_full[s], (it / a.stages) & 1, abort_flag));
-        if (ok && t == s0) ok = __all_sync(0xffffffffu, wait_or_abort(&tail->q_full[qb], (seg >> 1) & 1, abort_flag));
-        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->s_empty[sb], ((it >> 1) & 1) ^ 1, abort_flag));
-        if (!ok) break;
-        ptx::tc_fence_after_sync();
-        if (ptx::elect_one()) {
-#pragma unroll
-          for (int y = 0; y < kBoxes; ++y) {
-            const uint64_t kd = ptx::smem_desc_k_sw128(ptx::smem_u32(ring) + (uint32_t)(s * L::kStage + y * kTileKeys * 128));
-            const uint64_t qd = ptx::smem_desc_k_sw128(ptx::smem_u32(q_sm) + (uint32_t)(qb * L::kQ + y * L::kN1 * 128));
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (y * 4 + k < ksteps)
-                umma_e4m3(tmem + (uint32_t)(sb * L::kN1), kd + 2 * k, qd + 2 * k, idesc1, y + k > 0 ? 1u : 0u);
+              for (int k = 0; k < 4; ++k)
+                if (y * 4 + k < ksteps)
+                  umma_e4m3(tmem + (uint32_t)(sb * L::kN1), kd + 2 * k, qd + 2 * k, idesc1, y + k > 0 ? 1u : 0u);
+            }
+            ptx::umma_commit(&tail->s_full[sb]);
+            ptx::umma_commit(&tail->k_empty[ks]);
+            if (at.t == at.s1 - 1) ptx::umma_commit(&tail->q_empty[qb]);
           }
-          ptx::umma_commit(&tail->s_full[sb]);
-          if (t == s1 - 1) ptx::umma_commit(&tail->q_empty[qb]);
+          __syncwarp();
+          at.next_tile();
+          if (++ks == a.k_slots) { ks = 0; k_phase ^= 1u; }
+          moved = true;
         }
-        __syncwarp();
-        if (prev.valid) second();
-        prev = {it, seg, t == s0, t == s1 - 1, true};
       }
-      ++seg;
+      if (behind.it < at.it) {
+        const int pb = behind.it % L::kBuffers, turn = behind.it % L::kTurns;
+        const bool first = behind.t - behind.s0 < L::kTurns, last = behind.t + L::kTurns >= behind.s1;
+        if (ready(&tail->p_full[pb], (behind.it / L::kBuffers) & 1) && ready(&tail->v_full[vs], v_phase) &&
+            (!first || ready(&tail->o_empty[turn], ((o_uses >> turn) & 1) ^ 1))) {
+          if (first) o_uses ^= 1u << turn;
+          ptx::tc_fence_after_sync();
+          if (ptx::elect_one()) {
+            const uint64_t pd = smem_desc_mn_plain(ptx::smem_u32(p_sm) + (uint32_t)pb * L::kP, 16 * kTileKeys);
+#pragma unroll
+            for (int y = 0; y < kBoxes; ++y) {
+              const uint64_t vd = ptx::smem_desc_k_sw128(ptx::smem_u32(v_ring) + (uint32_t)(vs * L::kSlot + y * kTileKeys * 128));
+#pragma unroll
+              for (int k = 0; k < kTileKeys / 32; ++k)                 // 32 keys: 4 KB of V, 512 bytes of P
+                umma_e4m3(tmem + (uint32_t)(L::kO + (turn * kBoxes + y) * L::kN2), vd + (uint64_t)(k * (32 * 128 / 16)),
+                          pd + (uint64_t)(k * (32 * 16 / 16)), idesc2, first && k == 0 ? 0u : 1u);
+            }
+            ptx::umma_commit(&tail->p_empty[pb]);
+            ptx::umma_commit(&tail->v_empty[vs]);
+            if (last) ptx::umma_commit(&tail->o_full[turn]);
+          }
+          __syncwarp();
+          behind.next_tile();
+          if (++vs == a.v_slots) { vs = 0; v_phase ^= 1u; }
+          moved = true;
+        }
+      }
+      if (moved) {
+        polls = 0;
+      } else if (++polls > (1u << 24) || ((polls & 255u) == 255u && *abort_flag)) {
+        *abort_flag = 1;
+        ok = false;
+      }
     }
-    if (ok && prev.valid) second();
-  } else if (warp < 4) {
+  } else if (warp == 3) {
     // ------------------------------------------------------------------ Q as three e4m3 terms, a segment ahead
-    int seg = 0;
-    for (int e = e_first; ok && e < entries && pref[e] < t1; ++e) {
-      if (pref[e + 1] == pref[e]) continue;
-      const int qb = seg & 1;
-      const Entry x = entry_of(a, e);
+    for (int i = lane; i < 2 * kBoxes * (L::kN1 - 3 * L::kRows) * 8; i += 32) {     // the rows behind the last term are zero
+      constexpr int kPer = (L::kN1 - 3 * L::kRows) * 8 > 0 ? (L::kN1 - 3 * L::kRows) * 8 : 1;
+      *reinterpret_cast<uint4*>(q_sm + (i / kPer) * L::kN1 * 128 + 3 * L::kRows * 128 + (i % kPer) * 16) = make_uint4(0, 0, 0, 0);
+    }
+    for (; ok && !at.done(); at.next_segment()) {
+      const int qb = at.seg & 1;
+      const Entry x = entry_of(a, at.e);
       const int rows = x.nq * a.G;
-      ok = __all_sync(0xffffffffu, wait_or_abort(&tail->q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag));
+      ok = __all_sync(0xffffffffu, wait_or_abort(&tail->q_empty[qb], ((at.seg >> 1) & 1) ^ 1, abort_flag));
       if (!ok) break;
       uint8_t* dst = q_sm + qb * L::kQ;
-      for (int row = warp - 2; row < (L::kN1 - 2 * kRows); row += 2) {  // the rows, then the padding behind the third term
-        const int qrow = group0 + row;
-        const bool holds = row < kRows && qrow < rows;
-        const int token = holds ? qrow / a.G : 0, g = holds ? qrow - token * a.G : 0;
-        const __nv_bfloat16* src = a.Q + (int64_t)(x.q0 + token) * a.q_tok + (int64_t)(x.h * a.G + g) * a.q_head;
-        uint2 v[kBoxes];
-        uint32_t top = 0;                                              // the largest magnitude's bits
+#pragma unroll 1
+      for (int rb = 0; rb < kRb; ++rb) {
+        uint2 v[kR][kBoxes];                                           // all of a group's rows on their way at once
 #pragma unroll
-        for (int y = 0; y < kBoxes; ++y) {
-          const int d = y * 128 + lane * 4;
-          v[y] = holds && d < a.d_k ? *reinterpret_cast<const uint2*>(src + d) : make_uint2(0, 0);
-          const uint32_t m = __vmaxu2(v[y].x & 0x7fff7fffu, v[y].y & 0x7fff7fffu);
-          top = max(top, max(m & 0xffffu, m >> 16));
-        }
+        for (int i = 0; i < kR; ++i) {
+          const int qrow = group0 + rb * kR + i;
+          const bool holds = qrow < rows;
+          const int token = holds ? qrow / a.G : 0, g = holds ? qrow - token * a.G : 0;
+          const __nv_bfloat16* src = a.Q + (int64_t)(x.q0 + token) * a.q_tok + (int64_t)(x.h * a.G + g) * a.q_head;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        // entries up to 2^8: multiply by 2^(7 - exponent); the exponent is kept where both factors are normal numbers
-        const int ex = min(max((int)(top >> 7) - 127, -100), 127);
-        const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
-#pragma unroll
-        for (int y = 0; y < kBoxes; ++y) {
-          float f[4] = {__uint_as_float(v[y].x << 16) * up, __uint_as_float(v[y].x & 0xffff0000u) * up,
-                        __uint_as_float(v[y].y << 16) * up, __uint_as_float(v[y].y & 0xffff0000u) * up};
-          if (top >= 0x7f80u) {                                        // an infinity is no 448: NaN, like a NaN
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = fabsf(f[i]) <= 3.4e38f ? f[i] : __uint_as_float(0x7fffffffu);
-          }
-#pragma unroll
-          for (int term = 0; term < 3; ++term) {
-            const int n = row < kRows ? term * kRows + row : 2 * kRows + row;
-            const uint32_t c = take_term(f);
-            if (row < kRows || term == 0)
-              *reinterpret_cast<uint32_t*>(dst + (y * L::kN1 + n) * 128 + (((lane >> 2) ^ (n & 7)) << 4) + (lane & 3) * 4) = c;
+          for (int y = 0; y < kBoxes; ++y) {
+            const int d = y * 128 + lane * 4;
+            v[i][y] = holds && d < a.d_k ? *reinterpret_cast<const uint2*>(src + d) : make_uint2(0, 0);
           }
         }
-        if (lane == 0 && row < kRows) {
-          factor_sm[qb * kRows + row] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale2;
-          limit_sm[qb * kRows + row] = holds ? x.n - (x.nq - 1 - token) : 0;
+#pragma unroll
+        for (int i = 0; i < kR; ++i) {
+          const int row = rb * kR + i, qrow = group0 + row;
+          uint32_t top = 0;                                            // the largest magnitude's bits
+#pragma unroll
+          for (int y = 0; y < kBoxes; ++y) {
+            const uint32_t m = __vmaxu2(v[i][y].x & 0x7fff7fffu, v[i][y].y & 0x7fff7fffu);
+            top = max(top, max(m & 0xffffu, m >> 16));
+          }
+          top = __reduce_max_sync(0xffffffffu, top);
+          // entries up to 2^8: multiply by 2^(7 - exponent); the exponent is kept where both factors are normal numbers
+          const int ex = min(max((int)(top >> 7) - 127, -100), 127);
+          const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+#pragma unroll
+          for (int y = 0; y < kBoxes; ++y) {
+            const uint2 u = v[i][y];
+            float f[4] = {__uint_as_float(u.x << 16) * up, __uint_as_float(u.x & 0xffff0000u) * up,
+                          __uint_as_float(u.y << 16) * up, __uint_as_float(u.y & 0xffff0000u) * up};
+            if (top >= 0x7f80u) {                                      // an infinity is no 448: NaN, like a NaN
+#pragma unroll
+              for (int k = 0; k < 4; ++k) f[k] = fabsf(f[k]) <= 3.4e38f ? f[k] : __uint_as_float(0x7fffffffu);
+            }
+#pragma unroll
+            for (int term = 0; term < 3; ++term) {
+              const int n = rb * 3 * kR + term * kR + i;               // groups one after the other, a group's rows term by term
+              *reinterpret_cast<uint32_t*>(dst + (y * L::kN1 + n) * 128 + (((lane >> 2) ^ (n & 7)) << 4) + (lane & 3) * 4) = take_term(f);
+            }
+          }
+          if (lane == 0) {
+            factor_sm[qb * L::kRows + row] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale2;
+            limit_sm[qb * L::kRows + row] = qrow < rows ? x.n - (x.nq - 1 - qrow / a.G) : 0;
+          }
         }
       }
-      if (warp == 2 && lane == 0) tail->entry[qb] = x;
+      if (lane == 0) tail->entry[qb] = x;
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&tail->q_full[qb]);
-      ++seg;
     }
   } else {
     // ------------------------------------------------------------------ softmax: thread = row of the tile, channel of O
-    const int w = warp - 4, key_in = w * 32 + lane;
+    const int group = (warp - 4) >> 2, turn = group / kRb, rb = group % kRb, bar_id = 1 + group;
+    const int w = warp & 3, key_in = w * 32 + lane;
     const uint32_t lane_addr = tmem + ((uint32_t)(w * 32) << 16);
-    float refd[kRows], refn[kRows], sum[kRows];                        // of the logits; of the weights times scale_v
-    int it = 0, seg = 0;
-    for (int e = e_first; e < entries && pref[e] < t1; ++e) {
-      if (pref[e + 1] == pref[e]) continue;
-      const int s0 = max(t0, pref[e]), s1 = min(t1, pref[e + 1]), qb = seg & 1;
-      ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->q_full[qb], (seg >> 1) & 1, abort_flag));
+    const uint32_t o_addr = lane_addr + (uint32_t)(L::kO + turn * kBoxes * L::kN2 + rb * 4 * kR);
+    float* red_sm = red_all + group * 4 * 2 * kR;
+    float refd[kR], refn[kR], sum[kR];                                 // of the logits; of the weights times scale_v
+    int o_uses = 0;
+    for (; !at.done(); at.next_segment()) {
+      const int qb = at.seg & 1, e = at.e, s0 = at.s0, s1 = at.s1;
+      ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->q_full[qb], (at.seg >> 1) & 1, abort_flag));
       const Entry x = tail->entry[qb];
-      const int nrows = min(kRows, x.nq * a.G - group0), all_see = x.n - (x.nq - 1);
+      const int row0 = group0 + rb * kR, nrows = min(kR, x.nq * a.G - row0), all_see = x.n - (x.nq - 1);
+      const float* factor = factor_sm + qb * L::kRows + rb * kR;
+      const int* limit = limit_sm + qb * L::kRows + rb * kR;
 #pragma unroll
-      for (int g = 0; g < kRows; ++g) { refd[g] = refn[g] = kNoRef; sum[g] = 0.f; }
+      for (int g = 0; g < kR; ++g) { refd[g] = refn[g] = kNoRef; sum[g] = 0.f; }
+      uint32_t* nan_sm = nan_all + (qb * L::kGroups + turn * kRb) * L::kNanWords;       // of the groups that share my tiles
+      if (rb == 0 && x.nq > 1) {                                       // (the marks of two segments ago have been read)
+        for (int i = key_in; i < kRb * L::kNanWords; i += 128) nan_sm[i] = 0;
+        if (key_in == 0) tail->any_nan[qb][turn] = 0;
+        group_any(bar_id, false);
+      }
       const int64_t sb0 = (int64_t)x.h * a.row_blocks + block8_offset(x.start, x.r);
       auto scales = [&](int t) {
         const int key = (t - pref[e]) * kTileKeys + key_in;
         return key < x.n ? make_float2(a.k_scale[sb0 + (key >> 6)], a.v_scale[sb0 + (key >> 6)]) : make_float2(0.f, 1.f);
       };
-      float2 next_scale = ok ? scales(s0) : make_float2(0.f, 1.f);
-      for (int t = s0; t < s1; ++t, ++it) {
-        const int sb = it & 1, key0 = (t - pref[e]) * kTileKeys, key = key0 + key_in;
+      // Tile it is turn it mod kTurns', and buffer it mod kBuffers is always the same turn's: a group meets every phase of
+      // the barriers that it waits on (by parity, a wait for a phase passes while the one before it is still open).
+      const int first = s0 + (turn + L::kTurns - at.it % L::kTurns) % L::kTurns;
+      const bool any_tile = first < s1;
+      float2 next_scale = ok && any_tile ? scales(first) : make_float2(0.f, 1.f);
+      for (int t = first; t < s1; t += L::kTurns) {
+        const int it = at.it + t - s0, sb = it % L::kBuffers, phase = (it / L::kBuffers) & 1;
+        const int key0 = (t - pref[e]) * kTileKeys, key = key0 + key_in;
         const float2 sc = next_scale;
-        if (ok && t + 1 < s1) next_scale = scales(t + 1);
-        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->s_full[sb], (it >> 1) & 1, abort_flag));
-        float l[kRows];
-        const float lv = log2f(sc.y);                                  // (a power of two: exact)
+        if (ok && t + L::kTurns < s1) next_scale = scales(t + L::kTurns);
+        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->s_full[sb], phase, abort_flag));
+        float l[kR];
+        const float lv = (float)((int)(__float_as_uint(sc.y) >> 23) - 127);     // log2 of a power of two
         bool over = false;
         if (ok) {
           ptx::tc_fence_after_sync();
-          uint32_t c[L::kN1 / 16][16];
-#pragma unroll
-          for (int i = 0; i < L::kN1 / 16; ++i) ptx::tmem_ld_32x16(lane_addr + (uint32_t)(sb * L::kN1 + i * 16), c[i]);
+          uint32_t c[kR == 4 ? 16 : 24];
+          const uint32_t s_addr = lane_addr + (uint32_t)(sb * L::kN1 + rb * 3 * kR);
+          ptx::tmem_ld_32x16(s_addr, *reinterpret_cast<uint32_t(*)[16]>(&c[0]));
+          if (kR == 8) tmem_ld_32x8(s_addr + 16, &c[kR == 4 ? 0 : 16]);
           ptx::tmem_wait_ld();
           ptx::tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(&tail->s_empty[sb]);
           const bool edge = key0 + kTileKeys > all_see;
 #pragma unroll
-          for (int g = 0; g < kRows; ++g) {
-            auto term = [&](int k) { return __uint_as_float(c[(k * kRows + g) / 16][(k * kRows + g) % 16]); };
-            l[g] = fmaf(term(2), 0.00390625f, fmaf(term(1), 0.0625f, term(0))) * (sc.x * factor_sm[qb * kRows + g]);
-            if (edge && key >= limit_sm[qb * kRows + g]) l[g] = -INFINITY;
-            over = over || l[g] + lv > refn[g] + kUp || l[g] > refd[g] + 64.f;
+          for (int g = 0; g < kR; ++g) {
+            auto term = [&](int k) { return __uint_as_float(c[k * kR + g]); };
+            l[g] = fmaf(term(2), 0.00390625f, fmaf(term(1), 0.0625f, term(0))) * (sc.x * factor[g]);
+            if (edge && key >= limit[g]) l[g] = -INFINITY;
+            over = over || l[g] + lv > refn[g] + kSlack || l[g] > refd[g] + 64.f;
           }
           if (a.logits && key < x.n) {
-            float* dst = a.logits + ((int64_t)x.h * a.max_q * a.G + group0) * a.total + x.start + key;
+            float* dst = a.logits + ((int64_t)x.h * a.max_q * a.G + row0) * a.total + x.start + key;
 #pragma unroll
-            for (int g = 0; g < kRows; ++g)
+            for (int g = 0; g < kR; ++g)
               if (g < nrows) dst[(int64_t)g * a.total] = l[g];
           }
         }
-        if (softmax_any(over)) {
+        if (group_any(bar_id, over)) {
           // ---- some reference moves: the tile's largest exponents become the references, sums and O are rescaled
 #pragma unroll
-          for (int g = 0; g < kRows; ++g) {
-            const float d = warp_max(ok ? l[g] : -INFINITY), n = warp_max(ok ? l[g] + lv : -INFINITY);
-            if (lane == 0) { red_sm[w * 2 * kRows + 2 * g] = d; red_sm[w * 2 * kRows + 2 * g + 1] = n; }
+          for (int g = 0; g < kR; ++g) {
+            const float d = warp_redux_max(ok ? l[g] : -INFINITY), n = warp_redux_max(ok ? l[g] + lv : -INFINITY);
+            if (lane == 0) *reinterpret_cast<float2*>(&red_sm[w * 2 * kR + 2 * g]) = make_float2(d, n);
           }
-          softmax_any(false);
-          float shrink[kRows];
+          group_any(bar_id, false);
+          float shrink[kR];
 #pragma unroll
-          for (int g = 0; g < kRows; ++g) {
+          for (int g = 0; g < kR; ++g) {
             float d = refd[g], n = refn[g];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              d = fmaxf(d, red_sm[k * 2 * kRows + 2 * g]);
-              n = fmaxf(n, red_sm[k * 2 * kRows + 2 * g + 1]);
+              const float2 v = *reinterpret_cast<const float2*>(&red_sm[k * 2 * kR + 2 * g]);
+              d = fmaxf(d, v.x);
+              n = fmaxf(n, v.y);
             }
             sum[g] *= exp2_fast(refd[g] - d);
             shrink[g] = exp2_fast(refn[g] - n);
             refd[g] = d;
             refn[g] = n;
           }
-          if (ok && t > s0) {
-            ok = __all_sync(0xffffffffu, wait_or_abort(&tail->p_empty[(it - 1) & 1], ((it - 1) >> 1) & 1, abort_flag));
+          if (ok && t > first) {                                       // O holds this turn's tiles before this one
+            const int before = it - L::kTurns;
+            ok = __all_sync(0xffffffffu, wait_or_abort(&tail->p_empty[before % L::kBuffers], (before / L::kBuffers) & 1, abort_flag));
             if (ok) {
               ptx::tc_fence_after_sync();
 #pragma unroll
-              for (int i = 0; i < kBoxes * L::kN2 / 16; ++i) {
+              for (int i = 0; i < kBoxes * 4 * kR / 16; ++i) {
+                const uint32_t at_o = o_addr + (uint32_t)((i * 16 / (4 * kR)) * L::kN2 + i * 16 % (4 * kR));
                 uint32_t v[16];
-                ptx::tmem_ld_32x16(lane_addr + (uint32_t)(2 * L::kN1 + i * 16), v);
+                ptx::tmem_ld_32x16(at_o, v);
                 ptx::tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * shrink[(i * 16 + j) % kRows]);
-                tmem_st_32x16(lane_addr + (uint32_t)(2 * L::kN1 + i * 16), v);
+                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * shrink[(i * 16 + j) % kR]);
+                tmem_st_32x16(at_o, v);
               }
               ptx::tmem_wait_st();
               ptx::tc_fence_before_sync();
             }
           }
-          softmax_any(false);                                          // red_sm has been read
+          group_any(bar_id, false);                                    // red_sm has been read
         }
         // ---- weights and their terms
-        const int pb = it & 1;
-        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->p_empty[pb], ((it >> 1) & 1) ^ 1, abort_flag));
+        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->p_empty[sb], phase ^ 1, abort_flag));
         if (ok) {
-          uint32_t p[L::kN2 / 4];                                      // four codes: rows 4 q .. of term k at k kRows / 4 + q
+          uint32_t p[kR];                                              // four codes: rows 4 q .. of term k at k kR / 4 + q
 #pragma unroll
-          for (int q = 0; q < kRows / 4; ++q) {
+          for (int q = 0; q < kR / 4; ++q) {
             float f[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -503,84 +600,89 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
               f[i] = exp2_fast(l[g] + lv - refn[g] + kUp);
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) p[k * (kRows / 4) + q] = take_term(f);
+            for (int k = 0; k < 4; ++k) p[k * (kR / 4) + q] = take_term(f);
           }
-          uint8_t* dst = p_sm + pb * L::kP + key_in * 16;
+          uint8_t* dst = p_sm + sb * L::kP + rb * 4 * kR * kTileKeys + key_in * 16;
 #pragma unroll
-          for (int i = 0; i < L::kN2 / 16; ++i)
+          for (int i = 0; i < kR / 4; ++i)
             *reinterpret_cast<uint4*>(dst + i * 16 * kTileKeys) = make_uint4(p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
-          if (key0 + kTileKeys > all_see && key >= all_see) {
+          if (rb == 0 && key0 + kTileKeys > all_see && key >= all_see) {
             // A value behind the last row may be anything, and one that not every token sees may be NaN: neither must
             // reach the others through a weight of zero.  The first becomes zero, the second is noted for those who see it.
-            wait_or_abort(&tail->kv_full[it % a.stages], (it / a.stages) & 1, abort_flag);   // (complete: S came of this tile)
-            uint8_t* v = ring + (size_t)(it % a.stages) * L::kStage + (kBoxes * kTileKeys + key_in) * 128;
+            // V may come after S.  A wait by parity must not meet a phase two behind: the slot's tile before this one is
+            // done with, since this tile's weights had a free buffer, or (rings shorter than the buffers) after this wait.
+            if (a.v_slots < L::kBuffers && it >= a.v_slots)
+              wait_or_abort(&tail->p_empty[(it - a.v_slots) % L::kBuffers], ((it - a.v_slots) / L::kBuffers) & 1, abort_flag);
+            wait_or_abort(&tail->v_full[it % a.v_slots], (it / a.v_slots) & 1, abort_flag);
+            uint8_t* v = v_ring + (size_t)(it % a.v_slots) * L::kSlot + key_in * 128;
             for (int y = 0; y < kBoxes; ++y)
               for (int i = 0; i < 8; ++i) {
-                uint4* at = reinterpret_cast<uint4*>(v + y * kTileKeys * 128 + ((i ^ (key_in & 7)) << 4));
+                uint4* place = reinterpret_cast<uint4*>(v + y * kTileKeys * 128 + ((i ^ (key_in & 7)) << 4));
                 uint4 u = make_uint4(0, 0, 0, 0);
                 if (key < x.n) {
-                  u = *at;
+                  u = *place;
 #pragma unroll
                   for (int j = 0; j < 4; ++j) {
                     uint32_t& word = (&u.x)[j];
                     const uint32_t bad = __vcmpeq4(word & 0x7f7f7f7fu, 0x7f7f7f7fu);
                     if (!bad) continue;
                     word &= ~bad;
-                    tail->any_nan = 1;
+                    tail->any_nan[qb][turn] = 1;
                     const uint32_t four = (bad & 1u) | ((bad >> 7) & 2u) | ((bad >> 14) & 4u) | ((bad >> 21) & 8u);
                     const int d = y * 128 + i * 16 + j * 4;
-                    for (int g = 0; g < nrows; ++g)
-                      if (key < limit_sm[qb * kRows + g]) atomicOr(&nan_sm[g * kBoxes * 4 + (d >> 5)], four << (d & 31));
+                    for (int g = 0; g < L::kRows; ++g)                 // (a group's marks: [row][boxes * 4])
+                      if (key < limit_sm[qb * L::kRows + g]) atomicOr(&nan_sm[g * kBoxes * 4 + (d >> 5)], four << (d & 31));
                   }
                 }
-                *at = u;
+                *place = u;
               }
           }
           ptx::fence_proxy_async();
         }
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&tail->p_full[pb]);
+        if (lane == 0) ptx::mbar_arrive(&tail->p_full[sb]);
       }
 
       // ---- the segment's result
 #pragma unroll
-      for (int g = 0; g < kRows; ++g) {
+      for (int g = 0; g < kR; ++g) {
         float s = sum[g];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == 0) red_sm[w * 2 * kRows + g] = s;
+        if (lane == 0) red_sm[w * 2 * kR + g] = s;
       }
-      softmax_any(false);
-      const bool nan_seen = tail->any_nan != 0;
-      const bool whole = pref[e] >= t0 && pref[e + 1] <= t1;           // the entry lies within this CTA
-      const int64_t slot = ((int64_t)blockIdx.y * (entries + B) + e + b) * a.group_rows;
-      ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->o_full, seg & 1, abort_flag));
+      group_any(bar_id, false);
+      const bool whole = L::kTurns == 1 && pref[e] >= t0 && pref[e + 1] <= t1;   // this CTA alone has the entry, in one O
+      const int64_t slot = (((int64_t)blockIdx.y * (entries + B) + e + b) * L::kTurns + turn) * a.group_rows + rb * kR;
+      if (any_tile) {
+        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->o_full[turn], o_uses & 1, abort_flag));
+        ++o_uses;
+      }
       if (ok) {
-        ptx::tc_fence_after_sync();
-        constexpr int kPart = kRows < 16 ? kRows : 16;                 // rows at a time
+        const bool nan_seen = x.nq > 1 && *(volatile int*)&tail->any_nan[qb][turn] != 0;
+        if (any_tile) ptx::tc_fence_after_sync();
 #pragma unroll
         for (int y = 0; y < kBoxes; ++y) {
           const int d = y * 128 + key_in;
+          uint32_t v[4 * kR];
+          if (any_tile) {
 #pragma unroll
-          for (int g0 = 0; g0 < kRows; g0 += kPart) {
-            constexpr int kChunks = 4 * kPart / 16;
-            uint32_t v[kChunks][16];
-#pragma unroll
-            for (int i = 0; i < kChunks; ++i)                          // kPart = 16: term i; below: the terms lie side by side
-              ptx::tmem_ld_32x16(lane_addr + (uint32_t)(2 * L::kN1 + y * L::kN2 + (kPart == 16 ? i * kRows + g0 : i * 16)), v[i]);
+            for (int i = 0; i < kR / 4; ++i)
+              ptx::tmem_ld_32x16(o_addr + (uint32_t)(y * L::kN2 + i * 16), *reinterpret_cast<uint32_t(*)[16]>(&v[16 * i]));
             ptx::tmem_wait_ld();
-            if (d < a.d_k) {
+          }
+          if (d < a.d_k) {
 #pragma unroll
-              for (int i = 0; i < kPart; ++i) {
-                const int g = g0 + i;
-                if (g < nrows) {
-                  auto term = [&](int k) { return __uint_as_float(v[(k * kPart + i) / 16][(k * kPart + i) % 16]); };
+            for (int g = 0; g < kR; ++g) {
+              if (g < nrows) {
+                const float total = (red_sm[g] + red_sm[2 * kR + g]) + (red_sm[4 * kR + g] + red_sm[6 * kR + g]);
+                if (any_tile) {
+                  auto term = [&](int k) { return __uint_as_float(v[k * kR + g]); };
                   float o = fmaf(term(3), 0.000244140625f, fmaf(term(2), 0.00390625f, fmaf(term(1), 0.0625f, term(0))));
-                  const float total = (red_sm[g] + red_sm[2 * kRows + g]) + (red_sm[4 * kRows + g] + red_sm[6 * kRows + g]);
-                  const float f = exp2_fast(0.5f * (refn[g] - refd[g]));     // (in two steps: it may lie below 2^-126)
-                  o = total == 0.f ? 0.f : o * 0.0625f / total * f * f;
-                  if (nan_seen && ((nan_sm[g * kBoxes * 4 + (d >> 5)] >> (d & 31)) & 1u)) o = __uint_as_float(0x7fffffffu);
-                  const int qrow = group0 + g;
+                  const float f = exp2_fast(0.5f * (refn[g] - refd[g]));       // (in two steps: it may lie below 2^-126)
+                  o = total == 0.f ? 0.f : o * 0.25f / total * f * f;          // (kUp = 2)
+                  if (nan_seen && ((nan_sm[(rb * kR + g) * kBoxes * 4 + (d >> 5)] >> (d & 31)) & 1u)) o = __uint_as_float(0x7fffffffu);
+                  const int qrow = row0 + g;
                   if (whole) {
                     const int token = qrow / a.G, head = x.h * a.G + qrow - token * a.G;
                     a.out[(int64_t)(x.q0 + token) * a.o_tok + (int64_t)head * a.o_head + d] = __float2bfloat16(o);
@@ -589,8 +691,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
                   } else {
                     a.part_o[(slot + g) * a.d_k + d] = o;
                   }
-                  if (d == 0) a.part_ml[slot + g] = make_float2(total == 0.f ? -INFINITY : refd[g], total);
                 }
+                if (d == 0) a.part_ml[slot + g] = make_float2(total == 0.f ? -INFINITY : refd[g], total);
               }
             }
           }
@@ -598,14 +700,11 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         ptx::tc_fence_before_sync();
       }
       __syncwarp();
-      if (lane == 0) { ptx::mbar_arrive(&tail->o_empty); ptx::mbar_arrive(&tail->q_empty[qb]); }
-      softmax_any(false);                                              // red_sm and the NaN marks have been read
-      if (nan_seen) {
-        for (int i = key_in; i < L::kNan / 4; i += 128) nan_sm[i] = 0;
-        tail->any_nan = 0;
-        softmax_any(false);
+      if (lane == 0) {
+        if (any_tile) ptx::mbar_arrive(&tail->o_empty[turn]);
+        ptx::mbar_arrive(&tail->q_empty[qb]);
       }
-      ++seg;
+      group_any(bar_id, false);                                        // red_sm has been read
     }
   }
 
@@ -621,9 +720,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
 // What an entry's segments say of one row: the maximum, and the sum relative to it.  A whole warp asks; the segments are
 // spread over its lanes, so that their loads are in flight together.
 __device__ __forceinline__ float2 merged_ml(const AttendArgs& a, int B, int group, int e, int2 v, int in_group, int entries) {
-  const float2* ml = a.part_ml + ((int64_t)group * (entries + B) + e) * a.group_rows + in_group;
+  // (the turns of one CTA's slot and the slots of consecutive CTAs follow one another)
+  const float2* ml = a.part_ml + ((int64_t)group * (entries + B) + e) * a.turns * a.group_rows + in_group;
   float M = -INFINITY, L = 0.f;
-  for (int b = v.x + (int)(threadIdx.x & 31); v.x >= 0 && b <= v.y; b += 32) {
+  for (int b = v.x * a.turns + (int)(threadIdx.x & 31); v.x >= 0 && b < (v.y + 1) * a.turns; b += 32) {
     const float2 x = ml[(int64_t)b * a.group_rows];
     const float top = fmaxf(M, x.x);
     if (top != -INFINITY) L = L * exp2_fast(M - top) + x.y * exp2_fast(x.x - top);
@@ -642,6 +742,7 @@ __device__ __forceinline__ float2 merged_ml(const AttendArgs& a, int B, int grou
 __global__ void __launch_bounds__(256)
 attend8_finish_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows, int slot_blocks) {
   __shared__ float4 s_o[8][32 * 2];
+  __shared__ float s_f[4 * kSms];
   __shared__ float s_neg[GVOTE_ATTEND8_MAX_Q * kMaxGroup8];
   const int entries = a.batch * a.Hkv, tid = threadIdx.x;
   const bool merging = (int64_t)blockIdx.x < (int64_t)entries * max_rows;
@@ -651,23 +752,25 @@ attend8_finish_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows,
     if (row >= x.nq * a.G) return;
     const int group = row / a.group_rows, in_group = row - group * a.group_rows;
     const int2 v = a.info[(int64_t)group * entries + e];
-    if (v.x >= 0 && v.x == v.y) return;                 // the first kernel has written it
+    if (a.turns == 1 && v.x >= 0 && v.x == v.y) return; // the first kernel has written it
     const float2 ml = merged_ml(a, B, group, e, v, in_group, entries);
     const int quads = a.d_k >> 2, part = tid >> 5, lane = tid & 31;
-    const int64_t slot0 = ((int64_t)group * (entries + B) + e) * a.group_rows + in_group;
+    const int p0 = v.x * a.turns, parts = v.x < 0 ? 0 : (v.y + 1) * a.turns - p0;
+    const int64_t slot0 = (((int64_t)group * (entries + B) + e) * a.turns + p0) * a.group_rows + in_group;
+    for (int i = tid; i < parts; i += 256) {
+      const float2 m = a.part_ml[slot0 + (int64_t)i * a.group_rows];
+      s_f[i] = m.x == -INFINITY ? 0.f : exp2_fast(m.x - ml.x) * m.y;
+    }
+    __syncthreads();
     for (int q = lane; q < quads; q += 32) {
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (v.x >= 0) {
-#pragma unroll 4
-        for (int b = v.x + part; b <= v.y; b += 8) {
-          const int64_t slot = slot0 + (int64_t)b * a.group_rows;
-          const float2 m = a.part_ml[slot];
-          const float4 p = *reinterpret_cast<const float4*>(a.part_o + slot * a.d_k + q * 4);
-          const float f = m.x == -INFINITY ? 0.f : exp2_fast(m.x - ml.x) * m.y;
-          if (f != 0.f) { s.x = fmaf(f, p.x, s.x); s.y = fmaf(f, p.y, s.y); s.z = fmaf(f, p.z, s.z); s.w = fmaf(f, p.w, s.w); }
-        }
+#pragma unroll 8
+      for (int i = part; i < parts; i += 8) {
+        const float4 p = *reinterpret_cast<const float4*>(a.part_o + (slot0 + (int64_t)i * a.group_rows) * a.d_k + q * 4);
+        const float f = s_f[i];
+        if (f != 0.f) { s.x = fmaf(f, p.x, s.x); s.y = fmaf(f, p.y, s.y); s.z = fmaf(f, p.z, s.z); s.w = fmaf(f, p.w, s.w); }
       }
-      s_o[part][q] = s;
+      s_o[part][q] = s;                                 // (0: a turn without tiles has left nothing)
     }
     __syncthreads();
     const int token = row / a.G, g = x.h * a.G + row % a.G;
@@ -713,14 +816,17 @@ attend8_finish_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows,
   a.acc_out[slot] = (a.acc ? a.acc[slot] : 0.f) + s;
 }
 
-// How a launch is cut: query rows per group, ring, CTAs.
-struct Cut { int boxes, rows, groups, requests; int64_t ctas; };
+// How a launch is cut: query rows of a softmax group, groups that share a tile's rows, row groups, CTAs.
+struct Cut { int boxes, kr, rb, turns, rows, groups, requests; int64_t ctas; };
 Cut cut_of(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_q) {
   Cut c;
   const int64_t rows = max_q * (p->n_q_heads / p->n_kv_heads);
   c.boxes = p->d_k <= 128 ? 1 : 2;
-  // the padded rows cost columns of both products and the softmax's time; beyond 32 the codes are read again (from L2)
-  c.rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+  // beyond 32 rows the codes are read again (from L2)
+  c.kr = rows <= 4 ? 4 : 8;
+  c.rb = rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : 4;
+  c.turns = c.rb == 1 ? 4 : c.rb == 2 ? 2 : 1;
+  c.rows = c.kr * c.rb;
   c.groups = (int)ceil_div(rows > 0 ? rows : 1, c.rows);
   c.requests = kMaxEntries / p->n_kv_heads < batch ? kMaxEntries / p->n_kv_heads : batch;
   // a CTA per SM, and no more than one per tile
@@ -729,28 +835,32 @@ Cut cut_of(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t m
   return c;
 }
 
-template <int kBoxes, int kRows>
-int32_t run_attend(const Cut& c, const CUtensorMap& tmK, const CUtensorMap& tmV, AttendArgs a, cudaStream_t st) {
-  using L = Layout<kBoxes, kRows>;
-  const size_t fit = (227 * 1024 - L::fixed()) / L::kStage;
-  a.stages = (int)(fit < kMaxStages ? fit : kMaxStages);
-  const size_t smem = L::fixed() + (size_t)a.stages * L::kStage;
-  auto kernel = attend8_kernel<kBoxes, kRows>;
+template <int kBoxes, int kR, int kRb>
+int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], AttendArgs a, cudaStream_t st) {
+  using L = Layout<kBoxes, kR, kRb>;
+  // the slots that fit, five in twelve to K (a tile of V stays about half as long again)
+  const int fit = (int)((227 * 1024 - L::fixed()) / L::kSlot);
+  a.k_slots = fit * 5 / 12 < 2 ? 2 : fit * 5 / 12 > kMaxSlots ? kMaxSlots : fit * 5 / 12;
+  a.v_slots = fit - a.k_slots > kMaxSlots ? kMaxSlots : fit - a.k_slots;
+  const size_t smem = L::fixed() + (size_t)(a.k_slots + a.v_slots) * L::kSlot;
+  auto kernel = attend8_kernel<kBoxes, kR, kRb>;
   GVOTE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   {
     LaunchScope scope_("attend8_kernel", st);
-    launch_on(kernel, dim3((unsigned)c.ctas, (unsigned)c.groups), dim3(kThreads), smem, st, tmK, tmV, a);
+    launch_on(kernel, dim3((unsigned)c.ctas, (unsigned)c.groups), dim3(L::kThreads), smem, st, tm[0], tm[1], tm[2],
+              tm[3], a);
   }
   GVOTE_LAUNCH_CHECK("attend8_kernel");
   return GVOTE_OK;
 }
 template <int kBoxes>
-int32_t run_attend(const Cut& c, const CUtensorMap& tmK, const CUtensorMap& tmV, const AttendArgs& a, cudaStream_t st) {
-  switch (c.rows) {
-    case 4: return run_attend<kBoxes, 4>(c, tmK, tmV, a, st);
-    case 8: return run_attend<kBoxes, 8>(c, tmK, tmV, a, st);
-    case 16: return run_attend<kBoxes, 16>(c, tmK, tmV, a, st);
-    default: return run_attend<kBoxes, 32>(c, tmK, tmV, a, st);
+int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], const AttendArgs& a, cudaStream_t st) {
+  if (c.kr == 4) return run_attend<kBoxes, 4, 1>(c, tm, a, st);
+  switch (c.rb) {
+    case 1: return run_attend<kBoxes, 8, 1>(c, tm, a, st);
+    case 2: return run_attend<kBoxes, 8, 2>(c, tm, a, st);
+    case 3: return run_attend<kBoxes, 8, 3>(c, tm, a, st);
+    default: return run_attend<kBoxes, 8, 4>(c, tm, a, st);
   }
 }
 
@@ -762,7 +872,7 @@ AttendMap attend8_map(const gvote_params* p, int32_t batch, int64_t total_tokens
   const int64_t nq = max_q < GVOTE_ATTEND8_MAX_Q ? max_q : GVOTE_ATTEND8_MAX_Q;
   const Cut c = cut_of(p, batch, total_tokens, nq);
   const size_t entries = (size_t)c.requests * p->n_kv_heads;
-  const size_t rows = (size_t)c.groups * (entries + c.ctas) * c.rows;
+  const size_t rows = (size_t)c.groups * (entries + c.ctas) * c.turns * c.rows;
   m.o = kStatusBytes;
   m.ml = align_up(m.o + rows * p->d_k * 4, 256);
   m.info = align_up(m.ml + rows * 8, 256);
@@ -787,20 +897,21 @@ int32_t launch_attend8(const gvote_params* p, const __nv_bfloat16* Q, int64_t q_
   a.logits = acc_out ? (float*)(ws + m.logits) : nullptr;
   a.status = (int32_t*)ws;
   a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads; a.d_k = p->d_k; a.max_q = (int)max_q;
-  a.stages = 0; a.group_rows = cut.rows;
+  a.k_slots = a.v_slots = 0; a.group_rows = cut.rows; a.turns = cut.turns;
   a.scale2 = (float)(1.4426950408889634 / sqrt((double)p->d_k));
 
-  CUtensorMap tmK, tmV;
+  CUtensorMap tm[4];                                    // K, V in whole tiles, K, V in parts
   const uint64_t dims[3] = {(uint64_t)p->d_k, (uint64_t)c->total_tokens, (uint64_t)a.Hkv};
   const uint64_t strides[2] = {(uint64_t)c->tok_stride, (uint64_t)(a.Hkv > 1 ? c->head_stride : c->tok_stride)};
-  const uint32_t box[3] = {128, (uint32_t)kBoxRows, 1};
-  if (!encode_tensor_map_u8(&tmK, c->K, 3, dims, strides, box) || !encode_tensor_map_u8(&tmV, c->V, 3, dims, strides, box))
-    return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t box[3] = {128, (uint32_t)(i < 2 ? kTileKeys : kBoxRows), 1};
+    if (!encode_tensor_map_u8(&tm[i], i & 1 ? c->V : c->K, 3, dims, strides, box)) return GVOTE_ERR_UNSUPPORTED_SHAPE;
+  }
 
   for (int32_t r0 = 0; r0 < c->batch; r0 += cut.requests) {
     a.r0 = r0;
     a.batch = c->batch - r0 < cut.requests ? c->batch - r0 : cut.requests;
-    PROPAGATE(cut.boxes == 1 ? run_attend<1>(cut, tmK, tmV, a, st) : run_attend<2>(cut, tmK, tmV, a, st));
+    PROPAGATE(cut.boxes == 1 ? run_attend<1>(cut, tm, a, st) : run_attend<2>(cut, tm, a, st));
     const int64_t entries = (int64_t)a.batch * a.Hkv, rows = max_q * a.G;
     const int64_t slots = acc_out ? ((c->total_tokens >> 8) + a.batch) * a.Hkv : 0;
     LaunchScope scope_("attend8_finish_kernel", st);
