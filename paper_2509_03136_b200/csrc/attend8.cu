@@ -23,10 +23,11 @@
 // exponent so far, so that a block of large values neither overflows nor drowns what carries the output.  ref only moves
 // when it is passed by 2^6 (the accumulated O is then rescaled in tensor memory: mostly the first tile only).
 //
-// Warps 0 and 2 ask for the tiles of K and of V (TMA, only the 32-row parts that hold rows) into rings of their own - a tile
-// of K is done with as soon as S is there, a tile of V only after the softmax - warp 1 issues the MMAs, whichever has its
-// operands first, and warp 3 prepares the next segment's Q terms; then come up to four softmax groups of four warps,
-// thread = cached row of the tile (and channel of the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each with
+// Warp 0 asks for the tiles of K and of V (TMA, only the 32-row parts that hold rows) into rings of their own - a tile
+// of K is done with as soon as S is there, a tile of V only after the softmax - warps 1 and 2 issue the MMAs of S and of O
+// (one warp for both took 1500 clocks a tile, its waits and commits one after the other), and warp 3 prepares the next
+// segment's Q terms; then come up to four softmax groups of four warps, thread = cached row of the tile (and channel of
+// the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each with
 // references and an O of its own (one group alone needs 3000 clocks of latency for a tile, the memory 1400), with many
 // the groups share a tile's rows out.  S and P are buffered as deep as the MMAs run ahead.
 //
@@ -34,6 +35,8 @@
 // kernel turns them into weights once lse is known; a slot belongs to one thread, so the sum has one order.
 //
 // Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
+#include <cstddef>
+
 #include "cache8.cuh"
 #include "ptx.cuh"
 
@@ -157,14 +160,22 @@ __device__ __forceinline__ uint32_t take_term(float (&x)[4]) {
   return c;
 }
 
+// Counts: one arrival, 1 + 4 groups on q_empty, four per group that shares a tile's rows from s_empty on.
+struct Bars {
+  uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots], q_full[2], q_empty[2];
+  uint64_t s_full[kMaxBuffers], p_empty[kMaxBuffers], o_full[4];
+  uint64_t s_empty[kMaxBuffers], p_full[kMaxBuffers], o_empty[4];
+};
+enum { kWarpTma = 0, kWarpS = 1, kWarpO = 2, kWarpQ = 3, kWarpSoftmax = 4 };
+
 struct Tail {
-  uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
-  uint64_t q_full[2], q_empty[2];
-  uint64_t s_full[kMaxBuffers], s_empty[kMaxBuffers], p_full[kMaxBuffers], p_empty[kMaxBuffers], o_full[4], o_empty[4];
+  Bars bars;
   Entry entry[2];
   uint32_t tmem_slot;
   int any_nan[2][4];                   // [segment parity][turn]
   volatile int abort_flag;
+  int64_t out_at[2][32];               // where the query rows' outputs go (elements)
+  int lse_at[2][32];
   int warp_tot[32];
   int pref[kMaxEntries + 1];
 };
@@ -226,22 +237,19 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   const int entries = a.batch * a.Hkv;
   const int group0 = blockIdx.y * a.group_rows;                        // first query row of this row group
 
-  if (tid == 0) {
-    for (int s = 0; s < kMaxSlots; ++s) {
-      ptx::mbar_init(&tail->k_full[s], 1); ptx::mbar_init(&tail->k_empty[s], 1);
-      ptx::mbar_init(&tail->v_full[s], 1); ptx::mbar_init(&tail->v_empty[s], 1);
+  {                                                                    // a barrier per thread
+    constexpr int kBars = sizeof(Bars) / 8;
+    if (tid < kBars) {
+      const int at = tid * 8;
+      const uint32_t count = at >= (int)offsetof(Bars, q_empty) && at < (int)offsetof(Bars, s_full) ? 1 + 4 * L::kGroups
+                             : at >= (int)offsetof(Bars, s_empty) ? 4 * kRb : 1;
+      ptx::mbar_init(reinterpret_cast<uint64_t*>(&tail->bars) + tid, count);
+      ptx::fence_barrier_init();
     }
-    for (int b = 0; b < 2; ++b) { ptx::mbar_init(&tail->q_full[b], 1); ptx::mbar_init(&tail->q_empty[b], 1 + 4 * L::kGroups); }
-    for (int b = 0; b < kMaxBuffers; ++b) {
-      ptx::mbar_init(&tail->s_full[b], 1); ptx::mbar_init(&tail->s_empty[b], 4 * kRb);
-      ptx::mbar_init(&tail->p_full[b], 4 * kRb); ptx::mbar_init(&tail->p_empty[b], 1);
-    }
-    for (int b = 0; b < 4; ++b) {
-      ptx::mbar_init(&tail->o_full[b], 1); ptx::mbar_init(&tail->o_empty[b], 4 * kRb);
-      tail->any_nan[0][b] = tail->any_nan[1][b] = 0;
-    }
+  }
+  if (tid == kWarpQ * 32) {
+    for (int b = 0; b < 4; ++b) tail->any_nan[0][b] = tail->any_nan[1][b] = 0;
     tail->abort_flag = (ptx::smem_u32(smem) & 1023u) ? 1 : 0;
-    ptx::fence_barrier_init();
     ptx::prefetch_tensormap(&tmK);
     ptx::prefetch_tensormap(&tmV);
   }
@@ -271,8 +279,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
-    int run = inc - mine;
-    for (int w = 0; w < warp; ++w) run += tail->warp_tot[w];
+    const int before = lane < warp ? tail->warp_tot[lane] : 0;
+    int run = inc - mine + __reduce_add_sync(0xffffffffu, before);
     for (int e = e0; e < e1; ++e) { run += pref[e + 1]; pref[e + 1] = run; }
     if (tid == 0) pref[0] = 0;
     __syncthreads();
@@ -301,113 +309,126 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   Walk at(pref, t0, t1, entries, e_first);
   bool ok = true;
 
-  if (warp == 0 || warp == 2) {
-    // ------------------------------------------------------------------ TMA producers: K, V
+  if (warp == kWarpTma) {
+    // ------------------------------------------------------------------ TMA producer: K and V, each as its ring has room
     if (lane == 0) {
-      const bool is_k = warp == 0;
-      const CUtensorMap* whole_map = is_k ? &tmK : &tmV;
-      const CUtensorMap* part_map = is_k ? &tmKp : &tmVp;
-      uint8_t* ring = is_k ? k_ring : v_ring;
-      uint64_t* full = is_k ? tail->k_full : tail->v_full;
-      uint64_t* empty = is_k ? tail->k_empty : tail->v_empty;
-      const int slots = is_k ? a.k_slots : a.v_slots;
-      int s = 0;
-      uint32_t phase = 0;
-      for (; ok && !at.done(); at.next_segment()) {
-        const Entry x = entry_of(a, at.e);
-        for (int t = at.s0; t < at.s1; ++t) {
-          const int key0 = (t - pref[at.e]) * kTileKeys;
-          ok = wait_or_abort(&empty[s], phase ^ 1u, abort_flag);
-          if (!ok) break;
-          uint8_t* dst = ring + (size_t)s * L::kSlot;
-          const int parts = min(kTileKeys / kBoxRows, (x.n - key0 + kBoxRows - 1) / kBoxRows);
-          ptx::mbar_arrive_expect_tx(&full[s], (uint32_t)parts * kBoxes * kBoxRows * 128);
+      struct Feed {
+        const CUtensorMap *whole, *part;
+        uint8_t* ring;
+        uint64_t *full, *empty;
+        int slots, slot;
+        uint32_t phase;
+        Entry x;
+        int seg;
+      };
+      Feed feed[2] = {{&tmK, &tmKp, k_ring, tail->bars.k_full, tail->bars.k_empty, a.k_slots, 0, 0, {}, -1},
+                      {&tmV, &tmVp, v_ring, tail->bars.v_full, tail->bars.v_empty, a.v_slots, 0, 0, {}, -1}};
+      Walk walk[2] = {at, at};
+      uint32_t polls = 0;
+      while (ok && !(walk[0].done() && walk[1].done())) {
+        bool moved = false;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          Feed& f = feed[i];
+          Walk& w = walk[i];
+          if (w.done() || !ptx::mbar_test_wait(&f.empty[f.slot], f.phase ^ 1u)) continue;
+          if (f.seg != w.seg) { f.x = entry_of(a, w.e); f.seg = w.seg; }
+          const int key0 = (w.t - pref[w.e]) * kTileKeys, parts = min(kTileKeys / kBoxRows, (f.x.n - key0 + kBoxRows - 1) / kBoxRows);
+          uint8_t* dst = f.ring + (size_t)f.slot * L::kSlot;
+          uint64_t* full = &f.full[f.slot];
+          ptx::mbar_arrive_expect_tx(full, (uint32_t)parts * kBoxes * kBoxRows * 128);
 #pragma unroll
           for (int y = 0; y < kBoxes; ++y) {
             if (parts == kTileKeys / kBoxRows) {
-              ptx::tma_load_3d(dst + y * kTileKeys * 128, whole_map, &full[s], y * 128, x.start + key0, x.h);
+              ptx::tma_load_3d(dst + y * kTileKeys * 128, f.whole, full, y * 128, f.x.start + key0, f.x.h);
             } else {
               for (int g = 0; g < parts; ++g)
-                ptx::tma_load_3d(dst + (y * kTileKeys + g * kBoxRows) * 128, part_map, &full[s], y * 128, x.start + key0 + g * kBoxRows, x.h);
+                ptx::tma_load_3d(dst + (y * kTileKeys + g * kBoxRows) * 128, f.part, full, y * 128, f.x.start + key0 + g * kBoxRows, f.x.h);
             }
           }
-          if (++s == slots) { s = 0; phase ^= 1u; }
+          if (++f.slot == f.slots) { f.slot = 0; f.phase ^= 1u; }
+          w.next_tile();
+          moved = true;
+        }
+        if (moved) {
+          polls = 0;
+        } else if (++polls > (1u << 24) || ((polls & 255u) == 255u && *abort_flag)) {
+          *abort_flag = 1;
+          ok = false;
         }
       }
     }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
-    // S of the next tile, or O of the oldest tile whose weights are there: whichever can be issued.  (Taken in a fixed
-    // order, a tile's V waited for the arrival of the third K after it, and the rings stood half empty.)
-    const uint32_t idesc1 = instr_desc_e4m3(kTileKeys, L::kN1, false, false), idesc2 = instr_desc_e4m3(128, L::kN2, true, true);
+  } else if (warp == kWarpS) {
+    // ------------------------------------------------------------------ S = K Q^T (the whole warp walks, one lane issues)
+    const uint32_t idesc = instr_desc_e4m3(kTileKeys, L::kN1, false, false);
     const int ksteps = (a.d_k + 31) / 32;
-    Walk behind(pref, t0, t1, entries, e_first);
-    uint32_t o_uses = 0;                                               // bit i: parity of the uses of turn i's O
-    int ks = 0, vs = 0;                                                // ring slots and their phases
-    uint32_t k_phase = 0, v_phase = 0, polls = 0;
-    auto ready = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_test_wait(bar, parity)); };
-    while (ok && !behind.done()) {
-      bool moved = false;
-      if (!at.done()) {
-        const int sb = at.it % L::kBuffers, qb = at.seg & 1;
-        if (ready(&tail->s_empty[sb], ((at.it / L::kBuffers) & 1) ^ 1) && (at.t > at.s0 || ready(&tail->q_full[qb], (at.seg >> 1) & 1)) &&
-            ready(&tail->k_full[ks], k_phase)) {
-          ptx::tc_fence_after_sync();
-          if (ptx::elect_one()) {
+    const uint64_t kd0 = ptx::smem_desc_k_sw128(ptx::smem_u32(k_ring)), qd0 = ptx::smem_desc_k_sw128(ptx::smem_u32(q_sm));
+    int ks = 0;
+    uint32_t k_phase = 0;
+    for (; ok && !at.done(); at.next_segment()) {
+      const int qb = at.seg & 1;
+      ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.q_full[qb], (at.seg >> 1) & 1, abort_flag));
+      for (int t = at.s0, it = at.it; ok && t < at.s1; ++t, ++it) {
+        const int sb = it % L::kBuffers;
+        ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.s_empty[sb], ((it / L::kBuffers) & 1) ^ 1, abort_flag) &&
+                                         wait_or_abort(&tail->bars.k_full[ks], k_phase, abort_flag));
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        if (ptx::elect_one()) {
 #pragma unroll
-            for (int y = 0; y < kBoxes; ++y) {
-              const uint64_t kd = ptx::smem_desc_k_sw128(ptx::smem_u32(k_ring) + (uint32_t)(ks * L::kSlot + y * kTileKeys * 128));
-              const uint64_t qd = ptx::smem_desc_k_sw128(ptx::smem_u32(q_sm) + (uint32_t)(qb * L::kQ + y * L::kN1 * 128));
+          for (int y = 0; y < kBoxes; ++y) {
+            const uint64_t kd = kd0 + (uint64_t)((ks * L::kSlot + y * kTileKeys * 128) >> 4), qd = qd0 + (uint64_t)((qb * L::kQ + y * L::kN1 * 128) >> 4);
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (y * 4 + k < ksteps)
-                  umma_e4m3(tmem + (uint32_t)(sb * L::kN1), kd + 2 * k, qd + 2 * k, idesc1, y + k > 0 ? 1u : 0u);
-            }
-            ptx::umma_commit(&tail->s_full[sb]);
-            ptx::umma_commit(&tail->k_empty[ks]);
-            if (at.t == at.s1 - 1) ptx::umma_commit(&tail->q_empty[qb]);
+            for (int k = 0; k < 4; ++k)
+              if (y * 4 + k < ksteps)
+                umma_e4m3(tmem + (uint32_t)(sb * L::kN1), kd + 2 * k, qd + 2 * k, idesc, y + k > 0 ? 1u : 0u);
           }
-          __syncwarp();
-          at.next_tile();
-          if (++ks == a.k_slots) { ks = 0; k_phase ^= 1u; }
-          moved = true;
+          ptx::umma_commit(&tail->bars.s_full[sb]);
+          ptx::umma_commit(&tail->bars.k_empty[ks]);
+          if (t == at.s1 - 1) ptx::umma_commit(&tail->bars.q_empty[qb]);
         }
-      }
-      if (behind.it < at.it) {
-        const int pb = behind.it % L::kBuffers, turn = behind.it % L::kTurns;
-        const bool first = behind.t - behind.s0 < L::kTurns, last = behind.t + L::kTurns >= behind.s1;
-        if (ready(&tail->p_full[pb], (behind.it / L::kBuffers) & 1) && ready(&tail->v_full[vs], v_phase) &&
-            (!first || ready(&tail->o_empty[turn], ((o_uses >> turn) & 1) ^ 1))) {
-          if (first) o_uses ^= 1u << turn;
-          ptx::tc_fence_after_sync();
-          if (ptx::elect_one()) {
-            const uint64_t pd = smem_desc_mn_plain(ptx::smem_u32(p_sm) + (uint32_t)pb * L::kP, 16 * kTileKeys);
-#pragma unroll
-            for (int y = 0; y < kBoxes; ++y) {
-              const uint64_t vd = ptx::smem_desc_k_sw128(ptx::smem_u32(v_ring) + (uint32_t)(vs * L::kSlot + y * kTileKeys * 128));
-#pragma unroll
-              for (int k = 0; k < kTileKeys / 32; ++k)                 // 32 keys: 4 KB of V, 512 bytes of P
-                umma_e4m3(tmem + (uint32_t)(L::kO + (turn * kBoxes + y) * L::kN2), vd + (uint64_t)(k * (32 * 128 / 16)),
-                          pd + (uint64_t)(k * (32 * 16 / 16)), idesc2, first && k == 0 ? 0u : 1u);
-            }
-            ptx::umma_commit(&tail->p_empty[pb]);
-            ptx::umma_commit(&tail->v_empty[vs]);
-            if (last) ptx::umma_commit(&tail->o_full[turn]);
-          }
-          __syncwarp();
-          behind.next_tile();
-          if (++vs == a.v_slots) { vs = 0; v_phase ^= 1u; }
-          moved = true;
-        }
-      }
-      if (moved) {
-        polls = 0;
-      } else if (++polls > (1u << 24) || ((polls & 255u) == 255u && *abort_flag)) {
-        *abort_flag = 1;
-        ok = false;
+        __syncwarp();
+        if (++ks == a.k_slots) { ks = 0; k_phase ^= 1u; }
       }
     }
-  } else if (warp == 3) {
+  } else if (warp == kWarpO) {
+    // ------------------------------------------------------------------ O += V^T P
+    const uint32_t idesc = instr_desc_e4m3(128, L::kN2, true, true);
+    const uint64_t vd0 = ptx::smem_desc_k_sw128(ptx::smem_u32(v_ring)), pd0 = smem_desc_mn_plain(ptx::smem_u32(p_sm), 16 * kTileKeys);
+    uint32_t o_uses = 0;                                               // bit i: parity of the uses of turn i's O
+    int vs = 0;
+    uint32_t v_phase = 0;
+    for (; ok && !at.done(); at.next_segment()) {
+      for (int t = at.s0, it = at.it; ok && t < at.s1; ++t, ++it) {
+        const int pb = it % L::kBuffers, turn = it % L::kTurns;
+        const bool first = t - at.s0 < L::kTurns, last = t + L::kTurns >= at.s1;
+        ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.p_full[pb], (it / L::kBuffers) & 1, abort_flag) &&
+                                         wait_or_abort(&tail->bars.v_full[vs], v_phase, abort_flag));
+        if (ok && first) {
+          ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.o_empty[turn], ((o_uses >> turn) & 1) ^ 1, abort_flag));
+          o_uses ^= 1u << turn;
+        }
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        if (ptx::elect_one()) {
+          const uint64_t pd = pd0 + (uint64_t)((pb * L::kP) >> 4);
+#pragma unroll
+          for (int y = 0; y < kBoxes; ++y) {
+            const uint64_t vd = vd0 + (uint64_t)((vs * L::kSlot + y * kTileKeys * 128) >> 4);
+#pragma unroll
+            for (int k = 0; k < kTileKeys / 32; ++k)                   // 32 keys: 4 KB of V, 512 bytes of P
+              umma_e4m3(tmem + (uint32_t)(L::kO + (turn * kBoxes + y) * L::kN2), vd + (uint64_t)(k * (32 * 128 / 16)),
+                        pd + (uint64_t)(k * (32 * 16 / 16)), idesc, first && k == 0 ? 0u : 1u);
+          }
+          ptx::umma_commit(&tail->bars.p_empty[pb]);
+          ptx::umma_commit(&tail->bars.v_empty[vs]);
+          if (last) ptx::umma_commit(&tail->bars.o_full[turn]);
+        }
+        __syncwarp();
+        if (++vs == a.v_slots) { vs = 0; v_phase ^= 1u; }
+      }
+    }
+  } else if (warp == kWarpQ) {
     // ------------------------------------------------------------------ Q as three e4m3 terms, a segment ahead
     for (int i = lane; i < 2 * kBoxes * (L::kN1 - 3 * L::kRows) * 8; i += 32) {     // the rows behind the last term are zero
       constexpr int kPer = (L::kN1 - 3 * L::kRows) * 8 > 0 ? (L::kN1 - 3 * L::kRows) * 8 : 1;
@@ -417,7 +438,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       const int qb = at.seg & 1;
       const Entry x = entry_of(a, at.e);
       const int rows = x.nq * a.G;
-      ok = __all_sync(0xffffffffu, wait_or_abort(&tail->q_empty[qb], ((at.seg >> 1) & 1) ^ 1, abort_flag));
+      ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.q_empty[qb], ((at.seg >> 1) & 1) ^ 1, abort_flag));
       if (!ok) break;
       uint8_t* dst = q_sm + qb * L::kQ;
 #pragma unroll 1
@@ -465,18 +486,21 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           }
           if (lane == 0) {
             factor_sm[qb * L::kRows + row] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale2;
-            limit_sm[qb * L::kRows + row] = qrow < rows ? x.n - (x.nq - 1 - qrow / a.G) : 0;
+            const int token = qrow / a.G, head = x.h * a.G + qrow - token * a.G;
+            limit_sm[qb * L::kRows + row] = qrow < rows ? x.n - (x.nq - 1 - token) : 0;
+            tail->out_at[qb][row] = (int64_t)(x.q0 + token) * a.o_tok + (int64_t)head * a.o_head;
+            tail->lse_at[qb][row] = (x.q0 + token) * a.Hkv * a.G + head;
           }
         }
       }
       if (lane == 0) tail->entry[qb] = x;
       ptx::fence_proxy_async();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(&tail->q_full[qb]);
+      if (lane == 0) ptx::mbar_arrive(&tail->bars.q_full[qb]);
     }
   } else {
     // ------------------------------------------------------------------ softmax: thread = row of the tile, channel of O
-    const int group = (warp - 4) >> 2, turn = group / kRb, rb = group % kRb, bar_id = 1 + group;
+    const int group = (warp - kWarpSoftmax) >> 2, turn = group / kRb, rb = group % kRb, bar_id = 1 + group;
     const int w = warp & 3, key_in = w * 32 + lane;
     const uint32_t lane_addr = tmem + ((uint32_t)(w * 32) << 16);
     const uint32_t o_addr = lane_addr + (uint32_t)(L::kO + turn * kBoxes * L::kN2 + rb * 4 * kR);
@@ -485,7 +509,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     int o_uses = 0;
     for (; !at.done(); at.next_segment()) {
       const int qb = at.seg & 1, e = at.e, s0 = at.s0, s1 = at.s1;
-      ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->q_full[qb], (at.seg >> 1) & 1, abort_flag));
+      ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.q_full[qb], (at.seg >> 1) & 1, abort_flag));
       const Entry x = tail->entry[qb];
       const int row0 = group0 + rb * kR, nrows = min(kR, x.nq * a.G - row0), all_see = x.n - (x.nq - 1);
       const float* factor = factor_sm + qb * L::kRows + rb * kR;
@@ -513,7 +537,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         const int key0 = (t - pref[e]) * kTileKeys, key = key0 + key_in;
         const float2 sc = next_scale;
         if (ok && t + L::kTurns < s1) next_scale = scales(t + L::kTurns);
-        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->s_full[sb], phase, abort_flag));
+        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.s_full[sb], phase, abort_flag));
         float l[kR];
         const float lv = (float)((int)(__float_as_uint(sc.y) >> 23) - 127);     // log2 of a power of two
         bool over = false;
@@ -526,7 +550,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           ptx::tmem_wait_ld();
           ptx::tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(&tail->s_empty[sb]);
+          if (lane == 0) ptx::mbar_arrive(&tail->bars.s_empty[sb]);
           const bool edge = key0 + kTileKeys > all_see;
 #pragma unroll
           for (int g = 0; g < kR; ++g) {
@@ -567,7 +591,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           }
           if (ok && t > first) {                                       // O holds this turn's tiles before this one
             const int before = it - L::kTurns;
-            ok = __all_sync(0xffffffffu, wait_or_abort(&tail->p_empty[before % L::kBuffers], (before / L::kBuffers) & 1, abort_flag));
+            ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.p_empty[before % L::kBuffers], (before / L::kBuffers) & 1, abort_flag));
             if (ok) {
               ptx::tc_fence_after_sync();
 #pragma unroll
@@ -587,7 +611,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           group_any(bar_id, false);                                    // red_sm has been read
         }
         // ---- weights and their terms
-        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->p_empty[sb], phase ^ 1, abort_flag));
+        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.p_empty[sb], phase ^ 1, abort_flag));
         if (ok) {
           uint32_t p[kR];                                              // four codes: rows 4 q .. of term k at k kR / 4 + q
 #pragma unroll
@@ -612,8 +636,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             // V may come after S.  A wait by parity must not meet a phase two behind: the slot's tile before this one is
             // done with, since this tile's weights had a free buffer, or (rings shorter than the buffers) after this wait.
             if (a.v_slots < L::kBuffers && it >= a.v_slots)
-              wait_or_abort(&tail->p_empty[(it - a.v_slots) % L::kBuffers], ((it - a.v_slots) / L::kBuffers) & 1, abort_flag);
-            wait_or_abort(&tail->v_full[it % a.v_slots], (it / a.v_slots) & 1, abort_flag);
+              wait_or_abort(&tail->bars.p_empty[(it - a.v_slots) % L::kBuffers], ((it - a.v_slots) / L::kBuffers) & 1, abort_flag);
+            wait_or_abort(&tail->bars.v_full[it % a.v_slots], (it / a.v_slots) & 1, abort_flag);
             uint8_t* v = v_ring + (size_t)(it % a.v_slots) * L::kSlot + key_in * 128;
             for (int y = 0; y < kBoxes; ++y)
               for (int i = 0; i < 8; ++i) {
@@ -640,7 +664,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           ptx::fence_proxy_async();
         }
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&tail->p_full[sb]);
+        if (lane == 0) ptx::mbar_arrive(&tail->bars.p_full[sb]);
       }
 
       // ---- the segment's result
@@ -655,7 +679,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       const bool whole = L::kTurns == 1 && pref[e] >= t0 && pref[e + 1] <= t1;   // this CTA alone has the entry, in one O
       const int64_t slot = (((int64_t)blockIdx.y * (entries + B) + e + b) * L::kTurns + turn) * a.group_rows + rb * kR;
       if (any_tile) {
-        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->o_full[turn], o_uses & 1, abort_flag));
+        ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.o_full[turn], o_uses & 1, abort_flag));
         ++o_uses;
       }
       if (ok) {
@@ -680,19 +704,16 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
                   auto term = [&](int k) { return __uint_as_float(v[k * kR + g]); };
                   float o = fmaf(term(3), 0.000244140625f, fmaf(term(2), 0.00390625f, fmaf(term(1), 0.0625f, term(0))));
                   const float f = exp2_fast(0.5f * (refn[g] - refd[g]));       // (in two steps: it may lie below 2^-126)
-                  o = total == 0.f ? 0.f : o * 0.25f / total * f * f;          // (kUp = 2)
+                  o = total == 0.f ? 0.f : o * 0.25f * __frcp_rn(total) * f * f;   // (kUp = 2)
                   if (nan_seen && ((nan_sm[(rb * kR + g) * kBoxes * 4 + (d >> 5)] >> (d & 31)) & 1u)) o = __uint_as_float(0x7fffffffu);
-                  const int qrow = row0 + g;
-                  if (whole) {
-                    const int token = qrow / a.G, head = x.h * a.G + qrow - token * a.G;
-                    a.out[(int64_t)(x.q0 + token) * a.o_tok + (int64_t)head * a.o_head + d] = __float2bfloat16(o);
-                    if (d == 0 && a.lse)
-                      a.lse[(int64_t)(x.q0 + token) * a.Hkv * a.G + head] = total == 0.f ? -INFINITY : (refd[g] + log2f(total)) * 0.6931471805599453f;
-                  } else {
-                    a.part_o[(slot + g) * a.d_k + d] = o;
-                  }
+                  if (whole) a.out[tail->out_at[qb][rb * kR + g] + d] = __float2bfloat16(o);
+                  else a.part_o[(slot + g) * a.d_k + d] = o;
                 }
-                if (d == 0) a.part_ml[slot + g] = make_float2(total == 0.f ? -INFINITY : refd[g], total);
+                if (d == 0) {
+                  a.part_ml[slot + g] = make_float2(total == 0.f ? -INFINITY : refd[g], total);
+                  if (whole && a.lse)
+                    a.lse[tail->lse_at[qb][rb * kR + g]] = total == 0.f ? -INFINITY : (refd[g] + log2f(total)) * 0.6931471805599453f;
+                }
               }
             }
           }
@@ -701,8 +722,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       }
       __syncwarp();
       if (lane == 0) {
-        if (any_tile) ptx::mbar_arrive(&tail->o_empty[turn]);
-        ptx::mbar_arrive(&tail->q_empty[qb]);
+        if (any_tile) ptx::mbar_arrive(&tail->bars.o_empty[turn]);
+        ptx::mbar_arrive(&tail->bars.q_empty[qb]);
       }
       group_any(bar_id, false);                                        // red_sm has been read
     }
@@ -748,10 +769,10 @@ attend8_finish_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows,
   const bool merging = (int64_t)blockIdx.x < (int64_t)entries * max_rows;
   if (merging) {
     const int e = blockIdx.x / max_rows, row = blockIdx.x - e * max_rows;
-    const Entry x = entry_of(a, e);
-    if (row >= x.nq * a.G) return;
     const int group = row / a.group_rows, in_group = row - group * a.group_rows;
     const int2 v = a.info[(int64_t)group * entries + e];
+    const Entry x = entry_of(a, e);
+    if (row >= x.nq * a.G) return;
     if (a.turns == 1 && v.x >= 0 && v.x == v.y) return; // the first kernel has written it
     const float2 ml = merged_ml(a, B, group, e, v, in_group, entries);
     const int quads = a.d_k >> 2, part = tid >> 5, lane = tid & 31;
@@ -822,9 +843,10 @@ Cut cut_of(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t m
   Cut c;
   const int64_t rows = max_q * (p->n_q_heads / p->n_kv_heads);
   c.boxes = p->d_k <= 128 ? 1 : 2;
-  // beyond 32 rows the codes are read again (from L2)
-  c.kr = rows <= 4 ? 4 : 8;
-  c.rb = rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : 4;
+  // Groups of four rows while there are groups enough (a group of eight takes twice as long and spills); beyond 32 rows
+  // the codes are read again (from L2).
+  c.kr = rows <= 16 ? 4 : 8;
+  c.rb = rows > 32 ? 4 : (int)ceil_div(rows > 0 ? rows : 1, c.kr);
   c.turns = c.rb == 1 ? 4 : c.rb == 2 ? 2 : 1;
   c.rows = c.kr * c.rb;
   c.groups = (int)ceil_div(rows > 0 ? rows : 1, c.rows);
@@ -855,12 +877,12 @@ int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], AttendArgs a, cudaS
 }
 template <int kBoxes>
 int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], const AttendArgs& a, cudaStream_t st) {
-  if (c.kr == 4) return run_attend<kBoxes, 4, 1>(c, tm, a, st);
+  if (c.kr == 8) return c.rb == 3 ? run_attend<kBoxes, 8, 3>(c, tm, a, st) : run_attend<kBoxes, 8, 4>(c, tm, a, st);
   switch (c.rb) {
-    case 1: return run_attend<kBoxes, 8, 1>(c, tm, a, st);
-    case 2: return run_attend<kBoxes, 8, 2>(c, tm, a, st);
-    case 3: return run_attend<kBoxes, 8, 3>(c, tm, a, st);
-    default: return run_attend<kBoxes, 8, 4>(c, tm, a, st);
+    case 1: return run_attend<kBoxes, 4, 1>(c, tm, a, st);
+    case 2: return run_attend<kBoxes, 4, 2>(c, tm, a, st);
+    case 3: return run_attend<kBoxes, 4, 3>(c, tm, a, st);
+    default: return run_attend<kBoxes, 4, 4>(c, tm, a, st);
   }
 }
 
