@@ -4,10 +4,10 @@
 // with k_n, v_n = code * scale of the row's block.  A few rows of queries against long K and V: bound by reading the codes
 // once, 2 d_k bytes per cached row.
 //
-// Split.  The rows of all (request, KV head) pairs ("entries") are cut into tiles of 128 and laid end to end; CTA b of the
-// grid takes tiles T b / grid .. T (b + 1) / grid - 1, whatever entries they belong to.  So pruned heads of very
-// different length load every SM alike, without knowing the lengths on the host: each CTA adds up the entries' tiles
-// itself.  What a CTA has of one entry is a segment; its result (reference, sum, output) goes to slot entry + CTA, or
+// Split.  The rows of all (request, KV head) pairs ("entries") are cut into tiles of 128 and laid end to end, each entry
+// behind a gap of kGap tiles, about what beginning and ending one costs; CTA b of the grid takes the tiles between C b / grid
+// and C (b + 1) / grid, whatever entries they belong to.  So pruned heads of very different length load every SM alike,
+// without knowing the lengths on the host: each CTA adds up the entries itself.  What a CTA has of one entry is a segment; its result (reference, sum, output) goes to slot entry + CTA, or
 // straight to the output when the entry lies within one CTA.  attend8_finish_kernel merges an entry's segments.
 //
 // The products run on the codes themselves (tcgen05.mma kind::f8f6f4, e4m3 x e4m3, 32-bit sums), with the cached rows on
@@ -46,6 +46,7 @@ namespace {
 constexpr int kTileKeys = 128;
 constexpr int kBoxRows = 32;
 constexpr int kMaxEntries = 1024;      // entries per launch: their tiles are added up in shared memory
+constexpr int kGap = 4;
 constexpr int kMaxSlots = 8;           // of a ring
 constexpr int kMaxBuffers = 4;         // of S and of P
 constexpr int kSms = 148;
@@ -193,20 +194,24 @@ struct Layout {                         // threads, tensor memory (columns), sha
   static constexpr size_t fixed() { return (size_t)2 * kQ + kBuffers * kP + kSmall + sizeof(Tail); }
 };
 
-// The tiles of a CTA in order: entries e with tiles, tiles t of the CTA's share, seg and it counting both.
+// The tiles of a CTA in order: segments (entry e, its tiles s0 .. s1 - 1), tiles t; seg and it count both.
+// pref: tiles and gaps before each entry; an entry without tiles has no gap.
 struct Walk {
   int e, t, s0, s1, seg, it;
   const int* pref;
   int t0, t1, entries;
   __device__ __forceinline__ Walk(const int* pref_, int t0_, int t1_, int entries_, int e_first)
       : e(e_first), seg(0), it(0), pref(pref_), t0(t0_), t1(t1_), entries(entries_) { enter(); }
-  __device__ __forceinline__ bool done() const { return e >= entries || pref[e] >= t1; }
+  __device__ __forceinline__ bool done() const { return e >= entries; }
   __device__ __forceinline__ void enter() {
-    while (!done() && pref[e + 1] == pref[e]) ++e;
-    if (done()) return;
-    s0 = max(t0, pref[e]);
-    s1 = min(t1, pref[e + 1]);
-    t = s0;
+    for (; e < entries; ++e) {
+      const int p = pref[e];
+      if (p >= t1) break;
+      s0 = max(t0 - p - kGap, 0);
+      s1 = min(t1, pref[e + 1]) - p - kGap;
+      if (s0 < s1) { t = s0; return; }
+    }
+    e = entries;
   }
   __device__ __forceinline__ void next_segment() { it += s1 - t; ++e; ++seg; enter(); }
   __device__ __forceinline__ void next_tile() {
@@ -258,7 +263,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     ptx::tmem_alloc(&tail->tmem_slot, L::kAlloc);
     ptx::tmem_relinquish();
   }
-  // ---- tiles before each entry
+  // ---- tiles and gaps before each entry
   {
     const int per = (entries + L::kThreads - 1) / L::kThreads;         // consecutive entries per thread
     const int e0 = min(tid * per, entries), e1 = min(e0 + per, entries);
@@ -266,8 +271,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     for (int e = e0; e < e1; ++e) {
       const Entry x = entry_of(a, e);
       const int t = group0 < x.nq * a.G ? (x.n + kTileKeys - 1) / kTileKeys : 0;
-      pref[e + 1] = t;
-      mine += t;
+      pref[e + 1] = t > 0 ? t + kGap : 0;
+      mine += pref[e + 1];
     }
     int inc = mine;
 #pragma unroll
@@ -288,11 +293,11 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   const uint32_t tmem = __shfl_sync(0xffffffffu, tail->tmem_slot, 0);
   const int T = pref[entries], B = gridDim.x, b = blockIdx.x;
   const int t0 = (int)((int64_t)T * b / B), t1 = (int)((int64_t)T * (b + 1) / B);
-  // which CTAs hold an entry: the CTA of tile t is the largest c with T c / B <= t
+  // which CTAs hold an entry: the CTA of the tile at place t is the largest c with T c / B <= t
   if (b == 0) {
     int2* info = a.info + (int64_t)blockIdx.y * entries;
     for (int e = tid; e < entries; e += L::kThreads) {
-      const int f = pref[e], l = pref[e + 1] - 1;
+      const int f = pref[e] + kGap, l = pref[e + 1] - 1;
       int2 v = make_int2(-1, -1);
       if (l >= f) v = make_int2((int)((((int64_t)f + 1) * B - 1) / T), (int)((((int64_t)l + 1) * B - 1) / T));
       info[e] = v;
@@ -333,7 +338,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           Walk& w = walk[i];
           if (w.done() || !ptx::mbar_test_wait(&f.empty[f.slot], f.phase ^ 1u)) continue;
           if (f.seg != w.seg) { f.x = entry_of(a, w.e); f.seg = w.seg; }
-          const int key0 = (w.t - pref[w.e]) * kTileKeys, parts = min(kTileKeys / kBoxRows, (f.x.n - key0 + kBoxRows - 1) / kBoxRows);
+          const int key0 = w.t * kTileKeys, parts = min(kTileKeys / kBoxRows, (f.x.n - key0 + kBoxRows - 1) / kBoxRows);
           uint8_t* dst = f.ring + (size_t)f.slot * L::kSlot;
           uint64_t* full = &f.full[f.slot];
           ptx::mbar_arrive_expect_tx(full, (uint32_t)parts * kBoxes * kBoxRows * 128);
@@ -438,8 +443,6 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       const int qb = at.seg & 1;
       const Entry x = entry_of(a, at.e);
       const int rows = x.nq * a.G;
-      ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.q_empty[qb], ((at.seg >> 1) & 1) ^ 1, abort_flag));
-      if (!ok) break;
       uint8_t* dst = q_sm + qb * L::kQ;
 #pragma unroll 1
       for (int rb = 0; rb < kRb; ++rb) {
@@ -453,9 +456,11 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
 #pragma unroll
           for (int y = 0; y < kBoxes; ++y) {
             const int d = y * 128 + lane * 4;
-            v[i][y] = holds && d < a.d_k ? *reinterpret_cast<const uint2*>(src + d) : make_uint2(0, 0);
+            v[i][y] = holds && d < a.d_k ? __ldg(reinterpret_cast<const uint2*>(src + d)) : make_uint2(0, 0);
           }
         }
+        if (rb == 0) ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.q_empty[qb], ((at.seg >> 1) & 1) ^ 1, abort_flag));
+        if (!ok) break;
 #pragma unroll
         for (int i = 0; i < kR; ++i) {
           const int row = rb * kR + i, qrow = group0 + row;
@@ -493,6 +498,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           }
         }
       }
+      if (!ok) break;
       if (lane == 0) tail->entry[qb] = x;
       ptx::fence_proxy_async();
       __syncwarp();
@@ -524,7 +530,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       }
       const int64_t sb0 = (int64_t)x.h * a.row_blocks + block8_offset(x.start, x.r);
       auto scales = [&](int t) {
-        const int key = (t - pref[e]) * kTileKeys + key_in;
+        const int key = t * kTileKeys + key_in;
         return key < x.n ? make_float2(a.k_scale[sb0 + (key >> 6)], a.v_scale[sb0 + (key >> 6)]) : make_float2(0.f, 1.f);
       };
       // Tile it is turn it mod kTurns', and buffer it mod kBuffers is always the same turn's: a group meets every phase of
@@ -534,7 +540,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       float2 next_scale = ok && any_tile ? scales(first) : make_float2(0.f, 1.f);
       for (int t = first; t < s1; t += L::kTurns) {
         const int it = at.it + t - s0, sb = it % L::kBuffers, phase = (it / L::kBuffers) & 1;
-        const int key0 = (t - pref[e]) * kTileKeys, key = key0 + key_in;
+        const int key0 = t * kTileKeys, key = key0 + key_in;
         const float2 sc = next_scale;
         if (ok && t + L::kTurns < s1) next_scale = scales(t + L::kTurns);
         ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.s_full[sb], phase, abort_flag));
@@ -676,7 +682,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         if (lane == 0) red_sm[w * 2 * kR + g] = s;
       }
       group_any(bar_id, false);
-      const bool whole = L::kTurns == 1 && pref[e] >= t0 && pref[e + 1] <= t1;   // this CTA alone has the entry, in one O
+      const bool whole = L::kTurns == 1 && s0 == 0 && s1 == pref[e + 1] - pref[e] - kGap;   // all of the entry, in one O
       const int64_t slot = (((int64_t)blockIdx.y * (entries + B) + e + b) * L::kTurns + turn) * a.group_rows + rb * kR;
       if (any_tile) {
         ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.o_full[turn], o_uses & 1, abort_flag));
