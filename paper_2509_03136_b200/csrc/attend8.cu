@@ -8,7 +8,7 @@
 // behind a gap of kGap tiles, about what beginning and ending one costs; CTA b of the grid takes the tiles between C b / grid
 // and C (b + 1) / grid, whatever entries they belong to.  So pruned heads of very different length load every SM alike,
 // without knowing the lengths on the host: each CTA adds up the entries itself.  What a CTA has of one entry is a segment; its result (reference, sum, output) goes to slot entry + CTA, or
-// straight to the output when the entry lies within one CTA.  attend8_finish_kernel merges an entry's segments.
+// straight to the output when the entry lies within one CTA.  attend8_merge_kernel merges an entry's segments.
 //
 // The products run on the codes themselves (tcgen05.mma kind::f8f6f4, e4m3 x e4m3, 32-bit sums), with the cached rows on
 // the M axis, so that nothing has to be widened or transposed on the way from the TMA boxes to the tensor cores:
@@ -31,8 +31,8 @@
 // references and an O of its own (one group alone needs 3000 clocks of latency for a tile, the memory 1400), with many
 // the groups share a tile's rows out.  S and P are buffered as deep as the MMAs run ahead.
 //
-// Weights for the eviction: the logits are kept (4 bytes per row and query, against 2 d_k per row), and the finishing
-// kernel turns them into weights once lse is known; a slot belongs to one thread, so the sum has one order.
+// Weights for the eviction: the logits are kept (4 bytes per row and query, against 2 d_k per row), and
+// attend8_weights_kernel turns them into weights once lse is known; a slot belongs to one thread, so the sum has one order.
 //
 // Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
 #include <cstddef>
@@ -66,6 +66,7 @@ struct AttendArgs {
   __nv_bfloat16* out;
   int64_t o_tok, o_head;
   float* lse;            // or null
+  float* lse2;           // [total_q][n_q_heads] base 2
   const float* acc;
   float* acc_out;        // or null
   float* part_o;         // [row groups][entries + CTAs][turns][rows of a group][d_k], each divided by its own sum
@@ -159,6 +160,13 @@ __device__ __forceinline__ uint32_t take_term(float (&x)[4]) {
   x[2] = (x[2] - b.x) * 16.f;
   x[3] = (x[3] - b.y) * 16.f;
   return c;
+}
+
+// A query row's log-sum-exp: base 2 for the weights, natural for the caller.
+__device__ __forceinline__ void write_lse(const AttendArgs& a, int64_t at, float2 ml) {
+  const float l = ml.x == -INFINITY ? -INFINITY : ml.x + log2f(ml.y);
+  a.lse2[at] = l;
+  if (a.lse) a.lse[at] = l * 0.6931471805599453f;
 }
 
 // Counts: one arrival, 1 + 4 groups on q_empty, four per group that shares a tile's rows from s_empty on.
@@ -717,8 +725,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
                 }
                 if (d == 0) {
                   a.part_ml[slot + g] = make_float2(total == 0.f ? -INFINITY : refd[g], total);
-                  if (whole && a.lse)
-                    a.lse[tail->lse_at[qb][rb * kR + g]] = total == 0.f ? -INFINITY : (refd[g] + log2f(total)) * 0.6931471805599453f;
+                  if (whole) write_lse(a, tail->lse_at[qb][rb * kR + g], make_float2(total == 0.f ? -INFINITY : refd[g], total));
                 }
               }
             }
@@ -744,19 +751,13 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   }
 }
 
-// What an entry's segments say of one row: the maximum, and the sum relative to it.  A whole warp asks; the segments are
-// spread over its lanes, so that their loads are in flight together.
-__device__ __forceinline__ float2 merged_ml(const AttendArgs& a, int B, int group, int e, int2 v, int in_group, int entries) {
-  // (the turns of one CTA's slot and the slots of consecutive CTAs follow one another)
-  const float2* ml = a.part_ml + ((int64_t)group * (entries + B) + e) * a.turns * a.group_rows + in_group;
-  float M = -INFINITY, L = 0.f;
-  for (int b = v.x * a.turns + (int)(threadIdx.x & 31); v.x >= 0 && b < (v.y + 1) * a.turns; b += 32) {
-    const float2 x = ml[(int64_t)b * a.group_rows];
-    const float top = fmaxf(M, x.x);
-    if (top != -INFINITY) L = L * exp2_fast(M - top) + x.y * exp2_fast(x.x - top);
-    else L += x.y;                                      // (a NaN in the sum stays)
-    M = top;
-  }
+// Running (maximum, sum relative to it), joined with another pair; and over a warp.
+__device__ __forceinline__ void join(float& M, float& L, float2 x) {
+  const float top = fmaxf(M, x.x);
+  L = top == -INFINITY ? L + x.y : L * exp2_fast(M - top) + x.y * exp2_fast(x.x - top);     // (a NaN in the sum stays)
+  M = top;
+}
+__device__ __forceinline__ float2 warp_join(float M, float L) {
   const float all = warp_max(M);
   L = all == -INFINITY ? L : L == 0.f ? 0.f : L * exp2_fast(M - all);
 #pragma unroll
@@ -764,26 +765,33 @@ __device__ __forceinline__ float2 merged_ml(const AttendArgs& a, int B, int grou
   return make_float2(all, L);
 }
 
-// Blocks 0 .. entries * max_rows - 1: one row of one entry, merged from its segments when it has several (or none).
-// The others: 256 slots of one entry each, their weights added to acc.
+// Block = one row of one entry, merged from its segments when it has several (or none).  They are a few KB: what counts is how
+// many loads wait for one another, so the outputs are asked for before the maxima are known.
 __global__ void __launch_bounds__(256)
-attend8_finish_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows, int slot_blocks) {
+attend8_merge_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows) {
   __shared__ float4 s_o[8][32 * 2];
   __shared__ float s_f[4 * kSms];
-  __shared__ float s_neg[GVOTE_ATTEND8_MAX_Q * kMaxGroup8];
-  const int entries = a.batch * a.Hkv, tid = threadIdx.x;
-  const bool merging = (int64_t)blockIdx.x < (int64_t)entries * max_rows;
-  if (merging) {
+  const int entries = a.batch * a.Hkv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  {
     const int e = blockIdx.x / max_rows, row = blockIdx.x - e * max_rows;
     const int group = row / a.group_rows, in_group = row - group * a.group_rows;
     const int2 v = a.info[(int64_t)group * entries + e];
     const Entry x = entry_of(a, e);
     if (row >= x.nq * a.G) return;
     if (a.turns == 1 && v.x >= 0 && v.x == v.y) return; // the first kernel has written it
-    const float2 ml = merged_ml(a, B, group, e, v, in_group, entries);
-    const int quads = a.d_k >> 2, part = tid >> 5, lane = tid & 31;
+    const int quads = a.d_k >> 2;
     const int p0 = v.x * a.turns, parts = v.x < 0 ? 0 : (v.y + 1) * a.turns - p0;
     const int64_t slot0 = (((int64_t)group * (entries + B) + e) * a.turns + p0) * a.group_rows + in_group;
+    constexpr int kAhead = 8;
+    float4 pre[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int k = warp + 8 * i;
+      if (k < parts && lane < quads) pre[i] = *reinterpret_cast<const float4*>(a.part_o + (slot0 + (int64_t)k * a.group_rows) * a.d_k + lane * 4);
+    }
+    float M = -INFINITY, L = 0.f;
+    for (int k = lane; k < parts; k += 32) join(M, L, a.part_ml[slot0 + (int64_t)k * a.group_rows]);
+    const float2 ml = warp_join(M, L);
     for (int i = tid; i < parts; i += 256) {
       const float2 m = a.part_ml[slot0 + (int64_t)i * a.group_rows];
       s_f[i] = m.x == -INFINITY ? 0.f : exp2_fast(m.x - ml.x) * m.y;
@@ -791,18 +799,26 @@ attend8_finish_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows,
     __syncthreads();
     for (int q = lane; q < quads; q += 32) {
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int i = part; i < parts; i += 8) {
-        const float4 p = *reinterpret_cast<const float4*>(a.part_o + (slot0 + (int64_t)i * a.group_rows) * a.d_k + q * 4);
-        const float f = s_f[i];
+      auto add = [&](const float4& p, float f) {        // (0: a turn without tiles has left nothing)
         if (f != 0.f) { s.x = fmaf(f, p.x, s.x); s.y = fmaf(f, p.y, s.y); s.z = fmaf(f, p.z, s.z); s.w = fmaf(f, p.w, s.w); }
+      };
+      int k0 = warp;
+      if (q == lane) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+          if (warp + 8 * i < parts) add(pre[i], s_f[warp + 8 * i]);
+        k0 += 8 * kAhead;
       }
-      s_o[part][q] = s;                                 // (0: a turn without tiles has left nothing)
+#pragma unroll 8
+      for (int k = k0; k < parts; k += 8)
+        add(*reinterpret_cast<const float4*>(a.part_o + (slot0 + (int64_t)k * a.group_rows) * a.d_k + q * 4), s_f[k]);
+      s_o[warp][q] = s;
     }
     __syncthreads();
     const int token = row / a.G, g = x.h * a.G + row % a.G;
     if (tid < quads) {
       float4 s = s_o[0][tid];
+#pragma unroll
       for (int k = 1; k < 8; ++k) {
         const float4 p = s_o[k][tid];
         s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
@@ -811,36 +827,40 @@ attend8_finish_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows,
       __nv_bfloat162 out[2] = {__floats2bfloat162_rn(s.x * inv, s.y * inv), __floats2bfloat162_rn(s.z * inv, s.w * inv)};
       *reinterpret_cast<uint2*>(a.out + (int64_t)(x.q0 + token) * a.o_tok + (int64_t)g * a.o_head + tid * 4) = *reinterpret_cast<uint2*>(out);
     }
-    if (tid == 0 && a.lse)
-      a.lse[(int64_t)(x.q0 + token) * a.Hkv * a.G + g] = ml.x == -INFINITY ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
-    return;
+    if (tid == 0) write_lse(a, (int64_t)(x.q0 + token) * a.Hkv * a.G + g, ml);
   }
-  const int64_t k = (int64_t)blockIdx.x - (int64_t)entries * max_rows;
-  const int h = (int)(k % a.Hkv);
-  const int64_t gb = k / a.Hkv;                         // 256-slot blocks of the requests, request r from (cu[r] >> 8) + r on
-  const int r = a.r0 + (a.batch == 1 ? 0 : find_request_by(a.cu + a.r0, a.batch, gb + (a.cu[a.r0] >> 8), 8));
-  const int e = (r - a.r0) * a.Hkv + h;
+}
+
+// Thread = one slot: the weights its row of the cache gets from the request's tokens and the group's heads, added to acc.
+// Blocks of 256 slots: request r0 + i has those from (cu >> 8) - base + i on.
+__global__ void __launch_bounds__(256)
+attend8_weights_kernel(const __grid_constant__ AttendArgs a) {
+  const int tid = threadIdx.x, h = blockIdx.y;
+  const int64_t gb = blockIdx.x;
+  const int base = a.cu[a.r0] >> 8;
+  int i_req = -1;                                       // the last request whose first block is not behind gb
+  for (int i0 = 0; i0 < a.batch; i0 += 256) {
+    const int i = i0 + tid;
+    i_req += __syncthreads_count(i < a.batch && (int64_t)((a.cu[a.r0 + min(i, a.batch - 1)] >> 8) - base) + i <= gb);
+  }
+  const int e = i_req * a.Hkv + h;
   const Entry x = entry_of(a, e);
-  const int i0 = (int)(gb - ((x.start >> 8) - (a.cu[a.r0] >> 8) + (r - a.r0))) * 256;
-  if (i0 >= x.n || i0 < 0) return;
-  const int rows = x.nq * a.G;
-  for (int row = tid >> 5; row < rows; row += 8) {
-    const int group = row / a.group_rows;
-    const float2 ml = merged_ml(a, B, group, e, a.info[(int64_t)group * entries + e], row - group * a.group_rows, entries);
-    s_neg[row] = ml.x == -INFINITY ? -INFINITY : -(ml.x + log2f(ml.y));
-  }
-  __syncthreads();
-  const int i = i0 + tid;
+  const int i = (int)(gb - ((x.start >> 8) - base + i_req)) * 256 + tid;
   if (i >= x.n) return;
-  float s = 0.f;
+  const int rows = x.nq * a.G;
   const float* l = a.logits + (int64_t)h * a.max_q * a.G * a.total + x.start + i;
-#pragma unroll 4
-  for (int row = 0; row < rows; ++row) {
-    const float v = l[(int64_t)row * a.total];
-    if (v != -INFINITY) s += exp2_fast(v + s_neg[row]);
-  }
+  const float* lse = a.lse2 + (int64_t)x.q0 * a.Hkv * a.G + h * a.G;
   const int64_t slot = (int64_t)h * a.total + x.start + i;
-  a.acc_out[slot] = (a.acc ? a.acc[slot] : 0.f) + s;
+  float s = 0.f;
+  const float was = a.acc ? a.acc[slot] : 0.f;
+  for (int token = 0; token < x.nq; ++token, lse += a.Hkv * a.G) {
+#pragma unroll 4
+    for (int g = 0; g < a.G; ++g, l += a.total) {
+      const float v = *l;
+      if (v != -INFINITY) s += exp2_fast(v - lse[g]);
+    }
+  }
+  a.acc_out[slot] = was + s;
 }
 
 // How a launch is cut: query rows of a softmax group, groups that share a tile's rows, row groups, CTAs.
@@ -904,7 +924,8 @@ AttendMap attend8_map(const gvote_params* p, int32_t batch, int64_t total_tokens
   m.o = kStatusBytes;
   m.ml = align_up(m.o + rows * p->d_k * 4, 256);
   m.info = align_up(m.ml + rows * 8, 256);
-  m.logits = align_up(m.info + c.groups * entries * 8, 256);
+  m.lse = align_up(m.info + c.groups * entries * 8, 256);
+  m.logits = align_up(m.lse + (size_t)total_q * p->n_q_heads * 4, 256);
   m.total = align_up(m.logits + (size_t)p->n_q_heads * nq * total_tokens * 4, 256);
   return m;
 }
@@ -922,6 +943,7 @@ int32_t launch_attend8(const gvote_params* p, const __nv_bfloat16* Q, int64_t q_
   a.cu = c->cu_seqlens; a.kv_len = c->kv_len;
   a.out = out; a.o_tok = o_tok; a.o_head = o_head; a.lse = lse; a.acc = acc; a.acc_out = acc_out;
   a.part_o = (float*)(ws + m.o); a.part_ml = (float2*)(ws + m.ml); a.info = (int2*)(ws + m.info);
+  a.lse2 = (float*)(ws + m.lse);
   a.logits = acc_out ? (float*)(ws + m.logits) : nullptr;
   a.status = (int32_t*)ws;
   a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads; a.d_k = p->d_k; a.max_q = (int)max_q;
@@ -940,12 +962,17 @@ int32_t launch_attend8(const gvote_params* p, const __nv_bfloat16* Q, int64_t q_
     a.r0 = r0;
     a.batch = c->batch - r0 < cut.requests ? c->batch - r0 : cut.requests;
     PROPAGATE(cut.boxes == 1 ? run_attend<1>(cut, tm, a, st) : run_attend<2>(cut, tm, a, st));
-    const int64_t entries = (int64_t)a.batch * a.Hkv, rows = max_q * a.G;
-    const int64_t slots = acc_out ? ((c->total_tokens >> 8) + a.batch) * a.Hkv : 0;
-    LaunchScope scope_("attend8_finish_kernel", st);
-    launch_on(attend8_finish_kernel, dim3((unsigned)(entries * rows + slots)), dim3(256), 0, st, a, (int)cut.ctas, (int)rows,
-              (int)slots);
-    GVOTE_LAUNCH_CHECK("attend8_finish_kernel");
+    const int64_t rows = max_q * a.G;
+    {
+      LaunchScope scope_("attend8_merge_kernel", st);
+      launch_on(attend8_merge_kernel, dim3((unsigned)(a.batch * a.Hkv * rows)), dim3(256), 0, st, a, (int)cut.ctas, (int)rows);
+    }
+    GVOTE_LAUNCH_CHECK("attend8_merge_kernel");
+    if (acc_out) {
+      LaunchScope scope_("attend8_weights_kernel", st);
+      launch_on(attend8_weights_kernel, dim3((unsigned)((c->total_tokens >> 8) + a.batch), a.Hkv), dim3(256), 0, st, a);
+      GVOTE_LAUNCH_CHECK("attend8_weights_kernel");
+    }
   }
   return GVOTE_OK;
 }
