@@ -288,6 +288,8 @@ def _shaped(t: Optional[torch.Tensor], dtype, shape, name: str, dev: torch.devic
     """The pointer of a tensor of this type and shape on `dev`; None stays None."""
     if t is None:
         return None
+    if t.dtype is dtype and t.shape == shape and t.device == dev and t.is_cuda and t.is_contiguous():
+        return t.data_ptr() or None
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
