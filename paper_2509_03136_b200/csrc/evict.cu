@@ -3,12 +3,13 @@
 //
 // A cluster of CTAs per (head, request), each with a run of the row's mask words.  The weights are read once, as
 // order-preserving 32-bit images in shared memory.  A radix search of 11, 11 and 10 bits finds the smallest kept image T:
-// every CTA counts its images per digit, adds its peers' counts through distributed shared memory and finds the
-// digit for itself (no broadcast).  Then the mask words are written: images above T, and of those equal to T as many as
-// are left, lowest slots first; only when T is shared by more rows than are left does the order matter, and the equal
-// ones are then counted run by run.  Latency, not bytes, bounds this: 4 bytes per row are 0.1 us of memory time, the five
-// steps cost a microsecond or two each.  Cluster size: the largest of 8, 4, 2, 1 that leaves a CTA 2048 rows of the longest
-// slab and the grid no more than two CTAs per SM (one row of 128K weights: 17 us with eight CTAs, 138 with one).
+// every CTA counts its images per digit and per 32 digits, adds its peers' counts of the latter, then of the 32 digits in
+// question, through distributed shared memory, and so finds the digit for itself (no broadcast).  Then the mask words are
+// written: images above T, and of those equal to T as many as are left, lowest slots first; only when T is shared by more
+// rows than are left does the order matter, and the equal ones are then counted run by run.  Latency, not bytes,
+// bounds this: 4 bytes per row are 0.1 us of memory time, the five steps cost one to four microseconds each.  Cluster size:
+// the largest of 8, 4, 2, 1 that leaves a CTA 2048 rows of the longest slab and the grid no more CTAs than SMs
+// (four rows of 128K weights: 19 us with eight CTAs each, 138 with one; 128 rows of 300 to 12K: 15 us with one, 21 with two).
 // Shares beyond 36K rows per CTA are read from memory again in every step.
 #include <cooperative_groups.h>
 
@@ -218,7 +219,7 @@ int32_t launch_evict(const gvote_params* p, const float* acc, const int32_t* cu,
                      int64_t total_tokens, int64_t max_N, const int32_t* keep, int32_t n_recent, uint32_t* mask,
                      int32_t* budget, cudaStream_t st) {
   int C = 8;
-  while (C > 1 && (max_N / C < 2048 || (int64_t)batch * p->n_kv_heads * C > 2 * 148)) C >>= 1;
+  while (C > 1 && (max_N / C < 2048 || (int64_t)batch * p->n_kv_heads * C > 148)) C >>= 1;
   const int64_t share = (ceil_div(max_N, 32) + C - 1) / C * 32;
   const int shared_keys = (int)(share < kSharedKeys ? share : kSharedKeys);
   GVOTE_CUDA_CHECK(cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedKeys * 4));

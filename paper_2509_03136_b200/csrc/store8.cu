@@ -5,7 +5,7 @@
 //
 // Two kernels.  store8_scan_kernel turns each (request, head) bit row into an exclusive popcount prefix per
 // mask word, and notes for every destination block what its CTA would otherwise have to look up (struct Note).
-// store8_kernel gives one CTA one destination block of K and of V: its threads list the set bits of a word each from
+// store8_kernel gives one CTA one destination block of K and of V: its threads take a bit each of the words from
 // the noted one on, load all rows into registers (16 values per thread and unit, 16-byte loads), take the maximum
 // over the CTA, and write the codes.  Bound by memory: 6 d_k bytes per kept row from bf16, 4 d_k from e4m3; the rows are
 // read once, there is no second pass over them.  What a CTA waits for before it can ask for its rows is two rounds of
@@ -134,6 +134,7 @@ __device__ __forceinline__ uint32_t half2_abs_max(uint32_t a, uint32_t b) {     
 template <>
 struct Unit<false> {
   uint4 lo, hi;
+  bool finite;
   __device__ __forceinline__ void load(const void* base, int64_t elem, float) {
     const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + elem);
     lo = __ldg(q);
@@ -141,11 +142,12 @@ struct Unit<false> {
   }
   __device__ __forceinline__ uint32_t word(int i) const { return i < 4 ? (&lo.x)[i] : (&hi.x)[i - 4]; }
   // The largest finite magnitude.  Magnitudes of bf16 are ordered like their bits; 0x7f80 and above are not finite.
-  __device__ __forceinline__ float largest() const {
+  __device__ __forceinline__ float largest() {
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = __vmaxu2(m, word(i) & 0x7fff7fffu);
-    if ((m & 0xffffu) >= 0x7f80u || (m >> 16) >= 0x7f80u) {      // rare: leave out what is not finite
+    finite = (m & 0xffffu) < 0x7f80u && (m >> 16) < 0x7f80u;
+    if (!finite) {                                               // rare: leave out what is not
       m = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -157,15 +159,13 @@ struct Unit<false> {
   }
   __device__ __forceinline__ uint4 encode(float scale, float inv) const {
     uint4 out;
-    uint32_t top = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const uint32_t a = word(2 * q), b = word(2 * q + 1);
-      top = __vmaxu2(top, __vmaxu2(a & 0x7fff7fffu, b & 0x7fff7fffu));
       (&out.x)[q] = narrow8x4(__uint_as_float(a << 16) * inv, __uint_as_float(a & 0xffff0000u) * inv,
                               __uint_as_float(b << 16) * inv, __uint_as_float(b & 0xffff0000u) * inv);
     }
-    if ((top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u) {  // rare: an infinity is not 448 but the NaN code
+    if (!finite) {                                               // rare: an infinity is not 448 but the NaN code
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -184,7 +184,7 @@ struct Unit<true> {
     lo = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + elem));
     scale = s;
   }
-  __device__ __forceinline__ float largest() const {
+  __device__ __forceinline__ float largest() {
     uint32_t m = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -238,21 +238,25 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
     cnt = note.y; row0 = note.w; r = where.x; start = where.y; dstart = where.z;
     if (cnt <= 0) return;
     const int64_t woff = (int64_t)h * a.row_words + mask_word_offset(start, r);
-    for (int base = note.x;; base += kStoreThreads) {
-      const int w = base + tid;
-      int end = cnt;
-      if (w < note.z) {
-        // (bits behind the rows that count come after the last of the cnt ranks)
-        uint32_t bits = a.mask[woff + w];
-        int rank = a.prefix[woff + w] - row0;
-        while (bits && rank < cnt) {
-          if (rank >= 0) s_src[rank] = w * 32 + __ffs((int)bits) - 1;
-          bits &= bits - 1u;
-          ++rank;
-        }
-        end = rank;
+    // thread = one bit of a word, four words per warp and round
+    constexpr int kWarps = kStoreThreads / 32;
+    const int lane = tid & 31;
+    for (int base = note.x + (tid >> 5);; base += 4 * kWarps) {
+      uint32_t bits[4];
+      int rank[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int w = base + j * kWarps;
+        bits[j] = w < note.z ? a.mask[woff + w] : 0u;
+        rank[j] = w < note.z ? a.prefix[woff + w] - row0 : cnt;
       }
-      if (__syncthreads_or(end >= cnt)) break;                   // (ranks grow with the words)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // (bits behind the rows that count come after the last of the cnt ranks)
+        const int mine = rank[j] + __popc(bits[j] & ((1u << lane) - 1u));
+        if (((bits[j] >> lane) & 1u) && mine >= 0 && mine < cnt) s_src[mine] = (base + j * kWarps) * 32 + lane;
+      }
+      if (__syncthreads_or(rank[3] + __popc(bits[3]) >= cnt)) break;   // (ranks grow with the words)
     }
   } else {
     r = a.batch == 1 ? 0 : find_request_by(a.cu8, a.batch, gb, 6);
@@ -269,6 +273,13 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
     if (cnt <= 0) return;
     if (tid < cnt) s_src[tid] = row0 + tid;
     __syncthreads();
+  }
+  float weight = 0.f;                                            // of the side arrays, on their way with the rows
+  int position = 0;
+  if (tid < cnt) {
+    const int64_t s = (int64_t)h * a.s_total + start + s_src[tid];
+    if (a.side.acc_out) weight = a.side.acc[s];
+    if (a.side.pos_out) position = a.side.pos ? a.side.pos[s] : s_src[tid];
   }
   // thread = one unit of every (threads / units per row)-th row
   const int dc = a.d_k >> 4, step = kStoreThreads / dc, j0 = tid / dc, c0 = (tid - j0 * dc) * 16;
@@ -307,10 +318,9 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
       if (holds(i)) *reinterpret_cast<uint4*>(a.dst[t] + d0 + (j0 + i * step) * a.d_tok) = x[t][i].encode(scale, inv);
   }
   if (tid < cnt) {
-    const int64_t s = (int64_t)h * a.s_total + start + s_src[tid];
     const int64_t d = (int64_t)h * a.d_total + dstart + row0 + tid;
-    if (a.side.acc_out) a.side.acc_out[d] = a.side.acc[s];
-    if (a.side.pos_out) a.side.pos_out[d] = a.side.pos ? a.side.pos[s] : s_src[tid];
+    if (a.side.acc_out) a.side.acc_out[d] = weight;
+    if (a.side.pos_out) a.side.pos_out[d] = position;
   }
 }
 
