@@ -159,29 +159,37 @@ __device__ __forceinline__ int find_request_div(const int32_t* __restrict__ cu, 
   return lo;
 }
 
+// Of a batch's first request: where its keys and queries are (the only one's, when there is one).
+struct Only { int start, n, q0, nq; };
+
 // The unit this CTA takes in round k: left to right in even rounds, right to left in odd ones.
 __device__ __forceinline__ uint32_t unit_of(uint32_t k) {
   return k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
 }
 
 template <int kPass>
-__device__ __forceinline__ UnitInfo unit_info(const AccArgs& a, uint32_t u) {
+__device__ __forceinline__ UnitInfo unit_info(const AccArgs& a, const Only& only, uint32_t u) {
   UnitInfo x;
   uint32_t v = u / (uint32_t)a.Hkv;
   x.h = (int)(u - v * (uint32_t)a.Hkv);
-  const uint32_t w = v / (uint32_t)a.chunks;
-  x.chunk = (int)(v - w * (uint32_t)a.chunks);
-  v = w;
-  if (kPass == 1) {
-    v = a.pairs - 1 - v;                                   // long rows first
-    x.r = a.batch == 1 ? 0 : find_request_div(a.cu_q, a.batch, v, 2 * a.tpt);
-  } else {
-    x.r = a.batch == 1 ? 0 : find_request_by(a.cu, a.batch, v, 8);
+  x.chunk = 0;
+  if (a.chunks > 1) {
+    const uint32_t w = v / (uint32_t)a.chunks;
+    x.chunk = (int)(v - w * (uint32_t)a.chunks);
+    v = w;
   }
-  x.start = a.cu[x.r];
-  x.n = valid_keys(a.kv_len, x.r, a.Hkv, x.h, a.cu[x.r + 1] - x.start);
-  x.q0 = a.cu_q[x.r];
-  x.nq = a.cu_q[x.r + 1] - x.q0;
+  if (kPass == 1) v = a.pairs - 1 - v;                     // long rows first
+  if (a.batch == 1) {                                      // (the lookups cost a short unit a sixth of its time)
+    x.r = 0;
+    x.start = only.start; x.q0 = only.q0; x.nq = only.nq;
+    x.n = valid_keys(a.kv_len, 0, a.Hkv, x.h, only.n);
+  } else {
+    x.r = kPass == 1 ? find_request_div(a.cu_q, a.batch, v, 2 * a.tpt) : find_request_by(a.cu, a.batch, v, 8);
+    x.start = a.cu[x.r];
+    x.n = valid_keys(a.kv_len, x.r, a.Hkv, x.h, a.cu[x.r + 1] - x.start);
+    x.q0 = a.cu_q[x.r];
+    x.nq = a.cu_q[x.r + 1] - x.q0;
+  }
   const int q_tiles = (x.nq + a.tpt - 1) / a.tpt;
   if (kPass == 1) {
     x.stat0 = 2 * (int)(v - (x.q0 / (2 * a.tpt) + x.r));
@@ -249,6 +257,7 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   const uint32_t tmem = __shfl_sync(0xffffffffu, tail->tmem_slot, 0);
   volatile int* abort_flag = &tail->abort_flag;
   const int q_rows = a.G * a.tpt;                                  // rows a query box fills
+  const Only only = {a.cu[0], a.cu[1] - a.cu[0], a.cu_q[0], a.cu_q[1] - a.cu_q[0]};
   const uint32_t q_bytes = (uint32_t)a.boxes * q_rows * 128, k_bytes = tile_bytes;
 
   if (warp == 0) {
@@ -259,7 +268,7 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
       for (uint32_t k = 0; ok && k * gridDim.x < a.units; ++k) {
         const uint32_t u = unit_of(k);
         if (u >= a.units) continue;
-        const UnitInfo x = unit_info<kPass>(a, u);
+        const UnitInfo x = unit_info<kPass>(a, only, u);
         if (x.n_stat == 0 || x.s1 <= x.s0) continue;
         const int slot = unit % a.stat_slots;
         ok = wait_or_abort(&tail->stat_empty[slot], ((unit / a.stat_slots) & 1) ^ 1, abort_flag);
@@ -304,7 +313,7 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     for (uint32_t k = 0; ok && k * gridDim.x < a.units; ++k) {
       const uint32_t u = unit_of(k);
       if (u >= a.units) continue;
-      const UnitInfo x = unit_info<kPass>(a, u);
+      const UnitInfo x = unit_info<kPass>(a, only, u);
       if (x.n_stat == 0 || x.s1 <= x.s0) continue;
       const int slot = unit % a.stat_slots;
       ok = __all_sync(0xffffffffu, wait_or_abort(&tail->stat_full[slot], (unit / a.stat_slots) & 1, abort_flag));
@@ -355,7 +364,7 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     for (uint32_t k = 0; ok && k * gridDim.x < a.units; ++k) {
       const uint32_t u = unit_of(k);
       if (u >= a.units) continue;
-      const UnitInfo x = unit_info<kPass>(a, u);
+      const UnitInfo x = unit_info<kPass>(a, only, u);
       if (x.n_stat == 0) continue;
       const bool mine = i < x.n_stat;
       if (kPass == 1) {
@@ -554,6 +563,18 @@ accumulate_sum_kernel(const __grid_constant__ AccArgs a) {
   a.acc_out[slot] = (float)sum;
 }
 
+// Tokens of a query tile: as many as 128 rows hold, fewer where the longest request's tokens can then be dealt out evenly
+// (32 tokens of 7 heads are two tiles of 16 rather than 18 and 14: the last tile needs no mask).
+int tile_tokens(const gvote_params* p, int64_t max_q) {
+  const int64_t most = kTile / (p->n_q_heads / p->n_kv_heads);
+  if (max_q <= 0) return (int)most;
+  return (int)ceil_div(max_q, ceil_div(max_q, most));
+}
+
+// Entries of a list with one entry per `per` tokens begun of every request (request r from cu[r] / per + r on): an upper bound
+// for a batch, which does not know its lengths on the host, exact for one request.
+int64_t list_length(int64_t total, int64_t per, int32_t batch) { return batch == 1 ? ceil_div(total, per) : total / per + batch; }
+
 // Chunks a pass splits its units' streams into, no more than the longest stream has tiles.  Streams of uneven length:
 // about kUnitsPerSm units per SM, which the rounds even out.  Even ones (a window of few tokens): one unit per SM.
 int64_t chunk_count(int64_t units, int64_t tiles, bool even) {
@@ -567,11 +588,12 @@ int64_t chunk_count(int64_t units, int64_t tiles, bool even) {
 AccumulateMap accumulate_map(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N, int64_t total_q,
                              int64_t max_q) {
   AccumulateMap m;
-  const int64_t tpt = kTile / (p->n_q_heads / p->n_kv_heads);
+  m.tpt = tile_tokens(p, max_q);
+  const int64_t tpt = m.tpt;
   m.q_tiles = total_q / tpt + batch;
-  m.key_chunks = chunk_count((total_q / (2 * tpt) + batch) * p->n_kv_heads, ceil_div(max_N, kTile),
+  m.key_chunks = chunk_count(list_length(total_q, 2 * tpt, batch) * p->n_kv_heads, ceil_div(max_N, kTile),
                              batch == 1 && max_q <= max_N / 8);
-  m.q_chunks = chunk_count(((total_tokens >> 8) + batch) * p->n_kv_heads, ceil_div(max_q, tpt), false);
+  m.q_chunks = chunk_count(list_length(total_tokens, 2 * kTile, batch) * p->n_kv_heads, ceil_div(max_q, tpt), false);
   m.lse = kStatusBytes;
   const size_t rows = (size_t)p->n_kv_heads * m.q_tiles * kTile;
   m.part = align_up(m.lse + rows * 4, 256);
@@ -591,7 +613,7 @@ int32_t launch_accumulate(const gvote_params* p, const __nv_bfloat16* Q, int64_t
   a.cu_q = cu_q; a.cu = cu; a.kv_len = kv_len;
   a.lse2 = (float*)(ws + m.lse); a.part = (float2*)(ws + m.part); a.part_sum = (float*)(ws + m.part);
   a.acc = acc; a.acc_out = acc_out; a.status = (int32_t*)ws; a.total = total_tokens;
-  a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads; a.batch = batch; a.d_k = p->d_k; a.tpt = kTile / a.G;
+  a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads; a.batch = batch; a.d_k = p->d_k; a.tpt = m.tpt;
   a.q_tiles = m.q_tiles;
   a.c = (float)(1.4426950408889634 / sqrt((double)p->d_k));
   a.boxes = (p->d_k + 63) / 64;
@@ -617,7 +639,7 @@ int32_t launch_accumulate(const gvote_params* p, const __nv_bfloat16* Q, int64_t
   }
   a.chunks = 1;
   if (!lse) {
-    a.pairs = (uint32_t)(total_q / (2 * a.tpt) + batch);
+    a.pairs = (uint32_t)list_length(total_q, 2 * a.tpt, batch);
     a.chunks = (int)m.key_chunks;
     a.units = a.pairs * a.Hkv * a.chunks;
     GVOTE_CUDA_CHECK(cudaFuncSetAttribute(accumulate_umma_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
@@ -631,7 +653,7 @@ int32_t launch_accumulate(const gvote_params* p, const __nv_bfloat16* Q, int64_t
     launch_on(accumulate_lse_kernel, dim3((unsigned)(4 * a.q_tiles), a.Hkv), dim3(256), 0, st, a, lse);
     GVOTE_LAUNCH_CHECK("accumulate_lse_kernel");
   }
-  a.pairs = (uint32_t)((total_tokens >> 8) + batch);
+  a.pairs = (uint32_t)list_length(total_tokens, 2 * kTile, batch);
   a.chunks = (int)m.q_chunks;
   a.units = a.pairs * a.Hkv * a.chunks;
   GVOTE_CUDA_CHECK(cudaFuncSetAttribute(accumulate_umma_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));

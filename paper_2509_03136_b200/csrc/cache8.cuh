@@ -17,7 +17,7 @@ constexpr int kMaxGroup8 = 128;               // query heads per KV head
 // Scratch of one call behind the status block; the maps of the entry points overlap, since nothing outlives a call.
 struct StoreMap { size_t prefix, note, total; };
 struct AttendMap { size_t o, ml, info, lse, logits, total; };
-struct AccumulateMap { size_t lse, part, total; int64_t q_tiles, key_chunks, q_chunks; };
+struct AccumulateMap { size_t lse, part, total; int64_t q_tiles, key_chunks, q_chunks; int tpt; };
 
 StoreMap store8_map(const gvote_params* p, int32_t batch, int64_t total_tokens);
 AttendMap attend8_map(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N, int64_t total_q,
