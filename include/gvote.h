@@ -325,9 +325,9 @@ static inline int64_t gvote_cache8_block_offset(int64_t cu_seqlens_r, int32_t r)
 }
 
 /* Bytes of scratch the entry points of this part accept as `ws`, for slabs of this size and queries of this
- * size (total_q query tokens in all, max_q of one request at most; 0, 0 for calls without queries).  Where a
- * call has a source and a destination cache, the larger of both sizes.  Zero-fill it once; status word as
- * everywhere (gvote_poll_status).  0 on invalid arguments. */
+ * size (total_q query tokens in all, max_q of one request at most; 0, 0 for calls without queries), and for
+ * every call of no larger sizes.  Where a call has a source and a destination cache, the larger of both.  Zero-fill
+ * it once; status word as everywhere (gvote_poll_status).  0 on invalid arguments. */
 GVOTE_API size_t gvote_cache_workspace_bytes(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N,
                                    int64_t total_q, int64_t max_q);
 

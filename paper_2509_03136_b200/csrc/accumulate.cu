@@ -603,6 +603,16 @@ AccumulateMap accumulate_map(const gvote_params* p, int32_t batch, int64_t total
   return m;
 }
 
+// What any call of no larger sizes needs.  A smaller one may be cut into more chunks: the units of a pass with chunks are no
+// more than those without and kUnitsPerSm per SM besides, of two tiles each.
+size_t accumulate_workspace(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t total_q) {
+  const int64_t most = kTile / (p->n_q_heads / p->n_kv_heads), Hkv = p->n_kv_heads, units = kUnitsPerSm * kSms;
+  // a tile holds half of what it could at least, or a request's every token
+  const int64_t rows = Hkv * (2 * total_q / most + 2 * (int64_t)batch + 2) * kTile;
+  const int64_t p1 = (units * 2 * kTile + 2 * rows) * 8, p2 = (units * 2 * kTile + 2 * Hkv * total_tokens) * 4;
+  return kStatusBytes + (size_t)rows * 4 + (size_t)(p1 > p2 ? p1 : p2) + 1024;
+}
+
 int32_t launch_accumulate(const gvote_params* p, const __nv_bfloat16* Q, int64_t q_tok, int64_t q_head,
                           const int32_t* cu_q, int64_t total_q, int64_t max_q, const __nv_bfloat16* K, int64_t k_tok,
                           int64_t k_head, const int32_t* cu, const int32_t* kv_len, int32_t batch, int64_t total_tokens,

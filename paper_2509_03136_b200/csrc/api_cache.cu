@@ -36,11 +36,10 @@ bool overlap(const void* a, const void* b) { return a == b; }
 
 int64_t larger(int64_t a, int64_t b) { return a > b ? a : b; }
 
-size_t cache_workspace(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N, int64_t total_q,
-                       int64_t max_q) {
+size_t cache_workspace(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t total_q, int64_t max_q) {
   size_t n = store8_map(p, batch, total_tokens).total;
-  const size_t a = attend8_map(p, batch, total_tokens, max_N, total_q, max_q).total;
-  const size_t b = accumulate_map(p, batch, total_tokens, max_N, total_q, max_q).total;
+  const size_t a = attend8_workspace(p, batch, total_tokens, total_q, max_q);
+  const size_t b = max_q > 0 ? accumulate_workspace(p, batch, total_tokens, total_q) : 0;
   if (a > n) n = a;
   return b > n ? b : n;
 }
@@ -55,7 +54,7 @@ extern "C" {
 size_t gvote_cache_workspace_bytes(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N,
                                    int64_t total_q, int64_t max_q) {
   if (validate_shape(p, batch, total_tokens, max_N) != GVOTE_OK || validate_queries(p, total_q, max_q) != GVOTE_OK) return 0;
-  return cache_workspace(p, batch, total_tokens, max_N, total_q, max_q);
+  return cache_workspace(p, batch, total_tokens, total_q, max_q);
 }
 
 int32_t gvote_store8(const gvote_params* p, const void* K, const void* V, int64_t tok_stride, int64_t head_stride,
@@ -135,7 +134,7 @@ int32_t gvote_attend8(const gvote_params* p, const void* Q, int64_t q_tok_stride
   if (acc_or_null && !acc_out_or_null) return GVOTE_ERR_INVALID_ARG;
   if (q_head_stride < p->d_k || q_head_stride % 8 != 0 || q_tok_stride % 8 != 0) return GVOTE_ERR_UNALIGNED;
   if (out_head_stride < p->d_k || out_head_stride % 8 != 0 || out_tok_stride % 8 != 0) return GVOTE_ERR_UNALIGNED;
-  if (ws_bytes < attend8_map(p, cache->batch, cache->total_tokens, cache->max_N, total_q, max_q).total)
+  if (ws_bytes < attend8_map(p, cache->batch, cache->total_tokens, total_q, max_q).total)
     return GVOTE_ERR_WORKSPACE_TOO_SMALL;
   return launch_attend8(p, (const __nv_bfloat16*)Q, q_tok_stride, q_head_stride, cu_q, total_q, max_q, cache,
                         (__nv_bfloat16*)out, out_tok_stride, out_head_stride, lse_or_null, acc_or_null, acc_out_or_null,

@@ -871,7 +871,7 @@ Cut cut_of(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t m
   c.boxes = p->d_k <= 128 ? 1 : 2;
   // Groups of four rows while there are groups enough (a group of eight takes twice as long and spills); beyond 32 rows
   // the codes are read again (from L2).
-  c.kr = rows <= 16 ? 4 : 8;
+  c.kr = rows <= 20 ? 4 : 8;
   c.rb = rows > 32 ? 4 : (int)ceil_div(rows > 0 ? rows : 1, c.kr);
   c.turns = c.rb == 1 ? 4 : c.rb == 2 ? 2 : 1;
   c.rows = c.kr * c.rb;
@@ -908,17 +908,16 @@ int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], const AttendArgs& a
     case 1: return run_attend<kBoxes, 4, 1>(c, tm, a, st);
     case 2: return run_attend<kBoxes, 4, 2>(c, tm, a, st);
     case 3: return run_attend<kBoxes, 4, 3>(c, tm, a, st);
+    case 5: return run_attend<kBoxes, 4, 5>(c, tm, a, st);
     default: return run_attend<kBoxes, 4, 4>(c, tm, a, st);
   }
 }
 
 }  // namespace
 
-AttendMap attend8_map(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N, int64_t total_q,
-                      int64_t max_q) {
+AttendMap attend8_map(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t total_q, int64_t max_q) {
   AttendMap m;
-  const int64_t nq = max_q < GVOTE_ATTEND8_MAX_Q ? max_q : GVOTE_ATTEND8_MAX_Q;
-  const Cut c = cut_of(p, batch, total_tokens, nq);
+  const Cut c = cut_of(p, batch, total_tokens, max_q);
   const size_t entries = (size_t)c.requests * p->n_kv_heads;
   const size_t rows = (size_t)c.groups * (entries + c.ctas) * c.turns * c.rows;
   m.o = kStatusBytes;
@@ -926,14 +925,23 @@ AttendMap attend8_map(const gvote_params* p, int32_t batch, int64_t total_tokens
   m.info = align_up(m.ml + rows * 8, 256);
   m.lse = align_up(m.info + c.groups * entries * 8, 256);
   m.logits = align_up(m.lse + (size_t)total_q * p->n_q_heads * 4, 256);
-  m.total = align_up(m.logits + (size_t)p->n_q_heads * nq * total_tokens * 4, 256);
+  m.total = align_up(m.logits + (size_t)p->n_q_heads * max_q * total_tokens * 4, 256);
   return m;
+}
+
+size_t attend8_workspace(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t total_q, int64_t max_q) {
+  size_t most = 0;                                      // (fewer rows can need more: the groups then take turns)
+  for (int64_t q = 1; q <= max_q && q <= GVOTE_ATTEND8_MAX_Q; ++q) {
+    const size_t n = attend8_map(p, batch, total_tokens, total_q, q).total;
+    most = n > most ? n : most;
+  }
+  return most;
 }
 
 int32_t launch_attend8(const gvote_params* p, const __nv_bfloat16* Q, int64_t q_tok, int64_t q_head, const int32_t* cu_q,
                        int64_t total_q, int64_t max_q, const gvote_cache8* c, __nv_bfloat16* out, int64_t o_tok,
                        int64_t o_head, float* lse, const float* acc, float* acc_out, char* ws, cudaStream_t st) {
-  const AttendMap m = attend8_map(p, c->batch, c->total_tokens, c->max_N, total_q, max_q);
+  const AttendMap m = attend8_map(p, c->batch, c->total_tokens, total_q, max_q);
   const Cut cut = cut_of(p, c->batch, c->total_tokens, max_q);
   AttendArgs a;
   a.Q = Q; a.q_tok = q_tok; a.q_head = q_head; a.cu_q = cu_q;

@@ -20,10 +20,12 @@ struct AttendMap { size_t o, ml, info, lse, logits, total; };
 struct AccumulateMap { size_t lse, part, total; int64_t q_tiles, key_chunks, q_chunks; int tpt; };
 
 StoreMap store8_map(const gvote_params* p, int32_t batch, int64_t total_tokens);
-AttendMap attend8_map(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N, int64_t total_q,
-                      int64_t max_q);
+AttendMap attend8_map(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t total_q, int64_t max_q);
 AccumulateMap accumulate_map(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N, int64_t total_q,
                              int64_t max_q);
+// Sizes that suffice for a call of these sizes and for every smaller one.
+size_t attend8_workspace(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t total_q, int64_t max_q);
+size_t accumulate_workspace(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t total_q);
 
 struct SideArrays {            // per-slot arrays that move with the rows
   const float* acc;

@@ -347,6 +347,41 @@ def test_attend(gv, hq, hkv, d, lens, fill, n_q):
 
 
 @gpu
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("hq,hkv,n_q", [(3, 1, 1), (5, 1, 1), (9, 1, 1), (16, 1, 1), (5, 1, 4), (8, 1, 3), (7, 1, 4), (11, 1, 3), (128, 1, 2)])
+def test_attend_row_counts(gv, hq, hkv, n_q, d):
+    """Every way the query rows are dealt to the softmax groups: 1 to 4, 8, 12, 16, 20, 24, 32 rows, and more than one
+    group of 32, over several requests of very different length."""
+    run_attend(gv, hq, hkv, d, (700, 1, 130, 4000, 260), [[700], [1], [129], [3333], [256]], (n_q, 1, n_q, n_q, 0), seed=hq + n_q)
+
+
+@gpu
+def test_attend_many_short_requests(gv):
+    """More entries than one launch takes (1024), most of them of a single tile or empty, so that a CTA's tiles change
+    their head at every step."""
+    rng = np.random.default_rng(20)
+    lens = tuple(int(x) for x in rng.integers(1, 200, size=150))
+    fill = [[int(rng.integers(0, n + 1)) for _ in range(8)] for n in lens]
+    run_attend(gv, 16, 8, 64, lens, fill, tuple(int(x) for x in rng.integers(0, 4, size=150)), seed=21)
+
+
+@gpu
+def test_a_workspace_serves_every_smaller_call(gv):
+    p = params(gv, 7, 1, 64)
+    rng = np.random.default_rng(22)
+    c, held, cu = fill_cache(gv, p, (500, 300), [[500], [300]], rng)
+    ws = workspace(gv, p, c.geom, 64, 32)
+    K = bf16(rng, 1, 800, 64).cuda()
+    for n_q in (1, 2, 3, 4, 5, 9, 32):
+        for m in (n_q, 0):
+            Q = bf16(rng, n_q + m, 7, 64).cuda()
+            cq = dev(cumulative((n_q, m)))
+            gv.gvote_attend8(p, Q, cq, n_q, c, torch.empty_like(Q), ws, acc_out=torch.zeros(1, 800).cuda())
+            gv.gvote_accumulate(p, Q, cq, n_q, K, c.cu_seqlens, c.geom, torch.zeros(1, 800).cuda(), ws)
+    assert gv.gvote_poll_status(ws) == 0
+
+
+@gpu
 @pytest.mark.parametrize("acc", ["inplace", "zero", None])
 def test_attend_weights_in_place_from_zero_and_not_at_all(gv, acc):
     run_attend(gv, 8, 2, 128, (700, 70), [[700, 321], [70, 0]], (2, 1), seed=5, acc=acc)
@@ -397,6 +432,26 @@ def test_attend_shows_a_nan_that_a_seen_row_holds(gv):
     nan = out.isnan().cpu()
     assert nan[:, 0, 5].all() and nan[:, 0].sum() == 2             # one channel of the value, for both tokens
     assert nan[1, 1].all() and not nan[0, 1].any()                 # the key's row is hidden from the first token
+
+
+@gpu
+def test_attend_hides_a_nan_from_the_tokens_that_do_not_see_its_row(gv):
+    """The last token's own value is NaN in one channel: it must show in the last token's output and in no other."""
+    rng = np.random.default_rng(14)
+    p = params(gv, 4, 2, 80)
+    c, held, cu = fill_cache(gv, p, (300, 129), [[300, 200], [129, 5]], rng)
+    c.V[0, 299, 7] = 0xff                                              # request 0, head 0, last row
+    c.V[1, cu[1] + 3, 79] = 0x7f                                       # request 1, head 1, the last row but one
+    Q = bf16(rng, 6, 4, 80)
+    out, acc = torch.zeros(6, 4, 80, dtype=torch.bfloat16).cuda(), torch.zeros(2, 429).cuda()
+    ws = workspace(gv, p, c.geom, 6, 3)
+    for _ in range(2):                                                 # (the second call finds no mark of the first)
+        gv.gvote_attend8(p, Q.cuda(), dev(cumulative((3, 3))), 3, c, out, ws, acc_out=acc)
+        nan = out.isnan().cpu()
+        assert nan[2, 0:2, 7].all() and nan[4:6, 2:4, 79].all() and nan.sum() == 2 + 4
+        assert torch.isfinite(acc).all()
+    o, _, _ = co.attend(Q[0:3, 0:2].double().numpy(), co.values(*held[0, 0, 0]), co.values(*held[1, 0, 0]))
+    assert np.allclose(out[:2, 0:2].double().cpu().numpy(), o[:2], rtol=2.0 ** -7, atol=2.0 ** -7)
 
 
 @gpu
