@@ -371,7 +371,8 @@ GVOTE_API int32_t gvote_append8(const gvote_params* p, const void* K_new, const 
  * lse = -inf.  Per query head g of KV head h: logits q.k_n / sqrt(d_k), softmax, out = sum of weight * value
  * (products of the stored values; 32-bit sums), lse_or_null [total_q, n_q_heads] = log of the softmax's
  * denominator.  acc_out_or_null [n_kv_heads, total_tokens]: for the rows held, acc (null: 0) + the weights summed over
- * the request's tokens and the head's group; acc_or_null may be acc_out itself.  Deterministic. */
+ * the request's tokens and the head's group; acc_or_null may be acc_out itself.  Deterministic.  Where cu_q gives a
+ * request more than max_q tokens the status word reads GVOTE_ERR_INVALID_ARG and its outputs are not to be used. */
 #define GVOTE_ATTEND8_MAX_Q 32
 GVOTE_API int32_t gvote_attend8(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride,
                       const int32_t* cu_q, int64_t total_q, int64_t max_q, const gvote_cache8* cache,
@@ -392,10 +393,11 @@ GVOTE_API int32_t gvote_accumulate(const gvote_params* p, const void* Q, int64_t
                          const float* acc_or_null, float* acc_out, void* ws, size_t ws_bytes, void* stream);
 
 /* Eviction by collected weight: which rows stay.  Per request and KV head with n rows (kv_len, or the slab), k =
- * clamp(keep[r][h], 0, n) rows are kept: the last min(n_recent, k), then the first min(p->n_s, what is left of k and n),
- * then those of largest acc, ties to the lower slot (a NaN counts as the lowest weight).  keep [batch, n_kv_heads] int32 (device), so that heads may keep
- * different numbers of rows (a budget written by gvote_vote, for instance).  mask and budget (= k) as in gvote_vote:
- * gvote_compact, gvote_pack, gvote_store8 and gvote_prune8 take the mask. */
+ * clamp(keep[r][h], 0, n) rows are kept: the last min(n_recent, k), then the first min(p->n_s, what is left of k
+ * and n), then those of largest acc, ties to the lower slot (a NaN counts as the lowest weight).  keep
+ * [batch, n_kv_heads] int32 (device), so that heads may keep different numbers of rows (a budget written by
+ * gvote_vote, for instance).  mask and budget (= k) as in gvote_vote: gvote_compact, gvote_pack, gvote_store8 and
+ * gvote_prune8 take the mask. */
 GVOTE_API int32_t gvote_evict(const gvote_params* p, const float* acc, const int32_t* cu_seqlens,
                     const int32_t* kv_len_or_null, int32_t batch, int64_t total_tokens, int64_t max_N,
                     const int32_t* keep, int32_t n_recent, uint32_t* mask, int32_t* budget,

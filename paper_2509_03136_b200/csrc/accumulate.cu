@@ -65,6 +65,7 @@ struct Tail {
   uint64_t lse_full[kLseStages], lse_empty[kLseStages];
   uint64_t acc_full[2][2], acc_empty[2][2];
   uint64_t half_full[2], half_empty[2];
+  uint64_t drain;                       // the MMAs under way, after a wait that ran out
   uint32_t tmem_slot;
   volatile int abort_flag;
 };
@@ -76,6 +77,11 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, vo
   }
   *abort_flag = 1;
   return false;
+}
+// Before the producer leaves early: the loads of a ring that may still write to this CTA's memory.
+__device__ __forceinline__ void drain_copies(uint64_t* full, int slots, int issued) {
+  for (int i = issued > slots ? issued - slots : 0; i < issued; ++i)
+    for (int k = 0; k < (1 << 12) && !ptx::mbar_try_wait(&full[i % slots], (i / slots) & 1); ++k) {}
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -194,6 +200,7 @@ __device__ __forceinline__ UnitInfo unit_info(const AccArgs& a, const Only& only
   if (kPass == 1) {
     x.stat0 = 2 * (int)(v - (x.q0 / (2 * a.tpt) + x.r));
     x.n_stat = max(min(2, q_tiles - x.stat0), 0);
+    if (x.stat0 < 0) x.n_stat = 0;                         // (a list that starts behind token 0)
     const int last = min(x.nq, (x.stat0 + x.n_stat) * a.tpt) - 1;
     const int tiles = (max(x.n - (x.nq - 1 - last), 0) + kTile - 1) / kTile;
     x.s0 = 0;
@@ -201,6 +208,7 @@ __device__ __forceinline__ UnitInfo unit_info(const AccArgs& a, const Only& only
   } else {
     x.stat0 = 2 * (int)(v - ((x.start >> 8) + x.r));
     x.n_stat = max(min(2, (x.n + kTile - 1) / kTile - x.stat0), 0);
+    if (x.stat0 < 0) x.n_stat = 0;
     x.s0 = min(max(x.stat0 * kTile - (x.n - x.nq), 0) / a.tpt, q_tiles);
     x.s1 = q_tiles;
   }
@@ -242,6 +250,7 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
       ptx::mbar_init(&tail->half_full[s], 4);
       ptx::mbar_init(&tail->half_empty[s], 4);
     }
+    ptx::mbar_init(&tail->drain, 1);
     tail->abort_flag = (ptx::smem_u32(smem_raw) & 1023u) ? 1 : 0;
     ptx::fence_barrier_init();
     ptx::prefetch_tensormap(&tmQ);
@@ -263,7 +272,7 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
     if (lane == 0) {
-      int unit = 0, it = 0;
+      int unit = 0, it = 0, tiles = 0, rows = 0;                   // (tiles and lse rows asked for)
       bool ok = true;
       for (uint32_t k = 0; ok && k * gridDim.x < a.units; ++k) {
         const uint32_t u = unit_of(k);
@@ -286,6 +295,7 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
           ok = wait_or_abort(&tail->empty[s], ((it / a.stages) & 1) ^ 1, abort_flag);
           if (!ok) break;
           ptx::mbar_arrive_expect_tx(&tail->full[s], kPass == 1 ? k_bytes : q_bytes);
+          ++tiles;
           for (int c = 0; c < a.boxes; ++c) {
             uint8_t* dst = ring_sm + (size_t)s * tile_bytes + (size_t)c * kTile * 128;
             if (kPass == 1) ptx::tma_load_3d(dst, &tmK, &tail->full[s], c * 64, x.start + t * kTile, x.h);
@@ -296,10 +306,16 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             ok = wait_or_abort(&tail->lse_empty[l], ((it / kLseStages) & 1) ^ 1, abort_flag);
             if (!ok) break;
             ptx::mbar_arrive_expect_tx(&tail->lse_full[l], kTile * 4);
+            ++rows;
             ptx::bulk_load(lse_sm + l * kTile, a.lse2 + ((int64_t)x.h * a.q_tiles + x.q0 / a.tpt + x.r + t) * kTile, kTile * 4,
                            &tail->lse_full[l]);
           }
         }
+      }
+      if (!ok) {
+        drain_copies(tail->stat_full, a.stat_slots, unit);
+        drain_copies(tail->full, a.stages, tiles);
+        drain_copies(tail->lse_full, kLseStages, rows);
       }
     }
   } else if (warp == 1) {
@@ -351,6 +367,11 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
           }
         }
       }
+    }
+    if (!ok) {
+      if (ptx::elect_one()) ptx::umma_commit(&tail->drain);
+      __syncwarp();
+      for (int k = 0; k < (1 << 12) && !ptx::mbar_try_wait(&tail->drain, 0); ++k) {}
     }
   } else {
     // ------------------------------------------------------------------ read-out: thread = row of a stationary tile
@@ -522,7 +543,7 @@ accumulate_lse_kernel(const __grid_constant__ AccArgs a, const float* __restrict
   const int r = a.batch == 1 ? 0 : find_request_div(a.cu_q, a.batch, tile, a.tpt);
   const int q0 = a.cu_q[r], nq = a.cu_q[r + 1] - q0;
   const int tok0 = (int)(tile - (q0 / a.tpt + r)) * a.tpt, token = tok0 + row / a.G;
-  if (tok0 >= nq) return;
+  if (tok0 < 0 || tok0 >= nq) return;
   const bool holds = row < a.G * a.tpt && token < nq;
   const int64_t at = ((int64_t)h * a.q_tiles + tile) * kTile + row;
   float out = -INFINITY;
@@ -556,7 +577,7 @@ accumulate_sum_kernel(const __grid_constant__ AccArgs a) {
   const int h = blockIdx.y, r = a.batch == 1 ? 0 : find_request_by(a.cu, a.batch, blockIdx.x, 8);
   const int start = a.cu[r], n = valid_keys(a.kv_len, r, a.Hkv, h, a.cu[r + 1] - start);
   const int key = (int)(blockIdx.x - ((start >> 8) + r)) * 256 + threadIdx.x;
-  if (key >= n) return;
+  if (key < 0 || key >= n) return;
   const int64_t slot = (int64_t)h * a.total + start + key;
   double sum = a.acc ? (double)a.acc[slot] : 0.0;
   for (int x = 0; x < a.chunks; ++x) sum += (double)a.part_sum[(int64_t)x * a.Hkv * a.total + slot];

@@ -88,7 +88,7 @@ __device__ __forceinline__ Entry entry_of(const AttendArgs& a, int e) {
   x.start = a.cu[x.r];
   x.n = valid_keys(a.kv_len, x.r, a.Hkv, x.h, a.cu[x.r + 1] - x.start);
   x.q0 = a.cu_q[x.r];
-  x.nq = a.cu_q[x.r + 1] - x.q0;
+  x.nq = min(a.cu_q[x.r + 1] - x.q0, a.max_q);         // (the workspace holds no more; the excess is reported)
   return x;
 }
 
@@ -104,6 +104,16 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, vo
   }
   *abort_flag = 1;
   return false;
+}
+// Before a role leaves early: what it started may still write to this CTA's memory.
+__device__ __forceinline__ void drain_copies(uint64_t* full, int slots, uint32_t issued) {
+  for (uint32_t i = issued > (uint32_t)slots ? issued - slots : 0; i < issued; ++i)
+    for (int k = 0; k < (1 << 12) && !ptx::mbar_try_wait(&full[i % slots], (i / slots) & 1); ++k) {}
+}
+__device__ __forceinline__ void drain_mmas(uint64_t* bar) {
+  if (ptx::elect_one()) ptx::umma_commit(bar);
+  __syncwarp();
+  for (int k = 0; k < (1 << 12) && !ptx::mbar_try_wait(bar, 0); ++k) {}
 }
 // The or of a predicate over the four warps of a softmax group (named barrier `id`).
 __device__ __forceinline__ bool group_any(int id, bool x) {
@@ -174,6 +184,7 @@ struct Bars {
   uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots], q_full[2], q_empty[2];
   uint64_t s_full[kMaxBuffers], p_empty[kMaxBuffers], o_full[4];
   uint64_t s_empty[kMaxBuffers], p_full[kMaxBuffers], o_empty[4];
+  uint64_t drain[2];                   // the MMAs under way of the two issuers, after a wait that ran out
 };
 enum { kWarpTma = 0, kWarpS = 1, kWarpO = 2, kWarpQ = 3, kWarpSoftmax = 4 };
 
@@ -184,7 +195,7 @@ struct Tail {
   int any_nan[2][4];                   // [segment parity][turn]
   volatile int abort_flag;
   int64_t out_at[2][32];               // where the query rows' outputs go (elements)
-  int lse_at[2][32];
+  int64_t lse_at[2][32];
   int warp_tot[32];
   int pref[kMaxEntries + 1];
 };
@@ -255,7 +266,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     if (tid < kBars) {
       const int at = tid * 8;
       const uint32_t count = at >= (int)offsetof(Bars, q_empty) && at < (int)offsetof(Bars, s_full) ? 1 + 4 * L::kGroups
-                             : at >= (int)offsetof(Bars, s_empty) ? 4 * kRb : 1;
+                             : at >= (int)offsetof(Bars, s_empty) && at < (int)offsetof(Bars, drain) ? 4 * kRb : 1;
       ptx::mbar_init(reinterpret_cast<uint64_t*>(&tail->bars) + tid, count);
       ptx::fence_barrier_init();
     }
@@ -275,9 +286,11 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   {
     const int per = (entries + L::kThreads - 1) / L::kThreads;         // consecutive entries per thread
     const int e0 = min(tid * per, entries), e1 = min(e0 + per, entries);
+    const bool b0 = blockIdx.x == 0 && blockIdx.y == 0;
     int mine = 0;
     for (int e = e0; e < e1; ++e) {
       const Entry x = entry_of(a, e);
+      if (b0 && a.cu_q[x.r + 1] - x.q0 > a.max_q) { atomicExch(&a.status[0], GVOTE_ERR_INVALID_ARG); atomicExch(&a.status[1], 13); }
       const int t = group0 < x.nq * a.G ? (x.n + kTileKeys - 1) / kTileKeys : 0;
       pref[e + 1] = t > 0 ? t + kGap : 0;
       mine += pref[e + 1];
@@ -299,8 +312,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     __syncthreads();
   }
   const uint32_t tmem = __shfl_sync(0xffffffffu, tail->tmem_slot, 0);
-  const int T = pref[entries], B = gridDim.x, b = blockIdx.x;
-  const int t0 = (int)((int64_t)T * b / B), t1 = (int)((int64_t)T * (b + 1) / B);
+  // no more parts than places: an empty part between two of an entry's would leave its slot unwritten
+  const int T = pref[entries], B = max(min((int)gridDim.x, T), 1), b = blockIdx.x;
+  const int t0 = (int)((int64_t)T * min(b, B) / B), t1 = (int)((int64_t)T * min(b + 1, B) / B);
   // which CTAs hold an entry: the CTA of the tile at place t is the largest c with T c / B <= t
   if (b == 0) {
     int2* info = a.info + (int64_t)blockIdx.y * entries;
@@ -333,9 +347,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         uint32_t phase;
         Entry x;
         int seg;
+        uint32_t issued;
       };
-      Feed feed[2] = {{&tmK, &tmKp, k_ring, tail->bars.k_full, tail->bars.k_empty, a.k_slots, 0, 0, {}, -1},
-                      {&tmV, &tmVp, v_ring, tail->bars.v_full, tail->bars.v_empty, a.v_slots, 0, 0, {}, -1}};
+      Feed feed[2] = {{&tmK, &tmKp, k_ring, tail->bars.k_full, tail->bars.k_empty, a.k_slots, 0, 0, {}, -1, 0},
+                      {&tmV, &tmVp, v_ring, tail->bars.v_full, tail->bars.v_empty, a.v_slots, 0, 0, {}, -1, 0}};
       Walk walk[2] = {at, at};
       uint32_t polls = 0;
       while (ok && !(walk[0].done() && walk[1].done())) {
@@ -360,6 +375,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             }
           }
           if (++f.slot == f.slots) { f.slot = 0; f.phase ^= 1u; }
+          ++f.issued;
           w.next_tile();
           moved = true;
         }
@@ -369,6 +385,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           *abort_flag = 1;
           ok = false;
         }
+      }
+      if (!ok) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) drain_copies(feed[i].full, feed[i].slots, feed[i].issued);
       }
     }
   } else if (warp == kWarpS) {
@@ -404,6 +424,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         if (++ks == a.k_slots) { ks = 0; k_phase ^= 1u; }
       }
     }
+    if (!ok) drain_mmas(&tail->bars.drain[0]);
   } else if (warp == kWarpO) {
     // ------------------------------------------------------------------ O += V^T P
     const uint32_t idesc = instr_desc_e4m3(128, L::kN2, true, true);
@@ -441,6 +462,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         if (++vs == a.v_slots) { vs = 0; v_phase ^= 1u; }
       }
     }
+    if (!ok) drain_mmas(&tail->bars.drain[1]);
   } else if (warp == kWarpQ) {
     // ------------------------------------------------------------------ Q as three e4m3 terms, a segment ahead
     for (int i = lane; i < 2 * kBoxes * (L::kN1 - 3 * L::kRows) * 8; i += 32) {     // the rows behind the last term are zero
@@ -502,7 +524,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             const int token = qrow / a.G, head = x.h * a.G + qrow - token * a.G;
             limit_sm[qb * L::kRows + row] = qrow < rows ? x.n - (x.nq - 1 - token) : 0;
             tail->out_at[qb][row] = (int64_t)(x.q0 + token) * a.o_tok + (int64_t)head * a.o_head;
-            tail->lse_at[qb][row] = (x.q0 + token) * a.Hkv * a.G + head;
+            tail->lse_at[qb][row] = (int64_t)(x.q0 + token) * a.Hkv * a.G + head;
           }
         }
       }
@@ -691,7 +713,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       }
       group_any(bar_id, false);
       const bool whole = L::kTurns == 1 && s0 == 0 && s1 == pref[e + 1] - pref[e] - kGap;   // all of the entry, in one O
-      const int64_t slot = (((int64_t)blockIdx.y * (entries + B) + e + b) * L::kTurns + turn) * a.group_rows + rb * kR;
+      const int64_t slot = (((int64_t)blockIdx.y * (entries + (int)gridDim.x) + e + b) * L::kTurns + turn) * a.group_rows + rb * kR;
       if (any_tile) {
         ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.o_full[turn], o_uses & 1, abort_flag));
         ++o_uses;
@@ -768,7 +790,7 @@ __device__ __forceinline__ float2 warp_join(float M, float L) {
 // Block = one row of one entry, merged from its segments when it has several (or none).  They are a few KB: what counts is how
 // many loads wait for one another, so the outputs are asked for before the maxima are known.
 __global__ void __launch_bounds__(256)
-attend8_merge_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows) {
+attend8_merge_kernel(const __grid_constant__ AttendArgs a, int ctas, int max_rows) {
   __shared__ float4 s_o[8][32 * 2];
   __shared__ float s_f[4 * kSms];
   const int entries = a.batch * a.Hkv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -781,7 +803,7 @@ attend8_merge_kernel(const __grid_constant__ AttendArgs a, int B, int max_rows) 
     if (a.turns == 1 && v.x >= 0 && v.x == v.y) return; // the first kernel has written it
     const int quads = a.d_k >> 2;
     const int p0 = v.x * a.turns, parts = v.x < 0 ? 0 : (v.y + 1) * a.turns - p0;
-    const int64_t slot0 = (((int64_t)group * (entries + B) + e) * a.turns + p0) * a.group_rows + in_group;
+    const int64_t slot0 = (((int64_t)group * (entries + ctas) + e) * a.turns + p0) * a.group_rows + in_group;
     constexpr int kAhead = 8;
     float4 pre[kAhead];
 #pragma unroll

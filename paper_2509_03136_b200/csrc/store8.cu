@@ -87,8 +87,9 @@ store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict_
     __syncthreads();
   }
   const int m = min(carry, cap);
-  for (int b = tid; b < listed; b += kScan8Threads) {
-    my_note[b].cnt = min(kBlock8, m - b * kBlock8);                // (<= 0: no rows)
+  const int before = r == 0 ? (int)block8_offset(dstart, 0) : 0;   // (slabs that do not start at slot 0)
+  for (int b = tid - before; b < listed; b += kScan8Threads) {
+    my_note[b].cnt = b < 0 ? 0 : min(kBlock8, m - b * kBlock8);    // (<= 0: no rows)
     my_note[b].words = words;
     my_note[b].row0 = b * kBlock8;
     *reinterpret_cast<int4*>(&my_note[b].r) = make_int4(r, start, dstart, 0);
@@ -269,7 +270,7 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
       a.kv_len_out[r * a.Hkv + h] = m;
       if (n > cap) { atomicExch(&a.status[0], GVOTE_ERR_WORKSPACE_TOO_SMALL); atomicExch(&a.status[1], 8); }
     }
-    cnt = min(kBlock8, m - row0);
+    cnt = b < 0 ? 0 : min(kBlock8, m - row0);
     if (cnt <= 0) return;
     if (tid < cnt) s_src[tid] = row0 + tid;
     __syncthreads();

@@ -105,7 +105,10 @@ def same(got, want):
 
 
 def workspace(gv, p, geom, total_q=0, max_q=0):
-    return gv.alloc_cache_workspace(p, *geom, total_q, max_q)
+    """Behind the status word nothing of a workspace may matter: it holds NaNs there."""
+    ws = gv.alloc_cache_workspace(p, *geom, total_q, max_q)
+    ws[256:].fill_(0xff)
+    return ws
 
 
 # ----------------------------------------------------------------------------- store, prune
@@ -353,6 +356,14 @@ def test_attend_row_counts(gv, hq, hkv, n_q, d):
     """Every way the query rows are dealt to the softmax groups: 1 to 4, 8, 12, 16, 20, 24, 32 rows, and more than one
     group of 32, over several requests of very different length."""
     run_attend(gv, hq, hkv, d, (700, 1, 130, 4000, 260), [[700], [1], [129], [3333], [256]], (n_q, 1, n_q, n_q, 0), seed=hq + n_q)
+
+
+@gpu
+@pytest.mark.parametrize("n_q", [1, 2, 5])
+def test_attend_fewer_tiles_than_ctas(gv, n_q):
+    """Long slabs that hold a few rows: the grid is sized for the slabs, most of its CTAs have nothing."""
+    for rows in ((200, 129, 130), (1, 0, 300), (128, 257, 5), (0, 0, 1), (900, 385, 1)):
+        run_attend(gv, 4, 2, 64, (2000, 2000, 1500), [[n, max(n - n_q, 0)] for n in rows], (n_q, 1, n_q), seed=27)
 
 
 @gpu
@@ -614,7 +625,143 @@ def test_evict(gv, lens, hkv, n_recent, n_s, kind):
                 assert b[r, h] == want.sum()
 
 
+@gpu
+def test_evict_rows_that_outgrow_shared_memory(gv):
+    """400000 rows: eight shares of 50000, more than a CTA stages."""
+    rng = np.random.default_rng(23)
+    p, n = params(gv, 2, 2, 16), 400000
+    geom = (1, n, n)
+    for acc, keep in ((np.exp(rng.normal(size=(2, n)) * 3), [123457, 399990]), (rng.integers(0, 3, (2, n)), [200001, 17])):
+        acc = acc.astype(np.float32)
+        mask = torch.full((2, gv.mask_row_words(n, 1)), -1, dtype=torch.int32).cuda()
+        budget = torch.zeros(1, 2, dtype=torch.int32).cuda()
+        gv.gvote_evict(p, dev(acc), dev(cumulative((n,))), geom, dev(np.array([keep], dtype=np.int32)), 8, mask, budget,
+                       workspace(gv, p, geom))
+        m = mask.cpu().numpy()
+        for h in range(2):
+            assert np.array_equal(gv.unpack_mask(m[h], 0, n), co.evict(acc[h], keep[h], 8, 4))
+            assert budget[0, h] == keep[h]
+
+
 # ----------------------------------------------------------------------------- together
+def whole_flow(gv, p, t):
+    """A prompt's weights, eviction, store, two tokens, eviction and prune: every entry point once, into t's buffers."""
+    gv.gvote_accumulate(p, t.Q, t.cu_q, 300, t.K, t.cu, t.geom, t.acc, t.ws)
+    gv.gvote_evict(p, t.acc, t.cu, t.geom, t.keep, 8, t.mask, t.budget, t.ws)
+    gv.gvote_store8(p, t.K, t.V, t.cu, t.geom, t.c, t.ws, mask=t.mask, acc=t.acc, acc_out=t.acc8, token_pos_out=t.pos8)
+    gv.gvote_append8(p, t.kn, t.vn, t.cu_new, 2, t.c, t.c.kv_len, t.ws, acc=t.acc8, token_pos=t.pos8, pos_new=t.pos_new)
+    gv.gvote_attend8(p, t.qn, t.cu_new, 2, t.c, t.out, t.ws, acc=t.acc8, acc_out=t.acc8)
+    gv.gvote_evict(p, t.acc8, t.c.cu_seqlens, t.c.geom, t.keep2, 4, t.mask8, t.budget, t.ws, kv_len=t.c.kv_len)
+    gv.gvote_prune8(p, t.c, t.mask8, t.c2, t.ws, acc=t.acc8, acc_out=t.acc2, token_pos=t.pos8, token_pos_out=t.pos2)
+    return [x.clone() for x in (t.acc, t.mask, t.out, t.acc2, t.pos2, t.c2.kv_len, t.c2.K, t.c2.V, t.c2.k_scale, t.c2.v_scale)]
+
+
+def flow_tensors(gv, p, hq, hkv, d):
+    from types import SimpleNamespace
+    rng = np.random.default_rng(24)
+    lens, caps = (1000, 41, 300), (600, 50, 220)
+    cu, cu8 = cumulative(lens), cumulative(caps)
+    t = SimpleNamespace(geom=(3, 1341, 1000), cu=dev(cu), cu_q=dev(cumulative((300, 41, 300))), cu_new=dev(cumulative((1, 2, 0))))
+    t.K, t.V, t.Q = bf16(rng, hkv, 1341, d).cuda(), bf16(rng, hkv, 1341, d).cuda(), bf16(rng, 641, hq, d).cuda()
+    t.kn, t.vn, t.qn = bf16(rng, hkv, 3, d).cuda(), bf16(rng, hkv, 3, d).cuda(), bf16(rng, 3, hq, d).cuda()
+    t.keep = dev(np.tile(np.array([[500], [40], [100]], dtype=np.int32), (1, hkv)))
+    t.keep2 = dev(np.tile(np.array([[77], [30], [100]], dtype=np.int32), (1, hkv)))
+    t.pos_new = dev(np.array([1000, 41, 42], dtype=np.int32))
+    t.c, t.c2 = gv.alloc_cache8(p, cu8), gv.alloc_cache8(p, cu8)
+    t.acc, t.acc8, t.acc2 = (torch.zeros(hkv, n).cuda() for n in (1341, 870, 870))
+    t.pos8, t.pos2 = (torch.zeros(hkv, 870, dtype=torch.int32).cuda() for _ in range(2))
+    t.mask, t.mask8 = (torch.zeros(hkv, gv.mask_row_words(n, 3), dtype=torch.int32).cuda() for n in (1341, 870))
+    t.budget = torch.zeros(3, hkv, dtype=torch.int32).cuda()
+    t.out = torch.zeros(3, hq, d, dtype=torch.bfloat16).cuda()
+    t.ws = workspace(gv, p, t.geom, 641, 300)
+    return t
+
+
+@gpu
+def test_the_whole_flow_on_another_stream_and_in_a_graph(gv):
+    """The same bits eagerly, on a side stream, and from a captured graph that is replayed; two calls at once with a
+    workspace each."""
+    p = params(gv, 6, 2, 64)
+    t = flow_tensors(gv, p, 6, 2, 64)
+    want = whole_flow(gv, p, t)
+    others = [flow_tensors(gv, p, 6, 2, 64) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in others]
+    torch.cuda.synchronize()
+    for u, s in zip(others, streams):
+        with torch.cuda.stream(s):
+            for _ in range(3):
+                got = whole_flow(gv, p, u)
+            u.got = got
+    torch.cuda.synchronize()
+    for u in others:
+        assert all(torch.equal(a, b) for a, b in zip(u.got, want))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured = whole_flow(gv, p, t)
+    for _ in range(2):
+        for x in (t.acc, t.acc8, t.acc2, t.out, t.c2.K, t.c2.V):
+            x.zero_()
+        g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(captured, want))
+    assert all(gv.gvote_poll_status(u.ws) == 0 for u in (t, *others))
+
+
+@gpu
+def test_slabs_that_do_not_start_at_slot_zero(gv):
+    """The later requests of a batch by a view of its boundaries: their results, and nothing written before them."""
+    rng = np.random.default_rng(25)
+    p, lens = params(gv, 4, 2, 64), (777, 500, 130)
+    cu, total = cumulative(lens), 1407
+    K, V, Q = bf16(rng, 2, total, 64).cuda(), bf16(rng, 2, total, 64).cuda(), bf16(rng, total, 4, 64).cuda()
+    full, part = dev(cu), dev(cu[1:])
+    flags = rng.random((2, total)) < 0.4
+    for n_q in (lens, (777, 3, 130)):                                # (the first request's tokens: not looked at)
+        cq = cumulative(n_q)
+        geoms = ((3, total, 777), (2, total, 500))
+        acc = [torch.full((2, total), -1.0).cuda() for _ in range(2)]
+        ws = workspace(gv, p, geoms[0], int(cq[-1]), 777)
+        for a, cu_d, cq_d, geom in zip(acc, (full, part), (dev(cq), dev(cq[1:])), geoms):
+            gv.gvote_accumulate(p, Q[:cq[-1]], cq_d, 777, K, cu_d, geom, a, ws)
+        assert (acc[1][:, :777] == -1).all() and (acc[0] >= 0).all()
+        assert torch.allclose(acc[0][:, 777:], acc[1][:, 777:], rtol=1e-5, atol=0)
+    acc1 = torch.full((2, total), -1.0).cuda()                       # one request, behind others
+    gv.gvote_accumulate(p, Q, dev(cu[2:]), 130, K, dev(cu[2:]), (1, total, 130), acc1, ws)
+    gv.gvote_accumulate(p, Q, full, 777, K, full, (3, total, 777), acc[0], ws)
+    assert (acc1[:, :1277] == -1).all() and torch.allclose(acc[0][:, 1277:], acc1[:, 1277:], rtol=1e-5, atol=0)
+    for masked in (False, True):
+        caches = [gv.alloc_cache8(p, cu), gv.alloc_cache8(p, cu)]
+        b = gv.Cache8(*(getattr(caches[1], n) for n in ("K", "V")), *(torch.zeros(2, gv.cache8_row_blocks(total, 2)).cuda() for _ in range(2)),
+                      part, torch.zeros(2, 2, dtype=torch.int32).cuda(), (2, total, 500))
+        caches[1] = b
+        for c, cu_h, cu_d, geom in zip(caches, (cu, cu[1:]), (full, part), ((3, total, 777), (2, total, 500))):
+            gv.gvote_store8(p, K, V, cu_d, geom, c, ws, mask=pack(gv, flags, cu_h) if masked else None)
+        assert (b.K[:, :777] == 0).all() and torch.equal(b.K[:, 777:], caches[0].K[:, 777:])
+        assert torch.equal(b.V[:, 777:], caches[0].V[:, 777:]) and torch.equal(b.kv_len, caches[0].kv_len[1:])
+        outs = []
+        for c, cq in zip(caches, (cumulative((1, 1, 1)), np.array([1, 2, 3], dtype=np.int32))):
+            out, a = torch.zeros(3, 4, 64, dtype=torch.bfloat16).cuda(), torch.zeros(2, total).cuda()
+            gv.gvote_attend8(p, Q[:3], dev(cq), 1, c, out, ws, acc_out=a)
+            outs.append((out, a))
+        assert torch.allclose(outs[0][0][1:].float(), outs[1][0][1:].float(), rtol=2.0 ** -6, atol=2.0 ** -8)
+        assert (outs[1][0][0] == 0).all() and (outs[1][1][:, :777] == 0).all()
+        assert torch.allclose(outs[0][1][:, 777:], outs[1][1][:, 777:], rtol=1e-4, atol=1e-9)
+    assert gv.gvote_poll_status(ws) == 0
+
+
+@gpu
+def test_attend_reports_a_request_of_more_tokens_than_announced(gv):
+    rng = np.random.default_rng(26)
+    p = params(gv, 4, 2, 64)
+    c, _, _ = fill_cache(gv, p, (300, 200), [[300, 300], [200, 200]], rng)
+    ws = workspace(gv, p, c.geom, 6, 2)
+    Q = bf16(rng, 6, 4, 64).cuda()
+    out = torch.zeros_like(Q)
+    gv.gvote_attend8(p, Q, dev(cumulative((2, 4))), 2, c, out, ws, acc_out=torch.zeros(2, 500).cuda())
+    assert gv.gvote_poll_status(ws) == -1
+    assert (out[4:] == 0).all()                                      # the excess is left alone
+
+
 @gpu
 @pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (14, 2, 128)])
 def test_prompt_then_tokens_then_eviction(gv, hq, hkv, d):
