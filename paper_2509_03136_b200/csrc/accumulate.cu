@@ -263,6 +263,8 @@ accumulate_umma_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
+  ptx::let_next_begin();
+  ptx::wait_for_previous();                       // (pass 1, and the first kernel of a call: nothing to wait for)
   const uint32_t tmem = __shfl_sync(0xffffffffu, tail->tmem_slot, 0);
   volatile int* abort_flag = &tail->abort_flag;
   const int q_rows = a.G * a.tpt;                                  // rows a query box fills
@@ -543,6 +545,8 @@ accumulate_lse_kernel(const __grid_constant__ AccArgs a, const float* __restrict
   const int r = a.batch == 1 ? 0 : find_request_div(a.cu_q, a.batch, tile, a.tpt);
   const int q0 = a.cu_q[r], nq = a.cu_q[r + 1] - q0;
   const int tok0 = (int)(tile - (q0 / a.tpt + r)) * a.tpt, token = tok0 + row / a.G;
+  ptx::let_next_begin();
+  ptx::wait_for_previous();
   if (tok0 < 0 || tok0 >= nq) return;
   const bool holds = row < a.G * a.tpt && token < nq;
   const int64_t at = ((int64_t)h * a.q_tiles + tile) * kTile + row;
@@ -577,6 +581,7 @@ accumulate_sum_kernel(const __grid_constant__ AccArgs a) {
   const int h = blockIdx.y, r = a.batch == 1 ? 0 : find_request_by(a.cu, a.batch, blockIdx.x, 8);
   const int start = a.cu[r], n = valid_keys(a.kv_len, r, a.Hkv, h, a.cu[r + 1] - start);
   const int key = (int)(blockIdx.x - ((start >> 8) + r)) * 256 + threadIdx.x;
+  ptx::wait_for_previous();
   if (key < 0 || key >= n) return;
   const int64_t slot = (int64_t)h * a.total + start + key;
   double sum = a.acc ? (double)a.acc[slot] : 0.0;
@@ -681,7 +686,8 @@ int32_t launch_accumulate(const gvote_params* p, const __nv_bfloat16* Q, int64_t
   }
   if (lse || a.chunks > 1) {
     LaunchScope scope_("accumulate_lse_kernel", st);
-    launch_on(accumulate_lse_kernel, dim3((unsigned)(4 * a.q_tiles), a.Hkv), dim3(256), 0, st, a, lse);
+    if (lse) launch_on(accumulate_lse_kernel, dim3((unsigned)(4 * a.q_tiles), a.Hkv), dim3(256), 0, st, a, lse);
+    else launch_behind(accumulate_lse_kernel, dim3((unsigned)(4 * a.q_tiles), a.Hkv), dim3(256), 0, st, a, lse);
     GVOTE_LAUNCH_CHECK("accumulate_lse_kernel");
   }
   a.pairs = (uint32_t)list_length(total_tokens, 2 * kTile, batch);
@@ -690,13 +696,13 @@ int32_t launch_accumulate(const gvote_params* p, const __nv_bfloat16* Q, int64_t
   GVOTE_CUDA_CHECK(cudaFuncSetAttribute(accumulate_umma_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   {
     LaunchScope scope_("accumulate_weights_umma_kernel", st);
-    launch_on(accumulate_umma_kernel<2>, dim3((unsigned)(a.units < kSms ? a.units : kSms)), dim3(kAccThreads), smem, st, tmQ,
+    launch_behind(accumulate_umma_kernel<2>, dim3((unsigned)(a.units < kSms ? a.units : kSms)), dim3(kAccThreads), smem, st, tmQ,
               tmK, a);
   }
   GVOTE_LAUNCH_CHECK("accumulate_weights_umma_kernel");
   if (a.chunks > 1) {
     LaunchScope scope_("accumulate_sum_kernel", st);
-    launch_on(accumulate_sum_kernel, dim3((unsigned)a.pairs, a.Hkv), dim3(256), 0, st, a);
+    launch_behind(accumulate_sum_kernel, dim3((unsigned)a.pairs, a.Hkv), dim3(256), 0, st, a);
     GVOTE_LAUNCH_CHECK("accumulate_sum_kernel");
   }
   return GVOTE_OK;

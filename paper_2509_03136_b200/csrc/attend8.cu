@@ -278,6 +278,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     ptx::prefetch_tensormap(&tmV);
   }
   for (int i = tid; i < 2 * L::kGroups * L::kNanWords; i += L::kThreads) nan_all[i] = 0;
+  ptx::let_next_begin();
   if (warp == 1) {
     ptx::tmem_alloc(&tail->tmem_slot, L::kAlloc);
     ptx::tmem_relinquish();
@@ -797,8 +798,10 @@ attend8_merge_kernel(const __grid_constant__ AttendArgs a, int ctas, int max_row
   {
     const int e = blockIdx.x / max_rows, row = blockIdx.x - e * max_rows;
     const int group = row / a.group_rows, in_group = row - group * a.group_rows;
-    const int2 v = a.info[(int64_t)group * entries + e];
     const Entry x = entry_of(a, e);
+    ptx::wait_for_previous();
+    ptx::let_next_begin();
+    const int2 v = a.info[(int64_t)group * entries + e];
     if (row >= x.nq * a.G) return;
     if (a.turns == 1 && v.x >= 0 && v.x == v.y) return; // the first kernel has written it
     const int quads = a.d_k >> 2;
@@ -867,6 +870,7 @@ attend8_weights_kernel(const __grid_constant__ AttendArgs a) {
   }
   const int e = i_req * a.Hkv + h;
   const Entry x = entry_of(a, e);
+  ptx::wait_for_previous();
   const int i = (int)(gb - ((x.start >> 8) - base + i_req)) * 256 + tid;
   if (i >= x.n) return;
   const int rows = x.nq * a.G;
@@ -995,12 +999,12 @@ int32_t launch_attend8(const gvote_params* p, const __nv_bfloat16* Q, int64_t q_
     const int64_t rows = max_q * a.G;
     {
       LaunchScope scope_("attend8_merge_kernel", st);
-      launch_on(attend8_merge_kernel, dim3((unsigned)(a.batch * a.Hkv * rows)), dim3(256), 0, st, a, (int)cut.ctas, (int)rows);
+      launch_behind(attend8_merge_kernel, dim3((unsigned)(a.batch * a.Hkv * rows)), dim3(256), 0, st, a, (int)cut.ctas, (int)rows);
     }
     GVOTE_LAUNCH_CHECK("attend8_merge_kernel");
     if (acc_out) {
       LaunchScope scope_("attend8_weights_kernel", st);
-      launch_on(attend8_weights_kernel, dim3((unsigned)((c->total_tokens >> 8) + a.batch), a.Hkv), dim3(256), 0, st, a);
+      launch_behind(attend8_weights_kernel, dim3((unsigned)((c->total_tokens >> 8) + a.batch), a.Hkv), dim3(256), 0, st, a);
       GVOTE_LAUNCH_CHECK("attend8_weights_kernel");
     }
   }

@@ -256,6 +256,11 @@ __device__ __forceinline__ bool elect_one() {
   return pred != 0;
 }
 
+// Two kernels of one call, the second launched by launch_behind: the first lets the second's CTAs come as soon as its own have
+// all begun; the second waits until the first has ended and its writes are visible.
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 }  // namespace ptx
 
 // Host side: encode a tiled tensor map for a bf16 tensor (128-byte swizzle).  dims/strides are

@@ -13,6 +13,7 @@
 // word, a call took a third longer.
 // Out of place: nothing orders the blocks, and a pruned 8-bit cache is small.
 #include "cache8.cuh"
+#include "ptx.cuh"
 
 namespace gvote {
 namespace {
@@ -33,6 +34,7 @@ store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict_
                    int64_t row_blocks, Note* __restrict__ note, int32_t* __restrict__ kv_len_out, int32_t* status) {
   __shared__ int warp_tot[kScan8Threads / 32];
   __shared__ int carry;
+  ptx::let_next_begin();
   const int h = blockIdx.x, r = blockIdx.y;
   const int start = cu[r], n = valid_keys(kv_len, r, Hkv, h, cu[r + 1] - start);
   const int words = (n + 31) >> 5;
@@ -235,6 +237,7 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
   const int64_t db = (int64_t)h * a.d_row_blocks + gb;
   int r, start, dstart, row0, cnt;
   if (a.mask) {
+    ptx::wait_for_previous();
     const int4 note = *reinterpret_cast<const int4*>(&a.note[db]), where = *reinterpret_cast<const int4*>(&a.note[db].r);
     cnt = note.y; row0 = note.w; r = where.x; start = where.y; dstart = where.z;
     if (cnt <= 0) return;
@@ -331,7 +334,8 @@ int32_t run_store(const StoreArgs& a, unsigned ctas, cudaStream_t st) {
   auto kernel = units == 1 ? store8_kernel<kSrc8, 1> : units == 2 ? store8_kernel<kSrc8, 2> : store8_kernel<kSrc8, 4>;
   {
     LaunchScope scope_("store8_kernel", st);
-    launch_on(kernel, dim3(ctas), dim3(kStoreThreads), 0, st, a);
+    if (a.mask) launch_behind(kernel, dim3(ctas), dim3(kStoreThreads), 0, st, a);
+    else launch_on(kernel, dim3(ctas), dim3(kStoreThreads), 0, st, a);
   }
   GVOTE_LAUNCH_CHECK("store8_kernel");
   return GVOTE_OK;
