@@ -879,11 +879,15 @@ attend8_weights_kernel(const __grid_constant__ AttendArgs a) {
   const int64_t slot = (int64_t)h * a.total + x.start + i;
   float s = 0.f;
   const float was = a.acc ? a.acc[slot] : 0.f;
-  for (int token = 0; token < x.nq; ++token, lse += a.Hkv * a.G) {
-#pragma unroll 4
-    for (int g = 0; g < a.G; ++g, l += a.total) {
-      const float v = *l;
-      if (v != -INFINITY) s += exp2_fast(v - lse[g]);
+  constexpr int kAhead = 8;                             // logits on their way at once
+  for (int row0 = 0, g = 0; row0 < rows; row0 += kAhead, l += kAhead * a.total) {
+    float v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) v[k] = row0 + k < rows ? l[k * a.total] : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (v[k] != -INFINITY) s += exp2_fast(v[k] - lse[g]);
+      if (row0 + k < rows && ++g == a.G) { g = 0; lse += a.Hkv * a.G; }
     }
   }
   a.acc_out[slot] = was + s;
