@@ -871,26 +871,32 @@ attend8_weights_kernel(const __grid_constant__ AttendArgs a) {
   const int e = i_req * a.Hkv + h;
   const Entry x = entry_of(a, e);
   ptx::wait_for_previous();
-  const int i = (int)(gb - ((x.start >> 8) - base + i_req)) * 256 + tid;
-  if (i >= x.n) return;
+  const int i0 = (int)(gb - ((x.start >> 8) - base + i_req)) * 256, i = i0 + tid;
+  if (i0 >= x.n) return;
+  const bool holds = i < x.n;
   const int rows = x.nq * a.G;
   const float* l = a.logits + (int64_t)h * a.max_q * a.G * a.total + x.start + i;
   const float* lse = a.lse2 + (int64_t)x.q0 * a.Hkv * a.G + h * a.G;
   const int64_t slot = (int64_t)h * a.total + x.start + i;
+  constexpr int kRows = 128, kAhead = 8;                // rows whose lse is at hand, logits on their way at once
+  __shared__ float s_lse[kRows];
   float s = 0.f;
-  const float was = a.acc ? a.acc[slot] : 0.f;
-  constexpr int kAhead = 8;                             // logits on their way at once
-  for (int row0 = 0, g = 0; row0 < rows; row0 += kAhead, l += kAhead * a.total) {
-    float v[kAhead];
+  const float was = a.acc && holds ? a.acc[slot] : 0.f;
+  for (int row0 = 0; row0 < rows; row0 += kRows) {
+    const int some = min(kRows, rows - row0);
+    if (row0 > 0) __syncthreads();
+    if (tid < some) s_lse[tid] = lse[(int64_t)((row0 + tid) / a.G) * a.Hkv * a.G + (row0 + tid) % a.G];
+    for (int k0 = 0; k0 < some; k0 += kAhead, l += kAhead * a.total) {
+      float v[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) v[k] = row0 + k < rows ? l[k * a.total] : -INFINITY;
+      for (int k = 0; k < kAhead; ++k) v[k] = holds && k0 + k < some ? l[k * a.total] : -INFINITY;
+      if (k0 == 0) __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (v[k] != -INFINITY) s += exp2_fast(v[k] - lse[g]);
-      if (row0 + k < rows && ++g == a.G) { g = 0; lse += a.Hkv * a.G; }
+      for (int k = 0; k < kAhead; ++k)
+        if (v[k] != -INFINITY) s += exp2_fast(v[k] - s_lse[k0 + k]);
     }
   }
-  a.acc_out[slot] = was + s;
+  if (holds) a.acc_out[slot] = was + s;
 }
 
 // How a launch is cut: query rows of a softmax group, groups that share a tile's rows, row groups, CTAs.
