@@ -186,6 +186,7 @@ struct Bars {
   uint64_t s_empty[kMaxBuffers], p_full[kMaxBuffers], o_empty[4];
   uint64_t drain[2];                   // the MMAs under way of the two issuers, after a wait that ran out
 };
+constexpr int kFirstQ = 8;             // a named barrier; the softmax groups' are 1 to 5
 enum { kWarpTma = 0, kWarpS = 1, kWarpO = 2, kWarpQ = 3, kWarpSoftmax = 4 };
 
 struct Tail {
@@ -336,6 +337,43 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   }
   Walk at(pref, t0, t1, entries, e_first);
   bool ok = true;
+  // A warp's part in preparing a query row: its lanes' channels, then their terms.
+  auto load_row = [&](int64_t from, bool holds, uint2 (&v)[kBoxes]) {
+#pragma unroll
+    for (int y = 0; y < kBoxes; ++y) {
+      const int d = y * 128 + lane * 4;
+      v[y] = holds && d < a.d_k ? __ldg(reinterpret_cast<const uint2*>(a.Q + from + d)) : make_uint2(0, 0);
+    }
+  };
+  auto put_row = [&](int qb, int row, const uint2 (&v)[kBoxes]) {
+    uint32_t top = 0;                                                  // the largest magnitude's bits
+#pragma unroll
+    for (int y = 0; y < kBoxes; ++y) {
+      const uint32_t m = __vmaxu2(v[y].x & 0x7fff7fffu, v[y].y & 0x7fff7fffu);
+      top = max(top, max(m & 0xffffu, m >> 16));
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    // entries up to 2^8: multiply by 2^(7 - exponent); the exponent is kept where both factors are normal numbers
+    const int ex = min(max((int)(top >> 7) - 127, -100), 127);
+    const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+    const int rb = row / kR, n0 = rb * 3 * kR + row % kR;              // groups one after the other, a group's rows term by term
+#pragma unroll
+    for (int y = 0; y < kBoxes; ++y) {
+      const uint2 u = v[y];
+      float f[4] = {__uint_as_float(u.x << 16) * up, __uint_as_float(u.x & 0xffff0000u) * up,
+                    __uint_as_float(u.y << 16) * up, __uint_as_float(u.y & 0xffff0000u) * up};
+      if (top >= 0x7f80u) {                                            // an infinity is no 448: NaN, like a NaN
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] = fabsf(f[k]) <= 3.4e38f ? f[k] : __uint_as_float(0x7fffffffu);
+      }
+#pragma unroll
+      for (int term = 0; term < 3; ++term) {
+        const int n = n0 + term * kR;
+        *reinterpret_cast<uint32_t*>(q_sm + qb * L::kQ + (y * L::kN1 + n) * 128 + (((lane >> 2) ^ (n & 7)) << 4) + (lane & 3) * 4) = take_term(f);
+      }
+    }
+    if (lane == 0) factor_sm[qb * L::kRows + row] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale2;
+  };
 
   if (warp == kWarpTma) {
     // ------------------------------------------------------------------ TMA producer: K and V, each as its ring has room
@@ -473,64 +511,30 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     for (; ok && !at.done(); at.next_segment()) {
       const int qb = at.seg & 1;
       const Entry x = entry_of(a, at.e);
-      const int rows = x.nq * a.G;
-      uint8_t* dst = q_sm + qb * L::kQ;
+      const int qrow = group0 + lane, token = qrow / a.G, head = x.h * a.G + qrow - token * a.G;     // lane = row
+      const bool holds = lane < L::kRows && qrow < x.nq * a.G;
+      const int64_t from = holds ? (int64_t)(x.q0 + token) * a.q_tok + (int64_t)head * a.q_head : 0;
+      if (at.seg > 1) ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.q_empty[qb], ((at.seg >> 1) & 1) ^ 1, abort_flag));
+      if (!ok) break;
+      if (lane < L::kRows) {
+        limit_sm[qb * L::kRows + lane] = holds ? x.n - (x.nq - 1 - token) : 0;
+        tail->out_at[qb][lane] = (int64_t)(x.q0 + token) * a.o_tok + (int64_t)head * a.o_head;
+        tail->lse_at[qb][lane] = (int64_t)(x.q0 + token) * a.Hkv * a.G + head;
+      }
+      if (lane == 0) tail->entry[qb] = x;
+      if (at.seg == 0) {                                               // the softmax warps prepare the first one's rows
+        asm volatile("barrier.cta.sync %0, %1;" ::"r"(kFirstQ), "r"(L::kThreads - 96) : "memory");
+      } else {
+        const uint32_t held = __ballot_sync(0xffffffffu, holds);
 #pragma unroll 1
-      for (int rb = 0; rb < kRb; ++rb) {
-        uint2 v[kR][kBoxes];                                           // all of a group's rows on their way at once
+        for (int rb = 0; rb < kRb; ++rb) {
+          uint2 v[kR][kBoxes];                                         // all of a group's rows on their way at once
 #pragma unroll
-        for (int i = 0; i < kR; ++i) {
-          const int qrow = group0 + rb * kR + i;
-          const bool holds = qrow < rows;
-          const int token = holds ? qrow / a.G : 0, g = holds ? qrow - token * a.G : 0;
-          const __nv_bfloat16* src = a.Q + (int64_t)(x.q0 + token) * a.q_tok + (int64_t)(x.h * a.G + g) * a.q_head;
+          for (int i = 0; i < kR; ++i) load_row(__shfl_sync(0xffffffffu, from, rb * kR + i), (held >> (rb * kR + i)) & 1u, v[i]);
 #pragma unroll
-          for (int y = 0; y < kBoxes; ++y) {
-            const int d = y * 128 + lane * 4;
-            v[i][y] = holds && d < a.d_k ? __ldg(reinterpret_cast<const uint2*>(src + d)) : make_uint2(0, 0);
-          }
-        }
-        if (rb == 0) ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.q_empty[qb], ((at.seg >> 1) & 1) ^ 1, abort_flag));
-        if (!ok) break;
-#pragma unroll
-        for (int i = 0; i < kR; ++i) {
-          const int row = rb * kR + i, qrow = group0 + row;
-          uint32_t top = 0;                                            // the largest magnitude's bits
-#pragma unroll
-          for (int y = 0; y < kBoxes; ++y) {
-            const uint32_t m = __vmaxu2(v[i][y].x & 0x7fff7fffu, v[i][y].y & 0x7fff7fffu);
-            top = max(top, max(m & 0xffffu, m >> 16));
-          }
-          top = __reduce_max_sync(0xffffffffu, top);
-          // entries up to 2^8: multiply by 2^(7 - exponent); the exponent is kept where both factors are normal numbers
-          const int ex = min(max((int)(top >> 7) - 127, -100), 127);
-          const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
-#pragma unroll
-          for (int y = 0; y < kBoxes; ++y) {
-            const uint2 u = v[i][y];
-            float f[4] = {__uint_as_float(u.x << 16) * up, __uint_as_float(u.x & 0xffff0000u) * up,
-                          __uint_as_float(u.y << 16) * up, __uint_as_float(u.y & 0xffff0000u) * up};
-            if (top >= 0x7f80u) {                                      // an infinity is no 448: NaN, like a NaN
-#pragma unroll
-              for (int k = 0; k < 4; ++k) f[k] = fabsf(f[k]) <= 3.4e38f ? f[k] : __uint_as_float(0x7fffffffu);
-            }
-#pragma unroll
-            for (int term = 0; term < 3; ++term) {
-              const int n = rb * 3 * kR + term * kR + i;               // groups one after the other, a group's rows term by term
-              *reinterpret_cast<uint32_t*>(dst + (y * L::kN1 + n) * 128 + (((lane >> 2) ^ (n & 7)) << 4) + (lane & 3) * 4) = take_term(f);
-            }
-          }
-          if (lane == 0) {
-            factor_sm[qb * L::kRows + row] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale2;
-            const int token = qrow / a.G, head = x.h * a.G + qrow - token * a.G;
-            limit_sm[qb * L::kRows + row] = qrow < rows ? x.n - (x.nq - 1 - token) : 0;
-            tail->out_at[qb][row] = (int64_t)(x.q0 + token) * a.o_tok + (int64_t)head * a.o_head;
-            tail->lse_at[qb][row] = (int64_t)(x.q0 + token) * a.Hkv * a.G + head;
-          }
+          for (int i = 0; i < kR; ++i) put_row(qb, rb * kR + i, v[i]);
         }
       }
-      if (!ok) break;
-      if (lane == 0) tail->entry[qb] = x;
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&tail->bars.q_full[qb]);
@@ -544,6 +548,17 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     float* red_sm = red_all + group * 4 * 2 * kR;
     float refd[kR], refn[kR], sum[kR];                                 // of the logits; of the weights times scale_v
     int o_uses = 0;
+    if (!at.done()) {                                                  // the first segment's query rows (one or two per warp)
+      const Entry x = entry_of(a, at.e);
+      for (int row = warp - kWarpSoftmax; row < L::kRows; row += 4 * L::kGroups) {
+        const int qrow = group0 + row, token = qrow / a.G, head = x.h * a.G + qrow - token * a.G;
+        uint2 v[kBoxes];
+        load_row((int64_t)(x.q0 + token) * a.q_tok + (int64_t)head * a.q_head, qrow < x.nq * a.G, v);
+        put_row(0, row, v);
+      }
+      ptx::fence_proxy_async();
+      asm volatile("barrier.cta.arrive %0, %1;" ::"r"(kFirstQ), "r"(L::kThreads - 96) : "memory");
+    }
     for (; !at.done(); at.next_segment()) {
       const int qb = at.seg & 1, e = at.e, s0 = at.s0, s1 = at.s1;
       ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.q_full[qb], (at.seg >> 1) & 1, abort_flag));
