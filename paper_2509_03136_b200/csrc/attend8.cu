@@ -920,10 +920,12 @@ Cut cut_of(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t m
   Cut c;
   const int64_t rows = max_q * (p->n_q_heads / p->n_kv_heads);
   c.boxes = p->d_k <= 128 ? 1 : 2;
-  // Groups of four rows while there are groups enough (a group of eight takes twice as long and spills); beyond 32 rows
-  // the codes are read again (from L2).
-  c.kr = rows <= 20 ? 4 : 8;
-  c.rb = rows > 32 ? 4 : (int)ceil_div(rows > 0 ? rows : 1, c.kr);
+  // Up to five softmax groups of four rows; beyond 20 rows as few and as even row groups as hold them, each of which reads the
+  // codes again (from L2).  Groups of eight rows take twice as long for a tile, so three of them pay for 21 to 24
+  // rows only (24 rows over 32K: 47 us, as two row groups 52; 32 rows: four of eight 65, two row groups 60; 40 rows: 190
+  // and 122 in a ragged batch).
+  c.kr = rows > 20 && rows <= 24 ? 8 : 4;
+  c.rb = c.kr == 8 ? 3 : rows > 0 ? (int)ceil_div(ceil_div(rows, ceil_div(rows, 20)), 4) : 1;
   c.turns = c.rb == 1 ? 4 : c.rb == 2 ? 2 : 1;
   c.rows = c.kr * c.rb;
   c.groups = (int)ceil_div(rows > 0 ? rows : 1, c.rows);
@@ -954,7 +956,7 @@ int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], AttendArgs a, cudaS
 }
 template <int kBoxes>
 int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], const AttendArgs& a, cudaStream_t st) {
-  if (c.kr == 8) return c.rb == 3 ? run_attend<kBoxes, 8, 3>(c, tm, a, st) : run_attend<kBoxes, 8, 4>(c, tm, a, st);
+  if (c.kr == 8) return run_attend<kBoxes, 8, 3>(c, tm, a, st);
   switch (c.rb) {
     case 1: return run_attend<kBoxes, 4, 1>(c, tm, a, st);
     case 2: return run_attend<kBoxes, 4, 2>(c, tm, a, st);
