@@ -20,7 +20,12 @@
 // that accumulate_sum_kernel adds in order.
 //
 // Bound by the exponentials: one per logit and pass, 16 per clock and SM, twice the tensor cores' time.  So
-// kPoly of every 8 are evaluated on the FMA pipe instead, two at a time (exp2_poly2).
+// kPoly of every 8 pairs are evaluated on the FMA pipe instead (exp2_poly2); two or three of 8 were slower, the instructions
+// then bound it.  Measured (one B200): all tokens of a 32K prompt, 32 heads on 8: 10.6 ms, 4.8 in pass 1 and 5.8 in
+// pass 2 (8.8 TFLOP, the exponentials alone 7.6 ms on their unit, which is 82 % busy in pass 1 and 70 % in pass 2; the
+// tensor pipe 45 and 39 %); the last 32 tokens of a 128K prompt, 28 heads on 4: 110 us, 48 + 62, for 117 M exponentials
+// per pass (26 us each) and 134 MB.  One issuing lane behind a lane-number branch, eight read-out warps, fetching the
+// accumulator a tile ahead, and a pass 1 without a maximum were all slower.
 //
 // Every wait is bounded: when one runs out the CTA records GVOTE_ERR_TIMEOUT in the status word, frees its tensor
 // memory and returns.

@@ -5,10 +5,11 @@
 // once, 2 d_k bytes per cached row.
 //
 // Split.  The rows of all (request, KV head) pairs ("entries") are cut into tiles of 128 and laid end to end, each entry
-// behind a gap of kGap tiles, about what beginning and ending one costs; CTA b of the grid takes the tiles between C b / grid
-// and C (b + 1) / grid, whatever entries they belong to.  So pruned heads of very different length load every SM alike,
-// without knowing the lengths on the host: each CTA adds up the entries itself.  What a CTA has of one entry is a segment; its result (reference, sum, output) goes to slot entry + CTA, or
-// straight to the output when the entry lies within one CTA.  attend8_merge_kernel merges an entry's segments.
+// behind a gap of kGap tiles, about what beginning and ending one costs; CTA b takes the tiles between T b / B and
+// T (b + 1) / B of the T places, whatever entries they belong to.  So pruned heads of very different length load every SM
+// alike, without knowing the lengths on the host: each CTA adds up the entries itself.  (Without the gaps a ragged batch
+// took 55 us instead of 36.)  What a CTA has of one entry is a segment; its result (reference, sum, output) goes to slot
+// entry + CTA, or straight to the output when the entry lies within one CTA.  attend8_merge_kernel merges an entry's segments.
 //
 // The products run on the codes themselves (tcgen05.mma kind::f8f6f4, e4m3 x e4m3, 32-bit sums), with the cached rows on
 // the M axis, so that nothing has to be widened or transposed on the way from the TMA boxes to the tensor cores:
@@ -16,8 +17,10 @@
 //   O [128 channels x (4 terms, rows)] += V^T P^T   V as it lies, its channels on the M axis; P as a sum of four terms
 // A term is the e4m3 value nearest to what the terms before it left, times 16 per term, and its columns are added up
 // with the matching power of two in 32 bits.  Three terms hold a row of Q to 2^-12 of each entry and 2^-27 of the
-// row's largest (bf16 itself: 2^-8); four hold a weight to 2^-16 of itself and 2^-24 of the reference.  An mma.sync version
-// that widened the codes in registers issued 690 instructions per 32 rows and was bound by their latency.
+// row's largest (bf16 itself: 2^-8); four hold a weight to 2^-16 of itself and 2^-24 of the reference.  (A version that widened
+// the codes in registers for mma.sync issued 690 instructions per 32 rows: 39 us where this one takes 37, one token over 128K
+// rows of four heads, and 54 where this one takes 39, five tokens over 32K.  Three terms for
+// the weights save 3 % of a call with many rows.)
 //
 // The scale of K enters the logit; the scale of V goes into the weight: P = 2^(l + log2(scale_v) - ref), ref the largest such
 // exponent so far, so that a block of large values neither overflows nor drowns what carries the output.  ref only moves
@@ -26,13 +29,20 @@
 // Warp 0 asks for the tiles of K and of V (TMA, only the 32-row parts that hold rows) into rings of their own - a tile
 // of K is done with as soon as S is there, a tile of V only after the softmax - warps 1 and 2 issue the MMAs of S and of O
 // (one warp for both took 1500 clocks a tile, its waits and commits one after the other), and warp 3 prepares the next
-// segment's Q terms; then come up to four softmax groups of four warps, thread = cached row of the tile (and channel of
-// the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each with
+// segment's Q terms (the first segment's, which everything waits for, are shared out among the softmax warps: alone,
+// warp 3 took 16,000 clocks for 20 rows); then come up to five softmax groups of four warps, thread = cached row of the
+// tile (and channel of the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each with
 // references and an O of its own (one group alone needs 3000 clocks of latency for a tile, the memory 1400), with many
 // the groups share a tile's rows out.  S and P are buffered as deep as the MMAs run ahead.
 //
 // Weights for the eviction: the logits are kept (4 bytes per row and query, against 2 d_k per row), and
 // attend8_weights_kernel turns them into weights once lse is known; a slot belongs to one thread, so the sum has one order.
+//
+// Measured (one B200, warm): one token of 28 heads over 128K rows of 4 KV heads, 134 MB: 37 us, the first kernel 30 of them at
+// 4.4 TB/s from launch to end (5.9 TB/s between its first tile and its last: 3 us pass before the first bytes are asked
+// for and 4 from the last bytes to the end).  A ragged batch of 128 pruned heads, 63 MB: 37 us with the weights.  Five tokens over
+// 32K rows of 8 heads: 39 us, a tile every 3200 clocks; the twenty softmax warps issue on 56 % of the clocks and wait for
+// their group's vote, for tensor memory and for the scales in the others.  Smallest calls: 15 us, all of it latency.
 //
 // Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
 #include <cstddef>

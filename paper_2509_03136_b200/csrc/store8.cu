@@ -11,6 +11,9 @@
 // read once, there is no second pass over them.  What a CTA waits for before it can ask for its rows is two rounds of
 // small loads (the note; words and prefixes); with five rounds, looking the request up and searching for the first
 // word, a call took a third longer.
+// Measured: 17K rows of 8 heads from bf16 (110 MB) 31 us, 24 of them in the second kernel (4.6 TB/s); 89 MB pruned from one cache
+// into another 28 us.  Each CTA working out its rows from the whole bit row, without the first kernel, took as long (31 us) for
+// one request and longer (33 us) for a batch.
 // Out of place: nothing orders the blocks, and a pruned 8-bit cache is small.
 #include "cache8.cuh"
 #include "ptx.cuh"
