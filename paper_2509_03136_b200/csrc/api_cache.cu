@@ -76,7 +76,7 @@ int32_t gvote_store8(const gvote_params* p, const void* K, const void* V, int64_
   if (ws_bytes < store8_map(p, batch, larger(total_tokens, cache->total_tokens)).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
   const SideArrays side{acc_or_null, acc_out_or_null, token_pos_or_null, token_pos_out_or_null};
   return launch_store8(p, (const __nv_bfloat16*)K, (const __nv_bfloat16*)V, tok_stride, head_stride, nullptr, mask_or_null,
-                       cu_seqlens, kv_len_or_null, batch, total_tokens, cache, side, (char*)ws, (cudaStream_t)stream);
+                       cu_seqlens, kv_len_or_null, batch, total_tokens, max_N, cache, side, (char*)ws, (cudaStream_t)stream);
 }
 
 int32_t gvote_prune8(const gvote_params* p, const gvote_cache8* src, const uint32_t* mask_or_null,
@@ -96,7 +96,7 @@ int32_t gvote_prune8(const gvote_params* p, const gvote_cache8* src, const uint3
   if (ws_bytes < store8_map(p, src->batch, larger(src->total_tokens, dst->total_tokens)).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
   const SideArrays side{acc_or_null, acc_out_or_null, token_pos_or_null, token_pos_out_or_null};
   return launch_store8(p, nullptr, nullptr, src->tok_stride, src->head_stride, src, mask_or_null, src->cu_seqlens,
-                       src->kv_len, src->batch, src->total_tokens, dst, side, (char*)ws, (cudaStream_t)stream);
+                       src->kv_len, src->batch, src->total_tokens, src->max_N, dst, side, (char*)ws, (cudaStream_t)stream);
 }
 
 int32_t gvote_append8(const gvote_params* p, const void* K_new, const void* V_new, int64_t tok_stride,

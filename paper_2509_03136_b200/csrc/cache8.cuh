@@ -15,7 +15,7 @@ constexpr int kMaxHeadDim8 = 256;
 constexpr int kMaxGroup8 = 128;               // query heads per KV head
 
 // Scratch of one call behind the status block; the maps of the entry points overlap, since nothing outlives a call.
-struct StoreMap { size_t prefix, note, total; };
+struct StoreMap { size_t list, note, total; };
 struct AttendMap { size_t o, ml, info, lse, logits, total; };
 struct AccumulateMap { size_t lse, part, total; int64_t q_tiles, key_chunks, q_chunks; int tpt; };
 
@@ -36,8 +36,8 @@ struct SideArrays {            // per-slot arrays that move with the rows
 
 int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t tok, int64_t head,
                       const gvote_cache8* src8, const uint32_t* mask, const int32_t* cu, const int32_t* kv_len,
-                      int32_t batch, int64_t total_tokens, const gvote_cache8* dst, const SideArrays& side, char* ws,
-                      cudaStream_t st);
+                      int32_t batch, int64_t total_tokens, int64_t max_N, const gvote_cache8* dst,
+                      const SideArrays& side, char* ws, cudaStream_t st);
 int32_t launch_append8(const gvote_params* p, const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t tok, int64_t head,
                        const int32_t* cu_new, int64_t max_new, const gvote_cache8* c, int32_t* kv_len_out, float* acc,
                        int32_t* token_pos, const int32_t* pos_new, char* ws, cudaStream_t st);

@@ -3,106 +3,118 @@
 //
 //   scale_b = the smallest 2^e with max |x| <= 448 * 2^e over the block, code = e4m3(x / scale_b).
 //
-// Two kernels.  store8_scan_kernel turns each (request, head) bit row into an exclusive popcount prefix per
-// mask word, and notes for every destination block what its CTA would otherwise have to look up (struct Note).
-// store8_kernel gives one CTA one destination block of K and of V: its threads take a bit each of the words from
-// the noted one on, load all rows into registers (16 values per thread and unit, 16-byte loads), take the maximum
-// over the CTA, and write the codes.  Bound by memory: 6 d_k bytes per kept row from bf16, 4 d_k from e4m3; the rows are
-// read once, there is no second pass over them.  What a CTA waits for before it can ask for its rows is two rounds of
-// small loads (the note; words and prefixes); with five rounds, looking the request up and searching for the first
-// word, a call took a third longer.
-// Measured: 17K rows of 8 heads from bf16 (110 MB) 31 us, 24 of them in the second kernel (4.6 TB/s); 89 MB pruned from one cache
-// into another 28 us.  Each CTA working out its rows from the whole bit row, without the first kernel, took as long (31 us) for
-// one request and longer (33 us) for a batch.
+// Two kernels.  store8_scan_kernel turns each (request, head) bit row into the list of its kept rows, 64 to a
+// destination block, and notes for every block what its CTA would otherwise have to look up (struct Note).
+// store8_kernel gives one CTA one destination block of K and of V: it reads its note and its list, loads all rows into
+// registers (16 values per thread and unit, 16-byte loads), takes the maximum over the CTA, and writes the codes.  Bound
+// by memory: 6 d_k bytes per kept row from bf16, 4 d_k from e4m3; the rows are read once, there is no second pass
+// over them.  A CTA waits for one round of small loads before it can ask for its rows; with five rounds, looking the
+// request up and searching for the first word, a call took a third longer.
+// Measured: 17K rows of 8 heads from bf16 (110 MB) 31 us, 24 of them in the second kernel (4.6 TB/s); 89 MB pruned from one
+// cache into another 28 us; 275K rows of one head 39 us (48 with one CTA per bit row in the scan).  Each CTA working out
+// its rows from the whole bit row, without the first kernel, took as long for one request and longer (33 us) for a batch;
+// neither fewer instructions per value nor six CTAs per SM instead of five changed the second kernel's time.
 // Out of place: nothing orders the blocks, and a pruned 8-bit cache is small.
+#include <cooperative_groups.h>
+
 #include "cache8.cuh"
 #include "ptx.cuh"
 
 namespace gvote {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kStoreThreads = 256;
-constexpr int kScan8Threads = 1024;
+constexpr int kScan8Threads = 256;
 
 // One per (head, destination block), padding entries of the block list included.
 struct __align__(16) Note {
-  int word, cnt, words, row0;    // first mask word (of the request's), rows, mask words that count, first destination row
-  int r, start, dst, pad;        // request, its first source slot and first destination slot
+  int cnt, row0, start, dst;     // rows (<= 0: none), first destination row, the request's first source and destination slot
+  int r, pad[3];
 };
 
-// One CTA per (head, request): prefix[h][word] = kept keys among the n rows that count, before this word.
+// A cluster per (head, request), each CTA with a run of its mask words: the sources of the kept rows, in order, 64 to a
+// destination block, and the blocks' notes.
 __global__ void __launch_bounds__(kScan8Threads)
 store8_scan_kernel(const uint32_t* __restrict__ mask, const int32_t* __restrict__ cu, const int32_t* __restrict__ kv_len,
-                   int Hkv, int64_t row_words, int32_t* __restrict__ prefix, const int32_t* __restrict__ cu8,
+                   int Hkv, int64_t row_words, int32_t* __restrict__ list, const int32_t* __restrict__ cu8,
                    int64_t row_blocks, Note* __restrict__ note, int32_t* __restrict__ kv_len_out, int32_t* status) {
-  __shared__ int warp_tot[kScan8Threads / 32];
-  __shared__ int carry;
+  constexpr int kWarps = kScan8Threads / 32;
+  __shared__ int warp_tot[kWarps];
+  __shared__ int share_tot;
   ptx::let_next_begin();
-  const int h = blockIdx.x, r = blockIdx.y;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int h = blockIdx.y, r = blockIdx.z;
   const int start = cu[r], n = valid_keys(kv_len, r, Hkv, h, cu[r + 1] - start);
-  const int words = (n + 31) >> 5;
-  const int64_t woff = (int64_t)h * row_words + mask_word_offset(start, r);
+  const int words = (n + 31) >> 5, share = (words + C - 1) / C, w0 = min(rank * share, words), w1 = min(w0 + share, words);
+  const uint32_t* bits_of = mask + (int64_t)h * row_words + mask_word_offset(start, r);
   const int dstart = cu8[r], cap = cu8[r + 1] - dstart;
-  Note* my_note = note + (int64_t)h * row_blocks + block8_offset(dstart, r);
-  const int64_t list_end = r + 1 < (int)gridDim.y ? block8_offset(cu8[r + 1], r + 1) : row_blocks;
-  const int listed = (int)(list_end - block8_offset(dstart, r));
+  const int64_t first = (int64_t)h * row_blocks + block8_offset(dstart, r);       // the request's first block
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) carry = 0;
+  auto word_at = [&](int w) {
+    uint32_t v = w < w1 ? bits_of[w] : 0u;
+    if (w == words - 1 && (n & 31)) v &= (1u << (n & 31)) - 1u;
+    return v;
+  };
+  uint32_t v = word_at(w0 + tid);
+  int mine = __popc(v);
+  for (int w = w0 + tid + kScan8Threads; w < w1; w += kScan8Threads) mine += __popc(word_at(w));
+  mine = __reduce_add_sync(0xffffffffu, mine);
+  if (lane == 0) warp_tot[warp] = mine;
   __syncthreads();
-  for (int base = 0; base < words; base += 4 * kScan8Threads) {
-    const int w0 = base + 4 * tid;
-    int c[4], mine = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int w = w0 + j;
-      uint32_t v = w < words ? mask[woff + w] : 0u;
-      if (w == words - 1 && (n & 31)) v &= (1u << (n & 31)) - 1u;
-      c[j] = __popc(v);
-      mine += c[j];
-    }
-    int inc = mine;
+  if (warp == 0) {
+    const int t = __reduce_add_sync(0xffffffffu, lane < kWarps ? warp_tot[lane] : 0);
+    if (lane == 0) share_tot = t;
+  }
+  cluster.sync();
+  int before = 0, total = 0;                                       // kept rows of the CTAs before this one, and of all
+  for (int c = 0; c < C; ++c) {
+    const int t = *cluster.map_shared_rank(&share_tot, c);
+    before += c < rank ? t : 0;
+    total += t;
+  }
+  const int m = min(total, cap);
+  int32_t* out = list + first * kBlock8;
+  for (int base = w0; base < w1; base += kScan8Threads) {          // thread = word, then thread = bit
+    if (base > w0) v = word_at(base + tid);
+    int inc = __popc(v);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int u = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += u;
     }
+    __syncthreads();
     if (lane == 31) warp_tot[warp] = inc;
     __syncthreads();
-    if (warp == 0) {
-      int t = warp_tot[lane];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, t, o);
-        if (lane >= o) t += u;
-      }
-      warp_tot[lane] = t;
+    const int tot = lane < kWarps ? warp_tot[lane] : 0;
+    const int run = before + __reduce_add_sync(0xffffffffu, lane < warp ? tot : 0) + inc - __popc(v);
+    before += __reduce_add_sync(0xffffffffu, tot);
+    const int row = (base + warp * 32) * 32 + lane;
+#pragma unroll 8
+    for (int j = 0; j < 32; ++j) {
+      const uint32_t b = __shfl_sync(0xffffffffu, v, j);
+      const int at = __shfl_sync(0xffffffffu, run, j) + __popc(b & ((1u << lane) - 1u));
+      if (((b >> lane) & 1u) && at < m) out[at] = row + j * 32;
     }
-    __syncthreads();
-    int run = carry + (warp ? warp_tot[warp - 1] : 0) + inc - mine;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (w0 + j < words) prefix[woff + w0 + j] = run;
-      // the block whose first row is one of this word's
-      const int b = (run + kBlock8 - 1) >> 6;
-      if (b * kBlock8 < run + c[j] && b * kBlock8 < cap) my_note[b].word = w0 + j;
-      run += c[j];
-    }
-    __syncthreads();
-    if (tid == 0) carry += warp_tot[kScan8Threads / 32 - 1];
-    __syncthreads();
   }
-  const int m = min(carry, cap);
-  const int before = r == 0 ? (int)block8_offset(dstart, 0) : 0;   // (slabs that do not start at slot 0)
-  for (int b = tid - before; b < listed; b += kScan8Threads) {
-    my_note[b].cnt = b < 0 ? 0 : min(kBlock8, m - b * kBlock8);    // (<= 0: no rows)
-    my_note[b].words = words;
-    my_note[b].row0 = b * kBlock8;
-    *reinterpret_cast<int4*>(&my_note[b].r) = make_int4(r, start, dstart, 0);
+  const int64_t list_end = r + 1 < (int)gridDim.z ? block8_offset(cu8[r + 1], r + 1) : row_blocks;
+  const int listed = (int)(list_end - block8_offset(dstart, r));
+  const int ahead = r == 0 ? (int)block8_offset(dstart, 0) : 0;    // (slabs that do not start at slot 0)
+  for (int b = rank * kScan8Threads + tid - ahead; b < listed; b += C * kScan8Threads) {
+    Note x;
+    x.cnt = b < 0 ? 0 : min(kBlock8, m - b * kBlock8);
+    x.row0 = b * kBlock8; x.start = start; x.dst = dstart; x.r = r;
+    int4* q = reinterpret_cast<int4*>(note + first + b);
+    q[0] = make_int4(x.cnt, x.row0, x.start, x.dst);
+    q[1] = make_int4(x.r, 0, 0, 0);
   }
-  if (tid == 0) {
+  if (rank == 0 && tid == 0) {
     kv_len_out[r * Hkv + h] = m;
-    if (carry > cap) { atomicExch(&status[0], GVOTE_ERR_WORKSPACE_TOO_SMALL); atomicExch(&status[1], 8); }
+    if (total > cap) { atomicExch(&status[0], GVOTE_ERR_WORKSPACE_TOO_SMALL); atomicExch(&status[1], 8); }
   }
+  cluster.sync();                                                  // the shares' totals are read until here
 }
 
 struct StoreArgs {
@@ -110,7 +122,7 @@ struct StoreArgs {
   const float* src_scale[2];     // of an e4m3 source
   int64_t s_tok, s_head, s_total, s_row_blocks;
   const uint32_t* mask;          // or null: every row
-  const int32_t* prefix;
+  const int32_t* list;           // [Hkv][row_blocks of the destination][64] the rows' sources
   const Note* note;              // [Hkv][row_blocks of the destination]
   const int32_t* cu;
   const int32_t* kv_len;
@@ -241,30 +253,12 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
   int r, start, dstart, row0, cnt;
   if (a.mask) {
     ptx::wait_for_previous();
-    const int4 note = *reinterpret_cast<const int4*>(&a.note[db]), where = *reinterpret_cast<const int4*>(&a.note[db].r);
-    cnt = note.y; row0 = note.w; r = where.x; start = where.y; dstart = where.z;
+    const int4 note = *reinterpret_cast<const int4*>(&a.note[db]);
+    r = a.note[db].r;
+    if (tid < kBlock8) s_src[tid] = a.list[db * kBlock8 + tid];    // (beyond cnt: not looked at)
+    cnt = note.x; row0 = note.y; start = note.z; dstart = note.w;
     if (cnt <= 0) return;
-    const int64_t woff = (int64_t)h * a.row_words + mask_word_offset(start, r);
-    // thread = one bit of a word, four words per warp and round
-    constexpr int kWarps = kStoreThreads / 32;
-    const int lane = tid & 31;
-    for (int base = note.x + (tid >> 5);; base += 4 * kWarps) {
-      uint32_t bits[4];
-      int rank[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int w = base + j * kWarps;
-        bits[j] = w < note.z ? a.mask[woff + w] : 0u;
-        rank[j] = w < note.z ? a.prefix[woff + w] - row0 : cnt;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        // (bits behind the rows that count come after the last of the cnt ranks)
-        const int mine = rank[j] + __popc(bits[j] & ((1u << lane) - 1u));
-        if (((bits[j] >> lane) & 1u) && mine >= 0 && mine < cnt) s_src[mine] = (base + j * kWarps) * 32 + lane;
-      }
-      if (__syncthreads_or(rank[3] + __popc(bits[3]) >= cnt)) break;   // (ranks grow with the words)
-    }
+    __syncthreads();
   } else {
     r = a.batch == 1 ? 0 : find_request_by(a.cu8, a.batch, gb, 6);
     dstart = a.cu8[r];
@@ -348,16 +342,17 @@ int32_t run_store(const StoreArgs& a, unsigned ctas, cudaStream_t st) {
 
 StoreMap store8_map(const gvote_params* p, int32_t batch, int64_t total_tokens) {
   StoreMap m;
-  m.prefix = kStatusBytes;
-  m.note = align_up(m.prefix + (size_t)p->n_kv_heads * gvote_mask_row_words(total_tokens, batch) * 4, 256);
-  m.total = align_up(m.note + (size_t)p->n_kv_heads * gvote_cache8_row_blocks(total_tokens, batch) * sizeof(Note), 256);
+  const size_t blocks = (size_t)p->n_kv_heads * gvote_cache8_row_blocks(total_tokens, batch);
+  m.list = kStatusBytes;
+  m.note = align_up(m.list + blocks * kBlock8 * 4, 256);
+  m.total = align_up(m.note + blocks * sizeof(Note), 256);
   return m;
 }
 
 int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t tok, int64_t head,
                       const gvote_cache8* src8, const uint32_t* mask, const int32_t* cu, const int32_t* kv_len,
-                      int32_t batch, int64_t total_tokens, const gvote_cache8* dst, const SideArrays& side, char* ws,
-                      cudaStream_t st) {
+                      int32_t batch, int64_t total_tokens, int64_t max_N, const gvote_cache8* dst,
+                      const SideArrays& side, char* ws, cudaStream_t st) {
   const int Hkv = p->n_kv_heads;
   const StoreMap m = store8_map(p, batch, total_tokens > dst->total_tokens ? total_tokens : dst->total_tokens);
   StoreArgs a;
@@ -368,7 +363,7 @@ int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_
   a.s_tok = tok; a.s_head = head; a.s_total = total_tokens;
   a.s_row_blocks = gvote_cache8_row_blocks(total_tokens, batch);
   a.mask = mask;
-  a.prefix = reinterpret_cast<const int32_t*>(ws + m.prefix);
+  a.list = reinterpret_cast<const int32_t*>(ws + m.list);
   a.note = reinterpret_cast<const Note*>(ws + m.note);
   a.cu = cu; a.kv_len = kv_len;
   a.row_words = gvote_mask_row_words(total_tokens, batch);
@@ -381,9 +376,21 @@ int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_
   a.status = reinterpret_cast<int32_t*>(ws);
   a.Hkv = Hkv; a.batch = batch; a.d_k = p->d_k;
   if (mask) {
+    // CTAs per bit row: the largest of 8, 4, 2, 1 that leaves each 4096 rows of the longest slab and the grid four CTAs per SM
+    int C = 8;
+    while (C > 1 && (max_N / C < 4096 || (int64_t)batch * Hkv * C > 4 * 148)) C >>= 1;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    cfg.gridDim = dim3(C, Hkv, batch);
+    cfg.blockDim = dim3(kScan8Threads);
+    cfg.stream = st;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = C; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
     LaunchScope scope_("store8_scan_kernel", st);
-    launch_on(store8_scan_kernel, dim3(Hkv, batch), dim3(kScan8Threads), 0, st, mask, cu, kv_len, Hkv, a.row_words,
-              (int32_t*)(ws + m.prefix), a.cu8, a.d_row_blocks, (Note*)(ws + m.note), a.kv_len_out, a.status);
+    (void)cudaLaunchKernelEx(&cfg, store8_scan_kernel, mask, cu, kv_len, Hkv, a.row_words, (int32_t*)(ws + m.list), a.cu8,
+                             a.d_row_blocks, (Note*)(ws + m.note), a.kv_len_out, a.status);
     GVOTE_LAUNCH_CHECK("store8_scan_kernel");
   }
   const unsigned ctas = (unsigned)(a.d_row_blocks * Hkv);
