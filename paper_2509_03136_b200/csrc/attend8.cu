@@ -326,17 +326,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   const uint32_t tmem = __shfl_sync(0xffffffffu, tail->tmem_slot, 0);
   // no more parts than places: an empty part between two of an entry's would leave its slot unwritten
   const int T = pref[entries], B = max(min((int)gridDim.x, T), 1), b = blockIdx.x;
-  const int t0 = (int)((int64_t)T * min(b, B) / B), t1 = (int)((int64_t)T * min(b + 1, B) / B);
-  // which CTAs hold an entry: the CTA of the tile at place t is the largest c with T c / B <= t
-  if (b == 0) {
-    int2* info = a.info + (int64_t)blockIdx.y * entries;
-    for (int e = tid; e < entries; e += L::kThreads) {
-      const int f = pref[e] + kGap, l = pref[e + 1] - 1;
-      int2 v = make_int2(-1, -1);
-      if (l >= f) v = make_int2((int)((((int64_t)f + 1) * B - 1) / T), (int)((((int64_t)l + 1) * B - 1) / T));
-      info[e] = v;
-    }
-  }
+  const int per_cta = T / B, odd = T - per_cta * B;                    // floor(T c / B) = c (T / B) + c (T mod B) / B
+  const int t0 = min(b, B) * per_cta + min(b, B) * odd / B, t1 = min(b + 1, B) * per_cta + min(b + 1, B) * odd / B;
   int e_first = t0 < t1 ? 0 : entries;                                 // the entry of tile t0 (a CTA without tiles: none)
   {
     int hi = entries - 1;
@@ -512,6 +503,14 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       }
     }
     if (!ok) drain_mmas(&tail->bars.drain[1]);
+    // Which CTAs hold an entry, for the merge: the CTA of the tile at place t is the largest c with T c / B <= t.  (Divisions
+    // of 64 bits: the softmax is still at its last tile.)
+    for (int e = b + lane * B; b < B && e < entries; e += 32 * B) {
+      const int f = pref[e] + kGap, l = pref[e + 1] - 1;
+      int2 v = make_int2(-1, -1);
+      if (l >= f) v = make_int2((int)((((int64_t)f + 1) * B - 1) / T), (int)((((int64_t)l + 1) * B - 1) / T));
+      a.info[(int64_t)blockIdx.y * entries + e] = v;
+    }
   } else if (warp == kWarpQ) {
     // ------------------------------------------------------------------ Q as three e4m3 terms, a segment ahead
     for (int i = lane; i < 2 * kBoxes * (L::kN1 - 3 * L::kRows) * 8; i += 32) {     // the rows behind the last term are zero
