@@ -40,7 +40,7 @@
 //
 // Measured (one B200, warm): one token of 28 heads over 128K rows of 4 KV heads, 134 MB: 37 us, the first kernel 30 of them at
 // 4.4 TB/s from launch to end (5.9 TB/s between its first tile and its last: 3 us pass before the first bytes are asked
-// for and 4 from the last bytes to the end).  A ragged batch of 128 pruned heads, 63 MB: 37 us with the weights.  Five tokens over
+// for and 4 from the last bytes to the end).  A ragged batch of 128 pruned heads, 63 MB: 36 us with the weights.  Five tokens over
 // 32K rows of 8 heads: 39 us, a tile every 3200 clocks; the twenty softmax warps issue on 56 % of the clocks and wait for
 // their group's vote, for tensor memory and for the scales in the others.  Smallest calls: 15 us, all of it latency.
 //

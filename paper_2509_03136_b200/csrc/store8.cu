@@ -387,7 +387,7 @@ int32_t launch_store8(const gvote_params* p, const __nv_bfloat16* K, const __nv_
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = C; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = C > 1 ? 1 : 0;
     LaunchScope scope_("store8_scan_kernel", st);
     (void)cudaLaunchKernelEx(&cfg, store8_scan_kernel, mask, cu, kv_len, Hkv, a.row_words, (int32_t*)(ws + m.list), a.cu8,
                              a.d_row_blocks, (Note*)(ws + m.note), a.kv_len_out, a.status);
