@@ -75,6 +75,11 @@ class Cache8:
         self.cu_seqlens, self.kv_len, self.geom = cu_seqlens, kv_len, (batch, total, max_N)
         self.shape, self.device = (H, d), dev
 
+    def __setattr__(self, name, value):
+        if hasattr(self, name):
+            raise AttributeError(f"{name} of a Cache8 is fixed (its pointers are taken once): make another Cache8")
+        object.__setattr__(self, name, value)
+
 
 class GVoteError(RuntimeError):
     def __init__(self, status: int, where: str):

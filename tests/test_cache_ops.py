@@ -882,3 +882,12 @@ def test_python_face_refuses_other_shapes(gv):
             gv.gvote_attend8(p, **a)
     with pytest.raises(gv.GVoteError, match="workspace"):
         gv.gvote_attend8(p, Q, cq, 1, c, Q.clone(), ws[:512])
+
+
+@gpu
+def test_a_cache_keeps_its_tensors(gv):
+    """The pointers are taken once, so that another tensor in a field would not be seen: it is refused."""
+    c = gv.alloc_cache8(params(gv, 4, 2, 64), [0, 100])
+    for name in ("K", "V", "k_scale", "v_scale", "cu_seqlens", "kv_len", "geom", "args"):
+        with pytest.raises(AttributeError, match="fixed"):
+            setattr(c, name, getattr(c, name))
