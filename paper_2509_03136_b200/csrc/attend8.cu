@@ -812,59 +812,81 @@ __device__ __forceinline__ float2 warp_join(float M, float L) {
   return make_float2(all, L);
 }
 
-// Block = one row of one entry, merged from its segments when it has several (or none).  They are a few KB: what counts is how
-// many loads wait for one another, so the outputs are asked for before the maxima are known.
+// The rows of the entries that lie in several segments (or none), merged.  They are a few KB: what counts is how many loads wait
+// for one another, so a block takes a row and its outputs are asked for before the maxima are known.  With many entries, most
+// of them in one CTA or two (so of a few parts), it is the number of blocks that counts: then (kRows = 8) a warp takes a row
+// of up to 32 parts, and the block the others (512 entries of 2048 rows: 15 us with a block per row).
+template <int kRows>
 __global__ void __launch_bounds__(256)
 attend8_merge_kernel(const __grid_constant__ AttendArgs a, int ctas, int max_rows) {
   __shared__ float4 s_o[8][32 * 2];
   __shared__ float s_f[4 * kSms];
-  const int entries = a.batch * a.Hkv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  {
-    const int e = blockIdx.x / max_rows, row = blockIdx.x - e * max_rows;
-    const int group = row / a.group_rows, in_group = row - group * a.group_rows;
-    const Entry x = entry_of(a, e);
-    ptx::wait_for_previous();
-    ptx::let_next_begin();
+  __shared__ int s_left[8];
+  const int entries = a.batch * a.Hkv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quads = a.d_k >> 2;
+  struct Job { Entry x; int e, row, parts; int64_t slot0; };
+  auto entry_job = [&](int id) {
+    Job j = {};
+    if (id < entries * max_rows) {
+      j.e = id / max_rows;
+      j.row = id - j.e * max_rows;
+      j.x = entry_of(a, j.e);
+    }
+    return j;
+  };
+  auto job_of = [&](Job j) {                            // parts < 0: nothing to do
+    const int e = j.e;
+    j.parts = -1;
+    if (j.row >= j.x.nq * a.G) return j;
+    const int group = j.row / a.group_rows, in_group = j.row - group * a.group_rows;
     const int2 v = a.info[(int64_t)group * entries + e];
-    if (row >= x.nq * a.G) return;
-    if (a.turns == 1 && v.x >= 0 && v.x == v.y) return; // the first kernel has written it
-    const int quads = a.d_k >> 2;
-    const int p0 = v.x * a.turns, parts = v.x < 0 ? 0 : (v.y + 1) * a.turns - p0;
-    const int64_t slot0 = (((int64_t)group * (entries + ctas) + e) * a.turns + p0) * a.group_rows + in_group;
+    if (a.turns == 1 && v.x >= 0 && v.x == v.y) return j;            // the first kernel has written it
+    const int p0 = v.x * a.turns;
+    j.parts = v.x < 0 ? 0 : (v.y + 1) * a.turns - p0;
+    j.slot0 = (((int64_t)group * (entries + ctas) + e) * a.turns + p0) * a.group_rows + in_group;
+    return j;
+  };
+  auto part_o = [&](const Job& j, int k, int q) {
+    return *reinterpret_cast<const float4*>(a.part_o + (j.slot0 + (int64_t)k * a.group_rows) * a.d_k + q * 4);
+  };
+  auto add = [](float4& s, const float4& p, float f) {  // (0: a turn without tiles has left nothing)
+    if (f != 0.f) { s.x = fmaf(f, p.x, s.x); s.y = fmaf(f, p.y, s.y); s.z = fmaf(f, p.z, s.z); s.w = fmaf(f, p.w, s.w); }
+  };
+  auto finish = [&](const Job& j, int q, const float4& s, float2 ml) {
+    const int64_t token = j.x.q0 + j.row / a.G;
+    const int g = j.x.h * a.G + j.row % a.G;
+    const float inv = ml.x == -INFINITY && ml.y == 0.f ? 0.f : 1.f / ml.y;
+    __nv_bfloat162 out[2] = {__floats2bfloat162_rn(s.x * inv, s.y * inv), __floats2bfloat162_rn(s.z * inv, s.w * inv)};
+    *reinterpret_cast<uint2*>(a.out + token * a.o_tok + (int64_t)g * a.o_head + q * 4) = *reinterpret_cast<uint2*>(out);
+    if (q == 0) write_lse(a, token * a.Hkv * a.G + g, ml);
+  };
+  auto block_row = [&](const Job& j) {
     constexpr int kAhead = 8;
     float4 pre[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int k = warp + 8 * i;
-      if (k < parts && lane < quads) pre[i] = *reinterpret_cast<const float4*>(a.part_o + (slot0 + (int64_t)k * a.group_rows) * a.d_k + lane * 4);
-    }
+    for (int i = 0; i < kAhead; ++i)
+      if (warp + 8 * i < j.parts && lane < quads) pre[i] = part_o(j, warp + 8 * i, lane);
     float M = -INFINITY, L = 0.f;
-    for (int k = lane; k < parts; k += 32) join(M, L, a.part_ml[slot0 + (int64_t)k * a.group_rows]);
+    for (int k = lane; k < j.parts; k += 32) join(M, L, a.part_ml[j.slot0 + (int64_t)k * a.group_rows]);
     const float2 ml = warp_join(M, L);
-    for (int i = tid; i < parts; i += 256) {
-      const float2 m = a.part_ml[slot0 + (int64_t)i * a.group_rows];
+    for (int i = tid; i < j.parts; i += 256) {
+      const float2 m = a.part_ml[j.slot0 + (int64_t)i * a.group_rows];
       s_f[i] = m.x == -INFINITY ? 0.f : exp2_fast(m.x - ml.x) * m.y;
     }
     __syncthreads();
     for (int q = lane; q < quads; q += 32) {
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-      auto add = [&](const float4& p, float f) {        // (0: a turn without tiles has left nothing)
-        if (f != 0.f) { s.x = fmaf(f, p.x, s.x); s.y = fmaf(f, p.y, s.y); s.z = fmaf(f, p.z, s.z); s.w = fmaf(f, p.w, s.w); }
-      };
       int k0 = warp;
       if (q == lane) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
-          if (warp + 8 * i < parts) add(pre[i], s_f[warp + 8 * i]);
+          if (warp + 8 * i < j.parts) add(s, pre[i], s_f[warp + 8 * i]);
         k0 += 8 * kAhead;
       }
 #pragma unroll 8
-      for (int k = k0; k < parts; k += 8)
-        add(*reinterpret_cast<const float4*>(a.part_o + (slot0 + (int64_t)k * a.group_rows) * a.d_k + q * 4), s_f[k]);
+      for (int k = k0; k < j.parts; k += 8) add(s, part_o(j, k, q), s_f[k]);
       s_o[warp][q] = s;
     }
     __syncthreads();
-    const int token = row / a.G, g = x.h * a.G + row % a.G;
     if (tid < quads) {
       float4 s = s_o[0][tid];
 #pragma unroll
@@ -872,11 +894,40 @@ attend8_merge_kernel(const __grid_constant__ AttendArgs a, int ctas, int max_row
         const float4 p = s_o[k][tid];
         s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
       }
-      const float inv = ml.x == -INFINITY && ml.y == 0.f ? 0.f : 1.f / ml.y;
-      __nv_bfloat162 out[2] = {__floats2bfloat162_rn(s.x * inv, s.y * inv), __floats2bfloat162_rn(s.z * inv, s.w * inv)};
-      *reinterpret_cast<uint2*>(a.out + (int64_t)(x.q0 + token) * a.o_tok + (int64_t)g * a.o_head + tid * 4) = *reinterpret_cast<uint2*>(out);
+      finish(j, tid, s, ml);
     }
-    if (tid == 0) write_lse(a, (int64_t)(x.q0 + token) * a.Hkv * a.G + g, ml);
+  };
+  const Job mine = entry_job(kRows == 1 ? blockIdx.x : blockIdx.x * kRows + warp);
+  ptx::wait_for_previous();
+  ptx::let_next_begin();
+  if (kRows == 1) {
+    const Job j = job_of(mine);
+    if (j.parts >= 0) block_row(j);
+    return;
+  }
+  {
+    const Job j = job_of(mine);
+    if (lane == 0) s_left[warp] = j.parts > 32;
+    if (j.parts >= 0 && j.parts <= 32) {
+      const float2 m = lane < j.parts ? a.part_ml[j.slot0 + (int64_t)lane * a.group_rows] : make_float2(-INFINITY, 0.f);
+      const float2 ml = warp_join(m.x, m.y);
+      const float f = m.x == -INFINITY ? 0.f : exp2_fast(m.x - ml.x) * m.y;
+      for (int q = lane; q - lane < quads; q += 32) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < j.parts; ++k) {
+          const float fk = __shfl_sync(0xffffffffu, f, k);
+          if (q < quads) add(s, part_o(j, k, q), fk);
+        }
+        if (q < quads) finish(j, q, s, ml);
+      }
+    }
+  }
+  __syncthreads();
+  for (int w = 0; w < kRows; ++w) {
+    if (!s_left[w]) continue;
+    block_row(job_of(entry_job(blockIdx.x * kRows + w)));
+    __syncthreads();
   }
 }
 
@@ -1035,7 +1086,11 @@ int32_t launch_attend8(const gvote_params* p, const __nv_bfloat16* Q, int64_t q_
     const int64_t rows = max_q * a.G;
     {
       LaunchScope scope_("attend8_merge_kernel", st);
-      launch_behind(attend8_merge_kernel, dim3((unsigned)(a.batch * a.Hkv * rows)), dim3(256), 0, st, a, (int)cut.ctas, (int)rows);
+      const int64_t all = (int64_t)a.batch * a.Hkv * rows;
+      if (a.batch * a.Hkv < kSms)
+        launch_behind(attend8_merge_kernel<1>, dim3((unsigned)all), dim3(256), 0, st, a, (int)cut.ctas, (int)rows);
+      else
+        launch_behind(attend8_merge_kernel<8>, dim3((unsigned)ceil_div(all, 8)), dim3(256), 0, st, a, (int)cut.ctas, (int)rows);
     }
     GVOTE_LAUNCH_CHECK("attend8_merge_kernel");
     if (acc_out) {

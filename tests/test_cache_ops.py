@@ -377,6 +377,14 @@ def test_attend_many_short_requests(gv):
 
 
 @gpu
+@pytest.mark.parametrize("hq,d,n_q", [(4, 64, 1), (3, 256, 2)])
+def test_attend_one_long_request_among_many_short_ones(gv, hq, d, n_q):
+    """Most rows are merged from a few parts, the long request's from more than a hundred."""
+    lens = (20, 3) * 40 + (30000,) + (1, 20, 0) * 30
+    run_attend(gv, hq, 1, d, lens, [[n] for n in lens], tuple(min(n_q, n) for n in lens), seed=28)
+
+
+@gpu
 def test_a_workspace_serves_every_smaller_call(gv):
     p = params(gv, 7, 1, 64)
     rng = np.random.default_rng(22)
