@@ -40,7 +40,7 @@
 //
 // Measured (one B200, warm): one token of 28 heads over 128K rows of 4 KV heads, 134 MB: 37 us, the first kernel 30 of them at
 // 4.4 TB/s from launch to end (5.9 TB/s between its first tile and its last: 3 us pass before the first bytes are asked
-// for and 4 from the last bytes to the end).  A ragged batch of 128 pruned heads, 63 MB: 36 us with the weights.  Five tokens over
+// for and 4 from the last bytes to the end).  A ragged batch of 128 pruned heads, 63 MB: 34 us with the weights.  Five tokens over
 // 32K rows of 8 heads: 39 us, a tile every 3200 clocks; the twenty softmax warps issue on 56 % of the clocks and wait for
 // their group's vote, for tensor memory and for the scales in the others.  Smallest calls: 15 us, all of it latency.
 //
@@ -931,47 +931,56 @@ attend8_merge_kernel(const __grid_constant__ AttendArgs a, int ctas, int max_row
   }
 }
 
-// Thread = one slot: the weights its row of the cache gets from the request's tokens and the group's heads, added to acc.
-// Blocks of 256 slots: request r0 + i has those from (cu >> 8) - base + i on.
+// The weights a row of the cache gets from the request's tokens and the group's heads, added to acc: thread = kSpan / 256 slots.
+// Blocks of kSpan slots: request r0 + i has those from (cu >> kSpanBits) - base + i on.
+// Latency bound: two slots per thread rather than one halve the blocks (64 requests of 2048 rows 21 -> 15 us of events; a call
+// with 128 rows of queries loses 4 of its 224 us to the shorter runs of loads).
+constexpr int kSpanBits = 9, kSpan = 1 << kSpanBits;
 __global__ void __launch_bounds__(256)
 attend8_weights_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int kSlots = kSpan / 256, kRows = 128, kAhead = 4;       // rows whose lse is at hand, logits of a slot on their way at once
+  __shared__ float s_lse[kRows];
   const int tid = threadIdx.x, h = blockIdx.y;
   const int64_t gb = blockIdx.x;
-  const int base = a.cu[a.r0] >> 8;
+  const int base = a.cu[a.r0] >> kSpanBits;
   int i_req = -1;                                       // the last request whose first block is not behind gb
   for (int i0 = 0; i0 < a.batch; i0 += 256) {
     const int i = i0 + tid;
-    i_req += __syncthreads_count(i < a.batch && (int64_t)((a.cu[a.r0 + min(i, a.batch - 1)] >> 8) - base) + i <= gb);
+    i_req += __syncthreads_count(i < a.batch && (int64_t)((a.cu[a.r0 + min(i, a.batch - 1)] >> kSpanBits) - base) + i <= gb);
   }
   const int e = i_req * a.Hkv + h;
   const Entry x = entry_of(a, e);
   ptx::wait_for_previous();
-  const int i0 = (int)(gb - ((x.start >> 8) - base + i_req)) * 256, i = i0 + tid;
+  const int i0 = (int)(gb - ((x.start >> kSpanBits) - base + i_req)) * kSpan, i = i0 + tid;
   if (i0 >= x.n) return;
-  const bool holds = i < x.n;
   const int rows = x.nq * a.G;
   const float* l = a.logits + (int64_t)h * a.max_q * a.G * a.total + x.start + i;
   const float* lse = a.lse2 + (int64_t)x.q0 * a.Hkv * a.G + h * a.G;
   const int64_t slot = (int64_t)h * a.total + x.start + i;
-  constexpr int kRows = 128, kAhead = 8;                // rows whose lse is at hand, logits on their way at once
-  __shared__ float s_lse[kRows];
-  float s = 0.f;
-  const float was = a.acc && holds ? a.acc[slot] : 0.f;
+  float s[kSlots] = {}, was[kSlots];
+#pragma unroll
+  for (int c = 0; c < kSlots; ++c) was[c] = a.acc && i + c * 256 < x.n ? a.acc[slot + c * 256] : 0.f;
   for (int row0 = 0; row0 < rows; row0 += kRows) {
     const int some = min(kRows, rows - row0);
     if (row0 > 0) __syncthreads();
     if (tid < some) s_lse[tid] = lse[(int64_t)((row0 + tid) / a.G) * a.Hkv * a.G + (row0 + tid) % a.G];
     for (int k0 = 0; k0 < some; k0 += kAhead, l += kAhead * a.total) {
-      float v[kAhead];
+      float v[kSlots][kAhead];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) v[k] = holds && k0 + k < some ? l[k * a.total] : -INFINITY;
+      for (int c = 0; c < kSlots; ++c)
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) v[c][k] = i + c * 256 < x.n && k0 + k < some ? l[k * a.total + c * 256] : -INFINITY;
       if (k0 == 0) __syncthreads();
 #pragma unroll
       for (int k = 0; k < kAhead; ++k)
-        if (v[k] != -INFINITY) s += exp2_fast(v[k] - s_lse[k0 + k]);
+#pragma unroll
+        for (int c = 0; c < kSlots; ++c)
+          if (v[c][k] != -INFINITY) s[c] += exp2_fast(v[c][k] - s_lse[k0 + k]);
     }
   }
-  if (holds) a.acc_out[slot] = was + s;
+#pragma unroll
+  for (int c = 0; c < kSlots; ++c)
+    if (i + c * 256 < x.n) a.acc_out[slot + c * 256] = was[c] + s[c];
 }
 
 // How a launch is cut: query rows of a softmax group, groups that share a tile's rows, row groups, CTAs.
@@ -1095,7 +1104,7 @@ int32_t launch_attend8(const gvote_params* p, const __nv_bfloat16* Q, int64_t q_
     GVOTE_LAUNCH_CHECK("attend8_merge_kernel");
     if (acc_out) {
       LaunchScope scope_("attend8_weights_kernel", st);
-      launch_behind(attend8_weights_kernel, dim3((unsigned)((c->total_tokens >> 8) + a.batch), a.Hkv), dim3(256), 0, st, a);
+      launch_behind(attend8_weights_kernel, dim3((unsigned)((c->total_tokens >> kSpanBits) + a.batch), a.Hkv), dim3(256), 0, st, a);
       GVOTE_LAUNCH_CHECK("attend8_weights_kernel");
     }
   }
