@@ -531,6 +531,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         tail->lse_at[qb][lane] = (int64_t)(x.q0 + token) * a.Hkv * a.G + head;
       }
       if (lane == 0) tail->entry[qb] = x;
+      if (at.seg > 1 && a.max_q > 1) {                                 // the marks of two segments ago have been read
+        for (int i = lane; i < L::kGroups * L::kNanWords; i += 32) nan_all[qb * L::kGroups * L::kNanWords + i] = 0;
+        if (lane < 4) tail->any_nan[qb][lane] = 0;
+      }
       if (at.seg == 0) {                                               // the softmax warps prepare the first one's rows
         asm volatile("barrier.cta.sync %0, %1;" ::"r"(kFirstQ), "r"(L::kThreads - 96) : "memory");
       } else {
@@ -578,11 +582,6 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
 #pragma unroll
       for (int g = 0; g < kR; ++g) { refd[g] = refn[g] = kNoRef; sum[g] = 0.f; }
       uint32_t* nan_sm = nan_all + (qb * L::kGroups + turn * kRb) * L::kNanWords;       // of the groups that share my tiles
-      if (rb == 0 && x.nq > 1) {                                       // (the marks of two segments ago have been read)
-        for (int i = key_in; i < kRb * L::kNanWords; i += 128) nan_sm[i] = 0;
-        if (key_in == 0) tail->any_nan[qb][turn] = 0;
-        group_any(bar_id, false);
-      }
       const int64_t sb0 = (int64_t)x.h * a.row_blocks + block8_offset(x.start, x.r);
       auto scales = [&](int t) {
         const int key = t * kTileKeys + key_in;
