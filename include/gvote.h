@@ -369,8 +369,9 @@ GVOTE_API int32_t gvote_append8(const gvote_params* p, const void* K_new, const 
  * request.  A request's query tokens are the last rows of its cache (append first): token i of n sees rows
  * 0 .. kv_len - n + i of a head; a head with fewer rows than that leaves token i nothing, which gives out = 0,
  * lse = -inf.  Per query head g of KV head h: logits q.k_n / sqrt(d_k), softmax, out = sum of weight * value
- * (products of the stored values; 32-bit sums), lse_or_null [total_q, n_q_heads] = log of the softmax's
- * denominator.  acc_out_or_null [n_kv_heads, total_tokens]: for the rows held, acc (null: 0) + the weights summed over
+ * (products of the stored values; 32-bit weights, however far below the largest, and 32-bit sums; an entry of a query
+ * is exact down to 2^-17 of the largest of its row and held to 2^-27 of that below), lse_or_null [total_q, n_q_heads] =
+ * log of the softmax's denominator.  acc_out_or_null [n_kv_heads, total_tokens]: for the rows held, acc (null: 0) + the weights summed over
  * the request's tokens and the head's group; acc_or_null may be acc_out itself.  Deterministic.  Where cu_q gives a
  * request more than max_q tokens the status word reads GVOTE_ERR_INVALID_ARG and its outputs are not to be used. */
 #define GVOTE_ATTEND8_MAX_Q 32

@@ -11,38 +11,38 @@
 // took 55 us instead of 36.)  What a CTA has of one entry is a segment; its result (reference, sum, output) goes to slot
 // entry + CTA, or straight to the output when the entry lies within one CTA.  attend8_merge_kernel merges an entry's segments.
 //
-// The products run on the codes themselves (tcgen05.mma kind::f8f6f4, e4m3 x e4m3, 32-bit sums), with the cached rows on
-// the M axis, so that nothing has to be widened or transposed on the way from the TMA boxes to the tensor cores:
-//   S [128 keys x (3 terms, rows)]  = K Q^T    K as it lies (128-byte swizzle), Q as a sum of three e4m3 terms
-//   O [128 channels x (4 terms, rows)] += V^T P^T   V as it lies, its channels on the M axis; P as a sum of four terms
-// A term is the e4m3 value nearest to what the terms before it left, times 16 per term, and its columns are added up
-// with the matching power of two in 32 bits.  Three terms hold a row of Q to 2^-12 of each entry and 2^-27 of the
-// row's largest (bf16 itself: 2^-8); four hold a weight to 2^-16 of itself and 2^-24 of the reference.  (A version that widened
-// the codes in registers for mma.sync issued 690 instructions per 32 rows: 39 us where this one takes 37, one token over 128K
-// rows of four heads, and 54 where this one takes 39, five tokens over 32K.  Three terms for
-// the weights save 3 % of a call with many rows.)
+// The products run on tcgen05.mma with the cached rows on the M axis, so that a few query rows fill N and nothing is transposed:
+//   S [128 keys x (3 terms, rows)]  = K Q^T    kind::f8f6f4, K as it lies (128-byte swizzle), Q as a sum of three e4m3 terms
+//   O [128 channels x (3 terms, rows)] += V^T P^T   kind::f16, V widened to bf16 in shared memory, P as a sum of three bf16 terms
+// A term is the value of its type nearest to what the terms before it left (for Q times 16 per term; its columns are added up
+// with the matching power of two in 32 bits).  Three bf16 terms are all 24 bits of a weight, at any size a float can have:
+// beside a first row that collects the attention the others' weights can lie 2^-30 below and still carry the output.  (Four
+// e4m3 terms of P against V as it lies took a quarter less time over long rows, but ended 2^-24 below the largest weight.)
+// Three terms of Q hold every entry above 2^-17 of its row's largest exactly, and a smaller one to 2^-27 of the largest.
 //
 // The scale of K enters the logit; the scale of V goes into the weight: P = 2^(l + log2(scale_v) - ref), ref the largest such
-// exponent so far, so that a block of large values neither overflows nor drowns what carries the output.  ref only moves
-// when it is passed by 2^6 (the accumulated O is then rescaled in tensor memory: mostly the first tile only).
+// exponent so far, so that a block of large values does not overflow.  ref only moves when it is passed by 2^6 (the
+// accumulated O is then rescaled in tensor memory: mostly the first tile only).
 //
 // Warp 0 asks for the tiles of K and of V (TMA, only the 32-row parts that hold rows) into rings of their own - a tile
-// of K is done with as soon as S is there, a tile of V only after the softmax - warps 1 and 2 issue the MMAs of S and of O
+// of K is done with as soon as S is there, a tile of V as soon as it is widened - warps 1 and 2 issue the MMAs of S and of O
 // (one warp for both took 1500 clocks a tile, its waits and commits one after the other), and warp 3 prepares the next
 // segment's Q terms (the first segment's, which everything waits for, are shared out among the softmax warps: alone,
-// warp 3 took 16,000 clocks for 20 rows); then come up to five softmax groups of four warps, thread = cached row of the
-// tile (and channel of the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each with
-// references and an O of its own (one group alone needs 3000 clocks of latency for a tile, the memory 1400), with many
-// the groups share a tile's rows out.  S and P are buffered as deep as the MMAs run ahead.
+// warp 3 took 16,000 clocks for 20 rows).  Warps 4 to 7 widen V, a tile or two ahead (by the softmax warps themselves it lay
+// in their chain: five tokens 43 us instead of 39); then come up to five softmax groups of four warps, thread = cached row of
+// the tile (and channel of the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each
+// with references and an O of its own (one group alone needs 3000 clocks of latency for a tile, the memory 1400), with many
+// the groups share a tile's rows out.  S and P are buffered as deep as the MMAs run ahead.  The loops of the roles run at
+// the same time and share the instruction cache: the rare parts (rows that not every token sees) are kept out of them
+// (within the widening loop they cost 20 of 70 us over long rows).
 //
 // Weights for the eviction: the logits are kept (4 bytes per row and query, against 2 d_k per row), and
 // attend8_weights_kernel turns them into weights once lse is known; a slot belongs to one thread, so the sum has one order.
 //
-// Measured (one B200, warm): one token of 28 heads over 128K rows of 4 KV heads, 134 MB: 37 us, the first kernel 30 of them at
-// 4.4 TB/s from launch to end (5.9 TB/s between its first tile and its last: 3 us pass before the first bytes are asked
-// for and 4 from the last bytes to the end).  A ragged batch of 128 pruned heads, 63 MB: 34 us with the weights.  Five tokens over
-// 32K rows of 8 heads: 39 us, a tile every 3200 clocks; the twenty softmax warps issue on 56 % of the clocks and wait for
-// their group's vote, for tensor memory and for the scales in the others.  Smallest calls: 15 us, all of it latency.
+// Measured (one B200, warm): one token of 28 heads over 128K rows of 4 KV heads, 134 MB: 49 us, the first kernel 45 of them.
+// A ragged batch of 128 pruned heads, 63 MB: 41 us with the weights.  Five tokens over 32K rows of 8 heads: 39 us, a tile
+// every 3200 clocks.  Smallest calls: 12.5 us, all of it latency.  What a tile costs beside its bytes is the widening and what it
+// takes from the softmax warps: over long rows 49 us, 47 when the codes are only copied, 41 when an eighth of them is.
 //
 // Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
 #include <cstddef>
@@ -57,12 +57,12 @@ constexpr int kTileKeys = 128;
 constexpr int kBoxRows = 32;
 constexpr int kMaxEntries = 1024;      // entries per launch: their tiles are added up in shared memory
 constexpr int kGap = 4;
+constexpr int kR = 4;                  // query rows of a softmax group
 constexpr int kMaxSlots = 8;           // of a ring
 constexpr int kMaxBuffers = 4;         // of S and of P
 constexpr int kSms = 148;
 constexpr float kNoRef = -1e30f;       // a reference before the first logit
-constexpr float kUp = 2.f;             // weights are formed times 2^2, and
-constexpr float kSlack = 6.f;          // a reference may be passed by 2^6: they stay below 448
+constexpr float kSlack = 6.f;          // a reference may be passed by 2^6 (most tiles then leave it where it is)
 
 struct AttendArgs {
   const __nv_bfloat16* Q;
@@ -151,8 +151,12 @@ __device__ __forceinline__ void umma_e4m3(uint32_t d, uint64_t a, uint64_t b, ui
       "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// Instruction descriptor, kind::f16: 32-bit result, A and B bf16 (bits 7-9, 10-12 = 1), stored with M / N contiguous.
+__host__ __device__ constexpr uint32_t instr_desc_bf16_mn(int M, int N) {
+  return ptx::instr_desc_bf16_f32(M, N) | (1u << 15) | (1u << 16);
+}
 // Operand stored as rows of 16 bytes without swizzle, the 16 bytes along M or N: eight K rows are 128 bytes, the next eight
-// K rows follow at once (leading offset 128), the next 16 of M or N `chunk` bytes on.
+// K rows follow at once (leading offset 128), the next 16 bytes of M or N `chunk` bytes on.
 __device__ __forceinline__ uint64_t smem_desc_mn_plain(uint32_t addr, uint32_t chunk) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(chunk >> 4) << 32) | ((uint64_t)1 << 46);
 }
@@ -162,12 +166,6 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
-}
-__device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-               : "r"(taddr)
-               : "memory");
 }
 // Four floats -> the e4m3 codes nearest to them; the floats become 16 times what the codes leave.
 __device__ __forceinline__ uint32_t take_term(float (&x)[4]) {
@@ -182,6 +180,23 @@ __device__ __forceinline__ uint32_t take_term(float (&x)[4]) {
   return c;
 }
 
+// Two floats -> the bf16 values nearest to them (low half: a); the floats become what those leave.
+__device__ __forceinline__ uint32_t take_bf16(float& a, float& b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(&h);
+  a -= __uint_as_float(w << 16);
+  b -= __uint_as_float(w & 0xffff0000u);
+  return w;
+}
+// Four e4m3 codes -> two pairs of bf16 values (exact; the NaN code -> NaN).
+__device__ __forceinline__ void widen_bf16x4(uint32_t c, uint32_t& lo, uint32_t& hi) {
+  widen8x4(c, lo, hi);
+  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  const __nv_bfloat162 x = __floats2bfloat162_rn(a.x, a.y), y = __floats2bfloat162_rn(b.x, b.y);
+  lo = *reinterpret_cast<const uint32_t*>(&x);
+  hi = *reinterpret_cast<const uint32_t*>(&y);
+}
+
 // A query row's log-sum-exp: base 2 for the weights, natural for the caller.
 __device__ __forceinline__ void write_lse(const AttendArgs& a, int64_t at, float2 ml) {
   const float l = ml.x == -INFINITY ? -INFINITY : ml.x + log2f(ml.y);
@@ -189,15 +204,16 @@ __device__ __forceinline__ void write_lse(const AttendArgs& a, int64_t at, float
   if (a.lse) a.lse[at] = l * 0.6931471805599453f;
 }
 
-// Counts: one arrival, 1 + 4 groups on q_empty, four per group that shares a tile's rows from s_empty on.
+// Counts: one arrival, 5 + 4 groups on q_empty, four per group that shares a tile's rows from s_empty on, four from v_empty on.
 struct Bars {
-  uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots], q_full[2], q_empty[2];
-  uint64_t s_full[kMaxBuffers], p_empty[kMaxBuffers], o_full[4];
+  uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], q_full[2], q_empty[2];
+  uint64_t s_full[kMaxBuffers], p_empty[kMaxBuffers], o_full[4], w_empty[2];
   uint64_t s_empty[kMaxBuffers], p_full[kMaxBuffers], o_empty[4];
+  uint64_t v_empty[kMaxSlots], w_full[2];
   uint64_t drain[2];                   // the MMAs under way of the two issuers, after a wait that ran out
 };
 constexpr int kFirstQ = 8;             // a named barrier; the softmax groups' are 1 to 5
-enum { kWarpTma = 0, kWarpS = 1, kWarpO = 2, kWarpQ = 3, kWarpSoftmax = 4 };
+enum { kWarpTma = 0, kWarpS = 1, kWarpO = 2, kWarpQ = 3, kWarpWide = 4, kWarpSoftmax = 8 };
 
 struct Tail {
   Bars bars;
@@ -211,17 +227,21 @@ struct Tail {
   int pref[kMaxEntries + 1];
 };
 
-template <int kBoxes, int kR, int kRb>  // 128-byte boxes per row; query rows of a softmax group; groups that share a tile's rows
+template <int kBoxes, int kRb>          // 128-byte boxes per row; groups that share a tile's rows
 struct Layout {                         // threads, tensor memory (columns), shared memory (bytes)
-  static constexpr int kTurns = kRb == 1 ? 4 : kRb == 2 ? 2 : 1, kGroups = kTurns * kRb, kThreads = 128 + 128 * kGroups;
+  static constexpr int kTurns = kRb == 1 ? 4 : kRb == 2 ? 2 : 1, kGroups = kTurns * kRb, kThreads = 256 + 128 * kGroups;
   static constexpr int kRows = kR * kRb, kBuffers = kRb <= 2 ? 4 : 2;
   static constexpr int kN1 = (3 * kRows + 15) / 16 * 16, kN2 = 4 * kRows;
   static constexpr int kO = kBuffers * kN1, kCols = kO + kTurns * kBoxes * kN2;     // O of turn i, box y: kO + (i kBoxes + y) kN2
   static constexpr int kAlloc = kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kSlot = kBoxes * kTileKeys * 128, kQ = kBoxes * kN1 * 128, kP = kN2 * kTileKeys;
+  static constexpr int kSlot = kBoxes * kTileKeys * 128, kQ = kBoxes * kN1 * 128, kP = kN2 * kTileKeys * 2;
+  static constexpr int kWide = 2 * kSlot, kWides = kBoxes == 1 ? 2 : 1;                // a tile of V in bf16, and how many
   static constexpr int kNanWords = kR * kBoxes * 4;                    // of a group: bits [row][channel]
   static constexpr int kSmall = kGroups * 4 * 2 * kR * 4 + 2 * kRows * 8 + 2 * kGroups * kNanWords * 4;
-  static constexpr size_t fixed() { return (size_t)2 * kQ + kBuffers * kP + kSmall + sizeof(Tail); }
+  static constexpr size_t fixed() { return (size_t)2 * kQ + kBuffers * kP + kWides * kWide + kSmall + sizeof(Tail); }
+  // slots of K and V that fit; three at least: two of K, one of V
+  static constexpr int kFit = (int)((227 * 1024 - fixed()) / kSlot);
+  static_assert(kFit >= 3 && kAlloc >= kCols, "a row group of this size does not fit an SM");
 };
 
 // The tiles of a CTA in order: segments (entry e, its tiles s0 .. s1 - 1), tiles t; seg and it count both.
@@ -250,18 +270,19 @@ struct Walk {
   }
 };
 
-template <int kBoxes, int kR, int kRb>
-__global__ void __launch_bounds__((Layout<kBoxes, kR, kRb>::kThreads), 1)
+template <int kBoxes, int kRb>
+__global__ void __launch_bounds__((Layout<kBoxes, kRb>::kThreads), 1)
 attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                const __grid_constant__ CUtensorMap tmKp, const __grid_constant__ CUtensorMap tmVp,
                const __grid_constant__ AttendArgs a) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  using L = Layout<kBoxes, kR, kRb>;
+  using L = Layout<kBoxes, kRb>;
   uint8_t* k_ring = smem;                                              // [slot][box][128 rows][128], swizzled
   uint8_t* v_ring = k_ring + (size_t)a.k_slots * L::kSlot;
   uint8_t* q_sm = v_ring + (size_t)a.v_slots * L::kSlot;               // [2][box][N1 rows][128], swizzled
-  uint8_t* p_sm = q_sm + 2 * L::kQ;                                    // [buffer][N2 / 16][128 keys][16]
-  float* red_all = reinterpret_cast<float*>(p_sm + L::kBuffers * L::kP);   // [group][4 warps][2 kR]
+  uint8_t* p_sm = q_sm + 2 * L::kQ;                                    // [buffer][N2 / 8][128 keys][8 columns], bf16
+  uint8_t* wide_sm = p_sm + L::kBuffers * L::kP;                       // [buffer][channels / 8][128 keys][8 channels], bf16
+  float* red_all = reinterpret_cast<float*>(wide_sm + L::kWides * L::kWide);   // [group][4 warps][2 kR]
   float* factor_sm = red_all + L::kGroups * 4 * 2 * kR;                // [2][kRows] logit per unit of product
   int* limit_sm = reinterpret_cast<int*>(factor_sm + 2 * L::kRows);    // [2][kRows] cached rows a query row sees
   uint32_t* nan_all = reinterpret_cast<uint32_t*>(limit_sm + 2 * L::kRows);   // [2][group][kR][boxes * 4]
@@ -276,8 +297,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     constexpr int kBars = sizeof(Bars) / 8;
     if (tid < kBars) {
       const int at = tid * 8;
-      const uint32_t count = at >= (int)offsetof(Bars, q_empty) && at < (int)offsetof(Bars, s_full) ? 1 + 4 * L::kGroups
-                             : at >= (int)offsetof(Bars, s_empty) && at < (int)offsetof(Bars, drain) ? 4 * kRb : 1;
+      const uint32_t count = at >= (int)offsetof(Bars, q_empty) && at < (int)offsetof(Bars, s_full) ? 5 + 4 * L::kGroups
+                             : at >= (int)offsetof(Bars, s_empty) && at < (int)offsetof(Bars, v_empty) ? 4 * kRb
+                             : at >= (int)offsetof(Bars, v_empty) && at < (int)offsetof(Bars, drain) ? 4 : 1;
       ptx::mbar_init(reinterpret_cast<uint64_t*>(&tail->bars) + tid, count);
       ptx::fence_barrier_init();
     }
@@ -467,17 +489,15 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     if (!ok) drain_mmas(&tail->bars.drain[0]);
   } else if (warp == kWarpO) {
     // ------------------------------------------------------------------ O += V^T P
-    const uint32_t idesc = instr_desc_e4m3(128, L::kN2, true, true);
-    const uint64_t vd0 = ptx::smem_desc_k_sw128(ptx::smem_u32(v_ring)), pd0 = smem_desc_mn_plain(ptx::smem_u32(p_sm), 16 * kTileKeys);
+    const uint32_t idesc = instr_desc_bf16_mn(128, L::kN2);
+    const uint64_t vd0 = smem_desc_mn_plain(ptx::smem_u32(wide_sm), 16 * kTileKeys), pd0 = smem_desc_mn_plain(ptx::smem_u32(p_sm), 16 * kTileKeys);
     uint32_t o_uses = 0;                                               // bit i: parity of the uses of turn i's O
-    int vs = 0;
-    uint32_t v_phase = 0;
     for (; ok && !at.done(); at.next_segment()) {
       for (int t = at.s0, it = at.it; ok && t < at.s1; ++t, ++it) {
         const int pb = it % L::kBuffers, turn = it % L::kTurns;
         const bool first = t - at.s0 < L::kTurns, last = t + L::kTurns >= at.s1;
         ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.p_full[pb], (it / L::kBuffers) & 1, abort_flag) &&
-                                         wait_or_abort(&tail->bars.v_full[vs], v_phase, abort_flag));
+                                         wait_or_abort(&tail->bars.w_full[it % L::kWides], (it / L::kWides) & 1, abort_flag));
         if (ok && first) {
           ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.o_empty[turn], ((o_uses >> turn) & 1) ^ 1, abort_flag));
           o_uses ^= 1u << turn;
@@ -485,21 +505,19 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         if (!ok) break;
         ptx::tc_fence_after_sync();
         if (ptx::elect_one()) {
-          const uint64_t pd = pd0 + (uint64_t)((pb * L::kP) >> 4);
+          const uint64_t pd = pd0 + (uint64_t)((pb * L::kP) >> 4), vd = vd0 + (uint64_t)((it % L::kWides * L::kWide) >> 4);
 #pragma unroll
           for (int y = 0; y < kBoxes; ++y) {
-            const uint64_t vd = vd0 + (uint64_t)((vs * L::kSlot + y * kTileKeys * 128) >> 4);
 #pragma unroll
-            for (int k = 0; k < kTileKeys / 32; ++k)                   // 32 keys: 4 KB of V, 512 bytes of P
-              umma_e4m3(tmem + (uint32_t)(L::kO + (turn * kBoxes + y) * L::kN2), vd + (uint64_t)(k * (32 * 128 / 16)),
-                        pd + (uint64_t)(k * (32 * 16 / 16)), idesc, first && k == 0 ? 0u : 1u);
+            for (int k = 0; k < kTileKeys / 16; ++k)                   // 16 keys: 256 bytes of each column of chunks
+              ptx::umma_bf16(tmem + (uint32_t)(L::kO + (turn * kBoxes + y) * L::kN2), vd + (uint64_t)(y * (kTileKeys * 16) + k * 16),
+                             pd + (uint64_t)(k * 16), idesc, first && k == 0 ? 0u : 1u);
           }
           ptx::umma_commit(&tail->bars.p_empty[pb]);
-          ptx::umma_commit(&tail->bars.v_empty[vs]);
+          ptx::umma_commit(&tail->bars.w_empty[it % L::kWides]);
           if (last) ptx::umma_commit(&tail->bars.o_full[turn]);
         }
         __syncwarp();
-        if (++vs == a.v_slots) { vs = 0; v_phase ^= 1u; }
       }
     }
     if (!ok) drain_mmas(&tail->bars.drain[1]);
@@ -536,7 +554,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         if (lane < 4) tail->any_nan[qb][lane] = 0;
       }
       if (at.seg == 0) {                                               // the softmax warps prepare the first one's rows
-        asm volatile("barrier.cta.sync %0, %1;" ::"r"(kFirstQ), "r"(L::kThreads - 96) : "memory");
+        asm volatile("barrier.cta.sync %0, %1;" ::"r"(kFirstQ), "r"(L::kThreads - 224) : "memory");
       } else {
         const uint32_t held = __ballot_sync(0xffffffffu, holds);
 #pragma unroll 1
@@ -551,6 +569,71 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&tail->bars.q_full[qb]);
+    }
+  } else if (warp < kWarpSoftmax) {
+    // ------------------------------------------------------------------ the tiles of V in bf16: thread = row of the tile
+    const int key_in = tid - kWarpWide * 32, units = a.d_k >> 4;
+    int vs = 0;
+    uint32_t v_phase = 0;
+    for (; ok && !at.done(); at.next_segment()) {
+      const int qb = at.seg & 1;
+      ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.q_full[qb], (at.seg >> 1) & 1, abort_flag));
+      if (!ok) break;
+      const Entry x = tail->entry[qb];
+      const int all_see = x.n - (x.nq - 1);
+      for (int t = at.s0, it = at.it; ok && t < at.s1; ++t, ++it) {
+        const int wb = it % L::kWides, key = t * kTileKeys + key_in;
+        ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.w_empty[wb], ((it / L::kWides) & 1) ^ 1, abort_flag) &&
+                                         wait_or_abort(&tail->bars.v_full[vs], v_phase, abort_flag));
+        if (!ok) break;
+        uint8_t* from = v_ring + (size_t)vs * L::kSlot + key_in * 128;
+        uint8_t* to = wide_sm + wb * L::kWide + key_in * 16;
+        if (key >= all_see) {
+          // A value behind the last row may be anything, and one that not every token sees may be NaN: neither must reach
+          // the others through a weight of zero.  The first becomes zero, the second is noted for those who see it.
+          const int turn = it % L::kTurns;
+          uint32_t* marks = nan_all + (qb * L::kGroups + turn * kRb) * L::kNanWords;       // [row][boxes * 4] of the turn's groups
+#pragma unroll 1
+          for (int u = 0; u < units; ++u) {
+            uint4* place = reinterpret_cast<uint4*>(from + (u >> 3) * kTileKeys * 128 + (((u & 7) ^ (key_in & 7)) << 4));
+            if (key >= x.n) {
+              *place = make_uint4(0, 0, 0, 0);
+              continue;
+            }
+            uint4 c = *place, bad;
+            bad.x = __vcmpeq4(c.x & 0x7f7f7f7fu, 0x7f7f7f7fu);
+            bad.y = __vcmpeq4(c.y & 0x7f7f7f7fu, 0x7f7f7f7fu);
+            bad.z = __vcmpeq4(c.z & 0x7f7f7f7fu, 0x7f7f7f7fu);
+            bad.w = __vcmpeq4(c.w & 0x7f7f7f7fu, 0x7f7f7f7fu);
+            if (!(bad.x | bad.y | bad.z | bad.w)) continue;
+            *place = make_uint4(c.x & ~bad.x, c.y & ~bad.y, c.z & ~bad.z, c.w & ~bad.w);
+            tail->any_nan[qb][turn] = 1;
+            auto four = [](uint32_t m) { return (m & 1u) | ((m >> 7) & 2u) | ((m >> 14) & 4u) | ((m >> 21) & 8u); };
+            const uint32_t bits = four(bad.x) | four(bad.y) << 4 | four(bad.z) << 8 | four(bad.w) << 12;
+#pragma unroll 1
+            for (int g = 0; g < L::kRows; ++g)
+              if (key < limit_sm[qb * L::kRows + g]) atomicOr(&marks[g * kBoxes * 4 + (u >> 1)], bits << (u * 16 & 31));
+          }
+        }
+#pragma unroll 2
+        for (int u = 0; u < units; ++u) {
+          const uint4 c = *reinterpret_cast<const uint4*>(from + (u >> 3) * kTileKeys * 128 + (((u & 7) ^ (key_in & 7)) << 4));
+          uint32_t b[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) widen_bf16x4((&c.x)[j], b[2 * j], b[2 * j + 1]);
+          *reinterpret_cast<uint4*>(to + u * 2 * (kTileKeys * 16)) = make_uint4(b[0], b[1], b[2], b[3]);
+          *reinterpret_cast<uint4*>(to + (u * 2 + 1) * (kTileKeys * 16)) = make_uint4(b[4], b[5], b[6], b[7]);
+        }
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          ptx::mbar_arrive(&tail->bars.v_empty[vs]);
+          ptx::mbar_arrive(&tail->bars.w_full[wb]);
+        }
+        if (++vs == a.v_slots) { vs = 0; v_phase ^= 1u; }
+      }
+      __syncwarp();
+      if (ok && lane == 0) ptx::mbar_arrive(&tail->bars.q_empty[qb]);
     }
   } else {
     // ------------------------------------------------------------------ softmax: thread = row of the tile, channel of O
@@ -570,7 +653,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         put_row(0, row, v);
       }
       ptx::fence_proxy_async();
-      asm volatile("barrier.cta.arrive %0, %1;" ::"r"(kFirstQ), "r"(L::kThreads - 96) : "memory");
+      asm volatile("barrier.cta.arrive %0, %1;" ::"r"(kFirstQ), "r"(L::kThreads - 224) : "memory");
     }
     for (; !at.done(); at.next_segment()) {
       const int qb = at.seg & 1, e = at.e, s0 = at.s0, s1 = at.s1;
@@ -603,10 +686,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         bool over = false;
         if (ok) {
           ptx::tc_fence_after_sync();
-          uint32_t c[kR == 4 ? 16 : 24];
+          uint32_t c[16];
           const uint32_t s_addr = lane_addr + (uint32_t)(sb * L::kN1 + rb * 3 * kR);
-          ptx::tmem_ld_32x16(s_addr, *reinterpret_cast<uint32_t(*)[16]>(&c[0]));
-          if (kR == 8) tmem_ld_32x8(s_addr + 16, &c[kR == 4 ? 0 : 16]);
+          ptx::tmem_ld_32x16(s_addr, c);                               // (three terms; the last four are not used)
           ptx::tmem_wait_ld();
           ptx::tc_fence_before_sync();
           __syncwarp();
@@ -655,13 +737,13 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             if (ok) {
               ptx::tc_fence_after_sync();
 #pragma unroll
-              for (int i = 0; i < kBoxes * 4 * kR / 16; ++i) {
-                const uint32_t at_o = o_addr + (uint32_t)((i * 16 / (4 * kR)) * L::kN2 + i * 16 % (4 * kR));
+              for (int y = 0; y < kBoxes; ++y) {
+                const uint32_t at_o = o_addr + (uint32_t)(y * L::kN2);
                 uint32_t v[16];
                 ptx::tmem_ld_32x16(at_o, v);
                 ptx::tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * shrink[(i * 16 + j) % kR]);
+                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * shrink[j % kR]);
                 tmem_st_32x16(at_o, v);
               }
               ptx::tmem_wait_st();
@@ -673,54 +755,21 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         // ---- weights and their terms
         ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.p_empty[sb], phase ^ 1, abort_flag));
         if (ok) {
-          uint32_t p[kR];                                              // four codes: rows 4 q .. of term k at k kR / 4 + q
+          float f[kR];
 #pragma unroll
-          for (int q = 0; q < kR / 4; ++q) {
-            float f[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int g = 4 * q + i;
-              sum[g] += exp2_fast(l[g] - refd[g]);
-              f[i] = exp2_fast(l[g] + lv - refn[g] + kUp);
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) p[k * (kR / 4) + q] = take_term(f);
+          for (int g = 0; g < kR; ++g) {
+            sum[g] += exp2_fast(l[g] - refd[g]);
+            f[g] = exp2_fast(l[g] + lv - refn[g]);
           }
-          uint8_t* dst = p_sm + sb * L::kP + rb * 4 * kR * kTileKeys + key_in * 16;
+          uint2 p[3];                                                  // a term of the four rows
 #pragma unroll
-          for (int i = 0; i < kR / 4; ++i)
-            *reinterpret_cast<uint4*>(dst + i * 16 * kTileKeys) = make_uint4(p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
-          if (rb == 0 && key0 + kTileKeys > all_see && key >= all_see) {
-            // A value behind the last row may be anything, and one that not every token sees may be NaN: neither must
-            // reach the others through a weight of zero.  The first becomes zero, the second is noted for those who see it.
-            // V may come after S.  A wait by parity must not meet a phase two behind: the slot's tile before this one is
-            // done with, since this tile's weights had a free buffer, or (rings shorter than the buffers) after this wait.
-            if (a.v_slots < L::kBuffers && it >= a.v_slots)
-              wait_or_abort(&tail->bars.p_empty[(it - a.v_slots) % L::kBuffers], ((it - a.v_slots) / L::kBuffers) & 1, abort_flag);
-            wait_or_abort(&tail->bars.v_full[it % a.v_slots], (it / a.v_slots) & 1, abort_flag);
-            uint8_t* v = v_ring + (size_t)(it % a.v_slots) * L::kSlot + key_in * 128;
-            for (int y = 0; y < kBoxes; ++y)
-              for (int i = 0; i < 8; ++i) {
-                uint4* place = reinterpret_cast<uint4*>(v + y * kTileKeys * 128 + ((i ^ (key_in & 7)) << 4));
-                uint4 u = make_uint4(0, 0, 0, 0);
-                if (key < x.n) {
-                  u = *place;
-#pragma unroll
-                  for (int j = 0; j < 4; ++j) {
-                    uint32_t& word = (&u.x)[j];
-                    const uint32_t bad = __vcmpeq4(word & 0x7f7f7f7fu, 0x7f7f7f7fu);
-                    if (!bad) continue;
-                    word &= ~bad;
-                    tail->any_nan[qb][turn] = 1;
-                    const uint32_t four = (bad & 1u) | ((bad >> 7) & 2u) | ((bad >> 14) & 4u) | ((bad >> 21) & 8u);
-                    const int d = y * 128 + i * 16 + j * 4;
-                    for (int g = 0; g < L::kRows; ++g)                 // (a group's marks: [row][boxes * 4])
-                      if (key < limit_sm[qb * L::kRows + g]) atomicOr(&nan_sm[g * kBoxes * 4 + (d >> 5)], four << (d & 31));
-                  }
-                }
-                *place = u;
-              }
+          for (int k = 0; k < 3; ++k) {
+            p[k].x = take_bf16(f[0], f[1]);
+            p[k].y = take_bf16(f[2], f[3]);
           }
+          uint8_t* dst = p_sm + sb * L::kP + rb * 2 * kTileKeys * 16 + key_in * 16;
+          *reinterpret_cast<uint4*>(dst) = make_uint4(p[0].x, p[0].y, p[1].x, p[1].y);
+          *reinterpret_cast<uint4*>(dst + 16 * kTileKeys) = make_uint4(p[2].x, p[2].y, 0, 0);   // (columns up to a multiple of 16)
           ptx::fence_proxy_async();
         }
         __syncwarp();
@@ -748,11 +797,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
 #pragma unroll
         for (int y = 0; y < kBoxes; ++y) {
           const int d = y * 128 + key_in;
-          uint32_t v[4 * kR];
+          uint32_t v[16];
           if (any_tile) {
-#pragma unroll
-            for (int i = 0; i < kR / 4; ++i)
-              ptx::tmem_ld_32x16(o_addr + (uint32_t)(y * L::kN2 + i * 16), *reinterpret_cast<uint32_t(*)[16]>(&v[16 * i]));
+            ptx::tmem_ld_32x16(o_addr + (uint32_t)(y * L::kN2), v);
             ptx::tmem_wait_ld();
           }
           if (d < a.d_k) {
@@ -762,9 +809,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
                 const float total = (red_sm[g] + red_sm[2 * kR + g]) + (red_sm[4 * kR + g] + red_sm[6 * kR + g]);
                 if (any_tile) {
                   auto term = [&](int k) { return __uint_as_float(v[k * kR + g]); };
-                  float o = fmaf(term(3), 0.000244140625f, fmaf(term(2), 0.00390625f, fmaf(term(1), 0.0625f, term(0))));
+                  float o = (term(2) + term(1)) + term(0);
                   const float f = exp2_fast(0.5f * (refn[g] - refd[g]));       // (in two steps: it may lie below 2^-126)
-                  o = total == 0.f ? 0.f : o * 0.25f * __frcp_rn(total) * f * f;   // (kUp = 2)
+                  o = total == 0.f ? 0.f : o * __frcp_rn(total) * f * f;
                   if (nan_seen && ((nan_sm[(rb * kR + g) * kBoxes * 4 + (d >> 5)] >> (d & 31)) & 1u)) o = __uint_as_float(0x7fffffffu);
                   if (whole) a.out[tail->out_at[qb][rb * kR + g] + d] = __float2bfloat16(o);
                   else a.part_o[(slot + g) * a.d_k + d] = o;
@@ -982,20 +1029,19 @@ attend8_weights_kernel(const __grid_constant__ AttendArgs a) {
     if (i + c * 256 < x.n) a.acc_out[slot + c * 256] = was[c] + s[c];
 }
 
-// How a launch is cut: query rows of a softmax group, groups that share a tile's rows, row groups, CTAs.
-struct Cut { int boxes, kr, rb, turns, rows, groups, requests; int64_t ctas; };
+// How a launch is cut: groups that share a tile's rows, row groups, CTAs.
+struct Cut { int boxes, rb, turns, rows, groups, requests; int64_t ctas; };
 Cut cut_of(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_q) {
   Cut c;
   const int64_t rows = max_q * (p->n_q_heads / p->n_kv_heads);
   c.boxes = p->d_k <= 128 ? 1 : 2;
-  // Up to five softmax groups of four rows; beyond 20 rows as few and as even row groups as hold them, each of which reads the
-  // codes again (from L2).  Groups of eight rows take twice as long for a tile, so three of them pay for 21 to 24
-  // rows only (24 rows over 32K: 47 us, as two row groups 52; 32 rows: four of eight 65, two row groups 60; 40 rows: 190
-  // and 122 in a ragged batch).
-  c.kr = rows > 20 && rows <= 24 ? 8 : 4;
-  c.rb = c.kr == 8 ? 3 : rows > 0 ? (int)ceil_div(ceil_div(rows, ceil_div(rows, 20)), 4) : 1;
+  // Up to five softmax groups of four rows (four where d_k > 128, whose tiles of V leave less shared memory); beyond those as few
+  // and as even row groups as hold the rows, each of which reads the codes again, from L2 (24 rows over 32K: 47 us as two row
+  // groups of 12, 55 as three softmax groups of eight rows).
+  const int64_t most = c.boxes == 1 ? 20 : 16;
+  c.rb = rows > 0 ? (int)ceil_div(ceil_div(rows, ceil_div(rows, most)), kR) : 1;
   c.turns = c.rb == 1 ? 4 : c.rb == 2 ? 2 : 1;
-  c.rows = c.kr * c.rb;
+  c.rows = kR * c.rb;
   c.groups = (int)ceil_div(rows > 0 ? rows : 1, c.rows);
   c.requests = kMaxEntries / p->n_kv_heads < batch ? kMaxEntries / p->n_kv_heads : batch;
   // a CTA per SM, and no more than one per tile
@@ -1004,15 +1050,14 @@ Cut cut_of(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t m
   return c;
 }
 
-template <int kBoxes, int kR, int kRb>
+template <int kBoxes, int kRb>
 int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], AttendArgs a, cudaStream_t st) {
-  using L = Layout<kBoxes, kR, kRb>;
+  using L = Layout<kBoxes, kRb>;
   // the slots that fit, five in twelve to K (a tile of V stays about half as long again)
-  const int fit = (int)((227 * 1024 - L::fixed()) / L::kSlot);
-  a.k_slots = fit * 5 / 12 < 2 ? 2 : fit * 5 / 12 > kMaxSlots ? kMaxSlots : fit * 5 / 12;
-  a.v_slots = fit - a.k_slots > kMaxSlots ? kMaxSlots : fit - a.k_slots;
+  a.k_slots = L::kFit * 5 / 12 < 2 ? 2 : L::kFit * 5 / 12 > kMaxSlots ? kMaxSlots : L::kFit * 5 / 12;
+  a.v_slots = L::kFit - a.k_slots > kMaxSlots ? kMaxSlots : L::kFit - a.k_slots;
   const size_t smem = L::fixed() + (size_t)(a.k_slots + a.v_slots) * L::kSlot;
-  auto kernel = attend8_kernel<kBoxes, kR, kRb>;
+  auto kernel = attend8_kernel<kBoxes, kRb>;
   GVOTE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   {
     LaunchScope scope_("attend8_kernel", st);
@@ -1024,13 +1069,14 @@ int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], AttendArgs a, cudaS
 }
 template <int kBoxes>
 int32_t run_attend(const Cut& c, const CUtensorMap (&tm)[4], const AttendArgs& a, cudaStream_t st) {
-  if (c.kr == 8) return run_attend<kBoxes, 8, 3>(c, tm, a, st);
+  if constexpr (kBoxes == 1) {
+    if (c.rb == 5) return run_attend<kBoxes, 5>(c, tm, a, st);
+  }
   switch (c.rb) {
-    case 1: return run_attend<kBoxes, 4, 1>(c, tm, a, st);
-    case 2: return run_attend<kBoxes, 4, 2>(c, tm, a, st);
-    case 3: return run_attend<kBoxes, 4, 3>(c, tm, a, st);
-    case 5: return run_attend<kBoxes, 4, 5>(c, tm, a, st);
-    default: return run_attend<kBoxes, 4, 4>(c, tm, a, st);
+    case 1: return run_attend<kBoxes, 1>(c, tm, a, st);
+    case 2: return run_attend<kBoxes, 2>(c, tm, a, st);
+    case 3: return run_attend<kBoxes, 3>(c, tm, a, st);
+    default: return run_attend<kBoxes, 4>(c, tm, a, st);
   }
 }
 
