@@ -595,10 +595,11 @@ accumulate_sum_kernel(const __grid_constant__ AccArgs a) {
 }
 
 // Tokens of a query tile: as many as 128 rows hold, fewer where the longest request's tokens can then be dealt out evenly
-// (32 tokens of 7 heads are two tiles of 16 rather than 18 and 14: the last tile needs no mask).
-int tile_tokens(const gvote_params* p, int64_t max_q) {
+// (32 tokens of 7 heads are two tiles of 16 rather than 18 and 14: the last tile needs no mask).  Not where the list holds more
+// tokens than the batch can have (requests behind others, by a view of the boundaries): there is a tile for each of them.
+int tile_tokens(const gvote_params* p, int32_t batch, int64_t total_q, int64_t max_q) {
   const int64_t most = kTile / (p->n_q_heads / p->n_kv_heads);
-  if (max_q <= 0) return (int)most;
+  if (max_q <= 0 || total_q > batch * max_q) return (int)most;
   return (int)ceil_div(max_q, ceil_div(max_q, most));
 }
 
@@ -619,9 +620,9 @@ int64_t chunk_count(int64_t units, int64_t tiles, bool even) {
 AccumulateMap accumulate_map(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N, int64_t total_q,
                              int64_t max_q) {
   AccumulateMap m;
-  m.tpt = tile_tokens(p, max_q);
+  m.tpt = tile_tokens(p, batch, total_q, max_q);
   const int64_t tpt = m.tpt;
-  m.q_tiles = total_q / tpt + batch;
+  m.q_tiles = list_length(total_q, tpt, batch);
   m.key_chunks = chunk_count(list_length(total_q, 2 * tpt, batch) * p->n_kv_heads, ceil_div(max_N, kTile),
                              batch == 1 && max_q <= max_N / 8);
   m.q_chunks = chunk_count(list_length(total_tokens, 2 * kTile, batch) * p->n_kv_heads, ceil_div(max_q, tpt), false);
@@ -635,10 +636,11 @@ AccumulateMap accumulate_map(const gvote_params* p, int32_t batch, int64_t total
 }
 
 // What any call of no larger sizes needs.  A smaller one may be cut into more chunks: the units of a pass with chunks are no
-// more than those without and kUnitsPerSm per SM besides, of two tiles each.
+// more than those without and kUnitsPerSm per SM besides, of two tiles each (of two at most: as many pairs as units are
+// listed, ceil(n / 2) pairs for n tiles).
 size_t accumulate_workspace(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t total_q) {
   const int64_t most = kTile / (p->n_q_heads / p->n_kv_heads), Hkv = p->n_kv_heads, units = kUnitsPerSm * kSms;
-  // a tile holds half of what it could at least, or a request's every token
+  // a tile holds half of what it could at least, or a request's every token and there are two tiles a request at most
   const int64_t rows = Hkv * (2 * total_q / most + 2 * (int64_t)batch + 2) * kTile;
   const int64_t p1 = (units * 2 * kTile + 2 * rows) * 8, p2 = (units * 2 * kTile + 2 * Hkv * total_tokens) * 4;
   return kStatusBytes + (size_t)rows * 4 + (size_t)(p1 > p2 ? p1 : p2) + 1024;
