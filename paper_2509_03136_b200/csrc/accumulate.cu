@@ -129,10 +129,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 
 // 2^x for a pair, x <= 127, without the special-function unit: x = i + f with i the nearest integer (read off the low bits
 // of x + 1.5 * 2^23 + 127, which are i + 127), 2^f by the polynomial of degree 5 with the smallest largest relative error
-// on [-1/2, 1/2] (Remez exchange; 7.5e-8, 2.1e-7 in 32 bits).  Below 2^-126 the result is 2^-126; a NaN stays one.
+// on [-1/2, 1/2] (Remez exchange; 1.5e-7 with the coefficients as they are rounded here, 2.1e-7 in 32 bits).  x is taken to
+// -127 at least, where the power that i gives is zero: what lies below 2^-126.5 is zero, -inf too; a NaN stays one.
 __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
   float2 x = unpack2(x2);
-  x2 = pack2(max_nan(x.x, -126.f), max_nan(x.y, -126.f));
+  x2 = pack2(max_nan(x.x, -127.f), max_nan(x.y, -127.f));
   const uint64_t r2 = add2(x2, pack2(12583039.f, 12583039.f));
   const uint64_t i2 = add2(r2, pack2(-12583039.f, -12583039.f));
   const uint64_t f2 = fma2(i2, pack2(-1.f, -1.f), x2);
