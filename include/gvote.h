@@ -386,7 +386,9 @@ GVOTE_API int32_t gvote_attend8(const gvote_params* p, const void* Q, int64_t q_
  * its last tokens.  acc_out [n_kv_heads, total_tokens]: for the rows that count, acc (null: 0) + the softmax weights
  * summed over the tokens and over the head's group; other entries are left as they were.
  * lse_or_null [total_q, n_q_heads]: the logarithm of each query's softmax denominator over the keys it sees, when
- * the prompt's attention has left it (-inf where it sees none); computed here otherwise.  Deterministic. */
+ * the prompt's attention has left it (-inf where it sees none); computed here otherwise.  Deterministic.
+ * Weights below 2^-126 are zero.  A key that holds an infinity may get NaN also where every logit with it is -inf (query
+ * tiles have empty rows, and zero times an infinity is no number); no other key is touched by it. */
 GVOTE_API int32_t gvote_accumulate(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride,
                          const int32_t* cu_q, int64_t total_q, int64_t max_q, const void* K, int64_t k_tok_stride,
                          int64_t k_head_stride, const int32_t* cu_seqlens, const int32_t* kv_len_or_null,
