@@ -345,8 +345,9 @@ GVOTE_API int32_t gvote_store8(const gvote_params* p, const void* K, const void*
                      const float* acc_or_null, float* acc_out_or_null, const int32_t* token_pos_or_null,
                      int32_t* token_pos_out_or_null, void* ws, size_t ws_bytes, void* stream);
 
-/* The same from one 8-bit cache into another (the buffers must not overlap): the kept rows of `src`, scaled
- * anew block by block. */
+/* The same from one 8-bit cache into another: the kept rows of `src`, scaled anew block by block.  Here and in
+ * gvote_store8 what is read must not share a byte with what is written (GVOTE_ERR_INVALID_ARG).  Rows of the same strides may
+ * lie between each other, as windows of one wider buffer; with strides that differ the extents must be apart. */
 GVOTE_API int32_t gvote_prune8(const gvote_params* p, const gvote_cache8* src, const uint32_t* mask_or_null,
                      const gvote_cache8* dst, const float* acc_or_null, float* acc_out_or_null,
                      const int32_t* token_pos_or_null, int32_t* token_pos_out_or_null,

@@ -32,7 +32,50 @@ int32_t validate_cache(const gvote_params* p, const gvote_cache8* c) {
 
 bool rows_aligned(int64_t tok, int64_t head, int d_k) { return tok >= d_k && tok % 8 == 0 && head % 8 == 0; }
 
-bool overlap(const void* a, const void* b) { return a == b; }
+// Where `heads` x `rows` pieces of `width` bytes lie, at these strides in bytes.
+struct Extent {
+  int64_t at, head, tok, heads, rows, width;
+  int64_t lo() const { return at + (head < 0 ? (heads - 1) * head : 0); }
+  int64_t hi() const { return at + (head > 0 ? (heads - 1) * head : 0) + (rows - 1) * tok + width; }
+};
+Extent extent(const void* p, int64_t heads, int64_t head, int64_t rows, int64_t tok, int64_t width) {
+  return {(int64_t)reinterpret_cast<uintptr_t>(p), heads > 1 ? head : 0, tok, heads, rows, width};
+}
+Extent whole(const void* p, int64_t bytes) { return extent(p, 1, 0, 1, 0, bytes); }
+
+// Whether two arrays share a byte.  Rows of the same strides may lie between each other (windows of one wider buffer): for
+// every distance between heads, the row of b nearest to the start of a row of a, and the one before it, are looked at.  Where
+// the strides differ a common extent counts as shared.
+bool overlap(const Extent& a, const Extent& b) {
+  if (!a.at || !b.at || a.heads < 1 || b.heads < 1 || a.rows < 1 || b.rows < 1 || a.width < 1 || b.width < 1) return false;
+  if (a.hi() <= b.lo() || b.hi() <= a.lo()) return false;
+  const int64_t tok = a.rows > 1 ? a.tok : b.rows > 1 ? b.tok : a.width;
+  if (a.head != b.head || (b.rows > 1 && tok != b.tok) || a.heads != b.heads || a.width != b.width || tok < 1) return true;
+  for (int64_t dh = 1 - a.heads; dh < a.heads; ++dh) {
+    const int64_t apart = b.at - a.at + dh * a.head;                   // plus a multiple of tok: between 1 - a.rows and b.rows - 1 rows
+    const int64_t down = apart >= 0 ? -(apart / tok) : (-apart + tok - 1) / tok;
+    for (int64_t dt = down - 1; dt <= down; ++dt) {
+      const int64_t off = apart + dt * tok;
+      if (dt > -a.rows && dt < b.rows && off < a.width && -off < a.width) return true;
+    }
+  }
+  return false;
+}
+
+Extent codes_of(const gvote_params* p, const gvote_cache8* c, const void* t) {
+  return extent(t, p->n_kv_heads, c->head_stride, c->total_tokens, c->tok_stride, p->d_k);
+}
+Extent scales_of(const gvote_params* p, const gvote_cache8* c, const void* t) {
+  return whole(t, 4 * (int64_t)p->n_kv_heads * gvote_cache8_row_blocks(c->total_tokens, c->batch));
+}
+Extent lens_of(const gvote_params* p, int32_t batch, const void* t) { return whole(t, 4 * (int64_t)batch * p->n_kv_heads); }
+Extent slots_of(const gvote_params* p, int64_t total, const void* t) { return whole(t, 4 * (int64_t)p->n_kv_heads * total); }
+
+// What a call reads of K and V (the same strides) must not lie in the codes it writes.
+bool codes_overlap(const gvote_params* p, const Extent& K, const Extent& V, const gvote_cache8* dst) {
+  const Extent a = codes_of(p, dst, dst->K), b = codes_of(p, dst, dst->V);
+  return overlap(K, a) || overlap(K, b) || overlap(V, a) || overlap(V, b);
+}
 
 int64_t larger(int64_t a, int64_t b) { return a > b ? a : b; }
 
@@ -69,10 +112,12 @@ int32_t gvote_store8(const gvote_params* p, const void* K, const void* V, int64_
   OPTIONAL_PTR(mask_or_null); OPTIONAL_PTR(kv_len_or_null); OPTIONAL_PTR(acc_or_null); OPTIONAL_PTR(acc_out_or_null);
   OPTIONAL_PTR(token_pos_or_null); OPTIONAL_PTR(token_pos_out_or_null);
   if (!acc_or_null != !acc_out_or_null || (token_pos_or_null && !token_pos_out_or_null)) return GVOTE_ERR_INVALID_ARG;
-  if (overlap(acc_or_null, acc_out_or_null) && acc_or_null) return GVOTE_ERR_INVALID_ARG;
-  if (overlap(token_pos_or_null, token_pos_out_or_null) && token_pos_or_null) return GVOTE_ERR_INVALID_ARG;
-  if (kv_len_or_null == cache->kv_len) return GVOTE_ERR_INVALID_ARG;
   if (!rows_aligned(tok_stride, head_stride, p->d_k)) return GVOTE_ERR_UNALIGNED;
+  if (overlap(slots_of(p, total_tokens, acc_or_null), slots_of(p, cache->total_tokens, acc_out_or_null)) ||
+      overlap(slots_of(p, total_tokens, token_pos_or_null), slots_of(p, cache->total_tokens, token_pos_out_or_null)) ||
+      overlap(lens_of(p, batch, kv_len_or_null), lens_of(p, batch, cache->kv_len))) return GVOTE_ERR_INVALID_ARG;
+  if (codes_overlap(p, extent(K, p->n_kv_heads, 2 * head_stride, total_tokens, 2 * tok_stride, 2 * p->d_k),
+                    extent(V, p->n_kv_heads, 2 * head_stride, total_tokens, 2 * tok_stride, 2 * p->d_k), cache)) return GVOTE_ERR_INVALID_ARG;
   if (ws_bytes < store8_map(p, batch, larger(total_tokens, cache->total_tokens)).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
   const SideArrays side{acc_or_null, acc_out_or_null, token_pos_or_null, token_pos_out_or_null};
   return launch_store8(p, (const __nv_bfloat16*)K, (const __nv_bfloat16*)V, tok_stride, head_stride, nullptr, mask_or_null,
@@ -86,13 +131,17 @@ int32_t gvote_prune8(const gvote_params* p, const gvote_cache8* src, const uint3
   PROPAGATE(validate_cache(p, src));
   PROPAGATE(validate_cache(p, dst));
   if (src->batch != dst->batch) return GVOTE_ERR_INVALID_ARG;
-  if (overlap(src->K, dst->K) || overlap(src->V, dst->V) || overlap(src->k_scale, dst->k_scale) ||
-      overlap(src->v_scale, dst->v_scale) || overlap(src->kv_len, dst->kv_len)) return GVOTE_ERR_INVALID_ARG;
+  if (codes_overlap(p, codes_of(p, src, src->K), codes_of(p, src, src->V), dst)) return GVOTE_ERR_INVALID_ARG;
+  for (const void* s : {src->k_scale, src->v_scale})
+    for (const void* d : {dst->k_scale, dst->v_scale})
+      if (overlap(scales_of(p, src, s), scales_of(p, dst, d))) return GVOTE_ERR_INVALID_ARG;
+  if (overlap(lens_of(p, src->batch, src->kv_len), lens_of(p, dst->batch, dst->kv_len))) return GVOTE_ERR_INVALID_ARG;
   REQUIRE_PTR(ws); OPTIONAL_PTR(mask_or_null); OPTIONAL_PTR(acc_or_null); OPTIONAL_PTR(acc_out_or_null);
   OPTIONAL_PTR(token_pos_or_null); OPTIONAL_PTR(token_pos_out_or_null);
   if (!acc_or_null != !acc_out_or_null || (token_pos_or_null && !token_pos_out_or_null)) return GVOTE_ERR_INVALID_ARG;
-  if (overlap(acc_or_null, acc_out_or_null) && acc_or_null) return GVOTE_ERR_INVALID_ARG;
-  if (overlap(token_pos_or_null, token_pos_out_or_null) && token_pos_or_null) return GVOTE_ERR_INVALID_ARG;
+  if (overlap(slots_of(p, src->total_tokens, acc_or_null), slots_of(p, dst->total_tokens, acc_out_or_null)) ||
+      overlap(slots_of(p, src->total_tokens, token_pos_or_null), slots_of(p, dst->total_tokens, token_pos_out_or_null)))
+    return GVOTE_ERR_INVALID_ARG;
   if (ws_bytes < store8_map(p, src->batch, larger(src->total_tokens, dst->total_tokens)).total) return GVOTE_ERR_WORKSPACE_TOO_SMALL;
   const SideArrays side{acc_or_null, acc_out_or_null, token_pos_or_null, token_pos_out_or_null};
   return launch_store8(p, nullptr, nullptr, src->tok_stride, src->head_stride, src, mask_or_null, src->cu_seqlens,
