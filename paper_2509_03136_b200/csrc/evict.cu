@@ -209,7 +209,12 @@ evict_kernel(const float* __restrict__ acc, const int32_t* __restrict__ cu, cons
     }
   }
   for (; q < q1; ++q) words_at(q);
-  if (rank == 0 && tid == 0) budget[r * Hkv + h] = k;
+  if (rank == 0) {                                 // padding: words behind the request's last, or before the first request
+    const int64_t at = mask_word_offset(start, r), end = r + 1 < (int)gridDim.z ? mask_word_offset(cu[r + 1], r + 1) : row_words;
+    for (int64_t i = words + tid; i < end - at; i += kEvictThreads) m[i] = 0u;
+    for (int64_t i = tid; r == 0 && i < at; i += kEvictThreads) m[i - at] = 0u;
+    if (tid == 0) budget[r * Hkv + h] = k;
+  }
   cluster.sync();                                  // the counts are read until here
 }
 
