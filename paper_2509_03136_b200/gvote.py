@@ -306,7 +306,9 @@ def _shaped(t: Optional[torch.Tensor], dtype, shape, name: str, dev: torch.devic
     return t.data_ptr() or None
 
 
-def _cache8(p, c: Cache8, name: str):
+def _cache8(p, c: Cache8, name: str, dev: torch.device):
+    if c.device != dev:
+        raise ValueError(f"{name} is on {c.device}, must be on {dev}")
     if c.shape != (p.n_kv_heads, p.d_k):
         raise ValueError(f"{name} holds {c.shape[0]} heads of {c.shape[1]} values, the parameters say "
                          f"{p.n_kv_heads} of {p.d_k}")
@@ -490,7 +492,7 @@ def gvote_store8(p, K, V, cu_seqlens, geom, cache: Cache8, ws, mask=None, kv_len
             _shaped(V, torch.bfloat16, (H, total, p.d_k), "V", dev, dense=False), K.stride(1), K.stride(0),
             _shaped(mask, torch.int32, (H, mask_row_words(total, batch)), "mask", dev),
             _shaped(cu_seqlens, torch.int32, (batch + 1,), "cu_seqlens", dev),
-            _shaped(kv_len, torch.int32, (batch, H), "kv_len", dev), batch, total, max_N, _cache8(p, cache, "cache"),
+            _shaped(kv_len, torch.int32, (batch, H), "kv_len", dev), batch, total, max_N, _cache8(p, cache, "cache", dev),
             _shaped(acc, torch.float32, (H, total), "acc", dev), _shaped(acc_out, torch.float32, dst, "acc_out", dev),
             _shaped(token_pos, torch.int32, (H, total), "token_pos", dev),
             _shaped(token_pos_out, torch.int32, dst, "token_pos_out", dev), ws=ws)
@@ -501,10 +503,8 @@ def gvote_prune8(p, cache: Cache8, mask, out: Cache8, ws, acc=None, acc_out=None
     """The kept rows of one 8-bit cache into another (mask=None keeps all)."""
     batch, total, _ = cache.geom
     H, dst, dev = p.n_kv_heads, (p.n_kv_heads, out.geom[1]), cache.device
-    if out.device != dev:
-        raise ValueError(f"out is on {out.device}, must be on {dev}")
-    _launch(load().gvote_prune8, dev, p, _cache8(p, cache, "cache"),
-            _shaped(mask, torch.int32, (H, mask_row_words(total, batch)), "mask", dev), _cache8(p, out, "out"),
+    _launch(load().gvote_prune8, dev, p, _cache8(p, cache, "cache", dev),
+            _shaped(mask, torch.int32, (H, mask_row_words(total, batch)), "mask", dev), _cache8(p, out, "out", dev),
             _shaped(acc, torch.float32, (H, total), "acc", dev), _shaped(acc_out, torch.float32, dst, "acc_out", dev),
             _shaped(token_pos, torch.int32, (H, total), "token_pos", dev),
             _shaped(token_pos_out, torch.int32, dst, "token_pos_out", dev), ws=ws)
@@ -521,7 +521,7 @@ def gvote_append8(p, K_new, V_new, cu_new, max_new: int, cache: Cache8, kv_len_o
             _shaped(K_new, torch.bfloat16, (H, total_new, p.d_k), "K_new", dev, dense=False),
             _shaped(V_new, torch.bfloat16, (H, total_new, p.d_k), "V_new", dev, dense=False), K_new.stride(1),
             K_new.stride(0), _shaped(cu_new, torch.int32, (batch + 1,), "cu_new", dev), total_new, max_new,
-            _cache8(p, cache, "cache"), _shaped(kv_len_out, torch.int32, (batch, H), "kv_len_out", dev),
+            _cache8(p, cache, "cache", dev), _shaped(kv_len_out, torch.int32, (batch, H), "kv_len_out", dev),
             _shaped(acc, torch.float32, (H, total), "acc", dev),
             _shaped(token_pos, torch.int32, (H, total), "token_pos", dev),
             _shaped(pos_new, torch.int32, (total_new,), "pos_new", dev), ws=ws)
@@ -535,7 +535,7 @@ def gvote_attend8(p, Q, cu_q, max_q: int, cache: Cache8, out, ws, lse=None, acc=
     shape = (total_q, p.n_q_heads, p.d_k)
     _launch(load().gvote_attend8, dev, p, _shaped(Q, torch.bfloat16, shape, "Q", dev, dense=False), Q.stride(0),
             Q.stride(1), _shaped(cu_q, torch.int32, (batch + 1,), "cu_q", dev), total_q, max_q,
-            _cache8(p, cache, "cache"), _shaped(out, torch.bfloat16, shape, "out", dev, dense=False), out.stride(0),
+            _cache8(p, cache, "cache", dev), _shaped(out, torch.bfloat16, shape, "out", dev, dense=False), out.stride(0),
             out.stride(1), _shaped(lse, torch.float32, (total_q, p.n_q_heads), "lse", dev),
             _shaped(acc, torch.float32, (H, total), "acc", dev), _shaped(acc_out, torch.float32, (H, total), "acc_out", dev),
             ws=ws)
