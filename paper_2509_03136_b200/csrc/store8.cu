@@ -159,6 +159,7 @@ struct Unit<false> {
     hi = __ldg(q + 1);
   }
   __device__ __forceinline__ uint32_t word(int i) const { return i < 4 ? (&lo.x)[i] : (&hi.x)[i - 4]; }
+  static __device__ __forceinline__ float scale_of(float top) { return scale8_of(top); }
   // The largest finite magnitude.  Magnitudes of bf16 are ordered like their bits; 0x7f80 and above are not finite.
   __device__ __forceinline__ float largest() {
     uint32_t m = 0;
@@ -202,6 +203,11 @@ struct Unit<true> {
     lo = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + elem));
     scale = s;
   }
+  // the scale of a block whose largest value is twice `half`: exponents count from the half, whose least scale is 2^-126 / 2
+  static __device__ __forceinline__ float scale_of(float half) {
+    return half <= 224.f * 1.17549435e-38f ? 1.17549435e-38f : 2.f * scale8_of(half);
+  }
+  // Half of the largest finite magnitude.
   __device__ __forceinline__ float largest() {
     uint32_t m = 0;
 #pragma unroll
@@ -212,7 +218,7 @@ struct Unit<true> {
     }
     const __half2 h = *reinterpret_cast<const __half2*>(&m);
     const float x = __low2float(h), y = __high2float(h), top = fmaxf(x, y);     // (a NaN on both sides of a max stays)
-    return top == top ? finite_abs(top * scale) : 0.f;
+    return top == top ? top * (0.5f * scale) : 0.f;               // (the value itself may be 2^128)
   }
   // code * 2^j for the block's own scale: the codes themselves where the scales agree; in halves where 2^j is one (exact as
   // far as e4m3 can tell: a code has 4 significant bits and the least half, 2^-24, lies far below half its least step)
@@ -231,11 +237,13 @@ struct Unit<true> {
       }
       return out;
     }
+    // (a code that is not zero has a ratio of 2^18 at most; beyond that every code is zero, and must stay so)
+    const float f = fminf(ratio, 1.2676506e30f);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const uint32_t w = (&lo.x)[q];
       const float2 a = decode8x2(w & 0xffffu), b = decode8x2(w >> 16);
-      (&out.x)[q] = encode8x2(a.x * scale * inv, a.y * scale * inv) | (encode8x2(b.x * scale * inv, b.y * scale * inv) << 16);
+      (&out.x)[q] = encode8x2(a.x * f, a.y * f) | (encode8x2(b.x * f, b.y * f) << 16);
     }
     return out;
   }
@@ -312,7 +320,7 @@ store8_kernel(const __grid_constant__ StoreArgs a) {
     float top = s_max[t][0];
 #pragma unroll
     for (int w = 1; w < kStoreThreads / 32; ++w) top = fmaxf(top, s_max[t][w]);
-    const float scale = scale8_of(top), inv = inverse_pow2(scale);
+    const float scale = Unit<kSrc8>::scale_of(top), inv = inverse_pow2(scale);
     if (tid == t) a.dst_scale[t][db] = scale;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i)
