@@ -28,8 +28,10 @@
 // of K is done with as soon as S is there, a tile of V as soon as it is widened - warps 1 and 2 issue the MMAs of S and of O
 // (one warp for both took 1500 clocks a tile, its waits and commits one after the other), and warp 3 prepares the next
 // segment's Q terms (the first segment's, which everything waits for, are shared out among the softmax warps: alone,
-// warp 3 took 16,000 clocks for 20 rows).  Warps 4 to 7 widen V, a tile or two ahead (by the softmax warps themselves it lay
-// in their chain: five tokens 43 us instead of 39); then come up to five softmax groups of four warps, thread = cached row of
+// warp 3 took 16,000 clocks for 20 rows).  Four warps widen V, a tile or two ahead (by the softmax warps themselves it
+// lay in their chain: five tokens 43 us instead of 39), or two groups of four in turns where few query rows make a tile short (a
+// tile takes one group 2100 clocks: one token over long rows 49.5 us instead of 44; with 12 rows and more the second group's
+// registers cost more than it brings); then come up to five softmax groups of four warps, thread = cached row of
 // the tile (and channel of the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each
 // with references and an O of its own (one group alone needs 3000 clocks of latency for a tile, the memory 1400), with many
 // the groups share a tile's rows out.  S and P are buffered as deep as the MMAs run ahead.  The loops of the roles run at
@@ -39,10 +41,9 @@
 // Weights for the eviction: the logits are kept (4 bytes per row and query, against 2 d_k per row), and
 // attend8_weights_kernel turns them into weights once lse is known; a slot belongs to one thread, so the sum has one order.
 //
-// Measured (one B200, warm): one token of 28 heads over 128K rows of 4 KV heads, 134 MB: 49 us, the first kernel 45 of them.
-// A ragged batch of 128 pruned heads, 63 MB: 41 us with the weights.  Five tokens over 32K rows of 8 heads: 39 us, a tile
-// every 3200 clocks.  Smallest calls: 12.5 us, all of it latency.  What a tile costs beside its bytes is the widening and what it
-// takes from the softmax warps: over long rows 49 us, 47 when the codes are only copied, 41 when an eighth of them is.
+// Measured (one B200, warm): one token of 28 heads over 128K rows of 4 KV heads, 134 MB: 44 us, the first kernel 41 of them.
+// A ragged batch of 128 pruned heads, 63 MB: 38 us with the weights.  Five tokens over 32K rows of 8 heads: 39 us, a tile
+// every 3200 clocks.  Smallest calls: 12.5 us, all of it latency.
 //
 // Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
 #include <cstddef>
@@ -204,7 +205,7 @@ __device__ __forceinline__ void write_lse(const AttendArgs& a, int64_t at, float
   if (a.lse) a.lse[at] = l * 0.6931471805599453f;
 }
 
-// Counts: one arrival, 5 + 4 groups on q_empty, four per group that shares a tile's rows from s_empty on, four from v_empty on.
+// Counts: one arrival, 1 + 4 for every group on q_empty, four per group that shares a tile's rows from s_empty on, four from v_empty on.
 struct Bars {
   uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], q_full[2], q_empty[2];
   uint64_t s_full[kMaxBuffers], p_empty[kMaxBuffers], o_full[4], w_empty[2];
@@ -213,7 +214,7 @@ struct Bars {
   uint64_t drain[2];                   // the MMAs under way of the two issuers, after a wait that ran out
 };
 constexpr int kFirstQ = 8;             // a named barrier; the softmax groups' are 1 to 5
-enum { kWarpTma = 0, kWarpS = 1, kWarpO = 2, kWarpQ = 3, kWarpWide = 4, kWarpSoftmax = 8 };
+enum { kWarpTma = 0, kWarpS = 1, kWarpO = 2, kWarpQ = 3, kWarpWide = 4 };   // then the softmax warps
 
 struct Tail {
   Bars bars;
@@ -229,7 +230,9 @@ struct Tail {
 
 template <int kBoxes, int kRb>          // 128-byte boxes per row; groups that share a tile's rows
 struct Layout {                         // threads, tensor memory (columns), shared memory (bytes)
-  static constexpr int kTurns = kRb == 1 ? 4 : kRb == 2 ? 2 : 1, kGroups = kTurns * kRb, kThreads = 256 + 128 * kGroups;
+  static constexpr int kTurns = kRb == 1 ? 4 : kRb == 2 ? 2 : 1, kGroups = kTurns * kRb;
+  static constexpr int kWiden = kBoxes == 1 && kRb <= 2 ? 2 : 1;       // groups that widen V, in turns
+  static constexpr int kWarpSoftmax = kWarpWide + 4 * kWiden, kThreads = 32 * kWarpSoftmax + 128 * kGroups;
   static constexpr int kRows = kR * kRb, kBuffers = kRb <= 2 ? 4 : 2;
   static constexpr int kN1 = (3 * kRows + 15) / 16 * 16, kN2 = 4 * kRows;
   static constexpr int kO = kBuffers * kN1, kCols = kO + kTurns * kBoxes * kN2;     // O of turn i, box y: kO + (i kBoxes + y) kN2
@@ -297,7 +300,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     constexpr int kBars = sizeof(Bars) / 8;
     if (tid < kBars) {
       const int at = tid * 8;
-      const uint32_t count = at >= (int)offsetof(Bars, q_empty) && at < (int)offsetof(Bars, s_full) ? 5 + 4 * L::kGroups
+      const uint32_t count = at >= (int)offsetof(Bars, q_empty) && at < (int)offsetof(Bars, s_full) ? 1 + 4 * (L::kWiden + L::kGroups)
                              : at >= (int)offsetof(Bars, s_empty) && at < (int)offsetof(Bars, v_empty) ? 4 * kRb
                              : at >= (int)offsetof(Bars, v_empty) && at < (int)offsetof(Bars, drain) ? 4 : 1;
       ptx::mbar_init(reinterpret_cast<uint64_t*>(&tail->bars) + tid, count);
@@ -554,7 +557,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         if (lane < 4) tail->any_nan[qb][lane] = 0;
       }
       if (at.seg == 0) {                                               // the softmax warps prepare the first one's rows
-        asm volatile("barrier.cta.sync %0, %1;" ::"r"(kFirstQ), "r"(L::kThreads - 224) : "memory");
+        asm volatile("barrier.cta.sync %0, %1;" ::"r"(kFirstQ), "r"(32 + 128 * L::kGroups) : "memory");
       } else {
         const uint32_t held = __ballot_sync(0xffffffffu, holds);
 #pragma unroll 1
@@ -570,10 +573,12 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&tail->bars.q_full[qb]);
     }
-  } else if (warp < kWarpSoftmax) {
+  } else if (warp < L::kWarpSoftmax) {
     // ------------------------------------------------------------------ the tiles of V in bf16: thread = row of the tile
-    const int key_in = tid - kWarpWide * 32, units = a.d_k >> 4;
-    int vs = 0;
+    // Tile it is group it mod kWiden's.  With two groups so is its buffer; that the slot's tile before this one has come (a wait
+    // by parity must not meet a phase two behind) follows from the buffer's: there are no fewer slots than buffers.
+    const int group = (warp - kWarpWide) >> 2, key_in = tid & 127, units = a.d_k >> 4;
+    int vs = group;
     uint32_t v_phase = 0;
     for (; ok && !at.done(); at.next_segment()) {
       const int qb = at.seg & 1;
@@ -581,7 +586,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       if (!ok) break;
       const Entry x = tail->entry[qb];
       const int all_see = x.n - (x.nq - 1);
-      for (int t = at.s0, it = at.it; ok && t < at.s1; ++t, ++it) {
+      const int skip = (group + at.it) % L::kWiden;                    // (kWiden: 1 or 2)
+      for (int t = at.s0 + skip, it = at.it + skip; ok && t < at.s1; t += L::kWiden, it += L::kWiden) {
         const int wb = it % L::kWides, key = t * kTileKeys + key_in;
         ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.w_empty[wb], ((it / L::kWides) & 1) ^ 1, abort_flag) &&
                                          wait_or_abort(&tail->bars.v_full[vs], v_phase, abort_flag));
@@ -630,14 +636,15 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           ptx::mbar_arrive(&tail->bars.v_empty[vs]);
           ptx::mbar_arrive(&tail->bars.w_full[wb]);
         }
-        if (++vs == a.v_slots) { vs = 0; v_phase ^= 1u; }
+        vs += L::kWiden;
+        if (vs >= a.v_slots) { vs -= a.v_slots; v_phase ^= 1u; }
       }
       __syncwarp();
       if (ok && lane == 0) ptx::mbar_arrive(&tail->bars.q_empty[qb]);
     }
   } else {
     // ------------------------------------------------------------------ softmax: thread = row of the tile, channel of O
-    const int group = (warp - kWarpSoftmax) >> 2, turn = group / kRb, rb = group % kRb, bar_id = 1 + group;
+    const int group = (warp - L::kWarpSoftmax) >> 2, turn = group / kRb, rb = group % kRb, bar_id = 1 + group;
     const int w = warp & 3, key_in = w * 32 + lane;
     const uint32_t lane_addr = tmem + ((uint32_t)(w * 32) << 16);
     const uint32_t o_addr = lane_addr + (uint32_t)(L::kO + turn * kBoxes * L::kN2 + rb * 4 * kR);
@@ -646,14 +653,14 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     int o_uses = 0;
     if (!at.done()) {                                                  // the first segment's query rows (one or two per warp)
       const Entry x = entry_of(a, at.e);
-      for (int row = warp - kWarpSoftmax; row < L::kRows; row += 4 * L::kGroups) {
+      for (int row = warp - L::kWarpSoftmax; row < L::kRows; row += 4 * L::kGroups) {
         const int qrow = group0 + row, token = qrow / a.G, head = x.h * a.G + qrow - token * a.G;
         uint2 v[kBoxes];
         load_row((int64_t)(x.q0 + token) * a.q_tok + (int64_t)head * a.q_head, qrow < x.nq * a.G, v);
         put_row(0, row, v);
       }
       ptx::fence_proxy_async();
-      asm volatile("barrier.cta.arrive %0, %1;" ::"r"(kFirstQ), "r"(L::kThreads - 224) : "memory");
+      asm volatile("barrier.cta.arrive %0, %1;" ::"r"(kFirstQ), "r"(32 + 128 * L::kGroups) : "memory");
     }
     for (; !at.done(); at.next_segment()) {
       const int qb = at.seg & 1, e = at.e, s0 = at.s0, s1 = at.s1;
