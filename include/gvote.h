@@ -282,7 +282,7 @@ GVOTE_API int32_t gvote_recompress(const gvote_params* p, const float* mu, const
                          void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------------------
- * The pruned cache in use: rows held in 8 bits, single-token attention over them, and eviction by the
+ * The pruned cache in use: rows held in 8 bits, attention of a few tokens over them, and eviction by the
  * attention weight a row has collected (the other common rule for what a cache keeps; Section 4.1 compares
  * the method with such systems).  A prompt goes gvote_compress* or gvote_accumulate + gvote_evict ->
  * gvote_store8 (mask); a token goes gvote_append8 -> gvote_attend8; a full cache goes gvote_evict ->
@@ -326,7 +326,8 @@ static inline int64_t gvote_cache8_block_offset(int64_t cu_seqlens_r, int32_t r)
 
 /* Bytes of scratch the entry points of this part accept as `ws`, for slabs of this size and queries of this
  * size (total_q query tokens in all, max_q of one request at most; 0, 0 for calls without queries), and for
- * every call of no larger sizes.  Where a call has a source and a destination cache, the larger of both.  Zero-fill
+ * every call of no larger sizes.  gvote_attend8 of these very sizes without acc_out accepts 4 n_q_heads max_q total_tokens
+ * bytes less: it keeps no logits.  Where a call has a source and a destination cache, the larger of both.  Zero-fill
  * it once; status word as everywhere (gvote_poll_status).  0 on invalid arguments. */
 GVOTE_API size_t gvote_cache_workspace_bytes(const gvote_params* p, int32_t batch, int64_t total_tokens, int64_t max_N,
                                    int64_t total_q, int64_t max_q);
@@ -371,7 +372,7 @@ GVOTE_API int32_t gvote_append8(const gvote_params* p, const void* K_new, const 
  * 0 .. kv_len - n + i of a head; a head with fewer rows than that leaves token i nothing, which gives out = 0,
  * lse = -inf.  Per query head g of KV head h: logits q.k_n / sqrt(d_k), softmax, out = sum of weight * value
  * (products of the stored values; 32-bit weights, however far below the largest, and 32-bit sums; an entry of a query
- * is exact down to 2^-17 of the largest of its row and held to 2^-27 of that below), lse_or_null [total_q, n_q_heads] =
+ * is exact down to 2^-17 of the largest of its row and held to 2^-25 of that below), lse_or_null [total_q, n_q_heads] =
  * log of the softmax's denominator.  acc_out_or_null [n_kv_heads, total_tokens]: for the rows held, acc (null: 0) + the weights summed over
  * the request's tokens and the head's group; acc_or_null may be acc_out itself.  Deterministic.  Where cu_q gives a
  * request more than max_q tokens the status word reads GVOTE_ERR_INVALID_ARG and its outputs are not to be used. */

@@ -183,8 +183,8 @@ int32_t gvote_attend8(const gvote_params* p, const void* Q, int64_t q_tok_stride
   if (acc_or_null && !acc_out_or_null) return GVOTE_ERR_INVALID_ARG;
   if (q_head_stride < p->d_k || q_head_stride % 8 != 0 || q_tok_stride % 8 != 0) return GVOTE_ERR_UNALIGNED;
   if (out_head_stride < p->d_k || out_head_stride % 8 != 0 || out_tok_stride % 8 != 0) return GVOTE_ERR_UNALIGNED;
-  if (ws_bytes < attend8_map(p, cache->batch, cache->total_tokens, total_q, max_q).total)
-    return GVOTE_ERR_WORKSPACE_TOO_SMALL;
+  const AttendMap m = attend8_map(p, cache->batch, cache->total_tokens, total_q, max_q);
+  if (ws_bytes < (acc_out_or_null ? m.total : m.logits)) return GVOTE_ERR_WORKSPACE_TOO_SMALL;   // (the logits lie last)
   return launch_attend8(p, (const __nv_bfloat16*)Q, q_tok_stride, q_head_stride, cu_q, total_q, max_q, cache,
                         (__nv_bfloat16*)out, out_tok_stride, out_head_stride, lse_or_null, acc_or_null, acc_out_or_null,
                         (char*)ws, (cudaStream_t)stream);

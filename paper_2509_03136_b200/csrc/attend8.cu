@@ -18,7 +18,7 @@
 // with the matching power of two in 32 bits).  Three bf16 terms are all 24 bits of a weight, at any size a float can have:
 // beside a first row that collects the attention the others' weights can lie 2^-30 below and still carry the output.  (Four
 // e4m3 terms of P against V as it lies took a quarter less time over long rows, but ended 2^-24 below the largest weight.)
-// Three terms of Q hold every entry above 2^-17 of its row's largest exactly, and a smaller one to 2^-27 of the largest.
+// Three terms of Q hold every entry above 2^-17 of its row's largest exactly, and a smaller one to 2^-25 of the largest.
 //
 // The scale of K enters the logit; the scale of V goes into the weight: P = 2^(l + log2(scale_v) - ref), ref the largest such
 // exponent so far, so that a block of large values does not overflow.  ref only moves when it is passed by 2^6 (the

@@ -33,10 +33,10 @@ def accumulate(gv, p, ws_bytes, batch, total, max_n, total_q, max_q):
                                       4 * A, None, batch, total, max_n, None, None, 5 * A, 6 * A, ws_bytes, 0)
 
 
-def attend(gv, p, ws_bytes, batch, total, max_n, total_q, max_q):
+def attend(gv, p, ws_bytes, batch, total, max_n, total_q, max_q, acc_out=11 * A):
     c = gv.GVoteCache8(A, 2 * A, 3 * A, 4 * A, 5 * A, 6 * A, NO_MAP, p.d_k, total, max_n, batch, 0)
     return gv.load().gvote_attend8(ctypes.byref(p), 7 * A, p.n_q_heads * p.d_k, p.d_k, 8 * A, total_q, max_q, ctypes.byref(c), 9 * A,
-                                   p.n_q_heads * p.d_k, p.d_k, None, None, 10 * A, 11 * A, ws_bytes, 0)
+                                   p.n_q_heads * p.d_k, p.d_k, None, None, acc_out, 10 * A, ws_bytes, 0)
 
 
 def test_the_calls_here_end_before_a_launch(gv):
@@ -76,3 +76,13 @@ def test_the_size_suffices_for_every_smaller_call(gv):
             if mq <= gv.ATTEND8_MAX_Q:
                 assert attend(gv, p, n, b, t, mn, q, mq) == SHAPE, (hkv, g, p.d_k, (batch, total, max_n, total_q, max_q), (b, t, mn, q, mq))
     assert gv.gvote_launch_count() == n0
+
+
+@pytest.mark.parametrize("hkv,g,d,batch,total,total_q,max_q", [(8, 4, 128, 1, 1 << 20, 32, 32), (2, 4, 64, 3, 5000, 3, 1), (1, 1, 16, 1, 64, 1, 1),
+                                                              (4, 7, 256, 2, 131072, 40, 20)])
+def test_attention_without_weights_needs_no_room_for_logits(gv, hkv, g, d, batch, total, total_q, max_q):
+    p = params(gv, hkv, g, d)
+    n = size(gv, p, batch, total, total, total_q, max_q) - 4 * hkv * g * max_q * total
+    assert attend(gv, p, n, batch, total, total, total_q, max_q, acc_out=None) == SHAPE
+    assert attend(gv, p, 4 * hkv * g * max_q * total, batch, total, total, total_q, max_q) == SMALL
+    assert attend(gv, p, 256, batch, total, total, total_q, max_q, acc_out=None) == SMALL
