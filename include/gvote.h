@@ -370,12 +370,13 @@ GVOTE_API int32_t gvote_append8(const gvote_params* p, const void* K_new, const 
  * strides (tokens, heads), requests packed by cu_q [batch+1] (device); at most GVOTE_ATTEND8_MAX_Q tokens of a
  * request.  A request's query tokens are the last rows of its cache (append first): token i of n sees rows
  * 0 .. kv_len - n + i of a head; a head with fewer rows than that leaves token i nothing, which gives out = 0,
- * lse = -inf.  Per query head g of KV head h: logits q.k_n / sqrt(d_k), softmax, out = sum of weight * value
- * (products of the stored values; 32-bit weights, however far below the largest, and 32-bit sums; an entry of a query
- * is exact down to 2^-17 of the largest of its row and held to 2^-25 of that below), lse_or_null [total_q, n_q_heads] =
- * log of the softmax's denominator.  acc_out_or_null [n_kv_heads, total_tokens]: for the rows held, acc (null: 0) + the weights summed over
- * the request's tokens and the head's group; acc_or_null may be acc_out itself.  Deterministic.  Where cu_q gives a
- * request more than max_q tokens the status word reads GVOTE_ERR_INVALID_ARG and its outputs are not to be used. */
+ * lse = -inf.  Per query head g of KV head h: logits q.k_n / sqrt(d_k), softmax, out = sum of weight * value (products of
+ * the stored values, 32-bit sums; 32-bit weights, of every row whose weight times value scale is above 2^-126 of the
+ * largest such product; an entry of a query is exact down to 2^-17 of the largest of its row and held to 2^-25 of that
+ * below), lse_or_null [total_q, n_q_heads] = log of the softmax's denominator.  acc_out_or_null [n_kv_heads,
+ * total_tokens]: for the rows held, acc (null: 0) + the weights summed over the request's tokens and the head's group;
+ * acc_or_null may be acc_out itself.  Deterministic.  Where cu_q gives a request more than max_q tokens the status word
+ * reads GVOTE_ERR_INVALID_ARG and its outputs are not to be used. */
 #define GVOTE_ATTEND8_MAX_Q 32
 GVOTE_API int32_t gvote_attend8(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride,
                       const int32_t* cu_q, int64_t total_q, int64_t max_q, const gvote_cache8* cache,
