@@ -21,8 +21,8 @@
 // Three terms of Q hold every entry above 2^-17 of its row's largest exactly, and a smaller one to 2^-25 of the largest.
 //
 // The scale of K enters the logit; the scale of V goes into the weight: P = 2^(l + log2(scale_v) - ref), ref the largest such
-// exponent so far, so that a block of large values does not overflow.  ref only moves when it is passed by 2^6 (the
-// accumulated O is then rescaled in tensor memory: mostly the first tile only).
+// exponent so far, so that a block of large values does not overflow.  ref only moves when it is passed by 2^64 (the
+// accumulated O is then rescaled in tensor memory: the first tile sets it, and few ever move it).
 //
 // Warp 0 asks for the tiles of K and of V (TMA, only the 32-row parts that hold rows) into rings of their own - a tile
 // of K is done with as soon as S is there, a tile of V as soon as it is widened - warps 1 and 2 issue the MMAs of S and of O
@@ -30,20 +30,21 @@
 // segment's Q terms (the first segment's, which everything waits for, are shared out among the softmax warps: alone,
 // warp 3 took 16,000 clocks for 20 rows).  Four warps widen V, a tile or two ahead (by the softmax warps themselves it
 // lay in their chain: five tokens 43 us instead of 39), or two groups of four in turns where few query rows make a tile short (a
-// tile takes one group 2100 clocks: one token over long rows 49.5 us instead of 44; with 12 rows and more the second group's
+// tile takes one group 2100 clocks: one token over long rows 53 us instead of 43.5; with 12 rows and more the second group's
 // registers cost more than it brings); then come up to five softmax groups of four warps, thread = cached row of
 // the tile (and channel of the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each
 // with references and an O of its own (one group alone needs 3000 clocks of latency for a tile, the memory 1400), with many
 // the groups share a tile's rows out.  S and P are buffered as deep as the MMAs run ahead.  The loops of the roles run at
 // the same time and share the instruction cache: the rare parts (rows that not every token sees) are kept out of them
-// (within the widening loop they cost 20 of 70 us over long rows).
+// (within the widening loop they cost 20 of 70 us over long rows), and the widening loop is not unrolled (64 requests of
+// 2048 rows 97 -> 90 us).
 //
 // Weights for the eviction: the logits are kept (4 bytes per row and query, against 2 d_k per row), and
 // attend8_weights_kernel turns them into weights once lse is known; a slot belongs to one thread, so the sum has one order.
 //
-// Measured (one B200, warm): one token of 28 heads over 128K rows of 4 KV heads, 134 MB: 44 us, the first kernel 41 of them.
-// A ragged batch of 128 pruned heads, 63 MB: 38 us with the weights.  Five tokens over 32K rows of 8 heads: 39 us, a tile
-// every 3200 clocks.  Smallest calls: 12.5 us, all of it latency.
+// Measured (one B200, warm): one token of 28 heads over 128K rows of 4 KV heads, 134 MB: 43.5 us, the first kernel 40 of them.
+// A ragged batch of 128 pruned heads, 63 MB: 35 us with the weights.  Five tokens over 32K rows of 8 heads: 37 us.
+// Smallest calls: 12.5 us, all of it latency.
 //
 // Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
 #include <cstddef>
@@ -63,7 +64,7 @@ constexpr int kMaxSlots = 8;           // of a ring
 constexpr int kMaxBuffers = 4;         // of S and of P
 constexpr int kSms = 148;
 constexpr float kNoRef = -1e30f;       // a reference before the first logit
-constexpr float kSlack = 6.f;          // a reference may be passed by 2^6 (most tiles then leave it where it is)
+constexpr float kSlack = 64.f;         // a reference may be passed by 2^64: sums of up to 2^30 weights, times codes, stay below 2^127
 
 struct AttendArgs {
   const __nv_bfloat16* Q;
@@ -621,8 +622,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
               if (key < limit_sm[qb * L::kRows + g]) atomicOr(&marks[g * kBoxes * 4 + (u >> 1)], bits << (u * 16 & 31));
           }
         }
-#pragma unroll 2
-        for (int u = 0; u < units; ++u) {
+#pragma unroll 1
+        for (int u = 0; u < units; ++u) {                               // (unrolled, it took the others' instruction cache)
           const uint4 c = *reinterpret_cast<const uint4*>(from + (u >> 3) * kTileKeys * 128 + (((u & 7) ^ (key_in & 7)) << 4));
           uint32_t b[8];
 #pragma unroll
@@ -706,7 +707,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             auto term = [&](int k) { return __uint_as_float(c[k * kR + g]); };
             l[g] = fmaf(term(2), 0.00390625f, fmaf(term(1), 0.0625f, term(0))) * (sc.x * factor[g]);
             if (edge && key >= limit[g]) l[g] = -INFINITY;
-            over = over || l[g] + lv > refn[g] + kSlack || l[g] > refd[g] + 64.f;
+            over = over || l[g] + lv > refn[g] + kSlack || l[g] > refd[g] + kSlack;
           }
           if (a.logits && key < x.n) {
             float* dst = a.logits + ((int64_t)x.h * a.max_q * a.G + row0) * a.total + x.start + key;

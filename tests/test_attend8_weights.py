@@ -135,3 +135,23 @@ def test_a_first_row_with_nearly_all_weight_and_a_small_value(gv):
         logits.append(x)
         V.append(v)
     check(lens, *attend(gv, lens, 7, 128, np.concatenate(logits), np.concatenate(V)))
+
+
+@gpu
+@pytest.mark.parametrize("hq,d", [(4, 64), (8, 128), (12, 128), (16, 256), (20, 64), (3, 192)])
+@pytest.mark.parametrize("step", [46.0, 60.0, 80.0])
+def test_a_reference_that_moves_late(gv, hq, d, step):
+    """Every group of warps meets rows e^step above all it has seen, after several tiles: what it has summed up is scaled down by
+    2^66 and more, and still is the only output of its channels."""
+    n = 128 * 12 + 5
+    logits, V = np.full(n, -step), np.zeros((n, d))
+    logits[::3] = -step - 2
+    V[:, :d // 2] = np.random.default_rng(hq).choice([-1.0, 1.0], size=(n, d // 2))
+    V[:, 0] = 1.0
+    for tile in range(8, 13):
+        i = 128 * tile + tile % 5
+        logits[i], V[i] = 0.0, 0.0
+        V[i, d // 2:] = 1.0
+    out, lse, Q, held = attend(gv, (n,), hq, d, logits, V)
+    assert (out[0, :, 0] > 0).all()
+    check((n,), out, lse, Q, held)
