@@ -109,6 +109,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// x * 2^d in two steps: 2^d alone may lie below 2^-126.
+__device__ __forceinline__ float times_exp2(float x, float d) {
+  const float h = exp2_fast(0.5f * d);
+  return x * h * h;
+}
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
   for (uint32_t i = 0; i < (1u << 20); ++i) {
     if (ptx::mbar_try_wait(bar, parity)) return true;
@@ -734,8 +739,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
               d = fmaxf(d, v.x);
               n = fmaxf(n, v.y);
             }
-            sum[g] *= exp2_fast(refd[g] - d);
-            shrink[g] = exp2_fast(refn[g] - n);
+            sum[g] = times_exp2(sum[g], refd[g] - d);
+            shrink[g] = exp2_fast(0.5f * (refn[g] - n));             // (applied twice)
             refd[g] = d;
             refn[g] = n;
           }
@@ -751,7 +756,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
                 ptx::tmem_ld_32x16(at_o, v);
                 ptx::tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * shrink[j % kR]);
+                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * shrink[j % kR] * shrink[j % kR]);
                 tmem_st_32x16(at_o, v);
               }
               ptx::tmem_wait_st();
@@ -818,8 +823,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
                 if (any_tile) {
                   auto term = [&](int k) { return __uint_as_float(v[k * kR + g]); };
                   float o = (term(2) + term(1)) + term(0);
-                  const float f = exp2_fast(0.5f * (refn[g] - refd[g]));       // (in two steps: it may lie below 2^-126)
-                  o = total == 0.f ? 0.f : o * __frcp_rn(total) * f * f;
+                  o = total == 0.f ? 0.f : times_exp2(o * __frcp_rn(total), refn[g] - refd[g]);
                   if (nan_seen && ((nan_sm[(rb * kR + g) * kBoxes * 4 + (d >> 5)] >> (d & 31)) & 1u)) o = __uint_as_float(0x7fffffffu);
                   if (whole) a.out[tail->out_at[qb][rb * kR + g] + d] = __float2bfloat16(o);
                   else a.part_o[(slot + g) * a.d_k + d] = o;
@@ -855,12 +859,12 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
 // Running (maximum, sum relative to it), joined with another pair; and over a warp.
 __device__ __forceinline__ void join(float& M, float& L, float2 x) {
   const float top = fmaxf(M, x.x);
-  L = top == -INFINITY ? L + x.y : L * exp2_fast(M - top) + x.y * exp2_fast(x.x - top);     // (a NaN in the sum stays)
+  L = top == -INFINITY ? L + x.y : times_exp2(L, M - top) + times_exp2(x.y, x.x - top);     // (a NaN in the sum stays)
   M = top;
 }
 __device__ __forceinline__ float2 warp_join(float M, float L) {
   const float all = warp_max(M);
-  L = all == -INFINITY ? L : L == 0.f ? 0.f : L * exp2_fast(M - all);
+  L = all == -INFINITY ? L : L == 0.f ? 0.f : times_exp2(L, M - all);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
   return make_float2(all, L);
@@ -924,7 +928,7 @@ attend8_merge_kernel(const __grid_constant__ AttendArgs a, int ctas, int max_row
     const float2 ml = warp_join(M, L);
     for (int i = tid; i < j.parts; i += 256) {
       const float2 m = a.part_ml[j.slot0 + (int64_t)i * a.group_rows];
-      s_f[i] = m.x == -INFINITY ? 0.f : exp2_fast(m.x - ml.x) * m.y;
+      s_f[i] = m.x == -INFINITY ? 0.f : times_exp2(m.y, m.x - ml.x);
     }
     __syncthreads();
     for (int q = lane; q < quads; q += 32) {
@@ -965,7 +969,7 @@ attend8_merge_kernel(const __grid_constant__ AttendArgs a, int ctas, int max_row
     if (j.parts >= 0 && j.parts <= 32) {
       const float2 m = lane < j.parts ? a.part_ml[j.slot0 + (int64_t)lane * a.group_rows] : make_float2(-INFINITY, 0.f);
       const float2 ml = warp_join(m.x, m.y);
-      const float f = m.x == -INFINITY ? 0.f : exp2_fast(m.x - ml.x) * m.y;
+      const float f = m.x == -INFINITY ? 0.f : times_exp2(m.y, m.x - ml.x);
       for (int q = lane; q - lane < quads; q += 32) {
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4

@@ -40,7 +40,7 @@ def guards_of(body, call):
 
 def names(header, call_results):
     header = re.sub(r"group_any\([^()]*\)", "group_any", header)          # what a barrier returns is the same for all
-    header = re.sub(r"\.\w+", "", header)                                  # members: judged by what they are members of
+    header = re.sub(r"\.\w+", "", header)                                  # a member goes by what it is a member of
     return set(re.findall(r"[A-Za-z_]\w*", header)) - call_results
 
 

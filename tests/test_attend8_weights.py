@@ -155,3 +155,28 @@ def test_a_reference_that_moves_late(gv, hq, d, step):
     out, lse, Q, held = attend(gv, (n,), hq, d, logits, V)
     assert (out[0, :, 0] > 0).all()
     check((n,), out, lse, Q, held)
+
+
+@gpu
+@pytest.mark.parametrize("hq,d,n,batch", [(4, 64, 128 * 12, 150), (8, 128, 128 * 12, 150), (20, 64, 128 * 9, 150), (3, 192, 128 * 12, 150),
+                                          (4, 64, 128 * 600, 1), (12, 80, 128 * 900, 1), (1, 64, 128 * 5000, 1)])
+def test_three_levels_of_weight(gv, hq, d, n, batch):
+    """Rows at e^-88, behind them rows at e^-48, behind them one at 1: the second level stays below the point at which what is summed
+    up is scaled, and is then scaled by more than a float's exponents reach; across CTAs it is merged the same way.  (With 150
+    requests a CTA has all of one, or most.)"""
+    logits, V = np.full(n, -88.0), np.zeros((n, d))
+    a, b = n // 3 // 128 * 128, 2 * n // 3 // 128 * 128
+    logits[a:b] = -48.0
+    logits[b:] = -80.0
+    V[:, 3] = 1.0                                                    # (one value scale for all)
+    V[a:b, 0], V[a:b, 1] = 1.0, np.random.default_rng(n).choice([-1.0, 1.0], size=b - a)
+    if batch == 1:
+        b = n - 128                                                  # only the last CTA meets the largest
+    tail = np.arange(b + 5, n, 128)
+    logits[tail] = 0.0
+    V[tail, 2] = 1.0
+    lens = (n,) * batch
+    out, lse, Q, held = attend(gv, lens, hq, d, np.tile(logits, batch), np.tile(V, (batch, 1)))
+    assert (out[:, :, 0] > 0).all()
+    check(lens[:3], out, lse, Q, held)
+    assert (out == out[0]).all() or np.allclose(out, out[0], rtol=2.0 ** -6, atol=0)
