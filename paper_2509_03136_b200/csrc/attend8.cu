@@ -29,7 +29,8 @@
 // (one warp for both took 1500 clocks a tile, its waits and commits one after the other), and warp 3 prepares the next
 // segment's Q terms (the first segment's, which everything waits for, are shared out among the softmax warps: alone,
 // warp 3 took 16,000 clocks for 20 rows).  Four warps widen V, a tile or two ahead (by the softmax warps themselves it
-// lay in their chain: five tokens 43 us instead of 39), or two groups of four in turns where few query rows make a tile short (a
+// lay in their chain: five tokens 43 us instead of 39), or two groups of four: a box of 128 channels each where
+// d_k > 128 (one token over 64K rows of 256 channels 65 -> 57 us), and in turns where few query rows make a tile short (a
 // tile takes one group 2100 clocks: one token over long rows 53 us instead of 43.5; with 12 rows and more the second group's
 // registers cost more than it brings); then come up to five softmax groups of four warps, thread = cached row of
 // the tile (and channel of the output).  A group has kR query rows: with few rows the groups take turns at the tiles, each
@@ -211,12 +212,14 @@ __device__ __forceinline__ void write_lse(const AttendArgs& a, int64_t at, float
   if (a.lse) a.lse[at] = l * 0.6931471805599453f;
 }
 
-// Counts: one arrival, 1 + 4 for every group on q_empty, four per group that shares a tile's rows from s_empty on, four from v_empty on.
+// Counts: one arrival, 1 + 4 for every group on q_empty, four per group that shares a tile's rows from s_empty on, four
+// from w_full on, on v_empty for every group that widens a part of the tile.
 struct Bars {
   uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], q_full[2], q_empty[2];
   uint64_t s_full[kMaxBuffers], p_empty[kMaxBuffers], o_full[4], w_empty[2];
   uint64_t s_empty[kMaxBuffers], p_full[kMaxBuffers], o_empty[4];
-  uint64_t v_empty[kMaxSlots], w_full[2];
+  uint64_t v_empty[kMaxSlots];
+  uint64_t w_full[2];
   uint64_t drain[2];                   // the MMAs under way of the two issuers, after a wait that ran out
 };
 constexpr int kFirstQ = 8;             // a named barrier; the softmax groups' are 1 to 5
@@ -237,17 +240,19 @@ struct Tail {
 template <int kBoxes, int kRb>          // 128-byte boxes per row; groups that share a tile's rows
 struct Layout {                         // threads, tensor memory (columns), shared memory (bytes)
   static constexpr int kTurns = kRb == 1 ? 4 : kRb == 2 ? 2 : 1, kGroups = kTurns * kRb;
-  static constexpr int kWiden = kBoxes == 1 && kRb <= 2 ? 2 : 1;       // groups that widen V, in turns
+  // groups that widen V: a box each, or tiles in turns
+  static constexpr bool kByBox = kBoxes == 2;
+  static constexpr int kWiden = kByBox || kRb <= 2 ? 2 : 1;
   static constexpr int kWarpSoftmax = kWarpWide + 4 * kWiden, kThreads = 32 * kWarpSoftmax + 128 * kGroups;
   static constexpr int kRows = kR * kRb, kBuffers = kRb <= 2 ? 4 : 2;
   static constexpr int kN1 = (3 * kRows + 15) / 16 * 16, kN2 = 4 * kRows;
   static constexpr int kO = kBuffers * kN1, kCols = kO + kTurns * kBoxes * kN2;     // O of turn i, box y: kO + (i kBoxes + y) kN2
   static constexpr int kAlloc = kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
   static constexpr int kSlot = kBoxes * kTileKeys * 128, kQ = kBoxes * kN1 * 128, kP = kN2 * kTileKeys * 2;
-  static constexpr int kWide = 2 * kSlot, kWides = kBoxes == 1 ? 2 : 1;                // a tile of V in bf16, and how many
+  static constexpr int kWide = 256 * kTileKeys;                        // a box of a tile of V in bf16; there is room for two
   static constexpr int kNanWords = kR * kBoxes * 4;                    // of a group: bits [row][channel]
   static constexpr int kSmall = kGroups * 4 * 2 * kR * 4 + 2 * kRows * 8 + 2 * kGroups * kNanWords * 4;
-  static constexpr size_t fixed() { return (size_t)2 * kQ + kBuffers * kP + kWides * kWide + kSmall + sizeof(Tail); }
+  static constexpr size_t fixed() { return (size_t)2 * kQ + kBuffers * kP + 2 * kWide + kSmall + sizeof(Tail); }
   // slots of K and V that fit; three at least: two of K, one of V
   static constexpr int kFit = (int)((227 * 1024 - fixed()) / kSlot);
   static_assert(kFit >= 3 && kAlloc >= kCols, "a row group of this size does not fit an SM");
@@ -290,8 +295,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   uint8_t* v_ring = k_ring + (size_t)a.k_slots * L::kSlot;
   uint8_t* q_sm = v_ring + (size_t)a.v_slots * L::kSlot;               // [2][box][N1 rows][128], swizzled
   uint8_t* p_sm = q_sm + 2 * L::kQ;                                    // [buffer][N2 / 8][128 keys][8 columns], bf16
-  uint8_t* wide_sm = p_sm + L::kBuffers * L::kP;                       // [buffer][channels / 8][128 keys][8 channels], bf16
-  float* red_all = reinterpret_cast<float*>(wide_sm + L::kWides * L::kWide);   // [group][4 warps][2 kR]
+  uint8_t* wide_sm = p_sm + L::kBuffers * L::kP;                       // [box, or buffer][16][128 keys][8 channels], bf16
+  float* red_all = reinterpret_cast<float*>(wide_sm + 2 * L::kWide);   // [group][4 warps][2 kR]
   float* factor_sm = red_all + L::kGroups * 4 * 2 * kR;                // [2][kRows] logit per unit of product
   int* limit_sm = reinterpret_cast<int*>(factor_sm + 2 * L::kRows);    // [2][kRows] cached rows a query row sees
   uint32_t* nan_all = reinterpret_cast<uint32_t*>(limit_sm + 2 * L::kRows);   // [2][group][kR][boxes * 4]
@@ -308,7 +313,8 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       const int at = tid * 8;
       const uint32_t count = at >= (int)offsetof(Bars, q_empty) && at < (int)offsetof(Bars, s_full) ? 1 + 4 * (L::kWiden + L::kGroups)
                              : at >= (int)offsetof(Bars, s_empty) && at < (int)offsetof(Bars, v_empty) ? 4 * kRb
-                             : at >= (int)offsetof(Bars, v_empty) && at < (int)offsetof(Bars, drain) ? 4 : 1;
+                             : at >= (int)offsetof(Bars, v_empty) && at < (int)offsetof(Bars, w_full) ? (L::kByBox ? 8 : 4)
+                             : at >= (int)offsetof(Bars, w_full) && at < (int)offsetof(Bars, drain) ? 4 : 1;
       ptx::mbar_init(reinterpret_cast<uint64_t*>(&tail->bars) + tid, count);
       ptx::fence_barrier_init();
     }
@@ -505,28 +511,32 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       for (int t = at.s0, it = at.it; ok && t < at.s1; ++t, ++it) {
         const int pb = it % L::kBuffers, turn = it % L::kTurns;
         const bool first = t - at.s0 < L::kTurns, last = t + L::kTurns >= at.s1;
-        ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.p_full[pb], (it / L::kBuffers) & 1, abort_flag) &&
-                                         wait_or_abort(&tail->bars.w_full[it % L::kWides], (it / L::kWides) & 1, abort_flag));
+        ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.p_full[pb], (it / L::kBuffers) & 1, abort_flag));
         if (ok && first) {
           ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.o_empty[turn], ((o_uses >> turn) & 1) ^ 1, abort_flag));
           o_uses ^= 1u << turn;
         }
         if (!ok) break;
-        ptx::tc_fence_after_sync();
-        if (ptx::elect_one()) {
-          const uint64_t pd = pd0 + (uint64_t)((pb * L::kP) >> 4), vd = vd0 + (uint64_t)((it % L::kWides * L::kWide) >> 4);
 #pragma unroll
-          for (int y = 0; y < kBoxes; ++y) {
+        for (int y = 0; y < kBoxes; ++y) {
+          const int wb = L::kByBox ? y : it & 1;
+          ok = ok && __all_sync(0xffffffffu, wait_or_abort(&tail->bars.w_full[wb], (L::kByBox ? it : it >> 1) & 1, abort_flag));
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          if (ptx::elect_one()) {
+            const uint64_t pd = pd0 + (uint64_t)((pb * L::kP) >> 4), vd = vd0 + (uint64_t)((wb * L::kWide) >> 4);
 #pragma unroll
             for (int k = 0; k < kTileKeys / 16; ++k)                   // 16 keys: 256 bytes of each column of chunks
-              ptx::umma_bf16(tmem + (uint32_t)(L::kO + (turn * kBoxes + y) * L::kN2), vd + (uint64_t)(y * (kTileKeys * 16) + k * 16),
-                             pd + (uint64_t)(k * 16), idesc, first && k == 0 ? 0u : 1u);
+              ptx::umma_bf16(tmem + (uint32_t)(L::kO + (turn * kBoxes + y) * L::kN2), vd + (uint64_t)(k * 16), pd + (uint64_t)(k * 16),
+                             idesc, first && k == 0 ? 0u : 1u);
+            ptx::umma_commit(&tail->bars.w_empty[wb]);
+            if (y == kBoxes - 1) {
+              ptx::umma_commit(&tail->bars.p_empty[pb]);
+              if (last) ptx::umma_commit(&tail->bars.o_full[turn]);
+            }
           }
-          ptx::umma_commit(&tail->bars.p_empty[pb]);
-          ptx::umma_commit(&tail->bars.w_empty[it % L::kWides]);
-          if (last) ptx::umma_commit(&tail->bars.o_full[turn]);
+          __syncwarp();
         }
-        __syncwarp();
       }
     }
     if (!ok) drain_mmas(&tail->bars.drain[1]);
@@ -581,10 +591,12 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     }
   } else if (warp < L::kWarpSoftmax) {
     // ------------------------------------------------------------------ the tiles of V in bf16: thread = row of the tile
-    // Tile it is group it mod kWiden's.  With two groups so is its buffer; that the slot's tile before this one has come (a wait
-    // by parity must not meet a phase two behind) follows from the buffer's: there are no fewer slots than buffers.
-    const int group = (warp - kWarpWide) >> 2, key_in = tid & 127, units = a.d_k >> 4;
-    int vs = group;
+    // Either group y has box y of every tile, or tile it is group it mod kWiden's and its buffer it mod 2; that the slot's tile
+    // before this one has come (a wait by parity must not meet a phase two behind) follows from the buffer's: there are
+    // three slots and more.
+    const int group = (warp - kWarpWide) >> 2, key_in = tid & 127, box = L::kByBox ? group : 0, units = min(8, (a.d_k >> 4) - 8 * box);
+    constexpr int kStep = L::kByBox ? 1 : L::kWiden;                   // 1 or 2
+    int vs = L::kByBox ? 0 : group;
     uint32_t v_phase = 0;
     for (; ok && !at.done(); at.next_segment()) {
       const int qb = at.seg & 1;
@@ -592,13 +604,13 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       if (!ok) break;
       const Entry x = tail->entry[qb];
       const int all_see = x.n - (x.nq - 1);
-      const int skip = (group + at.it) % L::kWiden;                    // (kWiden: 1 or 2)
-      for (int t = at.s0 + skip, it = at.it + skip; ok && t < at.s1; t += L::kWiden, it += L::kWiden) {
-        const int wb = it % L::kWides, key = t * kTileKeys + key_in;
-        ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.w_empty[wb], ((it / L::kWides) & 1) ^ 1, abort_flag) &&
+      const int skip = (group + at.it) % kStep;
+      for (int t = at.s0 + skip, it = at.it + skip; ok && t < at.s1; t += kStep, it += kStep) {
+        const int wb = L::kByBox ? box : it & 1, key = t * kTileKeys + key_in;
+        ok = __all_sync(0xffffffffu, wait_or_abort(&tail->bars.w_empty[wb], ((L::kByBox ? it : it >> 1) & 1) ^ 1, abort_flag) &&
                                          wait_or_abort(&tail->bars.v_full[vs], v_phase, abort_flag));
         if (!ok) break;
-        uint8_t* from = v_ring + (size_t)vs * L::kSlot + key_in * 128;
+        uint8_t* from = v_ring + (size_t)vs * L::kSlot + (box * kTileKeys + key_in) * 128;
         uint8_t* to = wide_sm + wb * L::kWide + key_in * 16;
         if (key >= all_see) {
           // A value behind the last row may be anything, and one that not every token sees may be NaN: neither must reach
@@ -607,7 +619,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           uint32_t* marks = nan_all + (qb * L::kGroups + turn * kRb) * L::kNanWords;       // [row][boxes * 4] of the turn's groups
 #pragma unroll 1
           for (int u = 0; u < units; ++u) {
-            uint4* place = reinterpret_cast<uint4*>(from + (u >> 3) * kTileKeys * 128 + (((u & 7) ^ (key_in & 7)) << 4));
+            uint4* place = reinterpret_cast<uint4*>(from + ((u ^ (key_in & 7)) << 4));
             if (key >= x.n) {
               *place = make_uint4(0, 0, 0, 0);
               continue;
@@ -624,12 +636,12 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             const uint32_t bits = four(bad.x) | four(bad.y) << 4 | four(bad.z) << 8 | four(bad.w) << 12;
 #pragma unroll 1
             for (int g = 0; g < L::kRows; ++g)
-              if (key < limit_sm[qb * L::kRows + g]) atomicOr(&marks[g * kBoxes * 4 + (u >> 1)], bits << (u * 16 & 31));
+              if (key < limit_sm[qb * L::kRows + g]) atomicOr(&marks[g * kBoxes * 4 + box * 4 + (u >> 1)], bits << (u * 16 & 31));
           }
         }
 #pragma unroll 1
         for (int u = 0; u < units; ++u) {                               // (unrolled, it took the others' instruction cache)
-          const uint4 c = *reinterpret_cast<const uint4*>(from + (u >> 3) * kTileKeys * 128 + (((u & 7) ^ (key_in & 7)) << 4));
+          const uint4 c = *reinterpret_cast<const uint4*>(from + ((u ^ (key_in & 7)) << 4));
           uint32_t b[8];
 #pragma unroll
           for (int j = 0; j < 4; ++j) widen_bf16x4((&c.x)[j], b[2 * j], b[2 * j + 1]);
@@ -642,7 +654,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           ptx::mbar_arrive(&tail->bars.v_empty[vs]);
           ptx::mbar_arrive(&tail->bars.w_full[wb]);
         }
-        vs += L::kWiden;
+        vs += kStep;
         if (vs >= a.v_slots) { vs -= a.v_slots; v_phase ^= 1u; }
       }
       __syncwarp();
