@@ -409,6 +409,91 @@ GVOTE_API int32_t gvote_evict(const gvote_params* p, const float* acc, const int
                     const int32_t* keep, int32_t n_recent, uint32_t* mask, int32_t* budget,
                     void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------
+ * Attention over bf16 rows, and a paged cache that gives pruned rows' memory back.  A prompt goes gvote_attend (whose lse
+ * gvote_accumulate takes) -> gvote_compress* or gvote_evict -> gvote_page_tables (mask) -> gvote_page_write; a token goes
+ * gvote_page_tables (cu_new) -> gvote_page_write -> gvote_page_attend; a slab cache compacted in place is attended to by
+ * gvote_attend (kv_len).
+ *
+ * The paged cache.  K and V [n_pages, page_rows, d_k] bf16 with element strides; a page holds rows of ONE KV head of one
+ * request, because the heads of a pruned cache differ in length (Section 3.4).  Row j of head h of request r is row
+ * j mod page_rows of page tables[r][h][j / page_rows]; kv_len[r][h] rows are held.  Pages of no head lie on a stack,
+ * free_pages[0 .. n_free).  What lies in a page behind the last row may be anything, NaN too.  An engine starts with
+ * kv_len = 0, free_pages = every page, n_free = n_pages.
+ *
+ * Restrictions of all entry points of this part: d_k a multiple of 16, at most 256 (at most 128 where max_q >
+ * GVOTE_ATTEND_FEW_Q); at most 128 query heads per KV head, 1024 KV heads, 65535 requests; strides multiples of 8 elements;
+ * page_rows a power of two, 16 to 1024; n_pages * page_rows < 2^31; max_pages * page_rows <= 2^26.  A workspace
+ * (gvote_attend_workspace_bytes, zero-filled once) is for the entry points of this part alone - between calls it holds the
+ * status word and counters that are zero - and serves one call at a time: calls, or replays of captured graphs, that may
+ * overlap on the GPU need one each. */
+#define GVOTE_ATTEND_FEW_Q 32
+typedef struct {
+  void* K;                   /* [n_pages][page_rows][d_k] bf16, device */
+  void* V;                   /* with the same strides */
+  int32_t* tables;           /* [batch][n_kv_heads][max_pages] page of every page_rows rows */
+  int32_t* kv_len;           /* [batch][n_kv_heads] rows held; values are clamped to 0 .. max_pages * page_rows */
+  int32_t* free_pages;       /* [n_pages] stack of unused pages (gvote_page_tables only) */
+  int32_t* n_free;           /* [1] its height */
+  int64_t row_stride;        /* elements between the rows of a page, and between pages */
+  int64_t page_stride;
+  int32_t n_pages;
+  int32_t page_rows;
+  int32_t max_pages;         /* entries of a table */
+  int32_t batch;
+} gvote_pages;
+
+/* Bytes of scratch the entry points of this part accept as `ws`, for queries of this size (total_q tokens in all, max_q of one
+ * request at most; 0, 0 for calls without queries) and for every call of no larger sizes.  0 on invalid arguments. */
+GVOTE_API size_t gvote_attend_workspace_bytes(const gvote_params* p, int32_t batch, int64_t total_q, int64_t max_q);
+
+/* Block tables and slot map from lengths, in one call:
+ *  1. every head is cut to cut = min(kv_len, keep) rows (keep_or_null [batch, n_kv_heads]; negative: 0): rejected draft tokens,
+ *     requests that have ended (0).  Pages without rows go back on the stack.
+ *  2. it grows by the request's new tokens, packed by cu_new_or_null [batch+1] (total_new = cu_new[batch], max_new of one
+ *     request at most), or by those of them whose bit is set in mask_or_null (a keep-mask over the new tokens, laid out with
+ *     cu_new as everywhere).  Pages come off the stack; kv_len becomes cut + new rows.
+ *  3. slots_or_null [n_kv_heads, total_new]: page * page_rows + row of each new row, -1 where the mask drops it or the token
+ *     belongs to no request.
+ * Order: the k-th of K released pages (by request, head, row) goes to free_pages[n_free + K - 1 - k]; the k-th page taken
+ * comes from free_pages[n_free + K - 1 - k]; so cutting what was grown last restores the stack.  Table entries behind the
+ * last page, and stack entries above the top, keep what they held.
+ * All or nothing: where the stack or a table is too short nothing changes, slots are -1 and the status word reads
+ * GVOTE_ERR_WORKSPACE_TOO_SMALL; where n_free is not in 0 .. n_pages, or pages would be released twice (the stack would
+ * pass n_pages), it reads GVOTE_ERR_INVALID_ARG.  Without cu_new nothing grows; mask and slots are null then. */
+GVOTE_API int32_t gvote_page_tables(const gvote_params* p, const gvote_pages* pages, const int32_t* keep_or_null,
+                          const int32_t* cu_new_or_null, int64_t total_new, int64_t max_new, const uint32_t* mask_or_null,
+                          int32_t* slots_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/* New rows into their pages: row t of head h of K_new, V_new [n_kv_heads, total_new, d_k] (bf16, element strides) to place
+ * slots[h][t]; negative: dropped.  A slot behind the last page is dropped and the status word reads GVOTE_ERR_INVALID_ARG;
+ * of rows with the same slot one is kept.  K_new, V_new must not share memory with the pages. */
+GVOTE_API int32_t gvote_page_write(const gvote_params* p, const void* K_new, const void* V_new, int64_t tok_stride, int64_t head_stride,
+                         const int32_t* slots, int64_t total_new, const gvote_pages* pages, void* ws, size_t ws_bytes, void* stream);
+
+/* Attention over the paged cache.  Q, out [total_q, n_q_heads, d_k] bf16 with element strides (tokens, heads), requests packed
+ * by cu_q [batch+1] (device), max_q of one request at most: one token, a few drafts, or the next chunk of a prompt.  A
+ * request's query tokens are the last rows of its cache (write them first): token i of n sees rows 0 .. kv_len - n + i of a
+ * head; a head with fewer rows than that leaves token i nothing, which gives out = 0, lse = -inf.  Per query head of KV head
+ * h: logits q.k / sqrt(d_k), softmax, out = sum of weight * value, rounded to bf16 once; lse_or_null [total_q, n_q_heads] = log
+ * of the softmax's denominator.  32-bit logits, references and sums; weights enter the product with the values as 16 bits (two bf16
+ * terms) in calls of few query rows (one token, or at most 64 rows of tokens x query heads per KV head) and as bf16 in
+ * larger ones.  A row that a token does not see has no influence on it, whatever it holds.  Deterministic.  Tokens of no request
+ * (before cu_q[0], behind cu_q[batch]) keep their out and lse.  Where cu_q gives a request more than max_q tokens, or a
+ * page that rows are read from does not exist, the status word reads GVOTE_ERR_INVALID_ARG and the outputs are not to be used. */
+GVOTE_API int32_t gvote_page_attend(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride,
+                          const int32_t* cu_q, int64_t total_q, int64_t max_q, const gvote_pages* pages, void* out,
+                          int64_t out_tok_stride, int64_t out_head_stride, float* lse_or_null, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/* The same over slabs: K, V [n_kv_heads, total_tokens, d_k] bf16 as in gvote_vote, request r's rows from cu_seqlens[r] on, all of
+ * them or the first kv_len_or_null [batch, n_kv_heads].  With cu_q = cu_seqlens it is a prompt's causal attention. */
+GVOTE_API int32_t gvote_attend(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride, const int32_t* cu_q,
+                     int64_t total_q, int64_t max_q, const void* K, const void* V, int64_t tok_stride, int64_t head_stride,
+                     const int32_t* cu_seqlens, const int32_t* kv_len_or_null, int32_t batch, int64_t total_tokens,
+                     int64_t max_N, void* out, int64_t out_tok_stride, int64_t out_head_stride, float* lse_or_null, void* ws,
+                     size_t ws_bytes, void* stream);
+
 /* The same pass for a caller whose tensors live in HOST memory (pinned memory gives full copy
  * speed): all pointers are host pointers, K and V are dense ([n_kv_heads, total_tokens, d_k]),
  * h is dense [total_tokens, d_h].  The call copies the inputs to device buffers it keeps in a

@@ -168,13 +168,6 @@ __host__ __device__ constexpr uint32_t instr_desc_bf16_mn(int M, int N) {
 __device__ __forceinline__ uint64_t smem_desc_mn_plain(uint32_t addr, uint32_t chunk) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(chunk >> 4) << 32) | ((uint64_t)1 << 46);
 }
-__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
 // Four floats -> the e4m3 codes nearest to them; the floats become 16 times what the codes leave.
 __device__ __forceinline__ uint32_t take_term(float (&x)[4]) {
   const uint32_t c = narrow8x4(x[0], x[1], x[2], x[3]);
@@ -769,7 +762,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
                 ptx::tmem_wait_ld();
 #pragma unroll
                 for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * shrink[j % kR] * shrink[j % kR]);
-                tmem_st_32x16(at_o, v);
+                ptx::tmem_st_32x16(at_o, v);
               }
               ptx::tmem_wait_st();
               ptx::tc_fence_before_sync();

@@ -24,7 +24,7 @@ DTYPE_F32, DTYPE_BF16 = 0, 1
 EXPORTS = (
     "gvote_workspace_bytes", "gvote_workspace_queries", "gvote_fit", "gvote_fit_update", "gvote_fit_finish", "gvote_fit_static", "gvote_sample", "gvote_project", "gvote_vote", "gvote_select",
     "gvote_compact", "gvote_pack", "gvote_overlap", "gvote_compress", "gvote_compress_moments", "gvote_recompress", "gvote_cache_workspace_bytes", "gvote_store8", "gvote_prune8", "gvote_append8", "gvote_attend8",
-    "gvote_accumulate", "gvote_evict", "gvote_compress_host", "gvote_host_arena_release",
+    "gvote_accumulate", "gvote_evict", "gvote_attend_workspace_bytes", "gvote_page_tables", "gvote_page_write", "gvote_page_attend", "gvote_attend", "gvote_compress_host", "gvote_host_arena_release",
     "gvote_poll_status", "gvote_clear_status", "gvote_exact_heads", "gvote_profile_enable", "gvote_profile_report", "gvote_launch_count", "gvote_status_string", "gvote_last_cuda_error",
 )
 
@@ -81,6 +81,43 @@ class Cache8:
         object.__setattr__(self, name, value)
 
 
+class GVotePages(ctypes.Structure):
+    """Mirror of `gvote_pages`."""
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("tables", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+        ("free_pages", ctypes.c_void_p), ("n_free", ctypes.c_void_p), ("row_stride", ctypes.c_int64),
+        ("page_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("batch", ctypes.c_int32),
+    ]
+
+
+class PageCache:
+    """A paged cache: pages K, V (bfloat16 [n_pages, page_rows, d_k]), tables (int32 [batch, n_kv_heads, max_pages]), rows
+    held kv_len (int32 [batch, n_kv_heads]) and the stack of unused pages free (int32 [n_pages]) of height n_free (int32 [1]).
+    `alloc_pages` makes one.  The tensors are checked here, once; the entry points take the finished argument block."""
+    __slots__ = ("K", "V", "tables", "kv_len", "free", "n_free", "shape", "device", "args")
+
+    def __init__(self, K, V, tables, kv_len, free, n_free):
+        n_pages, page_rows, d = K.shape
+        batch, H, max_pages = tables.shape
+        if K.stride() != V.stride():
+            raise ValueError("K and V must share strides")
+        dev = K.device
+        self.args = GVotePages(
+            _shaped(K, torch.bfloat16, (n_pages, page_rows, d), "K", dev, dense=False),
+            _shaped(V, torch.bfloat16, (n_pages, page_rows, d), "V", dev, dense=False),
+            _shaped(tables, torch.int32, (batch, H, max_pages), "tables", dev),
+            _shaped(kv_len, torch.int32, (batch, H), "kv_len", dev), _shaped(free, torch.int32, (n_pages,), "free", dev),
+            _shaped(n_free, torch.int32, (1,), "n_free", dev), K.stride(1), K.stride(0), n_pages, page_rows, max_pages, batch)
+        self.K, self.V, self.tables, self.kv_len, self.free, self.n_free = K, V, tables, kv_len, free, n_free
+        self.shape, self.device = (H, d), dev
+
+    def __setattr__(self, name, value):
+        if hasattr(self, name):
+            raise AttributeError(f"{name} of a PageCache is fixed (its pointers are taken once): make another PageCache")
+        object.__setattr__(self, name, value)
+
+
 class GVoteError(RuntimeError):
     def __init__(self, status: int, where: str):
         lib = load()
@@ -100,6 +137,7 @@ def load():
                            "(there is no fallback path)")
     lib = ctypes.CDLL(_LIB_PATH)
     C8 = ctypes.POINTER(GVoteCache8)
+    PG = ctypes.POINTER(GVotePages)
     P, vp, i32, i64, sz = ctypes.POINTER(GVoteParams), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     lib.gvote_workspace_bytes.restype = sz
     lib.gvote_workspace_bytes.argtypes = [P, i32, i64, i64]
@@ -151,6 +189,17 @@ def load():
                                      sz, vp]
     lib.gvote_evict.restype = i32
     lib.gvote_evict.argtypes = [P, vp, vp, vp, i32, i64, i64, vp, i32, vp, vp, vp, sz, vp]
+    lib.gvote_attend_workspace_bytes.restype = sz
+    lib.gvote_attend_workspace_bytes.argtypes = [P, i32, i64, i64]
+    lib.gvote_page_tables.restype = i32
+    lib.gvote_page_tables.argtypes = [P, PG, vp, vp, i64, i64, vp, vp, vp, sz, vp]
+    lib.gvote_page_write.restype = i32
+    lib.gvote_page_write.argtypes = [P, vp, vp, i64, i64, vp, i64, PG, vp, sz, vp]
+    lib.gvote_page_attend.restype = i32
+    lib.gvote_page_attend.argtypes = [P, vp, i64, i64, vp, i64, i64, PG, vp, i64, i64, vp, vp, sz, vp]
+    lib.gvote_attend.restype = i32
+    lib.gvote_attend.argtypes = [P, vp, i64, i64, vp, i64, i64, vp, vp, i64, i64, vp, vp, i32, i64, i64, vp, i64, i64, vp,
+                                 vp, sz, vp]
     lib.gvote_compress_host.restype = i32
     lib.gvote_compress_host.argtypes = [P, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     lib.gvote_host_arena_release.restype = None
@@ -289,6 +338,27 @@ def alloc_cache_workspace(p: GVoteParams, batch: int, total_tokens: int, max_N: 
     return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
+ATTEND_FEW_Q = 32
+
+
+def alloc_pages(p: GVoteParams, batch: int, n_pages: int, page_rows: int, max_pages: int, device="cuda") -> PageCache:
+    """An empty paged cache: every page unused, tables of max_pages pages per head, the first page on top of the stack."""
+    K, V = (torch.zeros(n_pages, page_rows, p.d_k, dtype=torch.bfloat16, device=device) for _ in range(2))
+    return PageCache(K, V, torch.zeros(batch, p.n_kv_heads, max_pages, dtype=torch.int32, device=device),
+                     torch.zeros(batch, p.n_kv_heads, dtype=torch.int32, device=device),
+                     torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device),
+                     torch.full((1,), n_pages, dtype=torch.int32, device=device))
+
+
+def alloc_attend_workspace(p: GVoteParams, batch: int, total_q: int = 0, max_q: int = 0, device="cuda") -> torch.Tensor:
+    """A zero-filled workspace for the entry points of the paged cache and for gvote_attend: total_q query tokens in all and at
+    most max_q of one request.  It is for these entry points alone."""
+    n = int(load().gvote_attend_workspace_bytes(ctypes.byref(p), batch, total_q, max_q))
+    if n == 0:
+        raise GVoteError(-1, "gvote_attend_workspace_bytes")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
 def _shaped(t: Optional[torch.Tensor], dtype, shape, name: str, dev: torch.device, dense: bool = True) -> Optional[int]:
     """The pointer of a tensor of this type and shape on `dev`; None stays None."""
     if t is None:
@@ -312,6 +382,14 @@ def _cache8(p, c: Cache8, name: str, dev: torch.device):
     if c.shape != (p.n_kv_heads, p.d_k):
         raise ValueError(f"{name} holds {c.shape[0]} heads of {c.shape[1]} values, the parameters say "
                          f"{p.n_kv_heads} of {p.d_k}")
+    return ctypes.byref(c.args)
+
+
+def _pages(p, c: PageCache, dev: torch.device):
+    if c.device != dev:
+        raise ValueError(f"pages are on {c.device}, must be on {dev}")
+    if c.shape != (p.n_kv_heads, p.d_k):
+        raise ValueError(f"pages hold {c.shape[0]} heads of {c.shape[1]} values, the parameters say {p.n_kv_heads} of {p.d_k}")
     return ctypes.byref(c.args)
 
 
@@ -566,6 +644,57 @@ def gvote_evict(p, acc, cu_seqlens, geom, keep, n_recent: int, mask, budget, ws,
             _shaped(keep, torch.int32, (batch, H), "keep", dev), n_recent,
             _shaped(mask, torch.int32, (H, mask_row_words(total, batch)), "mask", dev),
             _shaped(budget, torch.int32, (batch, H), "budget", dev), ws=ws)
+
+
+def gvote_page_tables(p, pages: PageCache, ws, keep=None, cu_new=None, max_new: int = 0, slots=None, mask=None) -> None:
+    """Cuts every head to keep [batch, n_kv_heads] rows, then grows it by the request's new tokens (packed by cu_new, at most
+    max_new of one request), or by those that mask keeps; slots [n_kv_heads, total_new] says where each new row goes."""
+    H, dev, batch = p.n_kv_heads, pages.device, pages.tables.shape[0]
+    if cu_new is not None and slots is None:
+        raise ValueError("cu_new needs slots")
+    total_new = 0 if slots is None else slots.shape[1]
+    _launch(load().gvote_page_tables, dev, p, _pages(p, pages, dev), _shaped(keep, torch.int32, (batch, H), "keep", dev),
+            _shaped(cu_new, torch.int32, (batch + 1,), "cu_new", dev), total_new, max_new,
+            _shaped(mask, torch.int32, (H, mask_row_words(total_new, batch)), "mask", dev),
+            _shaped(slots, torch.int32, (H, total_new), "slots", dev), ws=ws)
+
+
+def gvote_page_write(p, K_new, V_new, slots, pages: PageCache, ws) -> None:
+    """Rows of K_new, V_new [n_kv_heads, total_new, d_k] to the places slots [n_kv_heads, total_new] names (negative: dropped)."""
+    H, total_new, dev = p.n_kv_heads, K_new.shape[1], pages.device
+    if total_new and K_new.stride() != V_new.stride():
+        raise ValueError("K_new and V_new must share strides")
+    _launch(load().gvote_page_write, dev, p, _shaped(K_new, torch.bfloat16, (H, total_new, p.d_k), "K_new", dev, dense=False),
+            _shaped(V_new, torch.bfloat16, (H, total_new, p.d_k), "V_new", dev, dense=False), K_new.stride(1), K_new.stride(0),
+            _shaped(slots, torch.int32, (H, total_new), "slots", dev), total_new, _pages(p, pages, dev), ws=ws)
+
+
+def gvote_page_attend(p, Q, cu_q, max_q: int, pages: PageCache, out, ws, lse=None) -> None:
+    """Attention of Q [total_q, n_q_heads, d_k] (a request's tokens are the last rows of its cache) over the pages into out."""
+    total_q, dev = Q.shape[0], pages.device
+    shape = (total_q, p.n_q_heads, p.d_k)
+    _launch(load().gvote_page_attend, dev, p, _shaped(Q, torch.bfloat16, shape, "Q", dev, dense=False), Q.stride(0), Q.stride(1),
+            _shaped(cu_q, torch.int32, (pages.tables.shape[0] + 1,), "cu_q", dev), total_q, max_q, _pages(p, pages, dev),
+            _shaped(out, torch.bfloat16, shape, "out", dev, dense=False), out.stride(0), out.stride(1),
+            _shaped(lse, torch.float32, (total_q, p.n_q_heads), "lse", dev), ws=ws)
+
+
+def gvote_attend(p, Q, cu_q, max_q: int, K, V, cu_seqlens, geom, out, ws, lse=None, kv_len=None) -> None:
+    """Attention of Q [total_q, n_q_heads, d_k] (a request's tokens are the last of its rows) over the bf16 slabs K, V: a
+    prompt's causal attention, or tokens over a cache compacted in place (kv_len)."""
+    batch, total, max_N = geom
+    H, total_q, dev = p.n_kv_heads, Q.shape[0], K.device
+    shape = (total_q, p.n_q_heads, p.d_k)
+    if total and K.stride() != V.stride():
+        raise ValueError("K and V must share strides")
+    _launch(load().gvote_attend, dev, p, _shaped(Q, torch.bfloat16, shape, "Q", dev, dense=False), Q.stride(0), Q.stride(1),
+            _shaped(cu_q, torch.int32, (batch + 1,), "cu_q", dev), total_q, max_q,
+            _shaped(K, torch.bfloat16, (H, total, p.d_k), "K", dev, dense=False),
+            _shaped(V, torch.bfloat16, (H, total, p.d_k), "V", dev, dense=False), K.stride(1), K.stride(0),
+            _shaped(cu_seqlens, torch.int32, (batch + 1,), "cu_seqlens", dev),
+            _shaped(kv_len, torch.int32, (batch, H), "kv_len", dev), batch, total, max_N,
+            _shaped(out, torch.bfloat16, shape, "out", dev, dense=False), out.stride(0), out.stride(1),
+            _shaped(lse, torch.float32, (total_q, p.n_q_heads), "lse", dev), ws=ws)
 
 
 def gvote_compress_host(p, h, W_q, b_q, K, V, cu_seqlens, mask, budget, b_step) -> None:
