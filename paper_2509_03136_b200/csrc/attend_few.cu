@@ -8,8 +8,9 @@
 // kGap tiles for what beginning one costs; CTA b of B takes the tiles from T b / B to T (b + 1) / B of the T places.  So heads
 // of very different length load every SM alike, and the lengths stay on the device.  What a CTA has of an entry is a segment.  An
 // entry within one CTA goes straight to the output; of the others every segment leaves its reference, sum and output in slot
-// entry + CTA, and the CTA that arrives last at the entry's counter adds them up in their order, so the result does not depend on
-// which one that is.
+// entry + CTA, and of kFan neighbouring segments the CTA that arrives last at their counter adds them up in their order, then
+// of up to kFan such sums.  So the result does not depend on which CTA that is, and the 74 segments of a long row are not one
+// CTA's work (one after the other they took 36 of 81 us).
 //
 // A CTA: four warps that compute and one that asks for tiles (TMA, 128-byte swizzle, boxes of a page or of 64 rows) into a ring
 // of units, K and V of a tile one unit each.  The products are mma.sync m16n8k16 with the query rows on M: a tile of one KV head
@@ -31,6 +32,8 @@ constexpr int kWarps = 4;                       // that compute
 constexpr int kThreads = 32 * (kWarps + 1);
 constexpr int kMaxUnits = 8;
 constexpr int kGap = 1;
+constexpr int kFan = 18;                        // two rounds join every segment of a launch
+static_assert(kFan * kFan >= kFewCtas, "");
 constexpr float kSlack = 8.f;
 
 struct FewArgs {
@@ -43,7 +46,7 @@ struct FewArgs {
   float* lse;            // or null
   float* part_o;         // [groups][entries + CTAs][rows of a group][d_k]
   float2* part_ml;       // [groups][entries + CTAs][rows of a group]
-  int32_t* arrived;      // [groups][entries], zero between calls
+  int32_t* arrived;      // [groups][kFewEntries + kFewCtas: first rounds, by slot][kFewEntries: second rounds], zero between calls
   int32_t* status;
   int Hq, Hkv, G, r0, batch, d_k, max_q;        // requests r0 .. r0 + batch - 1
   int group0, box_rows;                         // this launch's first group of query rows
@@ -71,6 +74,7 @@ struct Tail {
   Bars bars;
   volatile int stop;
   int last_one, odd;                            // odd: values that are not finite were taken out
+  float2 join[kFan][32];                        // references and sums of the segments that are joined
   int warp_sums[kThreads / 32];
   float2 ml[kWarps][32];
   int pref[kFewEntries + 1];
@@ -497,46 +501,65 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           if (c == 0) a.part_ml[slot * L::kRows + lr] = make_float2(top, total);
         }
       }
-      if (first != last) {
+      // the joins: of kFan segments, then of as many joined ones as there are
+      const int segs = last - first + 1;
+      int32_t* counts = a.arrived + (int64_t)blockIdx.y * (2 * kFewEntries + kFewCtas);
+      int k0 = (b - first) / kFan * kFan, n = min(segs - k0, kFan), apart = 1;      // the segments k0, k0 + apart, ..: n of them
+      int32_t* count = counts + w.e + first + k0;
+      while (segs > 1) {
         __threadfence();
         ptx::named_barrier_sync(1, 32 * kWarps);
         if (tid == 0) {
-          int32_t* count = a.arrived + (int64_t)blockIdx.y * entries + w.e;
           const int before = atomicAdd(count, 1);
-          tail->last_one = before == last - first;
-          if (before == last - first) *count = 0;
-          __threadfence();
+          tail->last_one = before == n - 1;
+          if (before == n - 1) *count = 0;
         }
         ptx::named_barrier_sync(1, 32 * kWarps);
-        if (tail->last_one) {
-          __threadfence();
-          const int64_t s_first = slot0 + w.e + first;
-          const int segs = last - first + 1;
-          for (int i = tid; i < rows * quads; i += 32 * kWarps) {
-            const int lr = i / quads, c = (i - lr * quads) * 4, row = row0 + lr, token = row / a.G, head = x.h * a.G + row - token * a.G;
-            const float2* ml = a.part_ml + s_first * L::kRows + lr;
-            const float* po = a.part_o + (s_first * L::kRows + lr) * a.d_k + c;
-            float top = -INFINITY;
-#pragma unroll 4
-            for (int k = 0; k < segs; ++k) top = fmaxf(top, __ldcg(ml + (int64_t)k * L::kRows).x);
-            const float off = top == -INFINITY ? 0.f : top;
-            float total = 0.f;
-            float4 r = make_float4(0, 0, 0, 0);
-#pragma unroll 4
-            for (int k = 0; k < segs; ++k) {
-              const float2 q = __ldcg(ml + (int64_t)k * L::kRows);
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(po + (int64_t)k * L::kRows * a.d_k));
-              const float f = exp2_approx(q.x - off);
-              total = fmaf(q.y, f, total);
-              r.x += scaled(v.x, f); r.y += scaled(v.y, f); r.z += scaled(v.z, f); r.w += scaled(v.w, f);
-            }
+        if (!tail->last_one) break;
+        __threadfence();
+        const bool final = segs <= kFan || apart > 1;
+        const int64_t s0 = slot0 + w.e + first + k0;
+        for (int i = tid; i < n * L::kRows; i += 32 * kWarps)
+          tail->join[i / L::kRows][i % L::kRows] = __ldcg(a.part_ml + (s0 + (int64_t)(i / L::kRows) * apart) * L::kRows + i % L::kRows);
+        ptx::named_barrier_sync(1, 32 * kWarps);
+        for (int i = tid; i < rows * quads; i += 32 * kWarps) {
+          const int lr = i / quads, c = (i - lr * quads) * 4, row = row0 + lr, token = row / a.G, head = x.h * a.G + row - token * a.G;
+          float* po = a.part_o + (s0 * L::kRows + lr) * a.d_k + c;
+          float top = -INFINITY, total = 0.f;
+          for (int k = 0; k < n; ++k) top = fmaxf(top, tail->join[k][lr].x);
+          const float off = top == -INFINITY ? 0.f : top;
+          float4 r = make_float4(0, 0, 0, 0);
+#pragma unroll 1
+          for (int k1 = 0; k1 < n; k1 += 6) {                      // six loads on their way
+            float4 v[6];
+#pragma unroll
+            for (int k = 0; k < 6; ++k)
+              if (k1 + k < n) v[k] = __ldcg(reinterpret_cast<const float4*>(po + (int64_t)(k1 + k) * apart * L::kRows * a.d_k));
+#pragma unroll
+            for (int k = 0; k < 6; ++k)
+              if (k1 + k < n) {
+                const float2 q = tail->join[k1 + k][lr];
+                const float f = exp2_approx(q.x - off);
+                total = fmaf(q.y, f, total);
+                r.x += scaled(v[k].x, f); r.y += scaled(v[k].y, f); r.z += scaled(v[k].z, f); r.w += scaled(v[k].w, f);
+              }
+          }
+          if (final) {
             if (total == 0.f) r = make_float4(0, 0, 0, 0);
             const float inv = total == 0.f ? 0.f : 1.f / total;
             *reinterpret_cast<uint2*>(a.out + (int64_t)(x.q0 + token) * a.o_tok + (int64_t)head * a.o_head + c) =
                 make_uint2(bf16_pair(r.x * inv, r.y * inv), bf16_pair(r.z * inv, r.w * inv));
             if (a.lse && c == 0) a.lse[(int64_t)(x.q0 + token) * a.Hq + head] = total == 0.f ? -INFINITY : off * 0.6931471805599453f + logf(total);
+          } else {
+            *reinterpret_cast<float4*>(po) = r;                    // (nobody else reads these slots any more)
+            if (c == 0) a.part_ml[s0 * L::kRows + lr] = make_float2(top, total);
           }
         }
+        if (final) break;
+        count = counts + kFewEntries + kFewCtas + w.e;
+        n = (segs + kFan - 1) / kFan;
+        k0 = 0;
+        apart = kFan;
       }
       if (tid == 0) tail->odd = 0;                                 // (everyone has read it: a barrier lies behind)
       ptx::named_barrier_sync(1, 32 * kWarps);

@@ -39,7 +39,7 @@ constexpr int kMaxStages = 12;
 constexpr int kInfos = 4;
 constexpr int kMarks = 8;                 // more than the tiles of V a ring holds
 static_assert(kMaxStages / 2 < kMarks, "");
-constexpr int kPoly = 2;                  // of 8 exponentials, those computed on the FMA pipe
+constexpr int kPoly = 1;                  // of 8 exponentials, those computed on the FMA pipe
 constexpr float kSlack = 8.f;
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(kSoftmaxRegs * 256 + kOtherRegs * 128 <= 168 * kThreads, "the registers a CTA is launched with");
@@ -130,6 +130,16 @@ template <int kRegs>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 template <int kRegs>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+
+// A place in the ring: slot and parity, without divisions (by a number that is not known here one takes a hundred clocks).
+struct Place {
+  uint32_t slot, parity;
+  int stages;
+  __device__ __forceinline__ explicit Place(int n) : slot(0), parity(0), stages(n) {}
+  __device__ __forceinline__ void step() {
+    if (++slot == (uint32_t)stages) { slot = 0; parity ^= 1; }
+  }
+};
 
 // A reader of the unit list.
 struct Units {
@@ -225,6 +235,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       // ---------------------------------------------------------------- asks for tiles
       Units units(tail);
       Unit x;
+      Place at(a.stages);
       uint32_t it = 0, asked_q = 0, raw = 0;
       bool ok = true, bad_page = false;
       const int boxes = (a.d_k + 63) >> 6, box = lane % boxes, part = lane / boxes;
@@ -258,9 +269,10 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           if (table && mine && (uint32_t)page >= (uint32_t)a.src.n_pages) bad_page = true;   // (the copy reads zeros)
 #pragma unroll
           for (int v = 0; v < 2; ++v, ++it) {
-            const uint32_t s = it % a.stages;
-            ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->empty[s], ((it / a.stages) & 1) ^ 1, stop));
+            const uint32_t s = at.slot;
+            ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->empty[s], at.parity ^ 1, stop));
             if (!ok) break;
+            at.step();
             // (values that warp 10 has to look at first: it tells when they are there)
             uint64_t* bar = v && t >= masked_from ? &tail->v_raw[raw++ % kMarks] : &tail->full[s];
             if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(parts * boxes * a.box_rows * 128));
@@ -286,21 +298,22 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       // ---------------------------------------------------------------- issues the MMAs
       Units units(tail);
       Unit x;
-      uint32_t it = 0, n_q = 0, n_p[2] = {0, 0};
+      Place at(a.stages);
+      uint32_t n_q = 0, n_p[2] = {0, 0};
       bool ok = true;
       const uint32_t idesc_s = ptx::instr_desc_bf16_f32(kTile, kTile);
       const uint32_t idesc_o = ptx::instr_desc_bf16_f32(kTile, a.d_k) | (1u << 16);     // V: channels contiguous
-      const int ksteps = a.d_k / 16;
       const uint32_t q_addr = ptx::smem_u32(q_sm), ring_addr = ptx::smem_u32(ring);
       auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_or_stop(bar, parity, stop)); };
+      const uint64_t qd0 = ptx::smem_desc_k_sw128(q_addr), kd0 = ptx::smem_desc_k_sw128(ring_addr);
+      // (channels behind d_k are zero: every step is taken)
       auto product_qk = [&](int i, uint32_t slot) {
+        const uint64_t qd = qd0 + (uint64_t)(i * (int)(kTileBytes >> 4)), kd = kd0 + (uint64_t)(slot * (kTileBytes >> 4));
         if (ptx::elect_one()) {
-          uint64_t ad = ptx::smem_desc_k_sw128(q_addr + i * kTileBytes), bd = ptx::smem_desc_k_sw128(ring_addr + slot * kTileBytes);
 #pragma unroll
-          for (int b = 0; b < kBoxes; ++b, ad += kTile * 128 / 16, bd += kTile * 128 / 16) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              if (b * 4 + q < ksteps) ptx::umma_bf16(tmem + i * kTile, ad + q * 2, bd + q * 2, idesc_s, b + q > 0 ? 1u : 0u);
+          for (int q = 0; q < kBoxes * 4; ++q) {
+            const int to = (q >> 2) * (kTile * 128 / 16) + (q & 3) * 2;
+            ptx::umma_bf16(tmem + i * kTile, qd + to, kd + to, idesc_s, q > 0 ? 1u : 0u);
           }
           ptx::umma_commit(&tail->s_full[i]);
         }
@@ -311,9 +324,9 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (tiles == 0) continue;
         ok = wait(&tail->q_full, n_q & 1);
         ++n_q;
-        uint32_t k_slot = it % a.stages;
-        ok = ok && wait(&tail->full[k_slot], (it / a.stages) & 1);
-        ++it;
+        uint32_t k_slot = at.slot;
+        ok = ok && wait(&tail->full[k_slot], at.parity);
+        at.step();
         if (!ok) break;
         ptx::tc_fence_after_sync();
 #pragma unroll
@@ -325,15 +338,10 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
         __syncwarp();
         for (int t = 0; ok && t < tiles; ++t) {
-          const uint32_t v_slot = it % a.stages;
-          ok = wait(&tail->full[v_slot], (it / a.stages) & 1);
-          ++it;
+          const uint32_t v_slot = at.slot;
+          ok = wait(&tail->full[v_slot], at.parity);
+          at.step();
           const bool more = t + 1 < tiles;
-          if (more) {
-            k_slot = it % a.stages;
-            ok = ok && wait(&tail->full[k_slot], (it / a.stages) & 1);
-            ++it;
-          }
           if (!ok) break;
           const uint64_t vd = smem_desc_mn_sw128(ring_addr + v_slot * kTileBytes, kTile * 128);
 #pragma unroll
@@ -358,6 +366,12 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 ptx::umma_commit(&tail->pv_done[i]);
               }
               __syncwarp();
+            }
+            if (i == 0 && more) {
+              k_slot = at.slot;
+              ok = wait(&tail->full[k_slot], at.parity);
+              at.step();
+              if (!ok) break;
             }
             if (t + 1 < x.tiles[i]) product_qk(i, k_slot);
           }

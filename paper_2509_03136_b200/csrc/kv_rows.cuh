@@ -14,8 +14,9 @@ constexpr int kNumSms = 148;
 // The few-row kernel: entries of a launch (their tiles are added up in shared memory) and groups of query rows.
 constexpr int kFewEntries = 1024;
 constexpr int kFewGroups = 4;
+constexpr int kFewCtas = 2 * kNumSms;
 // Behind the status block of a workspace: arrival counters, zero between calls; then the scratch of one call.
-constexpr size_t kScratchAt = kStatusBytes + (size_t)kFewGroups * kFewEntries * 4;
+constexpr size_t kScratchAt = kStatusBytes + (size_t)kFewGroups * (2 * kFewEntries + kFewCtas) * 4;
 
 // Cached rows, in slabs (K, V [n_kv_heads][total][d_k], request r's rows from cu[r] on) or in pages (K, V
 // [n_pages][page_rows][d_k], row j of (r, h) in page tables[r][h][j / page_rows]).
