@@ -199,6 +199,8 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   __syncthreads();
   ptx::tc_fence_after_sync();
   const uint32_t tmem = __shfl_sync(0xffffffffu, tail->tmem_slot, 0);
+  ptx::let_next_begin();
+  ptx::wait_for_previous();
 
   if (warp >= 8) {
     fewer_registers<kOtherRegs>();
@@ -589,7 +591,7 @@ int32_t launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& 
   GVOTE_CUDA_CHECK(cudaFuncSetAttribute(attend_many_kernel<kBoxes>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   LaunchScope scope_("attend_many_kernel", st);
   const unsigned grid = a.units < (uint32_t)kNumSms ? a.units : (unsigned)kNumSms;
-  (void)launch_on(attend_many_kernel<kBoxes>, dim3(grid), dim3(kThreads), smem, st, tq, tk, tv, a);
+  (void)launch_behind(attend_many_kernel<kBoxes>, dim3(grid), dim3(kThreads), smem, st, tq, tk, tv, a);
   GVOTE_LAUNCH_CHECK("attend_many_kernel");
   return GVOTE_OK;
 }

@@ -102,6 +102,7 @@ page_plan_kernel(const __grid_constant__ TableArgs a) {
   const int tid = threadIdx.x, log2 = a.p.page_log2;
   const int64_t entries = (int64_t)a.p.batch * a.p.Hkv;
   const int ctas = gridDim.x, me = blockIdx.x;                   // (one cluster)
+  ptx::let_next_begin();
   ptx::wait_for_previous();
   auto sync_all = [&] { if (ctas > 1) cooperative_groups::this_cluster().sync(); else __syncthreads(); };
 
@@ -202,6 +203,7 @@ page_count_kernel(const __grid_constant__ TableArgs a) {
   __shared__ int part[kSlotThreads / 32];
   const int h = blockIdx.x, r = blockIdx.y;
   ptx::let_next_begin();
+  ptx::wait_for_previous();
   const int start = a.cu_new[r], n = a.cu_new[r + 1] - start;
   const uint32_t* words = a.mask + (int64_t)h * a.mask_words + mask_word_offset(start, r);
   int sum = 0;
@@ -225,6 +227,7 @@ page_slots_kernel(const __grid_constant__ TableArgs a) {
   __shared__ int rank_of[kSlotTokens / 32];
   const int h = blockIdx.y, tid = threadIdx.x, log2 = a.p.page_log2;
   const int64_t g = blockIdx.x;
+  ptx::let_next_begin();
   ptx::wait_for_previous();
   // tile g of a list with (cu[r] >> 12) + r as the first of request r
   int lo = 0, hi = a.p.batch - 1;
@@ -291,6 +294,8 @@ page_write_kernel(const __nv_bfloat16* __restrict__ K, const __nv_bfloat16* __re
                   int64_t page_stride, int page_log2, int64_t n_slots, int pieces, int lanes_log2, int32_t* status) {
   const int lane = threadIdx.x & 31, h = blockIdx.y;
   const int64_t t0 = ((int64_t)blockIdx.x * (kWriteThreads / 32) + (threadIdx.x >> 5)) * 32;
+  ptx::let_next_begin();
+  ptx::wait_for_previous();
   if (t0 >= total) return;
   const int slot = t0 + lane < total ? slots[h * total + t0 + lane] : -1;
   const bool is_bad = (int64_t)slot >= n_slots;
@@ -349,7 +354,7 @@ int32_t launch_page_tables(const PageArgs& p, const int32_t* keep, const int32_t
   a.slots_here = n_slots > 0 && !mask && n_slots <= 8 * 1024 ? 1 : 0;
   if (mask) {
     LaunchScope scope_("page_count_kernel", st);
-    (void)launch_on(page_count_kernel, dim3(p.Hkv, p.batch), dim3(kSlotThreads), 0, st, a);
+    (void)launch_behind(page_count_kernel, dim3(p.Hkv, p.batch), dim3(kSlotThreads), 0, st, a);
     GVOTE_LAUNCH_CHECK("page_count_kernel");
   }
   {
@@ -364,14 +369,14 @@ int32_t launch_page_tables(const PageArgs& p, const int32_t* keep, const int32_t
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = mask ? 2 : 1;
+    cfg.numAttrs = 2;
     LaunchScope scope_("page_plan_kernel", st);
     (void)cudaLaunchKernelEx(&cfg, page_plan_kernel, a);
   }
   GVOTE_LAUNCH_CHECK("page_plan_kernel");
   if (n_slots > 0 && !a.slots_here) {
     LaunchScope scope_("page_slots_kernel", st);
-    (void)launch_on(page_slots_kernel, dim3((unsigned)((total_new >> 12) + p.batch), p.Hkv), dim3(kSlotThreads), 0, st, a);
+    (void)launch_behind(page_slots_kernel, dim3((unsigned)((total_new >> 12) + p.batch), p.Hkv), dim3(kSlotThreads), 0, st, a);
     GVOTE_LAUNCH_CHECK("page_slots_kernel");
   }
   return GVOTE_OK;
@@ -385,7 +390,7 @@ int32_t launch_page_write(const gvote_params* p, const __nv_bfloat16* K, const _
   int lanes_log2 = 1;
   while ((1 << lanes_log2) < pieces) ++lanes_log2;
   LaunchScope scope_("page_write_kernel", st);
-  (void)launch_on(page_write_kernel, dim3((unsigned)ceil_div(total_new, kWriteThreads), p->n_kv_heads), dim3(kWriteThreads), 0, st,
+  (void)launch_behind(page_write_kernel, dim3((unsigned)ceil_div(total_new, kWriteThreads), p->n_kv_heads), dim3(kWriteThreads), 0, st,
                   K, V, tok, head, slots, total_new, K_out, V_out, row_stride, page_stride, page_log2, n_slots, pieces, lanes_log2,
                   status);
   GVOTE_LAUNCH_CHECK("page_write_kernel");
