@@ -112,7 +112,7 @@ int32_t gvote_page_attend(const gvote_params* p, const void* Q, int64_t q_tok_st
   s.kv_len = pages->kv_len; s.tables = pages->tables;
   s.n_pages = pages->n_pages; s.page_log2 = log2_of(pages->page_rows); s.max_pages = pages->max_pages;
   const AttendCall c{(const __nv_bfloat16*)Q, q_tok_stride, q_head_stride, cu_q, total_q, max_q, (__nv_bfloat16*)out, out_tok_stride,
-                     out_head_stride, lse_or_null, pages->batch};
+                     out_head_stride, lse_or_null, pages->batch, (int64_t)pages->max_pages * pages->page_rows};
   return attend(p, c, s, ws, ws_bytes, stream);
 }
 
@@ -138,7 +138,7 @@ int32_t gvote_attend(const gvote_params* p, const void* Q, int64_t q_tok_stride,
   s.tok = tok_stride; s.outer = head_stride;
   s.cu = cu_seqlens; s.kv_len = kv_len_or_null; s.total = total_tokens;
   const AttendCall c{(const __nv_bfloat16*)Q, q_tok_stride, q_head_stride, cu_q, total_q, max_q, (__nv_bfloat16*)out, out_tok_stride,
-                     out_head_stride, lse_or_null, batch};
+                     out_head_stride, lse_or_null, batch, max_N};
   return attend(p, c, s, ws, ws_bytes, stream);
 }
 

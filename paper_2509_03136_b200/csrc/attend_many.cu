@@ -41,6 +41,12 @@ constexpr int kMarks = 8;                 // more than the tiles of V a ring hol
 static_assert(kMaxStages / 2 < kMarks, "");
 constexpr int kPoly = 1;                  // of 8 exponentials, those computed on the FMA pipe
 constexpr float kSlack = 8.f;
+// Cut lists (where there are few units): units of a list, places that a unit's beginning and end count as, and what a join takes.
+constexpr int kCutUnits = 2 * kNumSms;
+constexpr int kGap = 3;
+constexpr int kPiece = 8;                 // places of a CTA at least
+constexpr int kFan = 13;                  // two rounds join the segments of a unit
+static_assert(kFan * kFan >= kNumSms && (size_t)kCutUnits * 2 * (kFan + 1) * 4 <= kScratchAt - kStatusBytes, "");
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(kSoftmaxRegs * 256 + kOtherRegs * 128 <= 168 * kThreads, "the registers a CTA is launched with");
 
@@ -55,15 +61,20 @@ struct ManyArgs {
   int tpt;                // tokens of a query tile
   uint32_t pairs, units;  // pairs of tiles (upper bound), times KV heads
   int stages, box_rows;
+  float4* part_o;         // [2 per CTA][2 tiles][d_k / 4][128 rows]
+  float2* part_ml;        // [2 per CTA][2 tiles][128 rows]  (reference, sum), base 2
+  int32_t* arrived;       // [units][2 tiles][kFan: first rounds, then the second], zero between calls
   float c;                // log2(e) / sqrt(d_k)
 };
 
 struct Unit {
   int r, h, seq;
+  int k0;                 // first tile of keys
+  int id, first, segs;    // in a cut list: the unit, the first CTA that has a piece of it, the pieces
   int tok0;               // first token of the first tile, in the packed list
   int count[2];           // tokens of the tiles
   int see[2];             // rows a tile's first token sees (may be negative)
-  int tiles[2];           // tiles of keys
+  int tiles[2];           // tiles of keys, from k0 on
   int n;                  // rows the last token sees
 };
 
@@ -78,6 +89,9 @@ struct Tail {
   volatile int stop;
   int mark[kMarks];       // seq of a unit whose values were not all finite
   Unit info[kInfos];      // seq < 0: no more
+  int last_one[2];
+  int warp_sums[kThreads / 32];
+  int pref[kCutUnits + 1];   // a cut list: places before each unit
 };
 
 // The largest r with cu[r] / per + r <= g: request of pair g of a list that gives every request one more than it may need.
@@ -97,6 +111,8 @@ __device__ __forceinline__ uint32_t unit_of(uint32_t k) {
 
 // False: there is nothing at this place of the list.
 __device__ __forceinline__ bool unit_info(const ManyArgs& a, uint32_t u, Unit& x) {
+  x.k0 = 0;
+  x.segs = 1;
   const uint32_t w = u / (uint32_t)a.Hkv;
   x.h = (int)(u - w * (uint32_t)a.Hkv);
   const int64_t v = (int64_t)a.pairs - 1 - w;                      // long rows first
@@ -158,7 +174,52 @@ struct Units {
   }
 };
 
-template <int kBoxes>
+// What becomes of a row whose logits' pieces are joined: `n` pieces, the k-th in slot(k).  Thread = row of the tile.
+template <typename Slot>
+__device__ __forceinline__ void join_pieces(const ManyArgs& a, int i, int row, int n, Slot slot, bool final, bool holds, __nv_bfloat16* out,
+                                            float* lse) {
+  const int quads = a.d_k >> 2;
+  float top = -INFINITY, sum = 0.f;
+  for (int k = 0; k < n; ++k) top = fmaxf(top, __ldcg(a.part_ml + (slot(k) * 2 + i) * kTile + row).x);
+  const float off = top == -INFINITY ? 0.f : top;
+  for (int k = 0; k < n; ++k) {
+    const float2 q = __ldcg(a.part_ml + (slot(k) * 2 + i) * kTile + row);
+    sum = fmaf(q.y, exp2_fast(q.x - off), sum);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll 1
+  for (int c0 = 0; c0 < quads; c0 += 8) {                          // 32 channels at a time, eight loads on their way
+    float4 r[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) r[c] = make_float4(0, 0, 0, 0);
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {
+      const float2 q = __ldcg(a.part_ml + (slot(k) * 2 + i) * kTile + row);
+      if (q.x == -INFINITY && q.y == 0.f) continue;                // saw nothing: its outputs were not written
+      const float f = exp2_fast(q.x - off);
+      const float4* from = a.part_o + ((slot(k) * 2 + i) * quads + c0) * kTile + row;
+      float4 v[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (c0 + c < quads) v[c] = __ldcg(from + c * kTile);
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (c0 + c < quads) { r[c].x += scaled(v[c].x, f); r[c].y += scaled(v[c].y, f); r[c].z += scaled(v[c].z, f); r[c].w += scaled(v[c].w, f); }
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      if (c0 + c >= quads) break;
+      if (sum == 0.f) r[c] = make_float4(0, 0, 0, 0);
+      if (!final) a.part_o[((slot(0) * 2 + i) * quads + c0 + c) * kTile + row] = r[c];     // (nobody else reads these any more)
+      else if (holds) *reinterpret_cast<uint2*>(out + (c0 + c) * 4) = make_uint2(bf16_pair(r[c].x * inv, r[c].y * inv), bf16_pair(r[c].z * inv, r[c].w * inv));
+    }
+  }
+  if (!final) a.part_ml[(slot(0) * 2 + i) * kTile + row] = make_float2(top, sum);
+  else if (holds && lse) *lse = sum == 0.f ? -INFINITY : off * 0.6931471805599453f + logf(sum);
+}
+
+// kCut: the list may be cut (a kernel of its own: the joins cost a long prompt 4 % by the registers alone).
+template <int kBoxes, bool kCut>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ ManyArgs a) {
@@ -202,6 +263,35 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   ptx::let_next_begin();
   ptx::wait_for_previous();
 
+  // A cut list: the tiles of all units end to end, each behind kGap places for what beginning and ending one costs; this CTA
+  // takes the places t0 .. t1 - 1.
+  int t0 = 0, t1 = 0, B = 0, T = 0;
+  bool cut = false;
+  if (kCut) {
+    Unit x;
+    int places = 0;
+    if (tid < (int)a.units && unit_info(a, tid, x)) places = max(x.tiles[0], x.tiles[1]) + kGap;
+    int up = places;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, up, o);
+      if (lane >= o) up += y;
+    }
+    if (lane == 31) tail->warp_sums[warp] = up;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) up += tail->warp_sums[w];
+    if (tid == 0) tail->pref[0] = 0;
+    if (tid < (int)a.units) tail->pref[tid + 1] = up;
+    __syncthreads();
+    T = tail->pref[a.units];
+    B = min((int)gridDim.x, T / kPiece);
+    cut = T / kPiece > (int)a.units;                               // short units stay whole
+    if ((int)blockIdx.x < B) {
+      t0 = (int)((int64_t)T * blockIdx.x / B);
+      t1 = (int)((int64_t)T * (blockIdx.x + 1) / B);
+    }
+  }
+
   if (warp >= 8) {
     fewer_registers<kOtherRegs>();
     if (warp == 11) {
@@ -209,13 +299,30 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       int at = 0;
       bool ok = true;
       for (uint32_t k = 0; ok; ++k) {
-        const bool end = (uint64_t)k * gridDim.x >= a.units;
-        const uint32_t u = end ? 0 : unit_of(k);
-        if (!end && u >= a.units) continue;
+        bool end;
         Unit x;
-        x.seq = at;
-        if (end) x.seq = -1;
-        else if (!unit_info(a, u, x)) continue;
+        if (kCut && cut) {
+          end = k >= a.units || tail->pref[k] >= t1;
+          if (!end) {
+            const int p = tail->pref[k], p1 = tail->pref[k + 1];
+            if (p1 <= t0 || p1 == p || !unit_info(a, k, x)) continue;
+            const int s0 = max(t0 - p - kGap, 0), s1 = min(t1, p1) - p - kGap, n = p1 - p - kGap;     // of its n tiles
+            if (n > 0 ? s0 >= s1 : p < t0) continue;               // (without tiles: whose it begins in)
+            if (n > 0) {
+              x.id = (int)k;
+              x.k0 = s0;
+              x.first = (int)(((int64_t)(p + kGap + 1) * B - 1) / T);
+              x.segs = (int)(((int64_t)p1 * B - 1) / T) - x.first + 1;
+#pragma unroll
+              for (int i = 0; i < 2; ++i) x.tiles[i] = max(min(x.tiles[i], s1) - s0, 0);
+            }
+          }
+        } else {
+          end = (uint64_t)k * gridDim.x >= a.units;
+          const uint32_t u = end ? 0 : unit_of(k);
+          if (!end && (u >= a.units || !unit_info(a, u, x))) continue;
+        }
+        x.seq = end ? -1 : at;
         const int s = at % kInfos;
         ok = __all_sync(0xffffffffu, wait_or_stop(&tail->info_empty[s], ((at / kInfos) & 1) ^ 1, stop));
         if (!ok) break;
@@ -259,11 +366,11 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         __syncwarp();
         const int32_t* table = a.src.tables ? a.src.tables + ((int64_t)x.r * a.Hkv + x.h) * a.src.max_pages : nullptr;
         const int start = table ? 0 : a.src.cu[x.r];
-        const int masked_from = max(x.see[0], 0) / kTile;
-        int j = part * a.box_rows, page = 0;                       // this lane's first row of a tile
+        const int masked_from = max(x.see[0], 0) / kTile - x.k0;
+        int j = x.k0 * kTile + part * a.box_rows, page = 0;        // this lane's first row of a tile
         if (table && in_tile && j < x.n) page = table[j >> a.src.page_log2];
         for (int t = 0; t < tiles; ++t, j += kTile) {
-          const int parts = (min(x.n - t * kTile, kTile) + a.box_rows - 1) / a.box_rows;
+          const int parts = (min(x.n - (x.k0 + t) * kTile, kTile) + a.box_rows - 1) / a.box_rows;
           const bool mine = part < parts;
           int next = 0;
           if (table && in_tile && t + 1 < tiles && j + kTile < x.n) next = table[(j + kTile) >> a.src.page_log2];
@@ -399,13 +506,13 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       bool ok = true;
       while (ok && units.next(x, lane)) {
         const int tiles = max(x.tiles[0], x.tiles[1]), from = max(x.see[0], 0);
-        for (int t = from / kTile; t < tiles; ++t, ++raw) {
+        for (int t = max(from / kTile - x.k0, 0); t < tiles; ++t, ++raw) {
           ok = __all_sync(0xffffffffu, wait_or_stop(&tail->v_raw[raw % kMarks], (raw / kMarks) & 1, stop));
           if (!ok) break;
           const uint32_t s = (it + 2 * t + 1) % a.stages;
           bool found = false;
           uint8_t* v = ring + (size_t)s * kTileBytes;
-          const int r0 = max(from - t * kTile, 0), r1 = min(x.n - t * kTile, kTile);       // rows r1 .. are nobody's
+          const int r0 = max(from - (x.k0 + t) * kTile, 0), r1 = min(x.n - (x.k0 + t) * kTile, kTile);     // rows r1 .. are nobody's
           for (int b = 0; b < kBoxes; ++b) {
             uint8_t* p = v + b * (kTile * 128);
             const int boxes = (a.d_k + 63) >> 6;
@@ -454,8 +561,8 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll
         for (int b = 0; b < 4; ++b) ptx::tmem_ld_32x32(s_addr + b * 32, v[b]);
         ptx::tmem_wait_ld();
-        if ((t + 1) * kTile > see) {
-          const int seen = limit - t * kTile;
+        if ((x.k0 + t + 1) * kTile > see) {
+          const int seen = limit - (x.k0 + t) * kTile;
 #pragma unroll
           for (int k = 0; k < kTile; ++k)
             if (k >= seen) v[k >> 5][k & 31] = 0xff800000u;
@@ -520,7 +627,11 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const int64_t token = x.tok0 + i * a.tpt + tok_in;
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       __nv_bfloat16* out = a.out + token * a.o_tok + (int64_t)head * a.o_head;
+      // a piece of a unit leaves its sums: slot 2 CTA + 1 if it is the unit's first (the CTA's last), else slot 2 CTA
+      auto slot_of = [&](int seg) { return (int64_t)2 * (x.first + seg) + (seg == 0 ? 1 : 0); };
+      const int seg = (int)blockIdx.x - x.first;
       for (int b = 0; b < a.d_k; b += 16) {
+        if (kCut && x.segs > 1 && tiles == 0) break;
         uint32_t o[16];
         __syncwarp();
         if (tiles > 0) {
@@ -542,7 +653,8 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           float g[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) g[k] = 0.f;
-          for (int j = again ? 0 : max(x.see[0], 0); j < limit; ++j) {
+          const int end = min(limit, (x.k0 + tiles) * kTile);
+          for (int j = max(again ? 0 : x.see[0], x.k0 * kTile); j < end; ++j) {
             const int64_t at = row_offset(a.src, x.r, x.h, a.Hkv, j);
             if (at < 0) continue;
             const uint4* q = reinterpret_cast<const uint4*>(a.src.V + at + b);
@@ -558,6 +670,12 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           for (int k = 0; k < 16; ++k)
             if (g[k] != 0.f) f[k] = g[k];
         }
+        if (kCut && x.segs > 1) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            a.part_o[((slot_of(seg) * 2 + i) * (a.d_k >> 2) + (b >> 2) + k) * kTile + row] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+          continue;
+        }
         uint4 w[2];
 #pragma unroll
         for (int k = 0; k < 8; ++k) (&w[k >> 2].x)[k & 3] = bf16_pair(f[2 * k] * inv, f[2 * k + 1] * inv);
@@ -565,7 +683,32 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         reinterpret_cast<uint4*>(out + b)[1] = w[1];
       }
       ptx::tc_fence_before_sync();
-      if (holds && a.lse)
+      if (kCut && x.segs > 1) {
+        a.part_ml[(slot_of(seg) * 2 + i) * kTile + row] = make_float2(ref, sum);
+        // Of kFan neighbouring pieces the CTA that arrives last joins them in their order, then of as many joined ones.
+        int32_t* count = a.arrived + (x.id * 2 + i) * (kFan + 1);
+        int g0 = seg / kFan * kFan, n = min(x.segs - g0, kFan), apart = 1;
+        count += g0 / kFan;
+        while (true) {
+          __threadfence();
+          ptx::named_barrier_sync(1 + i, 128);
+          if ((tid & 127) == 0) {
+            const int before = atomicAdd(count, 1);
+            tail->last_one[i] = before == n - 1;
+            if (before == n - 1) *count = 0;
+          }
+          ptx::named_barrier_sync(1 + i, 128);
+          if (!tail->last_one[i]) break;
+          __threadfence();
+          const bool final = x.segs <= kFan || apart > 1;
+          join_pieces(a, i, row, n, [&](int k) { return slot_of(g0 + k * apart); }, final, holds, out, a.lse ? a.lse + token * a.Hq + head : nullptr);
+          if (final) break;
+          count = a.arrived + (x.id * 2 + i) * (kFan + 1) + kFan;
+          n = (x.segs + kFan - 1) / kFan;
+          g0 = 0;
+          apart = kFan;
+        }
+      } else if (holds && a.lse)
         a.lse[token * a.Hq + head] = sum == 0.f ? -INFINITY : (ref == -INFINITY ? 0.f : ref) * 0.6931471805599453f + logf(sum);
     }
   }
@@ -582,23 +725,27 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   }
 }
 
-template <int kBoxes>
+template <int kBoxes, bool kCut>
 int32_t launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, ManyArgs& a, cudaStream_t st) {
   const size_t tile = (size_t)kBoxes * kTile * 128;
   const size_t room = 227 * 1024 - sizeof(Tail) - 2 * tile;
   a.stages = (int)(room / tile) < kMaxStages ? (int)(room / tile) : kMaxStages;
   const size_t smem = (2 + a.stages) * tile + sizeof(Tail);
-  GVOTE_CUDA_CHECK(cudaFuncSetAttribute(attend_many_kernel<kBoxes>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  auto kernel = attend_many_kernel<kBoxes, kCut>;
+  GVOTE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   LaunchScope scope_("attend_many_kernel", st);
-  const unsigned grid = a.units < (uint32_t)kNumSms ? a.units : (unsigned)kNumSms;
-  (void)launch_behind(attend_many_kernel<kBoxes>, dim3(grid), dim3(kThreads), smem, st, tq, tk, tv, a);
+  const unsigned grid = !kCut && a.units < (uint32_t)kNumSms ? a.units : (unsigned)kNumSms;
+  (void)launch_behind(kernel, dim3(grid), dim3(kThreads), smem, st, tq, tk, tv, a);
   GVOTE_LAUNCH_CHECK("attend_many_kernel");
   return GVOTE_OK;
 }
 
 }  // namespace
 
-size_t attend_many_workspace(const gvote_params*, int32_t, int64_t, int64_t) { return kStatusBytes; }
+size_t attend_many_workspace(const gvote_params* p, int32_t, int64_t, int64_t max_q) {
+  if (attend_takes_few(p, max_q)) return 0;
+  return kScratchAt + (size_t)2 * kNumSms * 2 * kTile * (p->d_k * 4 + 8);
+}
 
 int32_t launch_attend_many(const gvote_params* p, const AttendCall& c, const RowSource& s, char* ws, cudaStream_t st) {
   ManyArgs a;
@@ -610,6 +757,11 @@ int32_t launch_attend_many(const gvote_params* p, const AttendCall& c, const Row
   a.tpt = kTile / a.G;
   a.pairs = (uint32_t)(c.batch == 1 ? ceil_div(c.max_q, 2 * a.tpt) : c.total_q / (2 * a.tpt) + c.batch);
   a.units = a.pairs * (uint32_t)a.Hkv;
+  // (no unit can be longer than the longest request; where that leaves no more than a piece nothing is cut)
+  const bool cut = a.units <= (uint32_t)kCutUnits && ceil_div(c.max_rows, kTile) + kGap > kPiece;
+  a.arrived = reinterpret_cast<int32_t*>(ws + kStatusBytes);
+  a.part_o = reinterpret_cast<float4*>(ws + kScratchAt);
+  a.part_ml = reinterpret_cast<float2*>(ws + kScratchAt + (size_t)2 * kNumSms * 2 * kTile * p->d_k * 4);
   a.c = (float)(1.4426950408889634 / sqrt((double)p->d_k));
   a.box_rows = s.tables && (1 << s.page_log2) < kTile ? 1 << s.page_log2 : kTile;
   // (the stride of a dimension of one is not used and may be anything)
@@ -618,7 +770,8 @@ int32_t launch_attend_many(const gvote_params* p, const AttendCall& c, const Row
   const uint32_t box[3] = {64, (uint32_t)a.G, (uint32_t)a.tpt};
   CUtensorMap tq, tk, tv;
   if (!encode_tensor_map_bf16(&tq, c.Q, 3, dims, strides, box) || !row_maps(p, s, a.box_rows, &tk, &tv)) return GVOTE_ERR_CUDA;
-  return p->d_k <= 64 ? launch<1>(tq, tk, tv, a, st) : launch<2>(tq, tk, tv, a, st);
+  if (p->d_k <= 64) return cut ? launch<1, true>(tq, tk, tv, a, st) : launch<1, false>(tq, tk, tv, a, st);
+  return cut ? launch<2, true>(tq, tk, tv, a, st) : launch<2, false>(tq, tk, tv, a, st);
 }
 
 }  // namespace gvote

@@ -40,6 +40,7 @@ struct AttendCall {
   int64_t o_tok, o_head;
   float* lse;                   // or null
   int32_t batch;
+  int64_t max_rows;             // a head holds at most
 };
 
 struct PageArgs {
