@@ -7,10 +7,10 @@
 // sum over entries per direction, and what a thread does next is found by bisecting it: entries that need hundreds of pages
 // and entries that need none cost the same per page.
 //
-// A few thousand integers: bound by latency.  So one CTA does all of a decode step (three phases between barriers: sums and
-// checks; releases; takes, and with them the slots), and one cluster of eight where there is more; each CTA of a cluster makes the
-// prefix sums for itself and takes its share of the pages.  The slots of long prompts, one per token and head, are
-// a kernel of their own, and with a keep-mask the kept rows are counted by one before.
+// A few thousand integers: bound by latency.  So one CTA does all of a decode step between barriers (lengths and prefix sums;
+// releases; takes; slots), and one cluster of eight where more pages or slots may change hands; each CTA of a cluster makes
+// the prefix sums for itself and takes its share of the pages.  The slots of long prompts, one per token and head, are a kernel of
+// their own, and with a keep-mask the kept rows are counted by one before.
 #include <cooperative_groups.h>
 
 #include "kv_rows.cuh"
@@ -19,6 +19,9 @@ namespace gvote {
 namespace {
 
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanEach = 4;           // entries of a thread
+constexpr int kPlanEntries = kPlanThreads * kPlanEach;   // held in shared memory; of more the lengths are read for every phase
+constexpr int kStepTokens = 8;         // new tokens of a request up to which a thread does an entry's slots
 constexpr int kSlotTokens = 4096;      // tokens of a CTA of the slot kernel
 constexpr int kSlotThreads = 256;
 
@@ -33,6 +36,7 @@ struct TableArgs {
   int32_t* status;
   int64_t total_new, mask_words;
   int slots_here;                      // the plan kernel writes the slots itself
+  int max_new;
 };
 
 struct Change { int held, cut, grown; };
@@ -43,7 +47,7 @@ __device__ __forceinline__ Change change_of(const TableArgs& a, int64_t e) {
   const int v = a.p.kv_len[e];
   c.held = v < 0 ? 0 : (v < cap ? v : (int)cap);
   c.cut = a.keep ? min(c.held, max(a.keep[e], 0)) : c.held;
-  const int r = (int)(e / a.p.Hkv);
+  const int r = (int)((uint32_t)e / (uint32_t)a.p.Hkv);
   int more = 0;
   if (a.cu_new) more = a.mask ? a.counts[e] : max(a.cu_new[r + 1] - a.cu_new[r], 0);
   const int64_t grown = (int64_t)c.cut + more;
@@ -93,43 +97,95 @@ __device__ __forceinline__ int request_of(const int32_t* cu, int batch, int64_t 
   return lo;
 }
 
+struct PlanShared {
+  int cut[kPlanEntries], grown[kPlanEntries];
+  int gone[kPlanEntries], want[kPlanEntries];      // pages released, taken by the entries before
+  int warp_sums[2][32];
+  long long totals[2];
+  int sums[2], too_long;
+};
+
+// Lengths and prefix sums of the entries e0 .. e0 + n - 1.
+__device__ void plan_entries(const TableArgs& a, PlanShared& s, int64_t e0, int n, bool count) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, log2 = a.p.page_log2;
+  int gone[kPlanEach], want[kPlanEach], all_gone = 0, all_want = 0;
+  bool too_long = false;
+#pragma unroll
+  for (int q = 0; q < kPlanEach; ++q) {
+    const int k = tid * kPlanEach + q;
+    gone[q] = want[q] = 0;
+    if (k < n) {
+      const Change c = change_of(a, e0 + k);
+      too_long |= c.grown < 0;
+      s.cut[k] = c.cut;
+      s.grown[k] = c.grown;
+      gone[q] = pages_of(c.held, log2) - pages_of(c.cut, log2);
+      want[q] = max(pages_of(c.grown, log2) - pages_of(c.cut, log2), 0);
+    }
+    all_gone += gone[q];
+    all_want += want[q];
+  }
+  if (count) {
+    const unsigned long long g = warp_sum_u64(all_gone), w = warp_sum_u64(all_want);
+    if (lane == 0) {
+      atomicAdd((unsigned long long*)&s.totals[0], g);
+      atomicAdd((unsigned long long*)&s.totals[1], w);
+    }
+    if (too_long) s.too_long = 1;
+  }
+  int up_g = all_gone, up_w = all_want;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, up_g, o), z = __shfl_up_sync(0xffffffffu, up_w, o);
+    if (lane >= o) { up_g += y; up_w += z; }
+  }
+  if (lane == 31) { s.warp_sums[0][warp] = up_g; s.warp_sums[1][warp] = up_w; }
+  __syncthreads();
+  if (warp < 2) {
+    int x = s.warp_sums[warp][lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    s.warp_sums[warp][lane] = x;
+    if (lane == 31) s.sums[warp] = x;
+  }
+  __syncthreads();
+  int at_g = up_g - all_gone + (warp ? s.warp_sums[0][warp - 1] : 0), at_w = up_w - all_want + (warp ? s.warp_sums[1][warp - 1] : 0);
+#pragma unroll
+  for (int q = 0; q < kPlanEach; ++q) {
+    const int k = tid * kPlanEach + q;
+    if (k < n) { s.gone[k] = at_g; s.want[k] = at_w; }
+    at_g += gone[q];
+    at_w += want[q];
+  }
+  __syncthreads();
+}
+
 __global__ void __launch_bounds__(kPlanThreads)
 page_plan_kernel(const __grid_constant__ TableArgs a) {
-  __shared__ int warp_sums[32];
-  __shared__ int first[kPlanThreads], at_page[kPlanThreads];
-  __shared__ long long totals[2];
-  __shared__ int too_long;
+  extern __shared__ __align__(16) uint8_t plan_smem[];
+  PlanShared& s = *reinterpret_cast<PlanShared*>(plan_smem);
   const int tid = threadIdx.x, log2 = a.p.page_log2;
   const int64_t entries = (int64_t)a.p.batch * a.p.Hkv;
+  const bool once = entries <= kPlanEntries;                     // what is read once stays in shared memory
   const int ctas = gridDim.x, me = blockIdx.x;                   // (one cluster)
+  if (tid == 0) { s.totals[0] = s.totals[1] = 0; s.too_long = 0; }
+  __syncthreads();
   ptx::let_next_begin();
   ptx::wait_for_previous();
   auto sync_all = [&] { if (ctas > 1) cooperative_groups::this_cluster().sync(); else __syncthreads(); };
+  auto count_of = [&](int64_t e0) { return (int)min((int64_t)kPlanEntries, entries - e0); };
 
   // sums and checks
-  if (tid == 0) { totals[0] = totals[1] = 0; too_long = 0; }
-  __syncthreads();
-  {
-    unsigned long long gone = 0, want = 0;
-    for (int64_t e = tid; e < entries; e += kPlanThreads) {
-      const Change c = change_of(a, e);
-      if (c.grown < 0) { too_long = 1; continue; }
-      gone += pages_of(c.held, log2) - pages_of(c.cut, log2);
-      want += pages_of(c.grown, log2) - pages_of(c.cut, log2);
-    }
-    gone = warp_sum_u64(gone);
-    want = warp_sum_u64(want);
-    if ((tid & 31) == 0) {
-      atomicAdd((unsigned long long*)&totals[0], gone);
-      atomicAdd((unsigned long long*)&totals[1], want);
-    }
-  }
   const int n_free = *a.p.n_free;
-  __syncthreads();
-  const long long K = totals[0], T = totals[1];
+  for (int64_t e0 = 0; e0 < entries; e0 += kPlanEntries) plan_entries(a, s, e0, count_of(e0), true);
+  const long long K = s.totals[0], T = s.totals[1];
   const bool bad = n_free < 0 || n_free > a.p.n_pages || n_free + K > a.p.n_pages;
-  const bool refuse = bad || too_long || T > n_free + K;
+  const bool refuse = bad || s.too_long || T > n_free + K;
   sync_all();                                                    // every CTA has read n_free and the lengths
+  const int64_t n_slots = a.total_new * a.p.Hkv;
   if (refuse) {
     if (me == 0 && tid == 0) {
       *a.refused = 1;
@@ -137,62 +193,69 @@ page_plan_kernel(const __grid_constant__ TableArgs a) {
       atomicExch(&a.status[1], 20);
     }
     if (a.slots_here)
-      for (int64_t i = (int64_t)me * kPlanThreads + tid; i < a.total_new * a.p.Hkv; i += (int64_t)ctas * kPlanThreads) a.slots[i] = -1;
+      for (int64_t i = (int64_t)me * kPlanThreads + tid; i < n_slots; i += (int64_t)ctas * kPlanThreads) a.slots[i] = -1;
     return;
   }
   if (me == 0 && tid == 0) *a.refused = 0;
   const int top = (int)(n_free + K);
 
-  // releases, then takes: both in chunks of as many entries as threads
+  // releases, then takes
 #pragma unroll 1
   for (int take = 0; take < 2; ++take) {
     if ((take ? T : K) > 0) {
       int before = 0;
-      for (int64_t e0 = 0; e0 < entries; e0 += kPlanThreads) {
-        const int n = (int)min((int64_t)kPlanThreads, entries - e0);
-        int count = 0, page = 0;
-        if (tid < n) {
-          const Change c = change_of(a, e0 + tid);
-          page = pages_of(c.cut, log2);
-          count = pages_of(take ? c.grown : c.held, log2) - page;
-        }
-        const int sum = scan_block(count, warp_sums);
-        first[tid] = sum - count;
-        at_page[tid] = page;
-        const int all = warp_sums[kPlanThreads / 32 - 1];
-        __syncthreads();
+      for (int64_t e0 = 0; e0 < entries; e0 += kPlanEntries) {
+        const int n = count_of(e0);
+        if (!once) plan_entries(a, s, e0, n, false);
+        const int* first = take ? s.want : s.gone;
+        const int all = s.sums[take];
         for (int k = me * kPlanThreads + tid; k < all; k += ctas * kPlanThreads) {
-          // (of entries that start at the same place the last one has the pages)
-          const int i = find_owner(first, n, k);
-          int32_t* place = a.p.tables + (e0 + i) * a.p.max_pages + at_page[i] + (k - first[i]);
+          const int i = find_owner(first, n, k);                 // (of entries that start at the same place the last one has the pages)
+          int32_t* place = a.p.tables + (e0 + i) * a.p.max_pages + pages_of(s.cut[i], log2) + (k - first[i]);
           int32_t* stack = a.p.free_pages + (top - 1 - before - k);
           if (take) *place = *stack; else *stack = *place;
         }
         before += all;
+        if (!once) __syncthreads();
       }
     }
     sync_all();
   }
 
-  // lengths; the slots where they are few
+  // the slots where they are few, then the lengths
   if (a.slots_here) {
-    for (int64_t i = (int64_t)me * kPlanThreads + tid; i < a.total_new * a.p.Hkv; i += (int64_t)ctas * kPlanThreads) {
-      const int h = (int)(i / a.total_new);
-      const int64_t t = i - h * a.total_new;
-      const int r = request_of(a.cu_new, a.p.batch, t);
-      const int64_t e = (int64_t)r * a.p.Hkv + h;
-      int slot = -1;
-      if (t >= a.cu_new[r] && t < a.cu_new[r + 1]) {
-        const int row = change_of(a, e).cut + (int)(t - a.cu_new[r]);
-        const int page = a.p.tables[e * a.p.max_pages + (row >> log2)];
-        slot = (page << log2) + (row & ((1 << log2) - 1));
+    if (a.max_new <= kStepTokens) {
+      for (int64_t e = (int64_t)me * kPlanThreads + tid; e < entries; e += (int64_t)ctas * kPlanThreads) {
+        const int r = (int)((uint32_t)e / (uint32_t)a.p.Hkv), h = (int)(e - (int64_t)r * a.p.Hkv);
+        const int from = a.cu_new[r], to = a.cu_new[r + 1], cut = once ? s.cut[e] : change_of(a, e).cut;
+        for (int t = from; t < to; ++t) {
+          const int row = cut + t - from;
+          a.slots[h * a.total_new + t] = (a.p.tables[e * a.p.max_pages + (row >> log2)] << log2) + (row & ((1 << log2) - 1));
+        }
       }
-      a.slots[i] = slot;
+      const int64_t lead = a.cu_new[0], tail = a.cu_new[a.p.batch];            // tokens of no request
+      for (int64_t i = (int64_t)me * kPlanThreads + tid; i < (lead + a.total_new - tail) * a.p.Hkv; i += (int64_t)ctas * kPlanThreads) {
+        const int64_t t = i / a.p.Hkv;
+        a.slots[(i - t * a.p.Hkv) * a.total_new + (t < lead ? t : tail + t - lead)] = -1;
+      }
+    } else {
+      for (int64_t i = (int64_t)me * kPlanThreads + tid; i < n_slots; i += (int64_t)ctas * kPlanThreads) {
+        const int h = (int)(i / a.total_new);
+        const int64_t t = i - h * a.total_new;
+        const int r = request_of(a.cu_new, a.p.batch, t);
+        const int64_t e = (int64_t)r * a.p.Hkv + h;
+        int slot = -1;
+        if (t >= a.cu_new[r] && t < a.cu_new[r + 1]) {
+          const int row = (once ? s.cut[e] : change_of(a, e).cut) + (int)(t - a.cu_new[r]);
+          slot = (a.p.tables[e * a.p.max_pages + (row >> log2)] << log2) + (row & ((1 << log2) - 1));
+        }
+        a.slots[i] = slot;
+      }
     }
-    sync_all();
+    if (!once) sync_all();                                       // (the lengths have been read again)
   }
   if (me == 0) {
-    for (int64_t e = tid; e < entries; e += kPlanThreads) a.p.kv_len[e] = change_of(a, e).grown;
+    for (int64_t e = tid; e < entries; e += kPlanThreads) a.p.kv_len[e] = once ? s.grown[e] : change_of(a, e).grown;
     if (tid == 0) *a.p.n_free = (int)(top - T);
   }
 }
@@ -351,6 +414,7 @@ int32_t launch_page_tables(const PageArgs& p, const int32_t* keep, const int32_t
   a.refused = reinterpret_cast<int32_t*>(ws + m.refused);
   a.status = reinterpret_cast<int32_t*>(ws);
   const int64_t entries = (int64_t)p.batch * p.Hkv, n_slots = slots ? total_new * p.Hkv : 0;
+  a.max_new = (int)max_new;
   a.slots_here = n_slots > 0 && !mask && n_slots <= 8 * 1024 ? 1 : 0;
   if (mask) {
     LaunchScope scope_("page_count_kernel", st);
@@ -358,11 +422,13 @@ int32_t launch_page_tables(const PageArgs& p, const int32_t* keep, const int32_t
     GVOTE_LAUNCH_CHECK("page_count_kernel");
   }
   {
-    const int ctas = entries * max_new <= 16 * 1024 && !keep ? 1 : 8;
+    const int ctas = entries <= kPlanEntries && !mask && n_slots <= 8 * 1024 ? 1 : 8;
+    GVOTE_CUDA_CHECK(cudaFuncSetAttribute(page_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PlanShared)));
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(kPlanThreads);
+    cfg.dynamicSmemBytes = sizeof(PlanShared);
     cfg.stream = st;
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;

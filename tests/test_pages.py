@@ -268,3 +268,13 @@ def test_prompt_to_decode(gv):
         accepted = held - rng.integers(0, n_new, (3, 1))              # some drafts are rejected, of every head alike
     gv.gvote_page_tables(p, pages, ws, keep=torch.zeros(3, H, dtype=torch.int32, device="cuda"))
     assert int(pages.n_free) == 80 and sorted(pages.free.tolist()) == list(range(80))
+
+
+def test_more_entries_than_a_thread_block_holds(gv):
+    """Beyond 4096 (request, head) pairs the lengths are read for every phase."""
+    rng = np.random.default_rng(7)
+    s = State(gv, 700, 8, 16, rng.integers(0, 40, (700, 8)), 6, 700 * 8 * 2, seed=9)
+    assert s.step(np.maximum(s.kv - rng.integers(0, 20, (700, 8)), 0), rng.integers(0, 3, 700).tolist()) == 0
+    assert s.step(None, rng.integers(0, 20, 700).tolist()) == 0
+    assert s.step(s.kv - 1, rng.integers(0, 2, 700).tolist(), lead=3, trail=2) == 0
+    assert s.step(np.zeros((700, 8), int)) == 0
