@@ -426,7 +426,7 @@ GVOTE_API int32_t gvote_evict(const gvote_params* p, const float* acc, const int
  * page_rows a power of two, 16 to 1024; n_pages * page_rows < 2^31; max_pages * page_rows <= 2^26.  A workspace
  * (gvote_attend_workspace_bytes, zero-filled once) is for the entry points of this part alone - between calls it holds the
  * status word and counters that are zero - and serves one call at a time: calls, or replays of captured graphs, that may
- * overlap on the GPU need one each. */
+ * overlap on the GPU need one each.  After GVOTE_ERR_TIMEOUT zero-fill it again. */
 #define GVOTE_ATTEND_FEW_Q 32
 typedef struct {
   void* K;                   /* [n_pages][page_rows][d_k] bf16, device */
@@ -477,7 +477,7 @@ GVOTE_API int32_t gvote_page_write(const gvote_params* p, const void* K_new, con
  * head; a head with fewer rows than that leaves token i nothing, which gives out = 0, lse = -inf.  Per query head of KV head
  * h: logits q.k / sqrt(d_k), softmax, out = sum of weight * value, rounded to bf16 once; lse_or_null [total_q, n_q_heads] = log
  * of the softmax's denominator.  32-bit logits, references and sums; weights enter the product with the values as 16 bits (two bf16
- * terms) in calls of few query rows (one token, or at most 64 rows of tokens x query heads per KV head) and as bf16 in
+ * terms) in calls of few query rows (max_q x query heads per KV head at most 16, or d_k > 128) and as bf16 in
  * larger ones.  A row that a token does not see has no influence on it, whatever it holds.  Deterministic.  Tokens of no request
  * (before cu_q[0], behind cu_q[batch]) keep their out and lse.  Where cu_q gives a request more than max_q tokens, or a
  * page that rows are read from does not exist, the status word reads GVOTE_ERR_INVALID_ARG and the outputs are not to be used. */

@@ -13,8 +13,8 @@
 // CTA's work (one after the other they took 36 of 81 us).
 //
 // A CTA: four warps that compute and one that asks for tiles (TMA, 128-byte swizzle, boxes of a page or of 64 rows) into a ring
-// of units, K and V of a tile one unit each.  The products are mma.sync m16n8k16 with the query rows on M: a tile of one KV head
-// has 16 or 32 of them, the tensor work is a tenth of what the memory allows, and this shape lets a warp keep its 16 cached rows
+// of units, K and V of a tile one unit each.  The products are mma.sync m16n8k16 with the query rows on M, 16 of them
+// to a group: the tensor work fits under the memory time, and this shape lets a warp keep its 16 cached rows
 // of a tile to itself: its own reference, sum and output in registers, no barrier within a segment.  Weights are held as a sum of
 // two bf16 terms (16 bits; the outputs have 8); all else in 32 bits.  A reference moves only when a logit passes it by 2^8.
 //
@@ -30,6 +30,7 @@ namespace {
 constexpr int kTileKeys = 64;
 constexpr int kWarps = 4;                       // that compute
 constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kRows = 16;                       // query rows of a group
 constexpr int kMaxUnits = 8;
 constexpr int kGap = 3;
 constexpr int kFan = 18;                        // two rounds join every segment of a launch
@@ -74,21 +75,20 @@ struct Tail {
   Bars bars;
   volatile int stop;
   int last_one, odd;                            // odd: values that are not finite were taken out
-  float2 join[kFan][32];                        // references and sums of the segments that are joined
+  float2 join[kFan][kRows];                        // references and sums of the segments that are joined
   int warp_sums[kThreads / 32];
-  float2 ml[kWarps][32];
+  float2 ml[kWarps][kRows];
   int pref[kFewEntries + 1];
 };
 
-template <int kBoxes, int kM>                   // 64-channel boxes of a row; 16-row tiles of query rows
+template <int kBoxes>                           // 64-channel boxes of a row
 struct Layout {
-  static constexpr int kRows = 16 * kM;
   static constexpr int kUnit = kBoxes * kTileKeys * 128;
   static constexpr int kQPitch = kBoxes * 128 + 16;                   // bytes
   static constexpr int kQ = kRows * kQPitch;
   static constexpr int kSumPitch = kBoxes * 64 + 8;                   // floats
   static constexpr int kSum = kRows * kSumPitch * 4;
-  static constexpr bool kTwo = kBoxes * kM <= 2;                      // two CTAs per SM
+  static constexpr bool kTwo = kBoxes <= 2;                           // two CTAs per SM
   static constexpr size_t fixed() { return (size_t)2 * kQ + 2 * kSum + sizeof(Tail); }
   static constexpr int kFit = (int)(((kTwo ? 112 : 226) * 1024 - fixed()) / kUnit);
   static constexpr int kUnits = kFit < kMaxUnits ? kFit : kMaxUnits;
@@ -140,21 +140,21 @@ struct Walk {
   __device__ __forceinline__ void next() { ++e; enter(); }
 };
 
-template <int kBoxes, int kM>
-__global__ void __launch_bounds__(kThreads, Layout<kBoxes, kM>::kTwo ? 2 : 1)
+template <int kBoxes>
+__global__ void __launch_bounds__(kThreads, Layout<kBoxes>::kTwo ? 2 : 1)
 attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   const __grid_constant__ FewArgs a) {
-  using L = Layout<kBoxes, kM>;
+  using L = Layout<kBoxes>;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* ring = smem;                                            // [unit][box][64 rows][128], swizzled
   uint8_t* q_sm = ring + (size_t)L::kUnits * L::kUnit;             // [2][rows][pitch]
   float* sum_sm = reinterpret_cast<float*>(q_sm + 2 * L::kQ);      // [2][rows][pitch]
-  Tail* tail = reinterpret_cast<Tail*>(sum_sm + 2 * L::kRows * L::kSumPitch);
+  Tail* tail = reinterpret_cast<Tail*>(sum_sm + 2 * kRows * L::kSumPitch);
   int* pref = tail->pref;
   volatile int* stop = &tail->stop;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int entries = a.batch * a.Hkv;
-  const int row0 = (a.group0 + blockIdx.y) * L::kRows, row_last = row0 + L::kRows - 1;   // query rows of this group
+  const int row0 = (a.group0 + blockIdx.y) * kRows, row_last = row0 + kRows - 1;   // query rows of this group
   const int boxes = (a.d_k + 63) >> 6, ksteps = a.d_k >> 4;
 
   if (tid < (int)(sizeof(Bars) / 8)) {
@@ -213,7 +213,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     bool ok = true, bad_page = false;
     for (Walk w(pref, t0, t1, entries); ok && !w.done(); w.next(), ++seg) {
       const Entry x = entry_of(a, w.e, row_last);
-      const int rows = min(x.nq * a.G - row0, L::kRows);
+      const int rows = min(x.nq * a.G - row0, kRows);
       ok = __all_sync(0xffffffffu, wait_or_stop(&tail->bars.q_empty[seg & 1], ((seg >> 1) & 1) ^ 1, stop));
       if (!ok) break;
       if (lane == 0) ptx::mbar_arrive_expect_tx(&tail->bars.q_full[seg & 1], (uint32_t)(rows * a.d_k * 2));
@@ -271,7 +271,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     for (int e = b; e < entries; e += gridDim.x) {
       if (pref[e + 1] > pref[e]) continue;
       const Entry x = entry_of(a, e, row_last);
-      const int rows = min(x.nq * a.G - row0, L::kRows);
+      const int rows = min(x.nq * a.G - row0, kRows);
       for (int i = tid; i < rows * (a.d_k >> 3); i += 32 * kWarps) {
         const int lr = i / (a.d_k >> 3), c = i - lr * (a.d_k >> 3), row = row0 + lr, token = row / a.G, head = x.h * a.G + row - token * a.G;
         *reinterpret_cast<uint4*>(a.out + (int64_t)(x.q0 + token) * a.o_tok + (int64_t)head * a.o_head + c * 8) = make_uint4(0, 0, 0, 0);
@@ -280,25 +280,22 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
     for (Walk w(pref, t0, t1, entries); !w.done(); w.next(), ++seg) {
       const Entry x = entry_of(a, w.e, row_last);
-      const int rows = min(x.nq * a.G - row0, L::kRows);
+      const int rows = min(x.nq * a.G - row0, kRows);
       const int all_see = x.n - (min(row_last / a.G, x.nq - 1) - row0 / a.G);   // rows that every token of the group sees
-      int limit[kM][2];
-#pragma unroll
-      for (int m = 0; m < kM; ++m)
+      int limit[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int lr = m * 16 + i * 8 + (lane >> 2);
-          limit[m][i] = lr < rows ? all_see + (row0 + lr) / a.G - row0 / a.G : 0;
+          const int lr = i * 8 + (lane >> 2);
+          limit[i] = lr < rows ? all_see + (row0 + lr) / a.G - row0 / a.G : 0;
         }
-      float o[kM][kBoxes * 8][4], ref[kM][2], sum[kM][2];
-#pragma unroll
-      for (int m = 0; m < kM; ++m) {
-        ref[m][0] = ref[m][1] = -INFINITY;
-        sum[m][0] = sum[m][1] = 0.f;
+      float o[kBoxes * 8][4], ref[2], sum[2];
+      {
+        ref[0] = ref[1] = -INFINITY;
+        sum[0] = sum[1] = 0.f;
 #pragma unroll
         for (int i = 0; i < kBoxes * 8; ++i)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[m][i][k] = 0.f;
+          for (int k = 0; k < 4; ++k) o[i][k] = 0.f;
       }
       ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->bars.q_full[seg & 1], (seg >> 1) & 1, stop));
       const uint32_t q_addr = ptx::smem_u32(q_sm) + (seg & 1) * L::kQ + ((lane & 15)) * L::kQPitch + (lane >> 4) * 16;
@@ -309,25 +306,22 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         uint32_t s = unit % L::kUnits;
         ok = __all_sync(0xffffffffu, wait_or_stop(&tail->bars.full[s], (unit / L::kUnits) & 1, stop));
         if (!ok) break;
-        float l[kM][2][4];
-#pragma unroll
-        for (int m = 0; m < kM; ++m)
+        float l[2][4];
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) l[m][i][k] = 0.f;
+            for (int k = 0; k < 4; ++k) l[i][k] = 0.f;
         const uint32_t k_addr = ptx::smem_u32(ring) + s * L::kUnit + k_row * 128;
 #pragma unroll
         for (int c = 0; c < kBoxes * 4; ++c) {
           if (c < ksteps) {
             uint32_t kf[4];
             ldmatrix4(kf, k_addr + (c >> 2) * (kTileKeys * 128) + (((((uint32_t)c & 3) * 2 + k_half) ^ (k_row & 7)) << 4));
-#pragma unroll
-            for (int m = 0; m < kM; ++m) {
+            {
               uint32_t qf[4];
-              ldmatrix4(qf, q_addr + m * 16 * L::kQPitch + c * 32);
-              mma(l[m][0], qf, kf[0], kf[1]);
-              mma(l[m][1], qf, kf[2], kf[3]);
+              ldmatrix4(qf, q_addr + c * 32);
+              mma(l[0], qf, kf[0], kf[1]);
+              mma(l[1], qf, kf[2], kf[3]);
             }
           }
         }
@@ -335,39 +329,38 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         if (lane == 0) ptx::mbar_arrive(&tail->bars.empty[s]);
         ++unit;
         // weights
-        uint32_t hi[kM][4], lo[kM][4];
+        uint32_t hi[4], lo[4];
         const int j0 = t * kTileKeys + key + (lane & 3) * 2;       // this lane's columns: j0, j0 + 1, j0 + 8, j0 + 9
         const bool masked = (t + 1) * kTileKeys > all_see;
-#pragma unroll
-        for (int m = 0; m < kM; ++m) {
+        {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float* p[4] = {&l[m][0][2 * i], &l[m][0][2 * i + 1], &l[m][1][2 * i], &l[m][1][2 * i + 1]};
+            float* p[4] = {&l[0][2 * i], &l[0][2 * i + 1], &l[1][2 * i], &l[1][2 * i + 1]};
             if (masked) {
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if (j0 + (k >> 1) * 8 + (k & 1) >= limit[m][i]) *p[k] = -INFINITY;
+                if (j0 + (k >> 1) * 8 + (k & 1) >= limit[i]) *p[k] = -INFINITY;
             }
             float top = fmaxf(fmaxf(*p[0], *p[1]), fmaxf(*p[2], *p[3]));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * a.scale2;
-            const bool move = top > ref[m][i] + kSlack;
+            const bool move = top > ref[i] + kSlack;
             if (__any_sync(0xffffffffu, move)) {
-              const float f = move ? exp2_approx(ref[m][i] - top) : 1.f;
-              if (move) ref[m][i] = top;
-              sum[m][i] *= f;
+              const float f = move ? exp2_approx(ref[i] - top) : 1.f;
+              if (move) ref[i] = top;
+              sum[i] *= f;
 #pragma unroll
-              for (int n = 0; n < kBoxes * 8; ++n) { o[m][n][2 * i] *= f; o[m][n][2 * i + 1] *= f; }
+              for (int n = 0; n < kBoxes * 8; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
             }
-            const float off = ref[m][i] == -INFINITY ? 0.f : ref[m][i];
+            const float off = ref[i] == -INFINITY ? 0.f : ref[i];
 #pragma unroll
             for (int k = 0; k < 4; ++k) *p[k] = exp2_approx(fmaf(*p[k], a.scale2, -off));
-            sum[m][i] += (*p[0] + *p[1]) + (*p[2] + *p[3]);
+            sum[i] += (*p[0] + *p[1]) + (*p[2] + *p[3]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {                          // fragment i + 2 k: columns j0 + 8 k, j0 + 8 k + 1
               const uint32_t h = bf16_pair(*p[2 * k], *p[2 * k + 1]);
-              hi[m][i + 2 * k] = h;
-              lo[m][i + 2 * k] = bf16_pair(*p[2 * k] - __uint_as_float(h << 16), *p[2 * k + 1] - __uint_as_float(h & 0xffff0000u));
+              hi[i + 2 * k] = h;
+              lo[i + 2 * k] = bf16_pair(*p[2 * k] - __uint_as_float(h << 16), *p[2 * k + 1] - __uint_as_float(h & 0xffff0000u));
             }
           }
         }
@@ -400,12 +393,11 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           if (c < ksteps) {
             uint32_t vf[4];
             ldmatrix4_trans(vf, v_addr + (c >> 2) * (kTileKeys * 128) + (((((uint32_t)c & 3) * 2 + v_half) ^ (v_row & 7)) << 4));
-#pragma unroll
-            for (int m = 0; m < kM; ++m) {
-              mma(o[m][2 * c], hi[m], vf[0], vf[1]);
-              mma(o[m][2 * c + 1], hi[m], vf[2], vf[3]);
-              mma(o[m][2 * c], lo[m], vf[0], vf[1]);
-              mma(o[m][2 * c + 1], lo[m], vf[2], vf[3]);
+            {
+              mma(o[2 * c], hi, vf[0], vf[1]);
+              mma(o[2 * c + 1], hi, vf[2], vf[3]);
+              mma(o[2 * c], lo, vf[0], vf[1]);
+              mma(o[2 * c + 1], lo, vf[2], vf[3]);
             }
           }
         }
@@ -418,38 +410,32 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 
       // the four warps' results meet: a common reference, then sums in shared memory (warps 2 and 3, then 0 and 1 onto them)
 #pragma unroll
-      for (int m = 0; m < kM; ++m)
-#pragma unroll
         for (int i = 0; i < 2; ++i) {
-          sum[m][i] += __shfl_xor_sync(0xffffffffu, sum[m][i], 1);
-          sum[m][i] += __shfl_xor_sync(0xffffffffu, sum[m][i], 2);
-          if ((lane & 3) == 0) tail->ml[warp][m * 16 + i * 8 + (lane >> 2)] = make_float2(ref[m][i], sum[m][i]);
+          sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+          sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+          if ((lane & 3) == 0) tail->ml[warp][i * 8 + (lane >> 2)] = make_float2(ref[i], sum[i]);
         }
       ptx::named_barrier_sync(1, 32 * kWarps);
       const int odd = tail->odd;
 #pragma unroll
-      for (int m = 0; m < kM; ++m)
-#pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int lr = m * 16 + i * 8 + (lane >> 2);
+          const int lr = i * 8 + (lane >> 2);
           float top = tail->ml[0][lr].x;
 #pragma unroll
           for (int k = 1; k < kWarps; ++k) top = fmaxf(top, tail->ml[k][lr].x);
-          const float f = exp2_approx(ref[m][i] - (top == -INFINITY ? 0.f : top));
+          const float f = exp2_approx(ref[i] - (top == -INFINITY ? 0.f : top));
 #pragma unroll
-          for (int n = 0; n < kBoxes * 8; ++n) { o[m][n][2 * i] *= f; o[m][n][2 * i + 1] *= f; }
+          for (int n = 0; n < kBoxes * 8; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
         }
 #pragma unroll
       for (int round = 1; round >= 0; --round) {
         if ((warp >> 1) == round) {
 #pragma unroll
-          for (int m = 0; m < kM; ++m)
-#pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
               for (int n = 0; n < kBoxes * 8; ++n) {
-                float2* at = reinterpret_cast<float2*>(sum_sm + ((warp & 1) * L::kRows + m * 16 + i * 8 + (lane >> 2)) * L::kSumPitch + n * 8 + (lane & 3) * 2);
-                float2 v = make_float2(o[m][n][2 * i], o[m][n][2 * i + 1]);
+                float2* at = reinterpret_cast<float2*>(sum_sm + ((warp & 1) * kRows + i * 8 + (lane >> 2)) * L::kSumPitch + n * 8 + (lane & 3) * 2);
+                float2 v = make_float2(o[n][2 * i], o[n][2 * i + 1]);
                 if (round == 0) { const float2 u = *at; v.x += u.x; v.y += u.y; }
                 *at = v;
               }
@@ -470,7 +456,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
         for (int k = 0; k < kWarps; ++k) total = fmaf(tail->ml[k][lr].y, exp2_approx(tail->ml[k][lr].x - off), total);
         const float4 u = *reinterpret_cast<const float4*>(sum_sm + lr * L::kSumPitch + c);
-        const float4 v = *reinterpret_cast<const float4*>(sum_sm + (L::kRows + lr) * L::kSumPitch + c);
+        const float4 v = *reinterpret_cast<const float4*>(sum_sm + (kRows + lr) * L::kSumPitch + c);
         float4 r = make_float4(u.x + v.x, u.y + v.y, u.z + v.z, u.w + v.w);
         // Not finite: a value of a row that this token sees was not, and a weight's terms times an infinity may have cancelled
         // or been zero; what such values add up to is the result.  Else those taken out of this segment's tiles are added back.
@@ -499,8 +485,8 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           if (a.lse && c == 0)
             a.lse[(int64_t)(x.q0 + token) * a.Hq + head] = total == 0.f ? -INFINITY : off * 0.6931471805599453f + logf(total);
         } else {
-          *reinterpret_cast<float4*>(a.part_o + (slot * L::kRows + lr) * a.d_k + c) = r;
-          if (c == 0) a.part_ml[slot * L::kRows + lr] = make_float2(top, total);
+          *reinterpret_cast<float4*>(a.part_o + (slot * kRows + lr) * a.d_k + c) = r;
+          if (c == 0) a.part_ml[slot * kRows + lr] = make_float2(top, total);
         }
       }
       // the joins: of kFan segments, then of as many joined ones as there are
@@ -521,12 +507,12 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         __threadfence();
         const bool final = segs <= kFan || apart > 1;
         const int64_t s0 = slot0 + w.e + first + k0;
-        for (int i = tid; i < n * L::kRows; i += 32 * kWarps)
-          tail->join[i / L::kRows][i % L::kRows] = __ldcg(a.part_ml + (s0 + (int64_t)(i / L::kRows) * apart) * L::kRows + i % L::kRows);
+        for (int i = tid; i < n * kRows; i += 32 * kWarps)
+          tail->join[i / kRows][i % kRows] = __ldcg(a.part_ml + (s0 + (int64_t)(i / kRows) * apart) * kRows + i % kRows);
         ptx::named_barrier_sync(1, 32 * kWarps);
         for (int i = tid; i < rows * quads; i += 32 * kWarps) {
           const int lr = i / quads, c = (i - lr * quads) * 4, row = row0 + lr, token = row / a.G, head = x.h * a.G + row - token * a.G;
-          float* po = a.part_o + (s0 * L::kRows + lr) * a.d_k + c;
+          float* po = a.part_o + (s0 * kRows + lr) * a.d_k + c;
           float top = -INFINITY, total = 0.f;
           for (int k = 0; k < n; ++k) top = fmaxf(top, tail->join[k][lr].x);
           const float off = top == -INFINITY ? 0.f : top;
@@ -536,7 +522,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             float4 v[6];
 #pragma unroll
             for (int k = 0; k < 6; ++k)
-              if (k1 + k < n) v[k] = __ldcg(reinterpret_cast<const float4*>(po + (int64_t)(k1 + k) * apart * L::kRows * a.d_k));
+              if (k1 + k < n) v[k] = __ldcg(reinterpret_cast<const float4*>(po + (int64_t)(k1 + k) * apart * kRows * a.d_k));
 #pragma unroll
             for (int k = 0; k < 6; ++k)
               if (k1 + k < n) {
@@ -554,7 +540,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             if (a.lse && c == 0) a.lse[(int64_t)(x.q0 + token) * a.Hq + head] = total == 0.f ? -INFINITY : off * 0.6931471805599453f + logf(total);
           } else {
             *reinterpret_cast<float4*>(po) = r;                    // (nobody else reads these slots any more)
-            if (c == 0) a.part_ml[s0 * L::kRows + lr] = make_float2(top, total);
+            if (c == 0) a.part_ml[s0 * kRows + lr] = make_float2(top, total);
           }
         }
         if (final) break;
@@ -574,46 +560,42 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   }
 }
 
-// Groups of query rows that share a pass over the cached rows: 16 rows, or 32 where there are more and d_k leaves the registers.
-int group_rows(const gvote_params* p, int64_t rows) { return rows > 16 && p->d_k <= 128 ? 32 : 16; }
 int boxes_of(const gvote_params* p) { return p->d_k <= 64 ? 1 : p->d_k <= 128 ? 2 : 4; }
 
 struct FewMap { size_t ml, o, total; int groups, ctas; };
 FewMap few_map(const gvote_params* p, int32_t batch, int64_t max_q) {
   FewMap m;
-  const int64_t rows = max_q * (p->n_q_heads / p->n_kv_heads);
-  const int per = group_rows(p, rows);
-  m.groups = (int)ceil_div(rows, per);
+  m.groups = (int)ceil_div(max_q * (p->n_q_heads / p->n_kv_heads), kRows);
   const int at_once = m.groups < kFewGroups ? m.groups : kFewGroups;
-  m.ctas = (per / 16 * boxes_of(p) <= 2 ? 2 : 1) * kNumSms / at_once;
+  m.ctas = (boxes_of(p) <= 2 ? 2 : 1) * kNumSms / at_once;
   const int64_t all = (int64_t)batch * p->n_kv_heads, slots = (all < kFewEntries ? all : kFewEntries) + m.ctas;
   m.ml = kScratchAt;
-  m.o = m.ml + align_up((size_t)at_once * slots * per * 8, 256);
-  m.total = m.o + align_up((size_t)at_once * slots * per * p->d_k * 4, 256);
+  m.o = m.ml + align_up((size_t)at_once * slots * kRows * 8, 256);
+  m.total = m.o + align_up((size_t)at_once * slots * kRows * p->d_k * 4, 256);
   return m;
 }
 
-template <int kBoxes, int kM>
+template <int kBoxes>
 int32_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const FewArgs& a, int ctas, int groups, cudaStream_t st) {
-  using L = Layout<kBoxes, kM>;
-  GVOTE_CUDA_CHECK(cudaFuncSetAttribute(attend_few_kernel<kBoxes, kM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::smem()));
+  using L = Layout<kBoxes>;
+  GVOTE_CUDA_CHECK(cudaFuncSetAttribute(attend_few_kernel<kBoxes>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::smem()));
   LaunchScope scope_("attend_few_kernel", st);
-  (void)launch_behind(attend_few_kernel<kBoxes, kM>, dim3(ctas, groups), dim3(kThreads), L::smem(), st, tk, tv, a);
+  (void)launch_behind(attend_few_kernel<kBoxes>, dim3(ctas, groups), dim3(kThreads), L::smem(), st, tk, tv, a);
   GVOTE_LAUNCH_CHECK("attend_few_kernel");
   return GVOTE_OK;
 }
 
 }  // namespace
 
-// The few-row kernel reads K and V once for every 32 query rows; the kernel for many rows once for 256, but cannot share a short
-// list of rows among the SMs as finely.
+// One group of rows is bound by memory; with a second the cached rows are read and multiplied twice, and the kernel for many
+// rows, which takes 256 of them at once, is as fast or faster (20 rows over 512 cached ones 12.5 us against 20).
 bool attend_takes_few(const gvote_params* p, int64_t max_q) {
-  return p->d_k > kMaxHeadDimMany || max_q == 1 || max_q * (p->n_q_heads / p->n_kv_heads) <= 64;
+  return p->d_k > kMaxHeadDimMany || max_q * (p->n_q_heads / p->n_kv_heads) <= kRows;
 }
 
 size_t attend_few_workspace(const gvote_params* p, int32_t batch, int64_t max_q) {
   size_t n = 0;
-  for (int64_t q = 1; q <= max_q && attend_takes_few(p, q) && q <= GVOTE_ATTEND_FEW_Q; ++q) {   // (groups of 16 or of 32 rows: not monotonic)
+  for (int64_t q = 1; q <= max_q && q <= GVOTE_ATTEND_FEW_Q && attend_takes_few(p, q); ++q) {   // (fewer groups have more CTAs: not monotonic)
     const size_t t = few_map(p, batch, q).total;
     if (t > n) n = t;
   }
@@ -644,16 +626,15 @@ int32_t launch_attend_few(const gvote_params* p, const AttendCall& c, const RowS
   a.box_rows = s.tables && (1 << s.page_log2) < kTileKeys ? 1 << s.page_log2 : kTileKeys;
   CUtensorMap tk, tv;
   if (!row_maps(p, s, a.box_rows, &tk, &tv)) return GVOTE_ERR_CUDA;
-  const bool wide = group_rows(p, c.max_q * a.G) == 32;
   const int boxes = boxes_of(p), most = kFewEntries / a.Hkv;
   for (int r0 = 0; r0 < c.batch; r0 += most) {
     a.r0 = r0;
     a.batch = c.batch - r0 < most ? c.batch - r0 : most;
     for (a.group0 = 0; a.group0 < m.groups; a.group0 += kFewGroups) {
       const int n = m.groups - a.group0 < kFewGroups ? m.groups - a.group0 : kFewGroups;
-      if (boxes == 4) PROPAGATE((launch<4, 1>(tk, tv, a, m.ctas, n, st)));
-      else if (boxes == 2) PROPAGATE((wide ? launch<2, 2>(tk, tv, a, m.ctas, n, st) : launch<2, 1>(tk, tv, a, m.ctas, n, st)));
-      else PROPAGATE((wide ? launch<1, 2>(tk, tv, a, m.ctas, n, st) : launch<1, 1>(tk, tv, a, m.ctas, n, st)));
+      if (boxes == 4) PROPAGATE(launch<4>(tk, tv, a, m.ctas, n, st));
+      else if (boxes == 2) PROPAGATE(launch<2>(tk, tv, a, m.ctas, n, st));
+      else PROPAGATE(launch<1>(tk, tv, a, m.ctas, n, st));
     }
   }
   return GVOTE_OK;

@@ -43,11 +43,12 @@ constexpr int kPoly = 1;                  // of 8 exponentials, those computed o
 constexpr float kSlack = 8.f;
 // Cut lists (where there are few units): units of a list, places that a unit's beginning and end count as, and what a join takes.
 constexpr int kCutUnits = 2 * kNumSms;
+constexpr size_t kPiecesBytes = 2560;
+static_assert(kCutUnits * sizeof(int2) <= kPiecesBytes && kCutUnits <= kThreads, "");
 constexpr int kGap = 3;
 constexpr int kPiece = 8;                 // places of a CTA at least
-constexpr int kFan = 13;                  // two rounds join the segments of a unit
-static_assert(kFan * kFan >= kNumSms && (size_t)kCutUnits * 2 * (kFan + 1) * 4 <= kScratchAt - kStatusBytes, "");
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
+constexpr int kJoinQuads = 8;             // channels / 4 of a CTA of the join
+constexpr int kSoftmaxRegs = 232, kOtherRegs = 40;
 static_assert(kSoftmaxRegs * 256 + kOtherRegs * 128 <= 168 * kThreads, "the registers a CTA is launched with");
 
 struct ManyArgs {
@@ -63,14 +64,14 @@ struct ManyArgs {
   int stages, box_rows;
   float4* part_o;         // [2 per CTA][2 tiles][d_k / 4][128 rows]
   float2* part_ml;        // [2 per CTA][2 tiles][128 rows]  (reference, sum), base 2
-  int32_t* arrived;       // [units][2 tiles][kFan: first rounds, then the second], zero between calls
+  int2* pieces;           // [units]  first CTA, pieces
   float c;                // log2(e) / sqrt(d_k)
 };
 
 struct Unit {
   int r, h, seq;
   int k0;                 // first tile of keys
-  int id, first, segs;    // in a cut list: the unit, the first CTA that has a piece of it, the pieces
+  int first, segs;        // in a cut list: the first CTA that has a piece of it, the pieces
   int tok0;               // first token of the first tile, in the packed list
   int count[2];           // tokens of the tiles
   int see[2];             // rows a tile's first token sees (may be negative)
@@ -89,7 +90,6 @@ struct Tail {
   volatile int stop;
   int mark[kMarks];       // seq of a unit whose values were not all finite
   Unit info[kInfos];      // seq < 0: no more
-  int last_one[2];
   int warp_sums[kThreads / 32];
   int pref[kCutUnits + 1];   // a cut list: places before each unit
 };
@@ -174,51 +174,59 @@ struct Units {
   }
 };
 
-// What becomes of a row whose logits' pieces are joined: `n` pieces, the k-th in slot(k).  Thread = row of the tile.
-template <typename Slot>
-__device__ __forceinline__ void join_pieces(const ManyArgs& a, int i, int row, int n, Slot slot, bool final, bool holds, __nv_bfloat16* out,
-                                            float* lse) {
-  const int quads = a.d_k >> 2;
+// Where piece `seg` of a unit that begins in CTA `first` leaves its sums: the unit's first piece is its CTA's last one, every
+// other piece its CTA's first one.
+__device__ __forceinline__ int64_t piece_slot(int first, int seg) { return (int64_t)2 * (first + seg) + (seg == 0 ? 1 : 0); }
+
+// The pieces of a unit added up, in their order: a CTA per unit, tile and 4 kJoinQuads channels, two threads per row.  (By the last
+// CTA to arrive at a counter, as the few-row kernel does it, a tile's 128 rows were too much for one SM: 70 of 107 us for five
+// draft tokens over 32K rows.)
+__global__ void __launch_bounds__(2 * kTile)
+attend_join_kernel(const __grid_constant__ ManyArgs a) {
+  const int u = blockIdx.x, i = blockIdx.y, row = threadIdx.x & (kTile - 1);
+  ptx::let_next_begin();
+  ptx::wait_for_previous();
+  const int2 piece = a.pieces[u];
+  const int first = piece.x, n = piece.y;
+  if (n < 2) return;
+  Unit x;
+  unit_info(a, (uint32_t)u, x);
+  const int tok_in = row / a.G, head = x.h * a.G + row - tok_in * a.G, quads = a.d_k >> 2;
+  if (tok_in >= (i ? x.count[1] : x.count[0]) || row >= a.G * a.tpt) return;
+  const int64_t token = x.tok0 + i * a.tpt + tok_in;
   float top = -INFINITY, sum = 0.f;
-  for (int k = 0; k < n; ++k) top = fmaxf(top, __ldcg(a.part_ml + (slot(k) * 2 + i) * kTile + row).x);
+  for (int k = 0; k < n; ++k) top = fmaxf(top, a.part_ml[(piece_slot(first, k) * 2 + i) * kTile + row].x);
   const float off = top == -INFINITY ? 0.f : top;
+  float4 r[kJoinQuads / 2];
+#pragma unroll
+  for (int c = 0; c < kJoinQuads / 2; ++c) r[c] = make_float4(0, 0, 0, 0);
+  const int c0 = blockIdx.z * kJoinQuads + (threadIdx.x >> 7) * (kJoinQuads / 2);
+#pragma unroll 2
   for (int k = 0; k < n; ++k) {
-    const float2 q = __ldcg(a.part_ml + (slot(k) * 2 + i) * kTile + row);
-    sum = fmaf(q.y, exp2_fast(q.x - off), sum);
+    const float2 q = a.part_ml[(piece_slot(first, k) * 2 + i) * kTile + row];
+    if (q.x == -INFINITY && q.y == 0.f) continue;                  // saw nothing: its outputs were not written
+    const float f = exp2_fast(q.x - off);
+    sum = fmaf(q.y, f, sum);
+    const float4* from = a.part_o + ((piece_slot(first, k) * 2 + i) * quads + c0) * kTile + row;
+#pragma unroll
+    for (int c = 0; c < kJoinQuads / 2; ++c)
+      if (c0 + c < quads) {
+        const float4 v = from[c * kTile];
+        r[c].x += scaled(v.x, f); r[c].y += scaled(v.y, f); r[c].z += scaled(v.z, f); r[c].w += scaled(v.w, f);
+      }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll 1
-  for (int c0 = 0; c0 < quads; c0 += 8) {                          // 32 channels at a time, eight loads on their way
-    float4 r[8];
+  __nv_bfloat16* out = a.out + token * a.o_tok + (int64_t)head * a.o_head;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) r[c] = make_float4(0, 0, 0, 0);
-#pragma unroll 1
-    for (int k = 0; k < n; ++k) {
-      const float2 q = __ldcg(a.part_ml + (slot(k) * 2 + i) * kTile + row);
-      if (q.x == -INFINITY && q.y == 0.f) continue;                // saw nothing: its outputs were not written
-      const float f = exp2_fast(q.x - off);
-      const float4* from = a.part_o + ((slot(k) * 2 + i) * quads + c0) * kTile + row;
-      float4 v[8];
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        if (c0 + c < quads) v[c] = __ldcg(from + c * kTile);
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        if (c0 + c < quads) { r[c].x += scaled(v[c].x, f); r[c].y += scaled(v[c].y, f); r[c].z += scaled(v[c].z, f); r[c].w += scaled(v[c].w, f); }
-    }
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      if (c0 + c >= quads) break;
+  for (int c = 0; c < kJoinQuads / 2; ++c)
+    if (c0 + c < quads) {
       if (sum == 0.f) r[c] = make_float4(0, 0, 0, 0);
-      if (!final) a.part_o[((slot(0) * 2 + i) * quads + c0 + c) * kTile + row] = r[c];     // (nobody else reads these any more)
-      else if (holds) *reinterpret_cast<uint2*>(out + (c0 + c) * 4) = make_uint2(bf16_pair(r[c].x * inv, r[c].y * inv), bf16_pair(r[c].z * inv, r[c].w * inv));
+      *reinterpret_cast<uint2*>(out + (c0 + c) * 4) = make_uint2(bf16_pair(r[c].x * inv, r[c].y * inv), bf16_pair(r[c].z * inv, r[c].w * inv));
     }
-  }
-  if (!final) a.part_ml[(slot(0) * 2 + i) * kTile + row] = make_float2(top, sum);
-  else if (holds && lse) *lse = sum == 0.f ? -INFINITY : off * 0.6931471805599453f + logf(sum);
+  if (a.lse && c0 == 0) a.lse[token * a.Hq + head] = sum == 0.f ? -INFINITY : off * 0.6931471805599453f + logf(sum);
 }
 
-// kCut: the list may be cut (a kernel of its own: the joins cost a long prompt 4 % by the registers alone).
+// kCut: the list may be cut.
 template <int kBoxes, bool kCut>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -286,6 +294,11 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     T = tail->pref[a.units];
     B = min((int)gridDim.x, T / kPiece);
     cut = T / kPiece > (int)a.units;                               // short units stay whole
+    if (blockIdx.x == 0 && tid < (int)a.units) {                   // for the join
+      const int p = tail->pref[tid] + kGap, p1 = tail->pref[tid + 1];
+      const int first = cut && p < p1 ? (int)(((int64_t)(p + 1) * B - 1) / T) : 0;
+      a.pieces[tid] = make_int2(first, cut && p < p1 ? (int)(((int64_t)p1 * B - 1) / T) - first + 1 : 0);
+    }
     if ((int)blockIdx.x < B) {
       t0 = (int)((int64_t)T * blockIdx.x / B);
       t1 = (int)((int64_t)T * (blockIdx.x + 1) / B);
@@ -309,7 +322,6 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             const int s0 = max(t0 - p - kGap, 0), s1 = min(t1, p1) - p - kGap, n = p1 - p - kGap;     // of its n tiles
             if (n > 0 ? s0 >= s1 : p < t0) continue;               // (without tiles: whose it begins in)
             if (n > 0) {
-              x.id = (int)k;
               x.k0 = s0;
               x.first = (int)(((int64_t)(p + kGap + 1) * B - 1) / T);
               x.segs = (int)(((int64_t)p1 * B - 1) / T) - x.first + 1;
@@ -553,9 +565,15 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const bool holds = tok_in < count && row < q_rows;
       const int limit = holds ? see + tok_in : 0;
       float ref = -INFINITY, sum = 0.f;
+      const bool idle = (warp & 3) * 32 >= min(count * a.G, q_rows);   // none of this warp's rows is a token's
       for (int t = 0; t < tiles; ++t, ++used) {
         ok = __all_sync(0xffffffffu, wait_or_stop(&tail->s_full[i], used & 1, stop));
         if (!ok) break;
+        if (idle) {                                                // (their weights may be anything)
+          if (lane == 0) { ptx::mbar_arrive(&tail->p_half[i]); ptx::mbar_arrive(&tail->p_full[i]); }
+          __syncwarp();
+          continue;
+        }
         ptx::tc_fence_after_sync();
         uint32_t v[4][32];
 #pragma unroll
@@ -627,9 +645,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const int64_t token = x.tok0 + i * a.tpt + tok_in;
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       __nv_bfloat16* out = a.out + token * a.o_tok + (int64_t)head * a.o_head;
-      // a piece of a unit leaves its sums: slot 2 CTA + 1 if it is the unit's first (the CTA's last), else slot 2 CTA
-      auto slot_of = [&](int seg) { return (int64_t)2 * (x.first + seg) + (seg == 0 ? 1 : 0); };
-      const int seg = (int)blockIdx.x - x.first;
+      const int64_t slot = kCut ? piece_slot(x.first, (int)blockIdx.x - x.first) : 0;
       for (int b = 0; b < a.d_k; b += 16) {
         if (kCut && x.segs > 1 && tiles == 0) break;
         uint32_t o[16];
@@ -673,7 +689,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (kCut && x.segs > 1) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            a.part_o[((slot_of(seg) * 2 + i) * (a.d_k >> 2) + (b >> 2) + k) * kTile + row] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+            a.part_o[((slot * 2 + i) * (a.d_k >> 2) + (b >> 2) + k) * kTile + row] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
           continue;
         }
         uint4 w[2];
@@ -684,30 +700,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
       ptx::tc_fence_before_sync();
       if (kCut && x.segs > 1) {
-        a.part_ml[(slot_of(seg) * 2 + i) * kTile + row] = make_float2(ref, sum);
-        // Of kFan neighbouring pieces the CTA that arrives last joins them in their order, then of as many joined ones.
-        int32_t* count = a.arrived + (x.id * 2 + i) * (kFan + 1);
-        int g0 = seg / kFan * kFan, n = min(x.segs - g0, kFan), apart = 1;
-        count += g0 / kFan;
-        while (true) {
-          __threadfence();
-          ptx::named_barrier_sync(1 + i, 128);
-          if ((tid & 127) == 0) {
-            const int before = atomicAdd(count, 1);
-            tail->last_one[i] = before == n - 1;
-            if (before == n - 1) *count = 0;
-          }
-          ptx::named_barrier_sync(1 + i, 128);
-          if (!tail->last_one[i]) break;
-          __threadfence();
-          const bool final = x.segs <= kFan || apart > 1;
-          join_pieces(a, i, row, n, [&](int k) { return slot_of(g0 + k * apart); }, final, holds, out, a.lse ? a.lse + token * a.Hq + head : nullptr);
-          if (final) break;
-          count = a.arrived + (x.id * 2 + i) * (kFan + 1) + kFan;
-          n = (x.segs + kFan - 1) / kFan;
-          g0 = 0;
-          apart = kFan;
-        }
+        a.part_ml[(slot * 2 + i) * kTile + row] = make_float2(ref, sum);
       } else if (holds && a.lse)
         a.lse[token * a.Hq + head] = sum == 0.f ? -INFINITY : (ref == -INFINITY ? 0.f : ref) * 0.6931471805599453f + logf(sum);
     }
@@ -737,6 +730,11 @@ int32_t launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& 
   const unsigned grid = !kCut && a.units < (uint32_t)kNumSms ? a.units : (unsigned)kNumSms;
   (void)launch_behind(kernel, dim3(grid), dim3(kThreads), smem, st, tq, tk, tv, a);
   GVOTE_LAUNCH_CHECK("attend_many_kernel");
+  if (kCut) {
+    LaunchScope join_("attend_join_kernel", st);
+    (void)launch_behind(attend_join_kernel, dim3(a.units, 2, (unsigned)ceil_div(a.d_k / 4, kJoinQuads)), dim3(2 * kTile), 0, st, a);
+    GVOTE_LAUNCH_CHECK("attend_join_kernel");
+  }
   return GVOTE_OK;
 }
 
@@ -744,7 +742,7 @@ int32_t launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& 
 
 size_t attend_many_workspace(const gvote_params* p, int32_t, int64_t, int64_t max_q) {
   if (attend_takes_few(p, max_q)) return 0;
-  return kScratchAt + (size_t)2 * kNumSms * 2 * kTile * (p->d_k * 4 + 8);
+  return kScratchAt + kPiecesBytes + (size_t)2 * kNumSms * 2 * kTile * (p->d_k * 4 + 8);
 }
 
 int32_t launch_attend_many(const gvote_params* p, const AttendCall& c, const RowSource& s, char* ws, cudaStream_t st) {
@@ -758,10 +756,11 @@ int32_t launch_attend_many(const gvote_params* p, const AttendCall& c, const Row
   a.pairs = (uint32_t)(c.batch == 1 ? ceil_div(c.max_q, 2 * a.tpt) : c.total_q / (2 * a.tpt) + c.batch);
   a.units = a.pairs * (uint32_t)a.Hkv;
   // (no unit can be longer than the longest request; where that leaves no more than a piece nothing is cut)
-  const bool cut = a.units <= (uint32_t)kCutUnits && ceil_div(c.max_rows, kTile) + kGap > kPiece;
-  a.arrived = reinterpret_cast<int32_t*>(ws + kStatusBytes);
-  a.part_o = reinterpret_cast<float4*>(ws + kScratchAt);
-  a.part_ml = reinterpret_cast<float2*>(ws + kScratchAt + (size_t)2 * kNumSms * 2 * kTile * p->d_k * 4);
+  const int64_t most = ceil_div(c.max_rows, kTile) + kGap;         // places of a unit
+  const bool cut = a.units <= (uint32_t)kCutUnits && most > kPiece && most * a.units < (int64_t)1 << 31;
+  a.pieces = reinterpret_cast<int2*>(ws + kScratchAt);
+  a.part_o = reinterpret_cast<float4*>(ws + kScratchAt + kPiecesBytes);
+  a.part_ml = reinterpret_cast<float2*>(ws + kScratchAt + kPiecesBytes + (size_t)2 * kNumSms * 2 * kTile * p->d_k * 4);
   a.c = (float)(1.4426950408889634 / sqrt((double)p->d_k));
   a.box_rows = s.tables && (1 << s.page_log2) < kTile ? 1 << s.page_log2 : kTile;
   // (the stride of a dimension of one is not used and may be anything)
