@@ -20,8 +20,20 @@
 // tiles hardly happens; the next unit's first P_i V waits for them in any case, so a unit's outputs are
 // stored while the next one's products run.
 //
-// P is rounded to bf16: half a step, 2^-9 of a weight, where the output has the same half step.  The sum is of the 32-bit
-// weights.
+// P is rounded to bf16, by at most 2^-8 of a weight, as the output is; two terms, as the few-row kernel has them, would
+// take half as much tensor time again.  The sum is of the 32-bit weights.
+//
+// What bounds it: a tile's chain.  The softmax of 128 x 128 logits takes its four warps 2000 clocks (S out of tensor memory and
+// its maximum 600, the exponentials 1200, P back 200), the products and their messages 1160, and the two tiles' chains overlap to 3600
+// clocks for 2 x 2 products of 128 x 128 x 128, of which the tensor cores work half: 51 % busy, the exponentials' unit 45 %.
+// Measured (one B200): a 32K prompt of 32 heads on 8 8.1 to 8.4 ms (8.8 TFLOP, 1.05 to 1.1 PFLOP/s), 8192 tokens 0.51 ms.
+// Slower, or no faster: two S of 64 keys to a tile, so that softmax and products of a tile overlap (the MMAs with N = 64 read
+// Q twice as often, 8.5 ms); sixteen softmax warps, two threads to a row (9.5 ms); an issuer for each tile; exponentials before the maximum,
+// with the reference of the tile before (registers); none, two or three of eight exponentials on the FMA pipe; a loop over halves with S read
+// twice; the units of a ragged batch sorted by length; outputs 64 channels at a time.
+//
+// Where there are few units (kCutUnits at most) the list is cut evenly over the CTAs, units into pieces, and attend_join_kernel adds
+// a unit's pieces up: 500 tokens of 32 heads over pruned 13K rows of 8 KV heads 130 us instead of 272, 7 of them the join.
 //
 // Rows that not every token of a unit sees may hold anything: logits are masked by index, values that are not finite are
 // set to 0 in the tile (0 * inf is no number) and added back at the end to the tokens that see them.
@@ -48,7 +60,7 @@ static_assert(kCutUnits * sizeof(int2) <= kPiecesBytes && kCutUnits <= kThreads,
 constexpr int kGap = 3;
 constexpr int kPiece = 8;                 // places of a CTA at least
 constexpr int kJoinQuads = 8;             // channels / 4 of a CTA of the join
-constexpr int kSoftmaxRegs = 232, kOtherRegs = 40;
+constexpr int kSoftmaxRegs = 232, kOtherRegs = 40;     // (with 208 the cut lists' kernel spills)
 static_assert(kSoftmaxRegs * 256 + kOtherRegs * 128 <= 168 * kThreads, "the registers a CTA is launched with");
 
 struct ManyArgs {

