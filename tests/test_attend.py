@@ -285,3 +285,88 @@ def test_not_finite_values_in_cut_lists(gv):
         case.V[0][h][2000, 5] = float("inf")
     case.check(*run_pages(gv, case, 16), MANY)
     case.check(*run_slabs(gv, case), MANY)
+
+
+@pytest.mark.parametrize("nq", [1, 30])
+def test_values_that_are_no_numbers_in_queries_and_keys(gv, nq):
+    """A query row that holds a NaN spoils itself alone; a key whose logit is +inf the tokens that see it."""
+    case = Case(8, 2, 64, [[200, 90], [150, nq + 1]], [nq, nq], seed=31)
+    case.Q[nq // 2, 3, 5] = float("nan")
+    case.K[1][0][149, 0] = float("inf")
+    case.Q[nq:, :, 0] = case.Q[nq:, :, 0].abs() + 0.5                 # +inf, not -inf
+    w = FEW if few(case) else MANY
+    case.check(*run_pages(gv, case, 16), w)
+    case.check(*run_slabs(gv, case), w)
+
+
+@pytest.mark.parametrize("hq,hkv,d,nq", [(100, 1, 64, 3), (65, 1, 128, 2), (33, 1, 32, 9), (3, 3, 112, 7)])
+def test_groups_that_leave_a_tile_rows(gv, hq, hkv, d, nq):
+    case = Case(hq, hkv, d, [[140 + 9 * h for h in range(hkv)], [nq] * hkv], [nq, nq], seed=hq)
+    w = FEW if few(case) else MANY
+    case.check(*run_pages(gv, case, 16), w)
+    case.check(*run_slabs(gv, case), w)
+
+
+@pytest.mark.parametrize("nq", [1, 100])
+def test_offsets_past_32_bits(gv, nq):
+    """Pages and slabs that lie behind the first 2^31 elements."""
+    case = Case(8, 2, 64, [[300, 170]], [nq], seed=41)
+    p = params(gv, 8, 2, 64)
+    want = run_pages(gv, case, 64)
+    small = case.pages(gv, 64)
+    far = (1 << 31) // (64 * 64) + 1                                  # pages of 64 rows x 64 channels
+    n = small.K.shape[0]
+    pool = torch.empty(2, far + n, 64, 64, dtype=torch.bfloat16, device="cuda")
+    pool[:, far:] = torch.stack([small.K, small.V])
+    pages = gv.PageCache(pool[0], pool[1], (small.tables + far).clamp_max(far + n), small.kv_len,
+                         torch.zeros(far + n, dtype=torch.int32, device="cuda"), small.n_free)
+    ws = gv.alloc_attend_workspace(p, *case.geom())
+    wide, out, lse = case.outputs()
+    gv.gvote_page_attend(p, case.Q.cuda(), dev(case.cu_q), nq, pages, out, ws, lse=lse)
+    assert gv.gvote_poll_status(ws) == 0 and torch.equal(out, want[1]) and torch.equal(lse, want[2])
+    # new rows to the last page, by the slot map
+    slots = torch.tensor([[(far + n - 1) * 64 + 63], [-1]], dtype=torch.int32, device="cuda")
+    new = torch.full((2, 1, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    before = pool[:, far:].clone()
+    gv.gvote_page_write(p, new, -new, slots, pages, ws)
+    before[0, n - 1, 63], before[1, n - 1, 63] = 3.0, -3.0
+    assert torch.equal(pool[:, far:].nan_to_num(7.0), before.nan_to_num(7.0))
+    # slabs: the second head 2^31 elements behind the first
+    K, V, cu, kv, geom = case.slabs()
+    flat = pool.view(-1)
+    stride = far * 64 * 64
+    slab = [flat.as_strided((2, geom[1], 64), (stride, 64, 1), at) for at in (0, geom[1] * 64)]
+    slab[0].copy_(K), slab[1].copy_(V)
+    wide, out, lse = case.outputs()
+    gv.gvote_attend(p, case.Q.cuda(), dev(case.cu_q), nq, *slab, cu, geom, out, ws, lse=lse, kv_len=kv)
+    assert gv.gvote_poll_status(ws) == 0 and torch.equal(out, want[1]) and torch.equal(lse, want[2])
+
+
+def test_requests_that_share_pages(gv):
+    """Two requests with the same prefix: their tables name the same pages."""
+    case = Case(8, 2, 64, [[128, 128]], [2], seed=51)
+    p = params(gv, 8, 2, 64)
+    pages = case.pages(gv, 16)
+    both = gv.PageCache(pages.K, pages.V, pages.tables.repeat(2, 1, 1).contiguous(), pages.kv_len.repeat(2, 1).contiguous(), pages.free, pages.n_free)
+    ws = gv.alloc_attend_workspace(p, 2, 4, 2)
+    Q = case.Q.cuda().repeat(2, 1, 1)
+    out, lse = torch.zeros(4, 8, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(4, 8, device="cuda")
+    gv.gvote_page_attend(p, Q, dev(np.array([0, 2, 4], np.int32)), 2, both, out, ws, lse=lse)
+    wide, one, one_lse = run_pages(gv, case, 16)
+    assert torch.equal(out[:2], one) and torch.equal(out[2:], one) and torch.equal(lse[2:], one_lse)
+
+
+def test_two_streams_with_workspaces_of_their_own(gv):
+    cases = [Case(8, 2, 128, [[4000, 3000]], [n], seed=60 + n) for n in (1, 200)]
+    p = params(gv, 8, 2, 128)
+    want = [run_pages(gv, c, 32) for c in cases]
+    held = [(c.pages(gv, 32), c.Q.cuda(), dev(c.cu_q), gv.alloc_attend_workspace(p, *c.geom()), torch.cuda.Stream()) for c in cases]
+    outs = [c.outputs() for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c, (pages, Q, cu, ws, stream), (_, out, lse) in zip(cases, held, outs):
+            with torch.cuda.stream(stream):
+                gv.gvote_page_attend(p, Q, cu, c.nq[0], pages, out, ws, lse=lse)
+    torch.cuda.synchronize()
+    for w, (_, out, lse) in zip(want, outs):
+        assert torch.equal(w[1], out) and torch.equal(w[2], lse)
