@@ -80,7 +80,9 @@ struct Bars {
 struct Tail {
   Bars bars;
   volatile int stop;
-  int last_one, odd;                            // odd: values that are not finite were taken out
+  int last_one;
+  int odd;                                      // bit 0: values that are not finite were taken out; bit 1: outputs are not finite
+  alignas(16) float none[kMaxHeadDim];          // what the values of rows that all see add up to, where they are not finite
   float2 join[kFan][kRows];                        // references and sums of the segments that are joined
   int warp_sums[kThreads / 32];
   float2 ml[kWarps][kRows];
@@ -389,7 +391,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
               }
             }
           }
-          if (__any_sync(0xffffffffu, found) && lane == 0) atomicExch(&tail->odd, 1);
+          if (__any_sync(0xffffffffu, found) && lane == 0) atomicOr(&tail->odd, 1);
           ptx::fence_proxy_async();                                // (before the unit is filled again)
           __syncwarp();
         }
@@ -414,6 +416,10 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&tail->bars.q_empty[seg & 1]);
 
+      float all = 0.f;
+#pragma unroll
+      for (int n = 0; n < kBoxes * 8; ++n) all += (o[n][0] + o[n][1]) + (o[n][2] + o[n][3]);
+      if (__any_sync(0xffffffffu, !isfinite(all)) && lane == 0) atomicOr(&tail->odd, 2);
       // the four warps' results meet: a common reference, then sums in shared memory (warps 2 and 3, then 0 and 1 onto them)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -448,10 +454,30 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         }
         ptx::named_barrier_sync(1, 32 * kWarps);
       }
+      const int quads = a.d_k >> 2;
+      // Not finite: a value of a row that some token sees was not, and a weight's terms times an infinity may have cancelled or
+      // been zero; what such values add up to is the result.  Those of rows that all tokens see are looked for together.
+      const int common = min(max(all_see, w.s0 * kTileKeys), w.s1 * kTileKeys);
+      if (odd & 2) {
+        for (int i = tid; i < a.d_k; i += 32 * kWarps) tail->none[i] = 0.f;
+        ptx::named_barrier_sync(1, 32 * kWarps);
+        const int per = 32 * kWarps / quads, c = tid % quads * 4;
+#pragma unroll 2
+        for (int j = w.s0 * kTileKeys + tid / quads; tid < per * quads && j < common; j += per) {
+          const int64_t at = row_offset(a.src, x.r, x.h, a.Hkv, j);
+          if (at < 0) continue;
+          const uint2 g = *reinterpret_cast<const uint2*>(a.src.V + at + c);
+          if (!any_not_finite(g.x) && !any_not_finite(g.y)) continue;
+          const uint32_t z[4] = {g.x << 16, g.x & 0xffff0000u, g.y << 16, g.y & 0xffff0000u};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!isfinite(__uint_as_float(z[e]))) atomicAdd(&tail->none[c + e], __uint_as_float(z[e]));   // (sums of infinities and NaN: any order)
+        }
+        ptx::named_barrier_sync(1, 32 * kWarps);
+      }
       const int p0 = pref[w.e] + kGap, p1 = pref[w.e + 1];
       const int first = (int)(((int64_t)(p0 + 1) * B - 1) / T), last = (int)(((int64_t)p1 * B - 1) / T);   // CTAs of this entry
       const int64_t slot = slot0 + w.e + b;
-      const int quads = a.d_k >> 2;
       for (int i = tid; i < rows * quads; i += 32 * kWarps) {
         const int lr = i / quads, c = (i - lr * quads) * 4, row = row0 + lr, token = row / a.G, head = x.h * a.G + row - token * a.G;
         float top = tail->ml[0][lr].x;
@@ -464,13 +490,11 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         const float4 u = *reinterpret_cast<const float4*>(sum_sm + lr * L::kSumPitch + c);
         const float4 v = *reinterpret_cast<const float4*>(sum_sm + (kRows + lr) * L::kSumPitch + c);
         float4 r = make_float4(u.x + v.x, u.y + v.y, u.z + v.z, u.w + v.w);
-        // Not finite: a value of a row that this token sees was not, and a weight's terms times an infinity may have cancelled
-        // or been zero; what such values add up to is the result.  Else those taken out of this segment's tiles are added back.
-        const bool again = !isfinite(r.x + r.y + r.z + r.w);
-        if (odd || again) {
-          const int lim = all_see + (row - row0 / a.G * a.G) / a.G, end = min(lim, w.s1 * kTileKeys);
+        if (odd) {                                                 // and those that were taken out, or that only this token sees
+          const int end = min(all_see + row / a.G - row0 / a.G, w.s1 * kTileKeys);
           float4 f = make_float4(0, 0, 0, 0);
-          for (int j = max(again ? 0 : max(all_see, 0), w.s0 * kTileKeys); j < end; ++j) {
+          if ((odd & 2) && end > w.s0 * kTileKeys) f = *reinterpret_cast<const float4*>(tail->none + c);
+          for (int j = common; j < end; ++j) {
             const int64_t at = row_offset(a.src, x.r, x.h, a.Hkv, j);
             if (at < 0) continue;
             const uint2 g = *reinterpret_cast<const uint2*>(a.src.V + at + c);

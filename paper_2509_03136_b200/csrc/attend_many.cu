@@ -666,7 +666,6 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           ptx::tmem_ld_32x16(o_addr + b, o);
           ptx::tmem_wait_ld();
         }
-        if (!holds) continue;
         float f[16];
         float all = 0.f;
 #pragma unroll
@@ -675,16 +674,18 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           all += f[k];
         }
         // Not finite: some value this token sees was not, and a weight of zero times an infinity may have spoilt it; what such
-        // values add up to is the result.  Else those taken out of the unit's tiles are added back.
-        const bool again = !isfinite(all);
-        if (odd || again) {
+        // values add up to is the result (rows that all tokens of the unit see: the warp looks for them together).  Values taken
+        // out of the unit's tiles are added back.  (A sum that is no number makes the outputs none by itself.)
+        const bool again = holds && !isfinite(all) && isfinite(sum);
+        const bool search = __any_sync(0xffffffffu, again);
+        if (search || odd) {
+          const int from = x.k0 * kTile, end = (x.k0 + tiles) * kTile, common = min(max(x.see[0], from), end);
           float g[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) g[k] = 0.f;
-          const int end = min(limit, (x.k0 + tiles) * kTile);
-          for (int j = max(again ? 0 : x.see[0], x.k0 * kTile); j < end; ++j) {
+          auto add_row = [&](int j) {
             const int64_t at = row_offset(a.src, x.r, x.h, a.Hkv, j);
-            if (at < 0) continue;
+            if (at < 0) return;
             const uint4* q = reinterpret_cast<const uint4*>(a.src.V + at + b);
             const uint4 w[2] = {q[0], q[1]};
             const uint32_t* z = &w[0].x;
@@ -693,11 +694,23 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
               g[2 * k] += not_finite_only(__uint_as_float(z[k] << 16));
               g[2 * k + 1] += not_finite_only(__uint_as_float(z[k] & 0xffff0000u));
             }
+          };
+          if (search) {
+#pragma unroll 2
+            for (int j = from + lane; j < common; j += 32) add_row(j);
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+#pragma unroll
+              for (int m = 16; m > 0; m >>= 1) g[k] += __shfl_xor_sync(0xffffffffu, g[k], m);
           }
+          if (holds)
+            for (int j = common; j < min(limit, end); ++j) add_row(j);
 #pragma unroll
           for (int k = 0; k < 16; ++k)
-            if (g[k] != 0.f) f[k] = g[k];
+            if (holds && limit > from && g[k] != 0.f) f[k] = g[k];
+          __syncwarp();
         }
+        if (!holds) continue;
         if (kCut && x.segs > 1) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)

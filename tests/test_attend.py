@@ -370,3 +370,20 @@ def test_two_streams_with_workspaces_of_their_own(gv):
     torch.cuda.synchronize()
     for w, (_, out, lse) in zip(want, outs):
         assert torch.equal(w[1], out) and torch.equal(w[2], lse)
+
+
+@pytest.mark.parametrize("nq", [1, 64])
+def test_infinities_in_a_long_cache(gv, nq):
+    """Rows that every token sees and that hold infinities: found without a walk over the cache for every output."""
+    case = Case(4, 2, 128, [[24000, 900]], [nq], seed=71)
+    case.V[0][0][5, 7] = float("inf")
+    case.V[0][0][20001, 7] = -float("inf")
+    case.V[0][0][20001, 100] = float("inf")
+    case.V[0][1][899, 0] = float("nan")
+    p = params(gv, 4, 2, 128)
+    pages, Q, cu = case.pages(gv, 32), case.Q.cuda(), dev(case.cu_q)
+    wide, out, lse = case.outputs()
+    ws = gv.alloc_attend_workspace(p, *case.geom())
+    gv.gvote_page_attend(p, Q, cu, nq, pages, out, ws, lse=lse)
+    assert gv.gvote_poll_status(ws) == 0
+    case.check(wide, out, lse, FEW if few(case) else MANY)
