@@ -17,7 +17,7 @@
 // of units, K and V of a tile one unit each.  The products are mma.sync m16n8k16 with the query rows on M, 16 of them
 // to a group: the tensor work fits under the memory time, and this shape lets a warp keep its 16 cached rows
 // of a tile to itself: its own reference, sum and output in registers, no barrier within a segment.  Weights are held as a sum of
-// two bf16 terms (16 bits; the outputs have 8); all else in 32 bits.  A reference moves only when a logit passes it by 2^8.
+// two bf16 terms (16 bits; the outputs have 8), of up to eight rows both in one product; all else in 32 bits.  A reference moves only when a logit passes it by 2^8.
 // (A second group of 16 rows in the same CTA was no gain: mma.sync then takes 6000 clocks a tile.)
 //
 // Measured (one B200): one token of 28 heads over 128K rows of 4 KV heads, 268 MB, 60 us: the first tile is there after 5.3 us, the
@@ -290,21 +290,20 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const Entry x = entry_of(a, w.e, row_last);
       const int rows = min(x.nq * a.G - row0, kRows);
       const int all_see = x.n - (min(row_last / a.G, x.nq - 1) - row0 / a.G);   // rows that every token of the group sees
+      const bool packed = rows <= 8;                               // rows 8 to 15 of the product with V are the weights' second terms
       int limit[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int lr = i * 8 + (lane >> 2);
-          limit[i] = lr < rows ? all_see + (row0 + lr) / a.G - row0 / a.G : 0;
-        }
-      float o[kBoxes * 8][4], ref[2], sum[2];
-      {
-        ref[0] = ref[1] = -INFINITY;
-        sum[0] = sum[1] = 0.f;
-#pragma unroll
-        for (int i = 0; i < kBoxes * 8; ++i)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) o[i][k] = 0.f;
+      for (int i = 0; i < 2; ++i) {
+        const int lr = i * 8 + (lane >> 2);
+        limit[i] = lr < rows ? all_see + (row0 + lr) / a.G - row0 / a.G : 0;
       }
+      float o[kBoxes * 8][4], ref[2], sum[2];
+      ref[0] = ref[1] = -INFINITY;
+      sum[0] = sum[1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kBoxes * 8; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[i][k] = 0.f;
       ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->bars.q_full[seg & 1], (seg >> 1) & 1, stop));
       const uint32_t q_addr = ptx::smem_u32(q_sm) + (seg & 1) * L::kQ + ((lane & 15)) * L::kQPitch + (lane >> 4) * 16;
       const int key = 16 * warp;                                   // this warp's rows of a tile
@@ -316,21 +315,19 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         if (!ok) break;
         float l[2][4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) l[i][k] = 0.f;
+          for (int k = 0; k < 4; ++k) l[i][k] = 0.f;
         const uint32_t k_addr = ptx::smem_u32(ring) + s * L::kUnit + k_row * 128;
 #pragma unroll
         for (int c = 0; c < kBoxes * 4; ++c) {
           if (c < ksteps) {
             uint32_t kf[4];
             ldmatrix4(kf, k_addr + (c >> 2) * (kTileKeys * 128) + (((((uint32_t)c & 3) * 2 + k_half) ^ (k_row & 7)) << 4));
-            {
-              uint32_t qf[4];
-              ldmatrix4(qf, q_addr + c * 32);
-              mma(l[0], qf, kf[0], kf[1]);
-              mma(l[1], qf, kf[2], kf[3]);
-            }
+            uint32_t qf[4];
+            ldmatrix4(qf, q_addr + c * 32);
+            mma(l[0], qf, kf[0], kf[1]);
+            mma(l[1], qf, kf[2], kf[3]);
           }
         }
         __syncwarp();
@@ -340,36 +337,43 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         uint32_t hi[4], lo[4];
         const int j0 = t * kTileKeys + key + (lane & 3) * 2;       // this lane's columns: j0, j0 + 1, j0 + 8, j0 + 9
         const bool masked = (t + 1) * kTileKeys > all_see;
-        {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float* p[4] = {&l[0][2 * i], &l[0][2 * i + 1], &l[1][2 * i], &l[1][2 * i + 1]};
-            if (masked) {
+        for (int i = 0; i < 2; ++i) {
+          if (i == 1 && packed) {
+            hi[1] = lo[0];
+            hi[3] = lo[2];
+            break;
+          }
+          float* p[4] = {&l[0][2 * i], &l[0][2 * i + 1], &l[1][2 * i], &l[1][2 * i + 1]};
+          if (masked) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (j0 + (k >> 1) * 8 + (k & 1) >= limit[i]) *p[k] = -INFINITY;
+            for (int k = 0; k < 4; ++k)
+              if (j0 + (k >> 1) * 8 + (k & 1) >= limit[i]) *p[k] = -INFINITY;
+          }
+          float top = fmaxf(fmaxf(*p[0], *p[1]), fmaxf(*p[2], *p[3]));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * a.scale2;
+          const bool move = top > ref[i] + kSlack;
+          if (__any_sync(0xffffffffu, move)) {
+            const float f = move ? exp2_approx(ref[i] - top) : 1.f;
+            if (move) ref[i] = top;
+            sum[i] *= f;
+#pragma unroll
+            for (int n = 0; n < kBoxes * 8; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
+            if (packed) {
+#pragma unroll
+              for (int n = 0; n < kBoxes * 8; ++n) { o[n][2] *= f; o[n][3] *= f; }
             }
-            float top = fmaxf(fmaxf(*p[0], *p[1]), fmaxf(*p[2], *p[3]));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * a.scale2;
-            const bool move = top > ref[i] + kSlack;
-            if (__any_sync(0xffffffffu, move)) {
-              const float f = move ? exp2_approx(ref[i] - top) : 1.f;
-              if (move) ref[i] = top;
-              sum[i] *= f;
+          }
+          const float off = ref[i] == -INFINITY ? 0.f : ref[i];
 #pragma unroll
-              for (int n = 0; n < kBoxes * 8; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
-            }
-            const float off = ref[i] == -INFINITY ? 0.f : ref[i];
+          for (int k = 0; k < 4; ++k) *p[k] = exp2_approx(fmaf(*p[k], a.scale2, -off));
+          sum[i] += (*p[0] + *p[1]) + (*p[2] + *p[3]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) *p[k] = exp2_approx(fmaf(*p[k], a.scale2, -off));
-            sum[i] += (*p[0] + *p[1]) + (*p[2] + *p[3]);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {                          // fragment i + 2 k: columns j0 + 8 k, j0 + 8 k + 1
-              const uint32_t h = bf16_pair(*p[2 * k], *p[2 * k + 1]);
-              hi[i + 2 * k] = h;
-              lo[i + 2 * k] = bf16_pair(*p[2 * k] - __uint_as_float(h << 16), *p[2 * k + 1] - __uint_as_float(h & 0xffff0000u));
-            }
+          for (int k = 0; k < 2; ++k) {                          // fragment i + 2 k: columns j0 + 8 k, j0 + 8 k + 1
+            const uint32_t h = bf16_pair(*p[2 * k], *p[2 * k + 1]);
+            hi[i + 2 * k] = h;
+            lo[i + 2 * k] = bf16_pair(*p[2 * k] - __uint_as_float(h << 16), *p[2 * k + 1] - __uint_as_float(h & 0xffff0000u));
           }
         }
         s = unit % L::kUnits;
@@ -401,9 +405,9 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           if (c < ksteps) {
             uint32_t vf[4];
             ldmatrix4_trans(vf, v_addr + (c >> 2) * (kTileKeys * 128) + (((((uint32_t)c & 3) * 2 + v_half) ^ (v_row & 7)) << 4));
-            {
-              mma(o[2 * c], hi, vf[0], vf[1]);
-              mma(o[2 * c + 1], hi, vf[2], vf[3]);
+            mma(o[2 * c], hi, vf[0], vf[1]);
+            mma(o[2 * c + 1], hi, vf[2], vf[3]);
+            if (!packed) {
               mma(o[2 * c], lo, vf[0], vf[1]);
               mma(o[2 * c + 1], lo, vf[2], vf[3]);
             }
@@ -418,39 +422,46 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 
       float all = 0.f;
 #pragma unroll
-      for (int n = 0; n < kBoxes * 8; ++n) all += (o[n][0] + o[n][1]) + (o[n][2] + o[n][3]);
+      for (int n = 0; n < kBoxes * 8; ++n) {
+        if (packed) { o[n][0] += o[n][2]; o[n][1] += o[n][3]; o[n][2] = o[n][3] = 0.f; }
+        all += (o[n][0] + o[n][1]) + (o[n][2] + o[n][3]);
+      }
       if (__any_sync(0xffffffffu, !isfinite(all)) && lane == 0) atomicOr(&tail->odd, 2);
-      // the four warps' results meet: a common reference, then sums in shared memory (warps 2 and 3, then 0 and 1 onto them)
+      // the four warps' results meet: a common reference, then sums in shared memory (warps 2 and 3, then 0 and 1 onto them); of
+      // 16 rows those that are a token's, eight at least
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
-          sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
-          if ((lane & 3) == 0) tail->ml[warp][i * 8 + (lane >> 2)] = make_float2(ref[i], sum[i]);
-        }
+      for (int i = 0; i < 2; ++i) {
+        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+        if ((lane & 3) == 0) tail->ml[warp][i * 8 + (lane >> 2)] = make_float2(ref[i], sum[i]);
+      }
       ptx::named_barrier_sync(1, 32 * kWarps);
       const int odd = tail->odd;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int lr = i * 8 + (lane >> 2);
-          float top = tail->ml[0][lr].x;
+      for (int i = 0; i < 2; ++i) {
+        if (i * 8 >= rows) break;
+        const int lr = i * 8 + (lane >> 2);
+        float top = tail->ml[0][lr].x;
 #pragma unroll
-          for (int k = 1; k < kWarps; ++k) top = fmaxf(top, tail->ml[k][lr].x);
-          const float f = exp2_approx(ref[i] - (top == -INFINITY ? 0.f : top));
+        for (int k = 1; k < kWarps; ++k) top = fmaxf(top, tail->ml[k][lr].x);
+        const float f = exp2_approx(ref[i] - (top == -INFINITY ? 0.f : top));
 #pragma unroll
-          for (int n = 0; n < kBoxes * 8; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
-        }
+        for (int n = 0; n < kBoxes * 8; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
+      }
 #pragma unroll
       for (int round = 1; round >= 0; --round) {
         if ((warp >> 1) == round) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 2; ++i) {
+            if (i * 8 >= rows) break;
 #pragma unroll
-              for (int n = 0; n < kBoxes * 8; ++n) {
-                float2* at = reinterpret_cast<float2*>(sum_sm + ((warp & 1) * kRows + i * 8 + (lane >> 2)) * L::kSumPitch + n * 8 + (lane & 3) * 2);
-                float2 v = make_float2(o[n][2 * i], o[n][2 * i + 1]);
-                if (round == 0) { const float2 u = *at; v.x += u.x; v.y += u.y; }
-                *at = v;
-              }
+            for (int n = 0; n < kBoxes * 8; ++n) {
+              float2* at = reinterpret_cast<float2*>(sum_sm + ((warp & 1) * kRows + i * 8 + (lane >> 2)) * L::kSumPitch + n * 8 + (lane & 3) * 2);
+              float2 v = make_float2(o[n][2 * i], o[n][2 * i + 1]);
+              if (round == 0) { const float2 u = *at; v.x += u.x; v.y += u.y; }
+              *at = v;
+            }
+          }
         }
         ptx::named_barrier_sync(1, 32 * kWarps);
       }
@@ -525,9 +536,9 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       int k0 = (b - first) / kFan * kFan, n = min(segs - k0, kFan), apart = 1;      // the segments k0, k0 + apart, ..: n of them
       int32_t* count = counts + w.e + first + k0;
       while (segs > 1) {
-        __threadfence();
         ptx::named_barrier_sync(1, 32 * kWarps);
         if (tid == 0) {
+          __threadfence();                                         // (of what all wrote: the barrier lies before it)
           const int before = atomicAdd(count, 1);
           tail->last_one = before == n - 1;
           if (before == n - 1) *count = 0;
