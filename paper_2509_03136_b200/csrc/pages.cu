@@ -23,7 +23,7 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanEach = 4;           // entries of a thread
 constexpr int kPlanEntries = kPlanThreads * kPlanEach;   // held in shared memory; of more the lengths are read for every phase
 constexpr int kStepTokens = 8;         // new tokens of a request up to which a thread does an entry's slots
-constexpr int kSlotTokens = 4096;      // tokens of a CTA of the slot kernel
+constexpr int kSlotLog2 = 10, kSlotTokens = 1 << kSlotLog2;      // tokens of a CTA of the slot kernel (4096: 8 us instead of 4)
 constexpr int kSlotThreads = 256;
 
 struct TableArgs {
@@ -293,14 +293,14 @@ page_slots_kernel(const __grid_constant__ TableArgs a) {
   const int64_t g = blockIdx.x;
   ptx::let_next_begin();
   ptx::wait_for_previous();
-  // tile g of a list with (cu[r] >> 12) + r as the first of request r
+  // tile g of a list with (cu[r] >> kSlotLog2) + r as the first of request r
   int lo = 0, hi = a.p.batch - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if ((int64_t)(a.cu_new[mid] >> 12) + mid <= g) lo = mid; else hi = mid - 1;
+    if ((int64_t)(a.cu_new[mid] >> kSlotLog2) + mid <= g) lo = mid; else hi = mid - 1;
   }
   const int r = lo, start = a.cu_new[r], n = a.cu_new[r + 1] - start;
-  const int64_t t0 = (g - ((start >> 12) + r)) * kSlotTokens;
+  const int64_t t0 = (g - ((start >> kSlotLog2) + r)) * kSlotTokens;
   // tokens of no request
   if (g == 0)
     for (int64_t i = tid; i < a.cu_new[0]; i += kSlotThreads) a.slots[(int64_t)h * a.total_new + i] = -1;
@@ -349,9 +349,9 @@ page_slots_kernel(const __grid_constant__ TableArgs a) {
 // ---------------------------------------------------------------------------------- rows into pages
 // Copies 4 d_k bytes per kept row: bound by memory.  A warp takes 32 slots, and for those that are kept as many lanes per row as
 // it has 16-byte pieces; kWriteUnroll rows of K and V per lane are asked for before the first is stored.  Measured: 164 MB (52 % of
-// 32K rows of 8 heads) 28.9 us, 5.7 TB/s; one row of 64 requests 4.8 us in a graph.
+// 32K rows of 8 heads) 28.2 us, 5.8 TB/s; one row of 64 requests 4.8 us in a graph.
 constexpr int kWriteThreads = 128;
-constexpr int kWriteUnroll = 4;
+constexpr int kWriteUnroll = 8;
 
 __global__ void __launch_bounds__(kWriteThreads)
 page_write_kernel(const __nv_bfloat16* __restrict__ K, const __nv_bfloat16* __restrict__ V, int64_t tok, int64_t head,
@@ -444,7 +444,7 @@ int32_t launch_page_tables(const PageArgs& p, const int32_t* keep, const int32_t
   GVOTE_LAUNCH_CHECK("page_plan_kernel");
   if (n_slots > 0 && !a.slots_here) {
     LaunchScope scope_("page_slots_kernel", st);
-    (void)launch_behind(page_slots_kernel, dim3((unsigned)((total_new >> 12) + p.batch), p.Hkv), dim3(kSlotThreads), 0, st, a);
+    (void)launch_behind(page_slots_kernel, dim3((unsigned)((total_new >> kSlotLog2) + p.batch), p.Hkv), dim3(kSlotThreads), 0, st, a);
     GVOTE_LAUNCH_CHECK("page_slots_kernel");
   }
   return GVOTE_OK;
