@@ -74,6 +74,7 @@ struct ManyArgs {
   int tpt;                // tokens of a query tile
   uint32_t pairs, units;  // pairs of tiles (upper bound), times KV heads
   int stages, box_rows;
+  int wide;               // out's rows start on 32 bytes
   float4* part_o;         // [2 per CTA][2 tiles][d_k / 4][128 rows]
   float2* part_ml;        // [2 per CTA][2 tiles][128 rows]  (reference, sum), base 2
   int2* pieces;           // [units]  first CTA, pieces
@@ -720,8 +721,12 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         uint4 w[2];
 #pragma unroll
         for (int k = 0; k < 8; ++k) (&w[k >> 2].x)[k & 3] = bf16_pair(f[2 * k] * inv, f[2 * k + 1] * inv);
-        reinterpret_cast<uint4*>(out + b)[0] = w[0];
-        reinterpret_cast<uint4*>(out + b)[1] = w[1];
+        if (a.wide) {                                              // (a lane's row is a line of its own: half as many stores)
+          ptx::store_32(out + b, w[0], w[1]);
+        } else {
+          reinterpret_cast<uint4*>(out + b)[0] = w[0];
+          reinterpret_cast<uint4*>(out + b)[1] = w[1];
+        }
       }
       ptx::tc_fence_before_sync();
       if (kCut && x.segs > 1) {
@@ -774,6 +779,7 @@ int32_t launch_attend_many(const gvote_params* p, const AttendCall& c, const Row
   ManyArgs a;
   a.src = s;
   a.cu_q = c.cu_q; a.out = c.out; a.o_tok = c.o_tok; a.o_head = c.o_head; a.lse = c.lse;
+  a.wide = ((reinterpret_cast<uintptr_t>(c.out) | (uintptr_t)(c.o_tok * 2) | (uintptr_t)(c.o_head * 2)) & 31) == 0;
   a.status = reinterpret_cast<int32_t*>(ws);
   a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads; a.batch = c.batch; a.d_k = p->d_k;
   a.max_q = (int)c.max_q;
