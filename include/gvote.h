@@ -481,7 +481,8 @@ GVOTE_API int32_t gvote_page_write(const gvote_params* p, const void* K_new, con
  * terms) in calls of few query rows (max_q x query heads per KV head at most 16, or d_k > 128) and as bf16 in
  * larger ones.  A row that a token does not see has no influence on it, whatever it holds.  Deterministic.  Tokens of no request
  * (before cu_q[0], behind cu_q[batch]) keep their out and lse.  Where cu_q gives a request more than max_q tokens, or a
- * page that rows are read from does not exist, the status word reads GVOTE_ERR_INVALID_ARG and the outputs are not to be used. */
+ * page that rows are read from does not exist, the status word reads GVOTE_ERR_INVALID_ARG and the outputs are not to be used.
+ * out and lse must not share memory with Q or with the pages. */
 GVOTE_API int32_t gvote_page_attend(const gvote_params* p, const void* Q, int64_t q_tok_stride, int64_t q_head_stride,
                           const int32_t* cu_q, int64_t total_q, int64_t max_q, const gvote_pages* pages, void* out,
                           int64_t out_tok_stride, int64_t out_head_stride, float* lse_or_null, void* ws, size_t ws_bytes,

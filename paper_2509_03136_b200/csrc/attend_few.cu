@@ -5,8 +5,8 @@
 // cached row.
 //
 // Split.  The rows of all (request, KV head) pairs ("entries") are cut into tiles of 64 and laid end to end, each entry behind
-// kGap tiles for what beginning and ending one costs (3.5 us a segment beyond the first, 1.35 a tile: a ragged batch took a tenth
-// longer with one); CTA b of B takes the tiles from T b / B to T (b + 1) / B of the T places.  So heads of very different length load every
+// kGap tiles for what beginning and ending one costs (about that many tiles' time; a ragged batch took a tenth longer with
+// one); CTA b of B takes the tiles from T b / B to T (b + 1) / B of the T places.  So heads of very different length load every
 // SM alike, and the lengths stay on the device.  What a CTA has of an entry is a segment.  An
 // entry within one CTA goes straight to the output; of the others every segment leaves its reference, sum and output in slot
 // entry + CTA, and of kFan neighbouring segments the CTA that arrives last at their counter adds them up in their order, then
@@ -20,9 +20,9 @@
 // two bf16 terms (16 bits; the outputs have 8), of up to eight rows both in one product; all else in 32 bits.  A reference moves only when a logit passes it by 2^8.
 // (A second group of 16 rows in the same CTA was no gain: mma.sync then takes 6000 clocks a tile.)
 //
-// Measured (one B200): one token of 28 heads over 128K rows of 4 KV heads, 268 MB, 60 us: the first tile is there after 5.3 us, the
-// last after 42 (7 TB/s between them), then the warps' results meet (1.4) and two rounds of joins.  A ragged batch of 128 pruned heads, 131
-// MB, 35 us.  The smallest call 8.6 us in a graph.
+// Measured (one B200): one token of 28 heads over 128K rows of 4 KV heads, 268 MB, 57.5 us: the first tile is there after 5.3 us, the
+// last after 41 (7.2 TB/s between them), then the warps' results meet (1.4) and two rounds of joins.  A ragged batch of 128 pruned heads, 131
+// MB, 31 us.  The smallest call 9 us in a graph.
 //
 // Rows that not every token of a group sees, and rows behind the last one, may hold anything: logits are masked by index, values
 // that are not finite are taken out of the tile (0 * inf is no number) and added back to the outputs of the tokens that see them.

@@ -25,15 +25,17 @@
 //
 // What bounds it: a tile's chain.  The softmax of 128 x 128 logits takes its four warps 2000 clocks (S out of tensor memory and
 // its maximum 600, the exponentials 1200, P back 200), the products and their messages 1160, and the two tiles' chains overlap to 3600
-// clocks for 2 x 2 products of 128 x 128 x 128, of which the tensor cores work half: 51 % busy, the exponentials' unit 45 %.
-// Measured (one B200): a 32K prompt of 32 heads on 8 8.1 to 8.4 ms (8.8 TFLOP, 1.05 to 1.1 PFLOP/s), 8192 tokens 0.51 ms.
+// clocks for 2 x 2 products of 128 x 128 x 128, of which the tensor cores work half: 52 % busy, the exponentials' unit 46 %.
+// Measured (one B200): a 32K prompt of 32 heads on 8 8.1 to 8.4 ms (8.8 TFLOP, 1.05 to 1.1 PFLOP/s), 8192 tokens 0.51 to
+// 0.56 ms as the power allows clocks.  Of that the outputs' stores take 3 %: a lane's 32 bytes are a line of their own, and with 16 at a time
+// they took 1 % (of short prompts 2 %) more.
 // Slower, or no faster: two S of 64 keys to a tile, so that softmax and products of a tile overlap (the MMAs with N = 64 read
 // Q twice as often, 8.5 ms); sixteen softmax warps, two threads to a row (9.5 ms); an issuer for each tile; exponentials before the maximum,
 // with the reference of the tile before (registers); none, two or three of eight exponentials on the FMA pipe; a loop over halves with S read
 // twice; the units of a ragged batch sorted by length; outputs 64 channels at a time.
 //
 // Where there are few units (kCutUnits at most) the list is cut evenly over the CTAs, units into pieces, and attend_join_kernel adds
-// a unit's pieces up: 500 tokens of 32 heads over pruned 13K rows of 8 KV heads 130 us instead of 272, 7 of them the join.
+// a unit's pieces up: 500 tokens of 32 heads over pruned 13K rows of 8 KV heads 121 us in a graph instead of 272, 7 of them the join.
 //
 // Rows that not every token of a unit sees may hold anything: logits are masked by index, values that are not finite are
 // set to 0 in the tile (0 * inf is no number) and added back at the end to the tokens that see them.
