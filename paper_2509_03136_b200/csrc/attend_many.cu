@@ -32,7 +32,8 @@
 // Slower, or no faster: two S of 64 keys to a tile, so that softmax and products of a tile overlap (the MMAs with N = 64 read
 // Q twice as often, 8.5 ms); sixteen softmax warps, two threads to a row (9.5 ms); an issuer for each tile; exponentials before the maximum,
 // with the reference of the tile before (registers); none, two or three of eight exponentials on the FMA pipe; a loop over halves with S read
-// twice; the units of a ragged batch sorted by length; outputs 64 channels at a time.
+// twice; S read in two halves, the maximum of one while the other comes (8.45 ms for 8.34); the units of a ragged batch sorted by length;
+// outputs 64 channels at a time.
 //
 // Where there are few units (kCutUnits at most) the list is cut evenly over the CTAs, units into pieces, and attend_join_kernel adds
 // a unit's pieces up: 500 tokens of 32 heads over pruned 13K rows of 8 KV heads 121 us in a graph instead of 272, 7 of them the join.

@@ -127,6 +127,19 @@ def test_cutting_what_was_grown_restores_the_stack(gv):
     assert s.n_free == n and np.array_equal(s.free[:n], stack)
 
 
+@pytest.mark.parametrize("H", [4, 5])
+@pytest.mark.parametrize("first_rows", [15, 16, 17, 33])
+@pytest.mark.parametrize("first_new", [0, 1, 17])
+def test_a_thousand_pages_change_hands(gv, H, first_rows, first_new):
+    """256 requests of 4 heads give back and take 1024 pages, a few more or less: all heads lose what they held and grow at once."""
+    rows = np.full((256, H), 16)
+    rows[0] = first_rows
+    s = State(gv, 256, H, 16, rows, 4, 9, seed=first_rows)
+    assert s.step(np.zeros((256, H), int), [first_new] + [1] * 255) == 0
+    assert s.step(s.kv - 1, [2] * 256) in (0, -3)                     # (pages of one row: back and out again, one more where there was none)
+    assert s.step(np.zeros((256, H), int), [1] * 255 + [0]) == 0
+
+
 @pytest.mark.parametrize("long_ones", [False, True])
 def test_refusals_change_nothing(gv, long_ones):
     n = 6000 if long_ones else 20
