@@ -475,7 +475,8 @@ GVOTE_API int32_t gvote_page_write(const gvote_params* p, const void* K_new, con
  * by cu_q [batch+1] (device), max_q of one request at most: one token, a few drafts, or the next chunk of a prompt.  A
  * request's query tokens are the last rows of its cache (write them first): token i of n sees rows 0 .. kv_len - n + i of a
  * head; a head with fewer rows than that leaves token i nothing, which gives out = 0, lse = -inf (logits that are all -inf
- * count as nothing, too).  Per query head of KV head
+ * count as nothing, too, whatever the values hold).  Beside other logits a value that is not finite reaches the out of every
+ * token that sees its row, though the weight be zero.  Per query head of KV head
  * h: logits q.k / sqrt(d_k), softmax, out = sum of weight * value, rounded to bf16 once; lse_or_null [total_q, n_q_heads] = log
  * of the softmax's denominator.  32-bit logits, references and sums; weights enter the product with the values as 16 bits (two bf16
  * terms) in calls of few query rows (max_q x query heads per KV head at most 16, or d_k > 128) and as bf16 in

@@ -21,14 +21,13 @@ def attend(q, k, v, weight_err):
                 continue
             l = (q[i] @ k[:seen].T) / np.sqrt(d)
             top = l.max(axis=1, keepdims=True)
-            if np.isneginf(top).any():
-                raise ValueError("a row whose logits are all -inf")
-            w = np.exp(l - top)
+            none = np.isneginf(top)                                   # logits that are all -inf: as if there were no rows
+            w = np.exp(l - np.where(none, 0.0, top))
             z = w.sum(axis=1, keepdims=True)
-            w /= z
+            w = np.where(none, 0.0, w / z)
             lse[i] = (top + np.log(z))[:, 0]
-            out[i] = _weighted(w, v[:seen])
-            size = (np.abs(q[i]) @ np.abs(k[:seen]).T) / np.sqrt(d)
+            out[i] = np.where(none, 0.0, _weighted(w, v[:seen]))
+            size = np.where(np.isneginf(l), 0.0, (np.abs(q[i]) @ np.abs(k[:seen]).T) / np.sqrt(d))
             dl = np.nan_to_num((d + 3) * U * size.max(axis=1, keepdims=True), posinf=0.0) + 2.0 ** -18
             spread = _weighted(w, np.abs(np.where(np.isfinite(v[:seen]), v[:seen], 0.0)))
             out_tol[i] = 2.0 ** -8 * np.abs(out[i]) + spread * (weight_err + 2 * dl) * 1.01 + 1e-30
@@ -37,7 +36,7 @@ def attend(q, k, v, weight_err):
 
 
 def _weighted(w, v):
-    """w @ v; where a value is not finite any positive weight counts, however small."""
+    """w @ v; a value that is not finite counts whatever its row's weight, zero (a logit of -inf) among them."""
     if np.isfinite(v).all():
         return w @ v
     o = w @ np.where(np.isfinite(v), v, 0.0)

@@ -42,6 +42,8 @@
 // set to 0 in the tile (0 * inf is no number) and added back at the end to the tokens that see them.
 //
 // Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
+#include <float.h>
+
 #include "f32x2.cuh"
 #include "kv_rows.cuh"
 
@@ -220,7 +222,7 @@ attend_join_kernel(const __grid_constant__ ManyArgs a) {
 #pragma unroll 2
   for (int k = 0; k < n; ++k) {
     const float2 q = a.part_ml[(piece_slot(first, k) * 2 + i) * kTile + row];
-    if (q.x == -INFINITY && q.y == 0.f) continue;                  // saw nothing: its outputs were not written
+    if (q.x == -INFINITY && q.y == 0.f) continue;                  // no tile: its outputs were not written
     const float f = exp2_fast(q.x - off);
     sum = fmaf(q.y, f, sum);
     const float4* from = a.part_o + ((piece_slot(first, k) * 2 + i) * quads + c0) * kTile + row;
@@ -662,8 +664,9 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       __nv_bfloat16* out = a.out + token * a.o_tok + (int64_t)head * a.o_head;
       const int64_t slot = kCut ? piece_slot(x.first, (int)blockIdx.x - x.first) : 0;
+      const bool piece = kCut && x.segs > 1;
       for (int b = 0; b < a.d_k; b += 16) {
-        if (kCut && x.segs > 1 && tiles == 0) break;
+        if (piece && tiles == 0) break;
         uint32_t o[16];
         __syncwarp();
         if (tiles > 0) {
@@ -674,7 +677,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         float all = 0.f;
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-          f[k] = sum == 0.f ? 0.f : __uint_as_float(o[k]);
+          f[k] = tiles > 0 ? __uint_as_float(o[k]) : 0.f;
           all += f[k];
         }
         // Not finite: some value this token sees was not, and a weight of zero times an infinity may have spoilt it; what such
@@ -715,11 +718,15 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           __syncwarp();
         }
         if (!holds) continue;
-        if (kCut && x.segs > 1) {
+        if (piece) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             a.part_o[((slot * 2 + i) * (a.d_k >> 2) + (b >> 2) + k) * kTile + row] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
           continue;
+        }
+        if (sum == 0.f) {                                          // no rows, or logits that are all -inf
+#pragma unroll
+          for (int k = 0; k < 16; ++k) f[k] = 0.f;
         }
         uint4 w[2];
 #pragma unroll
@@ -732,8 +739,8 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
       }
       ptx::tc_fence_before_sync();
-      if (kCut && x.segs > 1) {
-        a.part_ml[(slot * 2 + i) * kTile + row] = make_float2(ref, sum);
+      if (piece) {                                                 // (of weights that are all zero the outputs may be infinities all the same)
+        a.part_ml[(slot * 2 + i) * kTile + row] = make_float2(sum == 0.f && tiles > 0 ? -FLT_MAX : ref, sum);
       } else if (holds && a.lse)
         a.lse[token * a.Hq + head] = sum == 0.f ? -INFINITY : (ref == -INFINITY ? 0.f : ref) * 0.6931471805599453f + logf(sum);
     }
