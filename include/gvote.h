@@ -459,8 +459,11 @@ GVOTE_API size_t gvote_attend_workspace_bytes(const gvote_params* p, int32_t bat
  * comes from free_pages[n_free + K - 1 - k]; so cutting what was grown last restores the stack.  Table entries behind the
  * last page, and stack entries above the top, keep what they held.
  * All or nothing: where the stack or a table is too short nothing changes, slots are -1 and the status word reads
- * GVOTE_ERR_WORKSPACE_TOO_SMALL; where n_free is not in 0 .. n_pages, or pages would be released twice (the stack would
- * pass n_pages), it reads GVOTE_ERR_INVALID_ARG.  Without cu_new nothing grows; mask and slots are null then. */
+ * GVOTE_ERR_WORKSPACE_TOO_SMALL; where n_free is not in 0 .. n_pages, the stack would pass n_pages, or a number that is
+ * released or taken names no page, it reads GVOTE_ERR_INVALID_ARG.  New rows that go on in a page that does not exist get slots of
+ * -1, and the status word reads GVOTE_ERR_INVALID_ARG, too.  Every page belongs to one head of one request or lies on the
+ * stack: a page that two tables name (which gvote_page_attend may read) would be released twice, and that is not found out as
+ * long as the stack has room.  Without cu_new nothing grows; mask and slots are null then. */
 GVOTE_API int32_t gvote_page_tables(const gvote_params* p, const gvote_pages* pages, const int32_t* keep_or_null,
                           const int32_t* cu_new_or_null, int64_t total_new, int64_t max_new, const uint32_t* mask_or_null,
                           int32_t* slots_or_null, void* ws, size_t ws_bytes, void* stream);

@@ -70,6 +70,9 @@ def tables(tabs, kv_len, free, n_free, page_rows, keep=None, cu_new=None, kept=N
     top = int(n_free) + len(gone)
     if not 0 <= n_free <= len(free) or top > len(free) or need > top:
         return None
+    moved = gone + free[top - max(need, len(gone)):int(n_free)].tolist()
+    if any(not 0 <= page < len(free) for page in moved):
+        return None
     for i, page in enumerate(gone):
         free[top - 1 - i] = page
     for r in range(B):

@@ -5,7 +5,8 @@
 // Released page k of K, in the order of entries and of rows, goes to free[n_free + K - 1 - k]; taken page k comes from
 // free[n_free + K - 1 - k].  So what is cut next is what was grown last, and the stack is as it was.  Everything is one prefix
 // sum over entries per direction, and what a thread does next is found by bisecting it: entries that need hundreds of pages
-// and entries that need none cost the same per page.
+// and entries that need none cost the same per page.  The numbers of all pages that change hands are looked at before anything
+// is written: one that names no page refuses the call.
 //
 // A few thousand integers: bound by latency.  So one CTA does all of a decode step between barriers (lengths and prefix sums;
 // releases; takes; slots), and one cluster of eight where more pages or slots may change hands; each CTA of a cluster makes
@@ -22,6 +23,7 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanEach = 4;           // entries of a thread
 constexpr int kPlanEntries = kPlanThreads * kPlanEach;   // held in shared memory; of more the lengths are read for every phase
+constexpr int kHold = 4;               // pages that a thread keeps between looking at their numbers and passing them on
 constexpr int kStepTokens = 8;         // new tokens of a request up to which a thread does an entry's slots
 constexpr int kSlotLog2 = 10, kSlotTokens = 1 << kSlotLog2;      // tokens of a CTA of the slot kernel (4096: 8 us instead of 4)
 constexpr int kSlotThreads = 256;
@@ -56,6 +58,14 @@ __device__ __forceinline__ Change change_of(const TableArgs& a, int64_t e) {
   return c;
 }
 __device__ __forceinline__ int pages_of(int rows, int log2) { return (rows + (1 << log2) - 1) >> log2; }
+// The slot of a head's row; -1 where the table names no page (it has not come by this call: pages that change hands are looked at).
+__device__ __forceinline__ int slot_of(const TableArgs& a, int64_t e, int row) {
+  const int page = a.p.tables[e * a.p.max_pages + (row >> a.p.page_log2)];
+  if ((uint32_t)page < (uint32_t)a.p.n_pages) return (page << a.p.page_log2) + (row & ((1 << a.p.page_log2) - 1));
+  atomicExch(&a.status[0], GVOTE_ERR_INVALID_ARG);
+  atomicExch(&a.status[1], 28);
+  return -1;
+}
 
 // Inclusive sum over the CTA's threads.
 __device__ __forceinline__ int scan_block(int x, int* warp_sums) {
@@ -103,7 +113,7 @@ struct PlanShared {
   int gone[kPlanEntries], want[kPlanEntries];      // pages released, taken by the entries before
   int warp_sums[2][32];
   long long totals[2];
-  int sums[2], too_long;
+  int sums[2], too_long, no_page;
 };
 
 // Lengths and prefix sums of the entries e0 .. e0 + n - 1.
@@ -166,7 +176,7 @@ __device__ void plan_entries(const TableArgs& a, PlanShared& s, int64_t e0, int 
 
 // kCluster: one cluster, else one CTA.
 template <bool kCluster>
-__global__ void __launch_bounds__(kPlanThreads)
+__global__ void __launch_bounds__(kPlanThreads, 1)
 page_plan_kernel(const __grid_constant__ TableArgs a) {
   extern __shared__ __align__(16) uint8_t plan_smem[];
   PlanShared& s = *reinterpret_cast<PlanShared*>(plan_smem);
@@ -174,74 +184,102 @@ page_plan_kernel(const __grid_constant__ TableArgs a) {
   const int64_t entries = (int64_t)a.p.batch * a.p.Hkv;
   const bool once = entries <= kPlanEntries;                     // what is read once stays in shared memory
   const int ctas = kCluster ? gridDim.x : 1, me = kCluster ? blockIdx.x : 0;
-  if (tid == 0) { s.totals[0] = s.totals[1] = 0; s.too_long = 0; }
+  if (tid == 0) { s.totals[0] = s.totals[1] = 0; s.too_long = s.no_page = 0; }
   __syncthreads();
+  if (kCluster) cooperative_groups::this_cluster().barrier_arrive();       // (no_page is there for the others)
   ptx::let_next_begin();
   ptx::wait_for_previous();
   auto sync_all = [&] { if (kCluster) cooperative_groups::this_cluster().sync(); else __syncthreads(); };
   auto count_of = [&](int64_t e0) { return (int)min((int64_t)kPlanEntries, entries - e0); };
+  // Where page k of those that the entries e0 .. e0 + n - 1 release or take stands in their tables (of entries that start at the same
+  // place the last one has the pages).
+  auto place_of = [&](const int* first, int64_t e0, int n, int k) {
+    const int i = find_owner(first, n, k);
+    return a.p.tables + (e0 + i) * a.p.max_pages + pages_of(s.cut[i], log2) + (k - first[i]);
+  };
+  const int k0 = me * kPlanThreads + tid, stride = ctas * kPlanThreads;
 
   // sums and checks
   const int n_free = *a.p.n_free;
-  for (int64_t e0 = 0; e0 < entries; e0 += kPlanEntries) plan_entries(a, s, e0, count_of(e0), true);
+  bool none = false;                                             // a number that names no page
+  auto look = [&](int page) { none |= (uint32_t)page >= (uint32_t)a.p.n_pages; };
+  for (int64_t e0 = 0; e0 < entries; e0 += kPlanEntries) {
+    plan_entries(a, s, e0, count_of(e0), true);
+    if (once) break;
+    if (s.totals[0] <= a.p.n_pages)                              // (else the call is refused, and the prefix sums may have wrapped)
+      for (int k = k0; k < s.sums[0]; k += stride) look(*place_of(s.gone, e0, count_of(e0), k));
+    __syncthreads();
+  }
   const long long K = s.totals[0], T = s.totals[1];
   const bool bad = n_free < 0 || n_free > a.p.n_pages || n_free + K > a.p.n_pages;
-  const bool refuse = bad || s.too_long || T > n_free + K;
-  sync_all();                                                    // every CTA has read n_free and the lengths
+  bool refuse = bad || s.too_long || T > n_free + K;
+  const int top = (int)(n_free + K), most = (int)max(K, T);     // (of a call that is not refused)
+  // The k-th page taken lies where the k-th released one went.  So of the first kHold * stride a thread reads page k where it is, and
+  // after the barrier it goes to the stack and to the table that takes it (a step 11.3 -> 10.5 us against by way of the stack).
+  int page[kHold];
+  int32_t* place[kHold];
+  if (once && !refuse) {
+#pragma unroll
+    for (int u = 0; u < kHold; ++u) {
+      const int k = k0 + u * stride;
+      if (k >= most) break;
+      page[u] = k < K ? *place_of(s.gone, 0, (int)entries, k) : a.p.free_pages[top - 1 - k];
+      if (k < T) place[u] = place_of(s.want, 0, (int)entries, k);
+      look(page[u]);
+    }
+    for (int k = k0 + kHold * stride; k < most; k += stride)
+      look(k < K ? *place_of(s.gone, 0, (int)entries, k) : a.p.free_pages[top - 1 - k]);
+  } else if (!refuse) {
+    for (int k = (int)K + k0; k < T; k += stride) look(a.p.free_pages[top - 1 - k]);
+  }
+  if (kCluster) cooperative_groups::this_cluster().barrier_wait();
+  if (none)
+    for (int c = 0; c < ctas; ++c) *(kCluster ? cooperative_groups::this_cluster().map_shared_rank(&s.no_page, c) : &s.no_page) = 1;
+  sync_all();                                                    // every CTA has read n_free, the lengths and the pages
+  refuse |= s.no_page != 0;
   const int64_t n_slots = a.total_new * a.p.Hkv;
   if (refuse) {
     if (me == 0 && tid == 0) {
       *a.refused = 1;
-      atomicExch(&a.status[0], bad ? GVOTE_ERR_INVALID_ARG : GVOTE_ERR_WORKSPACE_TOO_SMALL);
+      atomicExch(&a.status[0], bad || s.no_page ? GVOTE_ERR_INVALID_ARG : GVOTE_ERR_WORKSPACE_TOO_SMALL);
       atomicExch(&a.status[1], 20);
     }
     if (a.slots_here)
-      for (int64_t i = (int64_t)me * kPlanThreads + tid; i < n_slots; i += (int64_t)ctas * kPlanThreads) a.slots[i] = -1;
+      for (int64_t i = k0; i < n_slots; i += stride) a.slots[i] = -1;
     return;
   }
   if (me == 0 && tid == 0) *a.refused = 0;
-  const int top = (int)(n_free + K);
 
-  // Releases, then takes.  The k-th page taken lies where the k-th released one went, so where one CTA's threads have one k each at
-  // most a page goes from table to table, and the stack's load is not behind the releases (a step 11.3 -> 10.5 us; a cluster gained nothing).
-  const bool one_each = !kCluster && max(K, T) <= kPlanThreads;
-  if (one_each) {
-    const int k = tid;
-    int page = 0;
-    int32_t *stack = a.p.free_pages + (top - 1 - k), *place = nullptr;
-    if (k < K) {
-      const int i = find_owner(s.gone, (int)entries, k);
-      page = a.p.tables[(int64_t)i * a.p.max_pages + pages_of(s.cut[i], log2) + (k - s.gone[i])];
-    } else if (k < T) {
-      page = *stack;
+  // releases, then takes
+  if (once) {
+    const int from = k0 + kHold * stride;
+    if (most > kHold * stride) {                                 // the others by way of the stack
+      for (int k = from; k < K; k += stride) a.p.free_pages[top - 1 - k] = *place_of(s.gone, 0, (int)entries, k);
+      sync_all();
     }
-    if (k < T) {
-      const int i = find_owner(s.want, (int)entries, k);
-      place = a.p.tables + (int64_t)i * a.p.max_pages + pages_of(s.cut[i], log2) + (k - s.want[i]);
+#pragma unroll
+    for (int u = 0; u < kHold; ++u) {
+      const int k = k0 + u * stride;
+      if (k < K) a.p.free_pages[top - 1 - k] = page[u];
+      if (k < T) *place[u] = page[u];
     }
-    __syncthreads();
-    if (k < K) *stack = page;
-    if (k < T) *place = page;
-    __syncthreads();
+    for (int k = from; k < T; k += stride) *place_of(s.want, 0, (int)entries, k) = a.p.free_pages[top - 1 - k];
+    sync_all();
   }
 #pragma unroll 1
-  for (int take = 0; take < 2 && !one_each; ++take) {
-    if ((take ? T : K) > 0) {
-      int before = 0;
-      for (int64_t e0 = 0; e0 < entries; e0 += kPlanEntries) {
-        const int n = count_of(e0);
-        if (!once) plan_entries(a, s, e0, n, false);
-        const int* first = take ? s.want : s.gone;
-        const int all = s.sums[take];
-        for (int k = me * kPlanThreads + tid; k < all; k += ctas * kPlanThreads) {
-          const int i = find_owner(first, n, k);                 // (of entries that start at the same place the last one has the pages)
-          int32_t* place = a.p.tables + (e0 + i) * a.p.max_pages + pages_of(s.cut[i], log2) + (k - first[i]);
-          int32_t* stack = a.p.free_pages + (top - 1 - before - k);
-          if (take) *place = *stack; else *stack = *place;
-        }
-        before += all;
-        if (!once) __syncthreads();
+  for (int take = 0; take < 2 && !once; ++take) {
+    int before = 0;
+    for (int64_t e0 = 0; e0 < entries && (take ? T : K) > 0; e0 += kPlanEntries) {
+      const int n = count_of(e0);
+      plan_entries(a, s, e0, n, false);
+      const int all = s.sums[take];
+      for (int k = k0; k < all; k += stride) {
+        int32_t* at = place_of(take ? s.want : s.gone, e0, n, k);
+        int32_t* stack = a.p.free_pages + (top - 1 - before - k);
+        if (take) *at = *stack; else *stack = *at;
       }
+      before += all;
+      __syncthreads();
     }
     sync_all();
   }
@@ -249,30 +287,25 @@ page_plan_kernel(const __grid_constant__ TableArgs a) {
   // the slots where they are few, then the lengths
   if (a.slots_here) {
     if (a.max_new <= kStepTokens) {
-      for (int64_t e = (int64_t)me * kPlanThreads + tid; e < entries; e += (int64_t)ctas * kPlanThreads) {
+      for (int64_t e = k0; e < entries; e += stride) {
         const int r = (int)((uint32_t)e / (uint32_t)a.p.Hkv), h = (int)(e - (int64_t)r * a.p.Hkv);
         const int from = a.cu_new[r], to = a.cu_new[r + 1], cut = once ? s.cut[e] : change_of(a, e).cut;
-        for (int t = from; t < to; ++t) {
-          const int row = cut + t - from;
-          a.slots[h * a.total_new + t] = (a.p.tables[e * a.p.max_pages + (row >> log2)] << log2) + (row & ((1 << log2) - 1));
-        }
+        for (int t = from; t < to; ++t) a.slots[h * a.total_new + t] = slot_of(a, e, cut + t - from);
       }
       const int64_t lead = a.cu_new[0], tail = a.cu_new[a.p.batch];            // tokens of no request
-      for (int64_t i = (int64_t)me * kPlanThreads + tid; i < (lead + a.total_new - tail) * a.p.Hkv; i += (int64_t)ctas * kPlanThreads) {
+      for (int64_t i = k0; i < (lead + a.total_new - tail) * a.p.Hkv; i += stride) {
         const int64_t t = i / a.p.Hkv;
         a.slots[(i - t * a.p.Hkv) * a.total_new + (t < lead ? t : tail + t - lead)] = -1;
       }
     } else {
-      for (int64_t i = (int64_t)me * kPlanThreads + tid; i < n_slots; i += (int64_t)ctas * kPlanThreads) {
+      for (int64_t i = k0; i < n_slots; i += stride) {
         const int h = (int)(i / a.total_new);
         const int64_t t = i - h * a.total_new;
         const int r = request_of(a.cu_new, a.p.batch, t);
         const int64_t e = (int64_t)r * a.p.Hkv + h;
         int slot = -1;
-        if (t >= a.cu_new[r] && t < a.cu_new[r + 1]) {
-          const int row = (once ? s.cut[e] : change_of(a, e).cut) + (int)(t - a.cu_new[r]);
-          slot = (a.p.tables[e * a.p.max_pages + (row >> log2)] << log2) + (row & ((1 << log2) - 1));
-        }
+        if (t >= a.cu_new[r] && t < a.cu_new[r + 1])
+          slot = slot_of(a, e, (once ? s.cut[e] : change_of(a, e).cut) + (int)(t - a.cu_new[r]));
         a.slots[i] = slot;
       }
     }
@@ -312,7 +345,7 @@ __global__ void __launch_bounds__(kSlotThreads)
 page_slots_kernel(const __grid_constant__ TableArgs a) {
   __shared__ int warp_sums[32];
   __shared__ int rank_of[kSlotTokens / 32];
-  const int h = blockIdx.y, tid = threadIdx.x, log2 = a.p.page_log2;
+  const int h = blockIdx.y, tid = threadIdx.x;
   const int64_t g = blockIdx.x;
   ptx::let_next_begin();
   ptx::wait_for_previous();
@@ -355,7 +388,6 @@ page_slots_kernel(const __grid_constant__ TableArgs a) {
   } else {
     cut = a.p.kv_len[e] - n;
   }
-  const int32_t* table = a.p.tables + e * a.p.max_pages;
   for (int i = tid; i < here; i += kSlotThreads) {
     int row = cut;
     if (a.mask) {
@@ -365,7 +397,7 @@ page_slots_kernel(const __grid_constant__ TableArgs a) {
     } else {
       row += (int)t0 + i;
     }
-    out[i] = (table[row >> log2] << log2) + (row & ((1 << log2) - 1));
+    out[i] = slot_of(a, e, row);
   }
 }
 
