@@ -27,7 +27,7 @@
 // Rows that not every token of a group sees, and rows behind the last one, may hold anything: logits are masked by index, values
 // that are not finite are taken out of the tile (0 * inf is no number) and added back to the outputs of the tokens that see them.
 //
-// Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
+// Every wait is bounded by the time without any work done (kv_rows.cuh); when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
 #include "kv_rows.cuh"
 
 namespace gvote {
@@ -80,7 +80,7 @@ struct Bars {
 };
 struct Tail {
   Bars bars;
-  volatile int stop;
+  Watch watch;
   int last_one;
   int odd;                                      // bit 0: values that are not finite were taken out; bit 1: outputs are not finite
   alignas(16) float none[kMaxHeadDim];          // what the values of rows that all see add up to, where they are not finite
@@ -160,7 +160,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   float* sum_sm = reinterpret_cast<float*>(q_sm + 2 * L::kQ);      // [2][rows][pitch]
   Tail* tail = reinterpret_cast<Tail*>(sum_sm + 2 * kRows * L::kSumPitch);
   int* pref = tail->pref;
-  volatile int* stop = &tail->stop;
+  Watch* watch = &tail->watch;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int entries = a.batch * a.Hkv;
   const int row0 = (a.group0 + blockIdx.y) * kRows, row_last = row0 + kRows - 1;   // query rows of this group
@@ -172,7 +172,8 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     ptx::fence_barrier_init();
   }
   if (tid == 0) {
-    tail->stop = (ptx::smem_u32(smem) & 1023u) ? 1 : 0;
+    tail->watch.stop = (ptx::smem_u32(smem) & 1023u) ? 1 : 0;
+    tail->watch.work = 0;
     tail->odd = 0;
     ptx::prefetch_tensormap(&tmK);
     ptx::prefetch_tensormap(&tmV);
@@ -224,7 +225,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     for (Walk w(pref, t0, t1, entries); ok && !w.done(); w.next(), ++seg) {
       const Entry x = entry_of(a, w.e, row_last);
       const int rows = min(x.nq * a.G - row0, kRows);
-      ok = __all_sync(0xffffffffu, wait_or_stop(&tail->bars.q_empty[seg & 1], ((seg >> 1) & 1) ^ 1, stop));
+      ok = __all_sync(0xffffffffu, wait_or_stop(&tail->bars.q_empty[seg & 1], ((seg >> 1) & 1) ^ 1, watch));
       if (!ok) break;
       if (lane == 0) ptx::mbar_arrive_expect_tx(&tail->bars.q_full[seg & 1], (uint32_t)(rows * a.d_k * 2));
       __syncwarp();
@@ -251,7 +252,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
         for (int v = 0; v < 2; ++v, ++unit) {
           const uint32_t s = unit % L::kUnits;
-          ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->bars.empty[s], ((unit / L::kUnits) & 1) ^ 1, stop));
+          ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->bars.empty[s], ((unit / L::kUnits) & 1) ^ 1, watch));
           if (!ok) break;
           if (lane == 0) ptx::mbar_arrive_expect_tx(&tail->bars.full[s], (uint32_t)(parts * boxes * a.box_rows * 128));
           __syncwarp();
@@ -306,14 +307,14 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       for (int i = 0; i < kBoxes * 8; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[i][k] = 0.f;
-      ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->bars.q_full[seg & 1], (seg >> 1) & 1, stop));
+      ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->bars.q_full[seg & 1], (seg >> 1) & 1, watch));
       const uint32_t q_addr = ptx::smem_u32(q_sm) + (seg & 1) * L::kQ + ((lane & 15)) * L::kQPitch + (lane >> 4) * 16;
       const int key = 16 * warp;                                   // this warp's rows of a tile
       const uint32_t k_row = key + ((lane >> 4) << 3) + (lane & 7), k_half = (lane >> 3) & 1;
       const uint32_t v_row = key + (((lane >> 3) & 1) << 3) + (lane & 7), v_half = lane >> 4;
       for (int t = w.s0; ok && t < w.s1; ++t) {
         uint32_t s = unit % L::kUnits;
-        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->bars.full[s], (unit / L::kUnits) & 1, stop));
+        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->bars.full[s], (unit / L::kUnits) & 1, watch));
         if (!ok) break;
         float l[2][4];
 #pragma unroll
@@ -379,7 +380,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           }
         }
         s = unit % L::kUnits;
-        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->bars.full[s], (unit / L::kUnits) & 1, stop));
+        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->bars.full[s], (unit / L::kUnits) & 1, watch));
         if (!ok) break;
         if (masked) {
           bool found = false;
@@ -475,8 +476,10 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         for (int i = tid; i < a.d_k; i += 32 * kWarps) tail->none[i] = 0.f;
         ptx::named_barrier_sync(1, 32 * kWarps);
         const int per = 32 * kWarps / quads, c = tid % quads * 4;
+        uint32_t rows_done = 0;
 #pragma unroll 2
         for (int j = w.s0 * kTileKeys + tid / quads; tid < per * quads && j < common; j += per) {
+          if ((++rows_done & 1023u) == 0 && tid == 0) count_work(watch);
           const int64_t at = row_offset(a.src, x.r, x.h, a.Hkv, j);
           if (at < 0) continue;
           const uint2 g = *reinterpret_cast<const uint2*>(a.src.V + at + c);
@@ -597,7 +600,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
   }
   __syncthreads();
-  if (tid == 0 && tail->stop) {
+  if (tid == 0 && watch->stop) {
     atomicExch(&a.status[0], GVOTE_ERR_TIMEOUT);
     atomicExch(&a.status[1], 24);
   }

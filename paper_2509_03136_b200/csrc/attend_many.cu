@@ -41,7 +41,7 @@
 // Rows that not every token of a unit sees may hold anything: logits are masked by index, values that are not finite are
 // set to 0 in the tile (0 * inf is no number) and added back at the end to the tokens that see them.
 //
-// Every wait is bounded; when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
+// Every wait is bounded by the time without any work done (kv_rows.cuh); when one runs out GVOTE_ERR_TIMEOUT is recorded and the outputs are not to be used.
 #include <float.h>
 
 #include "f32x2.cuh"
@@ -65,7 +65,7 @@ static_assert(kCutUnits * sizeof(int2) <= kPiecesBytes && kCutUnits <= kThreads,
 constexpr int kGap = 3;
 constexpr int kPiece = 8;                 // places of a CTA at least
 constexpr int kJoinQuads = 8;             // channels / 4 of a CTA of the join
-constexpr int kSoftmaxRegs = 232, kOtherRegs = 40;     // (with 208 the cut lists' kernel spills)
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;     // (with 232 and 40 or 224 and 56 the cut lists' kernel spills)
 static_assert(kSoftmaxRegs * 256 + kOtherRegs * 128 <= 168 * kThreads, "the registers a CTA is launched with");
 
 struct ManyArgs {
@@ -105,7 +105,7 @@ struct Tail {
   uint64_t info_full[kInfos], info_empty[kInfos];
   uint64_t drain;
   uint32_t tmem_slot;
-  volatile int stop;
+  Watch watch;
   int mark[kMarks];       // seq of a unit whose values were not all finite
   Unit info[kInfos];      // seq < 0: no more
   int warp_sums[kThreads / 32];
@@ -183,7 +183,7 @@ struct Units {
   // The whole warp: the next unit, or false at the end (or when a wait ran out).
   __device__ __forceinline__ bool next(Unit& x, int lane) {
     const int s = at % kInfos;
-    if (!__all_sync(0xffffffffu, wait_or_stop(&tail->info_full[s], (at / kInfos) & 1, &tail->stop))) return false;
+    if (!__all_sync(0xffffffffu, wait_or_stop(&tail->info_full[s], (at / kInfos) & 1, &tail->watch))) return false;
     x = tail->info[s];
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(&tail->info_empty[s]);
@@ -254,7 +254,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   uint8_t* q_sm = smem;                                            // [2][box][128 rows][128], swizzled
   uint8_t* ring = q_sm + 2 * kTileBytes;                           // [stage][box][128 rows][128], swizzled: K and V in turns
   Tail* tail = reinterpret_cast<Tail*>(ring + (size_t)a.stages * kTileBytes);
-  volatile int* stop = &tail->stop;
+  Watch* watch = &tail->watch;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int q_rows = a.G * a.tpt;                                  // rows a box of Q fills
 
@@ -271,7 +271,8 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     for (int s = 0; s < kMarks; ++s) ptx::mbar_init(&tail->v_raw[s], 1);
     for (int s = 0; s < kInfos; ++s) { ptx::mbar_init(&tail->info_full[s], 1); ptx::mbar_init(&tail->info_empty[s], 11); }
     ptx::mbar_init(&tail->drain, 1);
-    tail->stop = (ptx::smem_u32(smem) & 1023u) ? 1 : 0;
+    tail->watch.stop = (ptx::smem_u32(smem) & 1023u) ? 1 : 0;
+    tail->watch.work = 0;
     for (int s = 0; s < kMarks; ++s) tail->mark[s] = -1;
     ptx::fence_barrier_init();
     ptx::prefetch_tensormap(&tmQ);
@@ -330,6 +331,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       int at = 0;
       bool ok = true;
       for (uint32_t k = 0; ok; ++k) {
+        if ((k & 63u) == 63u && lane == 0) count_work(watch);      // (a list may be long and nearly empty)
         bool end;
         Unit x;
         if (kCut && cut) {
@@ -354,7 +356,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
         x.seq = end ? -1 : at;
         const int s = at % kInfos;
-        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->info_empty[s], ((at / kInfos) & 1) ^ 1, stop));
+        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->info_empty[s], ((at / kInfos) & 1) ^ 1, watch));
         if (!ok) break;
         if (lane == 0) {
           tail->info[s] = x;
@@ -383,7 +385,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       while (ok && units.next(x, lane)) {
         const int tiles = max(x.tiles[0], x.tiles[1]);
         if (tiles == 0) continue;
-        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->q_empty, (asked_q & 1) ^ 1, stop));
+        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->q_empty, (asked_q & 1) ^ 1, watch));
         if (!ok) break;
         ++asked_q;
         const int n_q = x.tiles[1] > 0 ? 2 : 1;                    // (the first tile sees less than the second)
@@ -409,7 +411,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll
           for (int v = 0; v < 2; ++v, ++it) {
             const uint32_t s = at.slot;
-            ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->empty[s], at.parity ^ 1, stop));
+            ok = ok && __all_sync(0xffffffffu, wait_or_stop(&tail->empty[s], at.parity ^ 1, watch));
             if (!ok) break;
             at.step();
             // (values that warp 10 has to look at first: it tells when they are there)
@@ -428,7 +430,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         atomicExch(&a.status[0], GVOTE_ERR_INVALID_ARG);
         atomicExch(&a.status[1], 26);
       }
-      if (*stop) {
+      if (watch->stop) {
         await_loads(tail->full, a.stages, it);
         await_loads(tail->v_raw, kMarks, raw);
         if (asked_q) await_loads(&tail->q_full, 1, asked_q);
@@ -443,7 +445,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const uint32_t idesc_s = ptx::instr_desc_bf16_f32(kTile, kTile);
       const uint32_t idesc_o = ptx::instr_desc_bf16_f32(kTile, a.d_k) | (1u << 16);     // V: channels contiguous
       const uint32_t q_addr = ptx::smem_u32(q_sm), ring_addr = ptx::smem_u32(ring);
-      auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_or_stop(bar, parity, stop)); };
+      auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_or_stop(bar, parity, watch)); };
       const uint64_t qd0 = ptx::smem_desc_k_sw128(q_addr), kd0 = ptx::smem_desc_k_sw128(ring_addr);
       // (channels behind d_k are zero: every step is taken)
       auto product_qk = [&](int i, uint32_t slot) {
@@ -519,11 +521,12 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             ptx::umma_commit(&tail->empty[v_slot]);
             if (more) ptx::umma_commit(&tail->empty[k_slot]);
             if (t + 2 == tiles) ptx::umma_commit(&tail->q_empty);
+            count_work(watch);
           }
           __syncwarp();
         }
       }
-      if (*stop) {
+      if (watch->stop) {
         if (ptx::elect_one()) ptx::umma_commit(&tail->drain);
         __syncwarp();
         for (int k = 0; k < (1 << 12) && !ptx::mbar_try_wait(&tail->drain, 0); ++k) {}
@@ -537,7 +540,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       while (ok && units.next(x, lane)) {
         const int tiles = max(x.tiles[0], x.tiles[1]), from = max(x.see[0], 0);
         for (int t = max(from / kTile - x.k0, 0); t < tiles; ++t, ++raw) {
-          ok = __all_sync(0xffffffffu, wait_or_stop(&tail->v_raw[raw % kMarks], (raw / kMarks) & 1, stop));
+          ok = __all_sync(0xffffffffu, wait_or_stop(&tail->v_raw[raw % kMarks], (raw / kMarks) & 1, watch));
           if (!ok) break;
           const uint32_t s = (it + 2 * t + 1) % a.stages;
           bool found = false;
@@ -585,7 +588,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       float ref = -INFINITY, sum = 0.f;
       const bool idle = (warp & 3) * 32 >= min(count * a.G, q_rows);   // none of this warp's rows is a token's
       for (int t = 0; t < tiles; ++t, ++used) {
-        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->s_full[i], used & 1, stop));
+        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->s_full[i], used & 1, watch));
         if (!ok) break;
         if (idle) {                                                // (their weights may be anything)
           if (lane == 0) { ptx::mbar_arrive(&tail->p_half[i]); ptx::mbar_arrive(&tail->p_full[i]); }
@@ -614,7 +617,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           if (move) ref = top;
           sum *= f;
           if (t > 0) {
-            ok = __all_sync(0xffffffffu, wait_or_stop(&tail->pv_done[i], (used - 1) & 1, stop));
+            ok = __all_sync(0xffffffffu, wait_or_stop(&tail->pv_done[i], (used - 1) & 1, watch));
             if (!ok) break;
             ptx::tc_fence_after_sync();
 #pragma unroll 1
@@ -653,7 +656,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
       if (!ok) break;
       if (tiles > 0) {
-        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->pv_done[i], (used - 1) & 1, stop));
+        ok = __all_sync(0xffffffffu, wait_or_stop(&tail->pv_done[i], (used - 1) & 1, watch));
         if (!ok) break;
         ptx::tc_fence_after_sync();
       }
@@ -704,7 +707,10 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           };
           if (search) {
 #pragma unroll 2
-            for (int j = from + lane; j < common; j += 32) add_row(j);
+            for (int j = from + lane; j < common; j += 32) {
+              if (((j - from) & 0xffff) == 0) count_work(watch);   // (the first lane)
+              add_row(j);
+            }
 #pragma unroll
             for (int k = 0; k < 16; ++k)
 #pragma unroll
@@ -748,7 +754,7 @@ attend_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 
   ptx::tc_fence_before_sync();
   __syncthreads();
-  if (tid == 0 && tail->stop) {
+  if (tid == 0 && watch->stop) {
     atomicExch(&a.status[0], GVOTE_ERR_TIMEOUT);
     atomicExch(&a.status[1], 27);
   }

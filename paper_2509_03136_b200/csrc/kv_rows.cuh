@@ -94,12 +94,25 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ bool wait_or_stop(uint64_t* bar, uint32_t parity, volatile int* stop) {
+// What the waits of a CTA look at: whether one of them ran out, and a counter of work done.
+struct Watch {
+  volatile int stop;
+  uint32_t work;
+};
+__device__ __forceinline__ void count_work(Watch* w) { atomicAdd(&w->work, 1u); }
+// Gives up after 2^20 tries (2 s: the hardware lets a try last 2 us) during which no work was done.  So a wait may last as long as
+// what it is for, two seconds of a unit of 2^28 rows for instance, as long as whoever is at work counts it at least once in that time.
+__device__ __forceinline__ bool wait_or_stop(uint64_t* bar, uint32_t parity, Watch* w) {
+  uint32_t seen = 0;
   for (uint32_t i = 0; i < (1u << 20); ++i) {
     if (ptx::mbar_try_wait(bar, parity)) return true;
-    if ((i & 255u) == 255u && *stop) return false;
+    if ((i & 255u) == 255u) {
+      if (w->stop) return false;
+      const uint32_t now = *reinterpret_cast<volatile uint32_t*>(&w->work);
+      if (now != seen) { seen = now; i = 0; }
+    }
   }
-  *stop = 1;
+  w->stop = 1;
   return false;
 }
 // Before a producer leaves early: the loads of a ring that may still write to this CTA's memory.
