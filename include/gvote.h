@@ -469,8 +469,9 @@ GVOTE_API int32_t gvote_page_tables(const gvote_params* p, const gvote_pages* pa
                           int32_t* slots_or_null, void* ws, size_t ws_bytes, void* stream);
 
 /* New rows into their pages: row t of head h of K_new, V_new [n_kv_heads, total_new, d_k] (bf16, element strides) to place
- * slots[h][t]; negative: dropped.  A slot behind the last page is dropped and the status word reads GVOTE_ERR_INVALID_ARG;
- * of rows with the same slot one is kept.  K_new, V_new must not share memory with the pages. */
+ * slots[h][t]; negative: dropped.  A slot behind the last page is dropped and the status word reads GVOTE_ERR_INVALID_ARG.
+ * Slots that are not negative are to differ, as those of gvote_page_tables do: where rows have the same one, its place holds pieces
+ * of 16 bytes of any of them afterwards, K and V each for itself, and this is not reported.  K_new, V_new must not share memory with the pages. */
 GVOTE_API int32_t gvote_page_write(const gvote_params* p, const void* K_new, const void* V_new, int64_t tok_stride, int64_t head_stride,
                          const int32_t* slots, int64_t total_new, const gvote_pages* pages, void* ws, size_t ws_bytes, void* stream);
 

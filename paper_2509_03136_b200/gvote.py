@@ -664,7 +664,8 @@ def gvote_page_tables(p, pages: PageCache, ws, keep=None, cu_new=None, max_new: 
 
 
 def gvote_page_write(p, K_new, V_new, slots, pages: PageCache, ws) -> None:
-    """Rows of K_new, V_new [n_kv_heads, total_new, d_k] to the places slots [n_kv_heads, total_new] names (negative: dropped)."""
+    """Rows of K_new, V_new [n_kv_heads, total_new, d_k] to the places slots [n_kv_heads, total_new] names (negative: dropped).
+    Slots that are not negative are to differ."""
     H, total_new, dev = p.n_kv_heads, K_new.shape[1], pages.device
     if total_new and K_new.stride() != V_new.stride():
         raise ValueError("K_new and V_new must share strides")
