@@ -91,6 +91,11 @@ class GVotePages(ctypes.Structure):
     ]
 
 
+def _same_strides(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether a and b are laid out alike (the stride of a dimension of one may be anything)."""
+    return a.stride() == b.stride() or all(n <= 1 or x == y for n, x, y in zip(a.shape, a.stride(), b.stride()))
+
+
 class PageCache:
     """A paged cache: pages K, V (bfloat16 [n_pages, page_rows, d_k]), tables (int32 [batch, n_kv_heads, max_pages]), rows
     held kv_len (int32 [batch, n_kv_heads]) and the stack of unused pages free (int32 [n_pages]) of height n_free (int32 [1]).
@@ -100,7 +105,7 @@ class PageCache:
     def __init__(self, K, V, tables, kv_len, free, n_free):
         n_pages, page_rows, d = K.shape
         batch, H, max_pages = tables.shape
-        if K.stride() != V.stride():
+        if not _same_strides(K, V):
             raise ValueError("K and V must share strides")
         dev = K.device
         self.args = GVotePages(
@@ -667,7 +672,7 @@ def gvote_page_write(p, K_new, V_new, slots, pages: PageCache, ws) -> None:
     """Rows of K_new, V_new [n_kv_heads, total_new, d_k] to the places slots [n_kv_heads, total_new] names (negative: dropped).
     Slots that are not negative are to differ."""
     H, total_new, dev = p.n_kv_heads, K_new.shape[1], pages.device
-    if total_new and K_new.stride() != V_new.stride():
+    if total_new and not _same_strides(K_new, V_new):
         raise ValueError("K_new and V_new must share strides")
     _launch(load().gvote_page_write, dev, p, _shaped(K_new, torch.bfloat16, (H, total_new, p.d_k), "K_new", dev, dense=False),
             _shaped(V_new, torch.bfloat16, (H, total_new, p.d_k), "V_new", dev, dense=False), K_new.stride(1), K_new.stride(0),
@@ -690,7 +695,7 @@ def gvote_attend(p, Q, cu_q, max_q: int, K, V, cu_seqlens, geom, out, ws, lse=No
     batch, total, max_N = geom
     H, total_q, dev = p.n_kv_heads, Q.shape[0], K.device
     shape = (total_q, p.n_q_heads, p.d_k)
-    if total and K.stride() != V.stride():
+    if total and not _same_strides(K, V):
         raise ValueError("K and V must share strides")
     _launch(load().gvote_attend, dev, p, _shaped(Q, torch.bfloat16, shape, "Q", dev, dense=False), Q.stride(0), Q.stride(1),
             _shaped(cu_q, torch.int32, (batch + 1,), "cu_q", dev), total_q, max_q,
