@@ -484,7 +484,8 @@ GVOTE_API int32_t gvote_page_write(const gvote_params* p, const void* K_new, con
  * h: logits q.k / sqrt(d_k), softmax, out = sum of weight * value, rounded to bf16 once; lse_or_null [total_q, n_q_heads] = log
  * of the softmax's denominator.  32-bit logits, references and sums; weights enter the product with the values as 16 bits (two bf16
  * terms) in calls of few query rows (max_q x query heads per KV head at most 16, or d_k > 128) and as bf16 in
- * larger ones.  A row that a token does not see has no influence on it, whatever it holds.  Deterministic.  Tokens of no request
+ * larger ones, before the division by the denominator: a sum of weights (2^8 at most) times values that passes 2^128 is an
+ * infinity.  A row that a token does not see has no influence on it, whatever it holds.  Deterministic.  Tokens of no request
  * (before cu_q[0], behind cu_q[batch]) keep their out and lse.  Where cu_q gives a request more than max_q tokens, or a
  * page that rows are read from does not exist, the status word reads GVOTE_ERR_INVALID_ARG and the outputs are not to be used.
  * out and lse must not share memory with Q or with the pages. */

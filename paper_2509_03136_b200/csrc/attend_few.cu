@@ -218,7 +218,9 @@ attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 
   if (warp == kWarps) {
     // ------------------------------------------------------------------ asks for tiles
-    const uint64_t policy = ptx::l2_policy_evict_first();          // rows that no other group reads (a ragged batch 32.7 -> 31.2 us)
+    // Rows that no other group reads (a ragged batch 32.7 -> 31.2 us).  Those of pages that requests share are read by several
+    // all the same, and may come out of memory once more.
+    const uint64_t policy = ptx::l2_policy_evict_first();
     uint32_t unit = 0;
     int seg = 0;
     bool ok = true, bad_page = false;

@@ -37,6 +37,8 @@
 //
 // Where there are few units (kCutUnits at most) the list is cut evenly over the CTAs, units into pieces, and attend_join_kernel adds
 // a unit's pieces up: 500 tokens of 32 heads over pruned 13K rows of 8 KV heads 121 us in a graph instead of 272, 7 of them the join.
+// With more units the list is not cut, and a request much longer than the others is one SM's work per KV head: five drafts of 36
+// requests, one of 128K rows among 2000, take 1.62 ms, of 32 such requests (272 units) 0.21.
 //
 // Rows that not every token of a unit sees may hold anything: logits are masked by index, values that are not finite are
 // set to 0 in the tile (0 * inf is no number) and added back at the end to the tokens that see them.
